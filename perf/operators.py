@@ -286,12 +286,13 @@ def _decoder(s):
     return _kept[key]
 
 
-def _cache(s, layer=None):
-    from paper_2412_11272_b200.binding import KvCache
-    parts = (s["k_pages"], s["v_pages"], s["k_scale"], s["v_scale"])
-    if s["fmt"] not in ("e4m3", "int8"):
-        parts = parts[:2] + (None, None)
-    return KvCache(*parts) if layer is None else KvCache(*(p if p is None else p[layer] for p in parts))
+def _caches(s):
+    """The framework's views of the state's caches (one, or one for each layer), kept beside them as a program keeps them."""
+    if "caches" not in s:
+        from paper_2412_11272_b200.binding import KvCache
+        parts = [s["k_pages"], s["v_pages"]] + ([s["k_scale"], s["v_scale"]] if s["fmt"] in ("e4m3", "int8") else [])
+        s["caches"] = [KvCache(*layer) for layer in (zip(*parts) if s["op"] == "reorder" else [parts])]
+    return s["caches"]
 
 
 def _rows_of(s):
@@ -311,7 +312,7 @@ def _values(pages, scale, page, at):
 
 def _attend(s):
     if own:
-        return _decoder(s).wf_tree_attention(_cache(s), s["table"], s["cu"], s["start"], s["q"], max_rows=s["rows"], max_len=s["most"],
+        return _decoder(s).wf_tree_attention(_caches(s)[0], s["table"], s["cu"], s["start"], s["q"], max_rows=s["rows"], max_len=s["most"],
                                              tail=s["tail"], mask=s["mask"])
     B, Hk, G, D = s["seqs"], s["kv_heads"], s["heads"] // s["kv_heads"], s["dim"]
     scaled = s["fmt"] in ("e4m3", "int8")
@@ -348,7 +349,7 @@ def _attend(s):
 def _store(s):
     """New keys and values into the cache, and the same rows read back (as a prompt's attention takes them)."""
     if own:
-        d, cache = _decoder(s), _cache(s)
+        d, cache = _decoder(s), _caches(s)[0]
         d.wf_cache_write(cache, s["table"], s["cu"], s["start"], s["k"], s["v"])
         return d.wf_cache_read(cache, s["table"], s["cu"], s["start"], s["n"])
     seq, _, pos = _rows_of(s)
@@ -392,7 +393,7 @@ def _select(s):
 def _reorder(s):
     B, W = s["seqs"], s["beams"]
     if own:
-        caches = [_cache(s, i) for i in range(s["layers"])] if s["page"] else []
+        caches = _caches(s) if s["page"] else []
         states = [s["history"]] if s["page"] else [s["history"]] + [r[:, :s["live"] // 4] for r in s["rows"].unbind(0)]
         _decoder(s).wf_beam_reorder(s["parents"], states=states, caches=caches, page_table=s["table"] if s["page"] else None,
                                     lengths=s["lengths"] if s["page"] else None)
