@@ -345,6 +345,106 @@ wf_status wf_beam_pruner_destroy(wf_beam_pruner *p);
 wf_status wf_attention_f32_static(const float *qkv, const int *cu_seqlens, int B, int d_model,
                                   float *out, void *stream);
 
+/* ---- Operators of the decoding stage (Sec. 3.2 "Operations": prompt prefill, then beam-search
+ * decoding over the encoder's output; Sec. 4.3.2).  The decoder's own GEMMs are the caller's; these
+ * are the pieces in between: a paged key/value cache that is quantised as it is written, attention
+ * of beams or of a tree of drafted tokens over it, beam selection and the reordering of states.
+ *
+ * A wf_decoder handle is host memory only: it holds the configuration and the last error message,
+ * no device memory and no weights, and is created without a GPU.  Every buffer and workspace is the
+ * caller's, so calls on several streams (or captured into several CUDA graphs) are independent as
+ * long as their buffers are.  No call synchronises, allocates or copies from host memory: all of
+ * them can be captured.  Calls work on the device that is current, which owns the buffers.  Sizes that decide the
+ * launch are host arguments; lengths, tables and parents are device arrays, read when the kernel
+ * runs.  What a kernel finds wrong in them (a page outside the cache, a position outside the page
+ * table, prefix sums that do not increase, a parent outside the beams) it passes over without
+ * touching memory, and records in `status` (dev int, may be NULL; bits are or-ed into it, the
+ * caller zeroes it):
+ *   1  a page index outside [0, n_pages): the position is treated as absent
+ *   2  prefix sums, a start or a length that do not fit the rows or the page table
+ *   4  a parent beam outside [0, n_beam): the row stays as it is
+ * A handle's calls come from one host thread at a time; distinct handles are independent. */
+typedef struct wf_decoder wf_decoder;
+
+/* Element type of a cache: WF_CACHE_PATH stores the path's own type (float32 or bfloat16);
+ * the other two store one byte per element and one bfloat16 scale s per vector of d_head elements
+ * (a key or a value of one position and head).  With a = max |x_i| over the vector:
+ *   WF_CACHE_E4M3   s = the least power of two with a / s <= 448;  code = x / s (exact) rounded to
+ *                   the nearest e4m3 value, ties to even
+ *   WF_CACHE_INT8   s = a / 127 (rounded to float32) rounded up to bfloat16;  code = the whole number
+ *                   nearest to x / s, ties to even, the quotient not rounded before
+ * s is at least 2^-126, and 1 if a = 0.  A vector that holds a NaN or an infinity gets s = NaN and
+ * zero codes, and reads back as NaN.  A stored element stands for code * s. */
+typedef enum { WF_CACHE_PATH = 0, WF_CACHE_E4M3 = 1, WF_CACHE_INT8 = 2 } wf_cache_format;
+
+/* n_kv_head divides n_head (query head h reads key/value head h / (n_head / n_kv_head)); d_head is
+ * 64 or 128; dtype (wf_dtype) is the type of queries, keys, values and outputs; page_size is a power
+ * of two from 16 to 256.  At most 1024 heads. */
+typedef struct {
+  int n_head, n_kv_head, d_head;
+  int dtype;
+  int cache_format;
+  int page_size;
+} wf_decoder_config;
+
+wf_status wf_decoder_create(const wf_decoder_config *cfg, wf_decoder **out);
+wf_status wf_decoder_destroy(wf_decoder *dec);
+const char *wf_decoder_last_error(const wf_decoder *dec);
+
+/* One layer's cache, caller-owned device memory, 16-byte aligned:
+ *   k, v              [n_pages][n_kv_head][page_size][d_head] elements or codes
+ *   k_scale, v_scale  bfloat16 [n_pages][n_kv_head][page_size]; NULL for WF_CACHE_PATH */
+typedef struct {
+  void *k, *v;
+  void *k_scale, *v_scale;
+  int n_pages;
+} wf_cache;
+
+/* New rows (tokens) of a batch of sequences, packed as everywhere in this library: sequence s has
+ * rows cu_rows[s] .. cu_rows[s + 1] of the row arrays, and its row i sits at cache position
+ * start[s] + i.  Position p is entry p % page_size of page page_table[s * table_stride + p / page_size].
+ * Rows at or behind cu_rows[n_seq] (padding of a batch with a fixed size) are neither read nor written.
+ *   n_seq, n_rows        host  sequences; rows that the row arrays have
+ *   cu_rows, start       dev   int [n_seq + 1], int [n_seq]
+ *   page_table           dev   int [n_seq][table_stride] */
+typedef struct {
+  int n_seq, n_rows;
+  const int *cu_rows, *start;
+  const int *page_table;
+  int table_stride;
+} wf_rows;
+
+/* wf_cache_write: quantises (or copies) the rows' keys and values into the cache.
+ *   k, v   dev  path dtype [n_rows][n_kv_head][d_head], heads contiguous, consecutive rows k_stride /
+ *               v_stride elements apart: for instance one layer's columns of what wf_cross_kv wrote
+ * wf_cache_read: the rows' values back, each rounded once to the path dtype, in the same layout.
+ * Pointers are 16-byte aligned and row strides whole multiples of 16 bytes. */
+wf_status wf_cache_write(wf_decoder *dec, const wf_cache *cache, const wf_rows *rows, const void *k,
+                         long k_stride, const void *v, long v_stride, int *status, void *stream);
+wf_status wf_cache_read(wf_decoder *dec, const wf_cache *cache, const wf_rows *rows, void *k, long k_stride,
+                        void *v, long v_stride, int *status, void *stream);
+
+/* wf_beam_reorder: after a selection every beam takes over the states of the beam it grew from:
+ * new[b][w] = old[b][parents[b][w]], in place; a negative parent leaves the row as it is.  One pass
+ * that moves only rows whose parent is another beam.
+ *   parents  dev   int [B][n_beam], n_beam <= 16
+ *   states   host  contiguous per-beam states (token histories, scores, unpaged caches): row b * n_beam + w
+ *                  of state i starts at ptr + (b * n_beam + w) * stride_bytes and its first row_bytes move
+ *   caches   host  paged caches (every layer's) that share one page table.  The beams of a sequence have
+ *                  one length: its pages that are full are shared, only their table entries move; the
+ *                  page being filled is each beam's own, and the positions that it holds so far are
+ *                  copied from the parent's.  (With n_beam pages set aside for every page index of a sequence no
+ *                  allocation is needed: a page is written only while it is its beam's last one.)
+ *   page_table, lengths  dev  int [B * n_beam][table_stride] (in place), int [B] positions held; NULL without caches
+ * No row of one state, cache or the table may overlap another one's. */
+typedef struct {
+  void *ptr;
+  long row_bytes, stride_bytes;
+} wf_beam_state;
+wf_status wf_beam_reorder(wf_decoder *dec, const int *parents, int B, int n_beam, const wf_beam_state *states,
+                          int n_states, const wf_cache *caches, int n_caches, int *page_table, int table_stride,
+                          const int *lengths, int *status, void *stream);
+
 #ifdef __cplusplus
 }
 #endif

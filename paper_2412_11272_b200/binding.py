@@ -49,6 +49,24 @@ class wf_weights(C.Structure):
                 ("lnp_g", C.c_void_p), ("lnp_b", C.c_void_p)]
 
 
+class wf_decoder_config(C.Structure):
+    _fields_ = [("n_head", C.c_int), ("n_kv_head", C.c_int), ("d_head", C.c_int), ("dtype", C.c_int), ("cache_format", C.c_int),
+                ("page_size", C.c_int)]
+
+
+class wf_cache(C.Structure):
+    _fields_ = [("k", C.c_void_p), ("v", C.c_void_p), ("k_scale", C.c_void_p), ("v_scale", C.c_void_p), ("n_pages", C.c_int)]
+
+
+class wf_rows(C.Structure):
+    _fields_ = [("n_seq", C.c_int), ("n_rows", C.c_int), ("cu_rows", C.c_void_p), ("start", C.c_void_p), ("page_table", C.c_void_p),
+                ("table_stride", C.c_int)]
+
+
+class wf_beam_state(C.Structure):
+    _fields_ = [("ptr", C.c_void_p), ("row_bytes", C.c_long), ("stride_bytes", C.c_long)]
+
+
 _PER_LAYER = ("ln1_g", "ln1_b", "wq", "bq", "wk", "wv", "bv", "wo", "bo", "ln2_g", "ln2_b",
               "w1", "b1", "w2", "b2")
 
@@ -56,7 +74,8 @@ EXPORTS = ("wf_encoder_create", "wf_logmel", "wf_encode", "wf_encode_raw_hush", 
            "wf_encoder_destroy", "wf_last_error", "wf_profile_enable", "wf_profile_read",
            "wf_plan", "wf_gemm_bf16", "wf_gemm_resid_bf16", "wf_ln_fold", "wf_gemm_ln_bf16", "wf_selftest_wait_timeout", "wf_attention", "wf_cross_kv", "wf_dtw",
            "wf_streams_create", "wf_streams_destroy", "wf_streams_length", "wf_streams_push", "wf_encode_streams", "wf_attention_f32_static",
-           "wf_beam_pruner_create", "wf_beam_pruner_step", "wf_beam_pruner_state", "wf_beam_pruner_destroy")
+           "wf_beam_pruner_create", "wf_beam_pruner_step", "wf_beam_pruner_state", "wf_beam_pruner_destroy",
+           "wf_decoder_create", "wf_decoder_destroy", "wf_decoder_last_error", "wf_cache_write", "wf_cache_read", "wf_beam_reorder")
 
 _lib = None
 
@@ -103,8 +122,16 @@ def load_library() -> C.CDLL:
     lib.wf_beam_pruner_step.argtypes = [vp, C.c_int]
     lib.wf_beam_pruner_state.argtypes = [vp, lp, ip, lp, lp]
     lib.wf_beam_pruner_destroy.argtypes = [vp]
+    lib.wf_decoder_create.argtypes = [C.POINTER(wf_decoder_config), C.POINTER(vp)]
+    lib.wf_decoder_destroy.argtypes = [vp]
+    lib.wf_decoder_last_error.argtypes = [vp]
+    lib.wf_decoder_last_error.restype = C.c_char_p
+    cp, rp = C.POINTER(wf_cache), C.POINTER(wf_rows)
+    lib.wf_cache_write.argtypes = [vp, cp, rp, vp, C.c_long, vp, C.c_long, vp, vp]
+    lib.wf_cache_read.argtypes = [vp, cp, rp, vp, C.c_long, vp, C.c_long, vp, vp]
+    lib.wf_beam_reorder.argtypes = [vp, vp, C.c_int, C.c_int, C.POINTER(wf_beam_state), C.c_int, cp, C.c_int, vp, C.c_int, vp, vp, vp]
     for name in EXPORTS:
-        if name != "wf_last_error":
+        if name not in ("wf_last_error", "wf_decoder_last_error"):
             getattr(lib, name).restype = C.c_int
     _lib = lib
     return lib
@@ -485,3 +512,199 @@ class BeamPruner:
             self.close()
         except Exception:
             pass
+
+
+# ---- operators of the decoding stage
+
+CACHE_FORMATS = {"path": 0, "e4m3": 1, "int8": 2}
+STATUS_BAD_PAGE, STATUS_BAD_ROWS, STATUS_BAD_PARENT = 1, 2, 4
+_INT, _U8, _F32, _BF16 = torch.int32, torch.uint8, torch.float32, torch.bfloat16
+
+
+def _refuse(message: str):
+    raise WfError(1, message)
+
+
+def _vector(t, name: str, device, dtype=_INT, n: int | None = None):
+    """Checks a contiguous device array of one type (and at least ``n`` elements); returns its address."""
+    if not isinstance(t, torch.Tensor) or t.dtype != dtype or t.device != device or not t.is_contiguous():
+        _refuse(f"{name} must be a contiguous {dtype} tensor on {device}")
+    if n is not None and t.numel() < n:
+        _refuse(f"{name} has {t.numel()} elements, {n} are needed")
+    return t.data_ptr()
+
+
+class KvCache:
+    """One decoder layer's paged keys and values: tensors the caller owns (see ``Decoder.cache``).
+    k, v: [n_pages, n_kv_head, page_size, d_head]; k_scale, v_scale: bfloat16 [n_pages, n_kv_head, page_size], None for a
+    cache of the path's own type."""
+
+    __slots__ = ("k", "v", "k_scale", "v_scale", "device", "shape", "c")
+
+    def __init__(self, k: torch.Tensor, v: torch.Tensor, k_scale: torch.Tensor | None = None, v_scale: torch.Tensor | None = None):
+        if k.shape != v.shape or k.dim() != 4 or k.dtype != v.dtype or k.device != v.device:
+            _refuse("k and v must be alike: [n_pages, n_kv_head, page_size, d_head]")
+        if not (k.is_contiguous() and v.is_contiguous()):
+            _refuse("cache pages must be contiguous")
+        if (k_scale is None) != (v_scale is None):
+            _refuse("k_scale and v_scale go together")
+        for s in (k_scale, v_scale):
+            if s is not None and (s.shape != k.shape[:3] or s.dtype != _BF16 or s.device != k.device or not s.is_contiguous()):
+                _refuse("scales must be contiguous bfloat16 [n_pages, n_kv_head, page_size] beside their pages")
+        self.k, self.v, self.k_scale, self.v_scale, self.device, self.shape = k, v, k_scale, v_scale, k.device, tuple(k.shape)
+        self.c = wf_cache(k.data_ptr(), v.data_ptr(), None if k_scale is None else k_scale.data_ptr(),
+                          None if v_scale is None else v_scale.data_ptr(), k.shape[0])
+
+
+class Decoder:
+    """Owns one ``wf_decoder`` handle: the heads, element types and page size of a decoder's attention.  The handle
+    holds no device memory; creating one needs no GPU.  Device arrays are int32 unless stated; every method enqueues
+    on ``stream`` (default: the current stream of the tensors' device) and returns without synchronising.  ``status``
+    (an int32 device tensor of one element, zeroed by the caller) collects what kernels find wrong in device arrays."""
+
+    def __init__(self, n_head: int, n_kv_head: int | None = None, d_head: int = 64, dtype: str = "bf16", cache_format: str = "path",
+                 page_size: int = 64):
+        self.handle = None
+        self.lib = load_library()
+        if dtype not in ("bf16", "f32") or cache_format not in CACHE_FORMATS:
+            _refuse(f"dtype is bf16 or f32, cache_format one of {', '.join(CACHE_FORMATS)}")
+        self.n_head, self.n_kv_head, self.d_head, self.page_size = int(n_head), int(n_kv_head or n_head), int(d_head), int(page_size)
+        self.dtype, self.cache_format = dtype, cache_format
+        self.torch_dtype = _BF16 if dtype == "bf16" else _F32
+        self.code_dtype = {"path": self.torch_dtype, "e4m3": torch.float8_e4m3fn, "int8": torch.int8}[cache_format]
+        cfg = wf_decoder_config(self.n_head, self.n_kv_head, self.d_head, WF_BF16 if dtype == "bf16" else WF_F32,
+                                CACHE_FORMATS[cache_format], self.page_size)
+        handle = C.c_void_p()
+        st = self.lib.wf_decoder_create(C.byref(cfg), C.byref(handle))
+        self.handle = handle
+        if st != 0:
+            msg = self.lib.wf_decoder_last_error(handle).decode() if handle else "create failed"
+            self.close()
+            raise WfError(st, msg)
+
+    def _check(self, st: int):
+        if st != 0:
+            raise WfError(st, self.lib.wf_decoder_last_error(self.handle).decode())
+
+    def close(self):
+        if getattr(self, "handle", None):
+            self.lib.wf_decoder_destroy(self.handle)
+            self.handle = None
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+    # -- helpers
+    def cache(self, n_pages: int, device="cuda") -> KvCache:
+        """A zeroed cache of ``n_pages`` pages for one layer."""
+        shape = (n_pages, self.n_kv_head, self.page_size, self.d_head)
+        k, v = (torch.zeros(shape, dtype=torch.uint8 if self.code_dtype.itemsize == 1 else self.code_dtype, device=device).view(self.code_dtype)
+                for _ in range(2))
+        if self.cache_format == "path":
+            return KvCache(k, v)
+        return KvCache(k, v, *(torch.ones(shape[:3], dtype=_BF16, device=device) for _ in range(2)))
+
+    def _cache(self, cache: KvCache):
+        if cache.shape[1:] != (self.n_kv_head, self.page_size, self.d_head) or cache.k.dtype != self.code_dtype:
+            _refuse(f"the cache is {cache.k.dtype} {cache.shape}, this decoder's pages are {self.code_dtype} "
+                    f"[n, {self.n_kv_head}, {self.page_size}, {self.d_head}]")
+        if (cache.k_scale is None) != (self.cache_format == "path"):
+            _refuse("scales belong to quantised caches, and only to them")
+        if cache.device.type != "cuda":
+            _refuse("the cache must be in device memory")
+        return cache.c
+
+    def _rows(self, page_table, cu_rows, start, n_rows, device):
+        n_seq = cu_rows.numel() - 1
+        if n_seq < 0 or page_table.dim() != 2 or page_table.shape[0] < n_seq:
+            _refuse("cu_rows has n_seq + 1 entries, page_table [n_seq, pages]")
+        return wf_rows(n_seq, n_rows, _vector(cu_rows, "cu_rows", device), _vector(start, "start", device, n=n_seq),
+                       _vector(page_table, "page_table", device), page_table.shape[1])
+
+    def _vectors(self, t, name, device, heads):
+        """A [n, heads, d_head] tensor with contiguous rows: (address, row stride)."""
+        if t.dtype != self.torch_dtype or t.device != device or t.dim() != 3 or t.shape[1] != heads or t.shape[2] != self.d_head:
+            _refuse(f"{name} must be {self.torch_dtype} [rows, {heads}, {self.d_head}] on {device}")
+        s = t.stride()
+        if s[2] != 1 or (heads > 1 and s[1] != self.d_head):
+            _refuse(f"{name}: the heads of a row must lie one after the other")
+        return t.data_ptr(), s[0] if t.shape[0] > 1 else max(s[0], heads * self.d_head)
+
+    @staticmethod
+    def _status(status, device):
+        return None if status is None else _vector(status, "status", device, n=1)
+
+    def _call(self, fn, device, stream, *args):
+        """Runs one entry point with the tensors' device current, on its stream."""
+        if torch.cuda.current_device() == device.index:
+            s = stream if stream is not None else torch.cuda.current_stream()
+            st = fn(self.handle, *args, s.cuda_stream)
+        else:
+            with torch.cuda.device(device):
+                s = stream if stream is not None else torch.cuda.current_stream()
+                st = fn(self.handle, *args, s.cuda_stream)
+        if st != 0:
+            self._check(st)
+
+    # -- entry points (same names as the C ABI)
+    def wf_cache_write(self, cache: KvCache, page_table, cu_rows, start, k: torch.Tensor, v: torch.Tensor, status=None, stream=None):
+        """Stores keys and values [n, n_kv_head, d_head] of new rows (row stride free) at their sequences' positions
+        start[s], start[s] + 1, ..."""
+        c, device = self._cache(cache), cache.device
+        if k.shape[0] != v.shape[0]:
+            _refuse("k and v have different numbers of rows")
+        (kp, ks), (vp, vs) = self._vectors(k, "k", device, self.n_kv_head), self._vectors(v, "v", device, self.n_kv_head)
+        rows = self._rows(page_table, cu_rows, start, k.shape[0], device)
+        self._call(self.lib.wf_cache_write, device, stream, c, rows, kp, ks, vp, vs, self._status(status, device))
+
+    def wf_cache_read(self, cache: KvCache, page_table, cu_rows, start, n_rows: int, k=None, v=None, status=None, stream=None):
+        """The values of the rows at positions start[s], start[s] + 1, ... of every sequence: (k, v) [n_rows, n_kv_head, d_head]
+        in the path's type.  Rows at or behind cu_rows[-1] are left as they are."""
+        c, device = self._cache(cache), cache.device
+        shape = (n_rows, self.n_kv_head, self.d_head)
+        k = torch.empty(shape, dtype=self.torch_dtype, device=device) if k is None else k
+        v = torch.empty(shape, dtype=self.torch_dtype, device=device) if v is None else v
+        if k.shape[0] < n_rows or v.shape[0] < n_rows:
+            _refuse("k and v must have n_rows rows")
+        (kp, ks), (vp, vs) = self._vectors(k, "k", device, self.n_kv_head), self._vectors(v, "v", device, self.n_kv_head)
+        rows = self._rows(page_table, cu_rows, start, n_rows, device)
+        self._call(self.lib.wf_cache_read, device, stream, c, rows, kp, ks, vp, vs, self._status(status, device))
+        return k, v
+
+    def wf_beam_reorder(self, parents: torch.Tensor, states=(), caches=(), page_table=None, lengths=None, status=None, stream=None):
+        """Moves every beam's states to the beams that grew from it, in place.  parents: [B, n_beam] (negative: stays).
+        states: tensors [B * n_beam, ...] whose rows are contiguous (row stride free); caches: paged caches that share
+        ``page_table`` [B * n_beam, pages], the beams of a sequence holding ``lengths`` [B] positions."""
+        device = parents.device
+        if parents.dim() != 2 or device.type != "cuda":
+            _refuse("parents must be a [B, n_beam] tensor in device memory")
+        B, W = parents.shape
+        pp = _vector(parents, "parents", device)
+        state_array = (wf_beam_state * len(states))()
+        for i, t in enumerate(states):
+            if t.device != device or t.dim() < 1 or t.shape[0] != B * W:
+                _refuse(f"state {i} must be a [{B * W}, ...] tensor on {device}")
+            row = t[0] if t.shape[0] else t
+            if not row.is_contiguous():
+                _refuse(f"state {i}: the elements of a row must be contiguous")
+            size = row.numel() * t.element_size() if t.shape[0] else 0
+            step = t.stride(0) * t.element_size() if t.shape[0] > 1 else size
+            if step < size:
+                _refuse(f"state {i}: rows overlap")
+            state_array[i] = wf_beam_state(t.data_ptr(), size, step)
+        cache_array = (wf_cache * len(caches))()
+        table = stride = lens = None
+        for i, c in enumerate(caches):
+            cache_array[i] = self._cache(c)
+            if c.device != device:
+                _refuse("caches and parents are on different devices")
+        if caches:
+            if page_table is None or lengths is None or page_table.dim() != 2 or page_table.shape[0] != B * W:
+                _refuse("paged caches need page_table [B * n_beam, pages] and lengths [B]")
+            table, stride = _vector(page_table, "page_table", device), page_table.shape[1]
+            lens = _vector(lengths, "lengths", device, n=B)
+        self._call(self.lib.wf_beam_reorder, device, stream, pp, B, W, state_array, len(states), cache_array, len(caches), table, stride or 0,
+                   lens, self._status(status, device))

@@ -1,0 +1,220 @@
+// C entry points of the decoding-stage operators: argument checks and launches.
+#include <algorithm>
+#include <cstdarg>
+#include <cstdio>
+#include <new>
+
+#include "wf_decoder.h"
+
+using namespace wf;
+
+struct wf_decoder {
+  wf_decoder_config cfg;
+  char err[512];
+};
+
+namespace {
+
+wf_status fail(wf_decoder* d, wf_status st, const char* fmt, ...) {
+  va_list ap;
+  va_start(ap, fmt);
+  vsnprintf(d->err, sizeof(d->err), fmt, ap);
+  va_end(ap);
+  return st;
+}
+
+bool aligned16(const void* p) { return ((uintptr_t)p & 15) == 0; }
+
+int path_bytes(const wf_decoder_config& c) { return c.dtype == WF_BF16 ? 2 : 4; }
+int code_bytes(const wf_decoder_config& c) { return c.cache_format == WF_CACHE_PATH ? path_bytes(c) : 1; }
+int log2_of(int v) {
+  int s = 0;
+  while ((1 << s) < v) ++s;
+  return s;
+}
+
+wf_status cuda_result(wf_decoder* d, const char* what, cudaError_t e) {
+  if (e == cudaSuccess) return WF_OK;
+  return fail(d, WF_ERR_CUDA, "%s: %s", what, cudaGetErrorString(e));
+}
+
+// The checks that every cache operator makes.
+wf_status check_cache(wf_decoder* d, const char* what, const wf_cache* c) {
+  if (!c || !c->k || !c->v || c->n_pages < 1) return fail(d, WF_ERR_INVALID_ARG, "%s: NULL cache or no pages", what);
+  if (!aligned16(c->k) || !aligned16(c->v)) return fail(d, WF_ERR_INVALID_ARG, "%s: cache pages must be 16-byte aligned", what);
+  if (d->cfg.cache_format != WF_CACHE_PATH) {
+    if (!c->k_scale || !c->v_scale) return fail(d, WF_ERR_INVALID_ARG, "%s: a quantised cache needs scales", what);
+    if (!aligned16(c->k_scale) || !aligned16(c->v_scale))
+      return fail(d, WF_ERR_INVALID_ARG, "%s: scales must be 16-byte aligned", what);
+  }
+  return WF_OK;
+}
+
+wf_status check_rows(wf_decoder* d, const char* what, const wf_rows* r) {
+  if (!r || r->n_seq < 0 || r->n_rows < 0) return fail(d, WF_ERR_INVALID_ARG, "%s: NULL rows or a negative size", what);
+  if (r->n_seq == 0 || r->n_rows == 0) return WF_OK;
+  if (!r->cu_rows || !r->start || !r->page_table || r->table_stride < 1)
+    return fail(d, WF_ERR_INVALID_ARG, "%s: NULL prefix sums, starts or page table", what);
+  if (r->n_rows > (1 << 27)) return fail(d, WF_ERR_CAPACITY, "%s: more than 2^27 rows", what);
+  return WF_OK;
+}
+
+CacheView view_of(const wf_decoder* d, const wf_cache* c) {
+  const bool q = d->cfg.cache_format != WF_CACHE_PATH;
+  return CacheView{c->k, c->v, q ? (__nv_bfloat16*)c->k_scale : nullptr, q ? (__nv_bfloat16*)c->v_scale : nullptr, c->n_pages,
+                   d->cfg.n_kv_head, log2_of(d->cfg.page_size)};
+}
+RowsView view_of(const wf_rows* r) { return RowsView{r->n_seq, r->n_rows, r->cu_rows, r->start, r->page_table, r->table_stride}; }
+
+wf_status check_vectors(wf_decoder* d, const char* what, const void* k, long k_stride, const void* v, long v_stride) {
+  const int esz = path_bytes(d->cfg);
+  const long row = (long)d->cfg.n_kv_head * d->cfg.d_head;
+  if (!k || !v) return fail(d, WF_ERR_INVALID_ARG, "%s: NULL keys or values", what);
+  if (!aligned16(k) || !aligned16(v) || k_stride * esz % 16 || v_stride * esz % 16)
+    return fail(d, WF_ERR_INVALID_ARG, "%s: keys and values need 16-byte aligned pointers and row strides", what);
+  if (k_stride < row || v_stride < row)
+    return fail(d, WF_ERR_INVALID_ARG, "%s: a row stride is shorter than a row of %ld elements", what, row);
+  return WF_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+wf_status wf_decoder_create(const wf_decoder_config* cfg, wf_decoder** out) {
+  if (!cfg || !out) return WF_ERR_INVALID_ARG;
+  *out = nullptr;
+  wf_decoder* d = new (std::nothrow) wf_decoder();
+  if (!d) return WF_ERR_INVALID_ARG;
+  d->cfg = *cfg;
+  d->err[0] = 0;
+  *out = d;  // returned even on failure so that the caller can read the message, then destroy
+  const wf_decoder_config& c = d->cfg;
+  if (c.n_head < 1 || c.n_head > 1024 || c.n_kv_head < 1 || c.n_head % c.n_kv_head)
+    return fail(d, WF_ERR_INVALID_ARG, "n_kv_head must divide n_head (1 .. 1024)");
+  if (c.d_head != 64 && c.d_head != 128) return fail(d, WF_ERR_INVALID_ARG, "d_head must be 64 or 128");
+  if (c.dtype != WF_F32 && c.dtype != WF_BF16) return fail(d, WF_ERR_INVALID_ARG, "unknown dtype");
+  if (c.cache_format < WF_CACHE_PATH || c.cache_format > WF_CACHE_INT8)
+    return fail(d, WF_ERR_INVALID_ARG, "unknown cache format");
+  if (c.page_size < 16 || c.page_size > 256 || (c.page_size & (c.page_size - 1)))
+    return fail(d, WF_ERR_INVALID_ARG, "page_size must be a power of two from 16 to 256");
+  return WF_OK;
+}
+
+wf_status wf_decoder_destroy(wf_decoder* d) {
+  delete d;
+  return WF_OK;
+}
+
+const char* wf_decoder_last_error(const wf_decoder* d) { return d ? d->err : "null decoder"; }
+
+wf_status wf_cache_write(wf_decoder* d, const wf_cache* cache, const wf_rows* rows, const void* k, long k_stride, const void* v,
+                         long v_stride, int* status, void* stream) {
+  if (!d) return WF_ERR_INVALID_ARG;
+  wf_status st = check_rows(d, "wf_cache_write", rows);
+  if (st != WF_OK) return st;
+  st = check_cache(d, "wf_cache_write", cache);
+  if (st != WF_OK) return st;
+  if (rows->n_seq == 0 || rows->n_rows == 0) return WF_OK;
+  st = check_vectors(d, "wf_cache_write", k, k_stride, v, v_stride);
+  if (st != WF_OK) return st;
+  return cuda_result(d, "wf_cache_write",
+                     launch_cache_write(view_of(d, cache), view_of(rows), d->cfg.d_head, d->cfg.dtype, d->cfg.cache_format, k, k_stride,
+                                        v, v_stride, status, (cudaStream_t)stream));
+}
+
+wf_status wf_cache_read(wf_decoder* d, const wf_cache* cache, const wf_rows* rows, void* k, long k_stride, void* v, long v_stride,
+                        int* status, void* stream) {
+  if (!d) return WF_ERR_INVALID_ARG;
+  wf_status st = check_rows(d, "wf_cache_read", rows);
+  if (st != WF_OK) return st;
+  st = check_cache(d, "wf_cache_read", cache);
+  if (st != WF_OK) return st;
+  if (rows->n_seq == 0 || rows->n_rows == 0) return WF_OK;
+  st = check_vectors(d, "wf_cache_read", k, k_stride, v, v_stride);
+  if (st != WF_OK) return st;
+  return cuda_result(d, "wf_cache_read",
+                     launch_cache_read(view_of(d, cache), view_of(rows), d->cfg.d_head, d->cfg.dtype, d->cfg.cache_format, k, k_stride, v,
+                                       v_stride, status, (cudaStream_t)stream));
+}
+
+wf_status wf_beam_reorder(wf_decoder* d, const int* parents, int B, int n_beam, const wf_beam_state* states, int n_states,
+                          const wf_cache* caches, int n_caches, int* page_table, int table_stride, const int* lengths, int* status,
+                          void* stream) {
+  if (!d) return WF_ERR_INVALID_ARG;
+  if (B < 0 || n_beam < 1 || n_beam > kMaxBeams || n_states < 0 || n_caches < 0)
+    return fail(d, WF_ERR_INVALID_ARG, "wf_beam_reorder: a negative size, or n_beam outside 1 .. %d", kMaxBeams);
+  if (B > 65535) return fail(d, WF_ERR_CAPACITY, "wf_beam_reorder: more than 65535 sequences");
+  if ((n_states > 0 && !states) || (n_caches > 0 && (!caches || !page_table || !lengths || table_stride < 1)) || (B > 0 && !parents))
+    return fail(d, WF_ERR_INVALID_ARG, "wf_beam_reorder: NULL argument");
+  for (int i = 0; i < n_states; ++i) {
+    const wf_beam_state& x = states[i];
+    if (x.row_bytes < 0 || x.stride_bytes < x.row_bytes || (x.row_bytes > 0 && !x.ptr))
+      return fail(d, WF_ERR_INVALID_ARG, "wf_beam_reorder: state %d has %ld bytes every %ld", i, x.row_bytes, x.stride_bytes);
+    if (x.row_bytes > (1L << 36)) return fail(d, WF_ERR_CAPACITY, "wf_beam_reorder: a row of more than 2^36 bytes");
+  }
+  for (int i = 0; i < n_caches; ++i) {
+    const wf_status st = check_cache(d, "wf_beam_reorder", caches + i);
+    if (st != WF_OK) return st;
+    if (caches[i].n_pages != caches[0].n_pages)
+      return fail(d, WF_ERR_INVALID_ARG, "wf_beam_reorder: caches that share a page table have the same number of pages");
+  }
+  if (B == 0 || n_beam == 1) return WF_OK;  // one beam can only have grown from itself
+  const wf_decoder_config& c = d->cfg;
+  ReorderPlan p{};
+  p.parents = parents;
+  p.n_beam = n_beam;
+  p.page_table = page_table;
+  p.table_stride = table_stride;
+  p.lengths = lengths;
+  p.page_shift = log2_of(c.page_size);
+  p.head_units = c.page_size * c.d_head * code_bytes(c) / 16;
+  p.n_kv_head = c.n_kv_head;
+  p.n_pages = n_caches > 0 ? caches[0].n_pages : 0;
+  p.status = status;
+  long blocks = 0;
+  cudaError_t e = cudaSuccess;
+  auto flush = [&]() {
+    if (p.n_items > 0 && e == cudaSuccess) e = launch_beam_reorder(p, B, (int)blocks, (cudaStream_t)stream);
+    p.n_items = 0;
+    blocks = 0;
+  };
+  auto add = [&](ReorderItem it, long threads) {
+    const long need = (threads + kReorderThreads - 1) / kReorderThreads;
+    if (need == 0) return;
+    if (p.n_items == kReorderItems || blocks + need > (1L << 30)) flush();
+    it.first_block = (int)blocks;
+    p.item[p.n_items++] = it;
+    blocks += need;
+  };
+  for (int i = 0; i < n_caches; ++i)
+    for (int side = 0; side < 2; ++side) {
+      ReorderItem it{};
+      it.kind = 1;
+      it.ptr = (char*)(side == 0 ? caches[i].k : caches[i].v);
+      it.scale = c.cache_format == WF_CACHE_PATH ? nullptr : (__nv_bfloat16*)(side == 0 ? caches[i].k_scale : caches[i].v_scale);
+      it.units = (long)p.head_units * c.n_kv_head;
+      it.stride = it.units * 16;
+      add(it, it.units + (it.scale ? (long)c.n_kv_head * c.page_size : 0));
+    }
+  if (n_caches > 0) {
+    ReorderItem it{};
+    it.kind = 2;
+    it.units = table_stride;
+    add(it, table_stride);
+  }
+  for (int i = 0; i < n_states; ++i) {
+    ReorderItem it{};
+    const uintptr_t bits = (uintptr_t)states[i].ptr | (uintptr_t)states[i].row_bytes | (uintptr_t)states[i].stride_bytes;
+    it.kind = 0;
+    it.ptr = (char*)states[i].ptr;
+    it.stride = states[i].stride_bytes;
+    it.unit = bits % 16 == 0 ? 16 : bits % 4 == 0 ? 4 : 1;
+    it.units = states[i].row_bytes / it.unit;
+    add(it, it.units);
+  }
+  flush();
+  return cuda_result(d, "wf_beam_reorder", e);
+}
+
+}  // extern "C"
