@@ -28,6 +28,8 @@
 #ifndef WF_ENCODER_H
 #define WF_ENCODER_H
 
+#include <stddef.h>
+
 #ifdef __cplusplus
 extern "C" {
 #endif
@@ -423,6 +425,39 @@ wf_status wf_cache_write(wf_decoder *dec, const wf_cache *cache, const wf_rows *
                          long k_stride, const void *v, long v_stride, int *status, void *stream);
 wf_status wf_cache_read(wf_decoder *dec, const wf_cache *cache, const wf_rows *rows, void *k, long k_stride,
                         void *v, long v_stride, int *status, void *stream);
+
+/* Which positions of its sequence a query row sees besides the start[s] committed ones. */
+typedef enum {
+  WF_TAIL_NONE = 0,    /* none: the rows are not in the cache.  Beams over one buffer's cross-attention cache */
+  WF_TAIL_CAUSAL = 1,  /* row i sees the batch rows 0 .. i of its sequence: a prompt, a chain of drafts, a single token */
+  WF_TAIL_MASK = 2     /* row i sees batch row t if bit t of its mask is set: a tree of drafted tokens */
+} wf_tail;
+
+/* wf_tree_attention: attention of the rows' queries over their sequences' cache.  Row i of sequence s
+ * sees the positions [0, start[s]), and with a tail those of the batch's own rows, start[s] + t (written with
+ * wf_cache_write before):
+ *   out_ih = sum_j p_ihj v_jg,  p_ih = softmax over the visible j of (scale <q_ih, k_jg>),  g = h n_kv_head / n_head
+ *   lse_ih = log sum_j exp(scale <q_ih, k_jg>)
+ * A row that sees nothing gets out = 0 and lse = -infinity.  What a row does not see has no influence
+ * on it, whatever it holds (NaN included).  Scores, softmax and sums are float32, keys and values are the stored ones
+ * (code * s).  WF_BF16: the products run on the tensor cores; a probability is rounded once, to
+ * bfloat16 (WF_CACHE_PATH) or to float16 after multiplication with its value's scale (quantised caches).
+ *   q          dev   path dtype [n_rows][n_head][d_head], rows q_stride elements apart
+ *   tail       host  wf_tail;  mask  dev  uint32 [n_rows][mask_words], bit t % 32 of word t / 32 (WF_TAIL_MASK only)
+ *   max_rows   host  no sequence has more rows in this call (mask_words * 32 >= max_rows)
+ *   max_len    host  no sequence has more positions, its own rows included; at most table_stride * page_size.
+ *                    Longer ones are cut there and reported.
+ *   out        dev   path dtype [n_rows][n_head][d_head], rows out_stride elements apart
+ *   lse        dev   float32 [n_rows][n_head], or NULL
+ *   workspace  dev   16-byte aligned, at least the bytes that wf_tree_attention_workspace gives for the same sizes (may be
+ *                    0: then NULL).  Nothing in it has to be set and nothing is kept in it between calls.
+ * Pointers are 16-byte aligned and row strides whole multiples of 16 bytes.  Results do not depend on the
+ * order in which blocks run.  n_seq <= 65535. */
+wf_status wf_tree_attention_workspace(wf_decoder *dec, int n_seq, int n_rows, int max_rows, int max_len, size_t *bytes);
+wf_status wf_tree_attention(wf_decoder *dec, const wf_cache *cache, const wf_rows *rows, const void *q, long q_stride,
+                            float scale, int tail, const unsigned *mask, int mask_words, int max_rows, int max_len,
+                            void *out, long out_stride, float *lse, void *workspace, size_t workspace_bytes,
+                            int *status, void *stream);
 
 /* wf_beam_reorder: after a selection every beam takes over the states of the beam it grew from:
  * new[b][w] = old[b][parents[b][w]], in place; a negative parent leaves the row as it is.  One pass

@@ -75,7 +75,8 @@ EXPORTS = ("wf_encoder_create", "wf_logmel", "wf_encode", "wf_encode_raw_hush", 
            "wf_plan", "wf_gemm_bf16", "wf_gemm_resid_bf16", "wf_ln_fold", "wf_gemm_ln_bf16", "wf_selftest_wait_timeout", "wf_attention", "wf_cross_kv", "wf_dtw",
            "wf_streams_create", "wf_streams_destroy", "wf_streams_length", "wf_streams_push", "wf_encode_streams", "wf_attention_f32_static",
            "wf_beam_pruner_create", "wf_beam_pruner_step", "wf_beam_pruner_state", "wf_beam_pruner_destroy",
-           "wf_decoder_create", "wf_decoder_destroy", "wf_decoder_last_error", "wf_cache_write", "wf_cache_read", "wf_beam_reorder")
+           "wf_decoder_create", "wf_decoder_destroy", "wf_decoder_last_error", "wf_cache_write", "wf_cache_read",
+           "wf_tree_attention_workspace", "wf_tree_attention", "wf_beam_reorder")
 
 _lib = None
 
@@ -129,6 +130,9 @@ def load_library() -> C.CDLL:
     cp, rp = C.POINTER(wf_cache), C.POINTER(wf_rows)
     lib.wf_cache_write.argtypes = [vp, cp, rp, vp, C.c_long, vp, C.c_long, vp, vp]
     lib.wf_cache_read.argtypes = [vp, cp, rp, vp, C.c_long, vp, C.c_long, vp, vp]
+    lib.wf_tree_attention_workspace.argtypes = [vp, C.c_int, C.c_int, C.c_int, C.c_int, C.POINTER(C.c_size_t)]
+    lib.wf_tree_attention.argtypes = [vp, cp, rp, vp, C.c_long, C.c_float, C.c_int, vp, C.c_int, C.c_int, C.c_int, vp, C.c_long, vp, vp,
+                                      C.c_size_t, vp, vp]
     lib.wf_beam_reorder.argtypes = [vp, vp, C.c_int, C.c_int, C.POINTER(wf_beam_state), C.c_int, cp, C.c_int, vp, C.c_int, vp, vp, vp]
     for name in EXPORTS:
         if name not in ("wf_last_error", "wf_decoder_last_error"):
@@ -516,6 +520,7 @@ class BeamPruner:
 
 # ---- operators of the decoding stage
 
+TAILS = {"none": 0, "causal": 1, "mask": 2, "tree": 2}
 CACHE_FORMATS = {"path": 0, "e4m3": 1, "int8": 2}
 STATUS_BAD_PAGE, STATUS_BAD_ROWS, STATUS_BAD_PARENT = 1, 2, 4
 _INT, _U8, _F32, _BF16 = torch.int32, torch.uint8, torch.float32, torch.bfloat16
@@ -565,6 +570,7 @@ class Decoder:
     def __init__(self, n_head: int, n_kv_head: int | None = None, d_head: int = 64, dtype: str = "bf16", cache_format: str = "path",
                  page_size: int = 64):
         self.handle = None
+        self._workspace_bytes = {}
         self.lib = load_library()
         if dtype not in ("bf16", "f32") or cache_format not in CACHE_FORMATS:
             _refuse(f"dtype is bf16 or f32, cache_format one of {', '.join(CACHE_FORMATS)}")
@@ -673,6 +679,55 @@ class Decoder:
         rows = self._rows(page_table, cu_rows, start, n_rows, device)
         self._call(self.lib.wf_cache_read, device, stream, c, rows, kp, ks, vp, vs, self._status(status, device))
         return k, v
+
+    def wf_tree_attention(self, cache: KvCache, page_table, cu_rows, start, q: torch.Tensor, max_rows: int, max_len: int | None = None,
+                          tail: str = "causal", mask=None, scale: float | None = None, out=None, lse=None, workspace=None, status=None,
+                          stream=None):
+        """Attention of queries [n_rows, n_head, d_head] over their sequences' cache; returns (out, lse float32 [n_rows, n_head]).
+        ``tail``: "none" (the start[s] committed positions alone), "causal" (and the sequence's rows up to the query's own) or "mask"
+        (and those rows t whose bit is set in the query's row of ``mask``, int32 or uint32 [n_rows, words]; "tree" is the same).
+        ``max_rows`` and ``max_len`` bound the rows and the positions (rows included) of any sequence.  ``scale`` defaults to
+        d_head ** -0.5.  ``workspace``: a uint8 tensor of ``tree_attention_workspace`` bytes, allocated per call if not given."""
+        c, device = self._cache(cache), cache.device
+        n = q.shape[0]
+        qp, qs = self._vectors(q, "q", device, self.n_head)
+        rows = self._rows(page_table, cu_rows, start, n, device)
+        if tail not in TAILS:
+            _refuse(f"tail is one of {', '.join(TAILS)}")
+        mp, words = None, 0
+        if TAILS[tail] == 2:
+            if mask is None or mask.dim() != 2 or mask.shape[0] < n or mask.dtype not in (_INT, torch.uint32):
+                _refuse("a tree needs mask: int32 or uint32 [n_rows, words]")
+            mp, words = _vector(mask, "mask", device, mask.dtype), mask.shape[1]
+        if max_len is None:
+            max_len = page_table.shape[1] * self.page_size
+        if out is None:
+            out = torch.empty((n, self.n_head, self.d_head), dtype=self.torch_dtype, device=device)
+        elif out.shape[0] < n:
+            _refuse("out must have the rows of q")
+        op, os_ = self._vectors(out, "out", device, self.n_head)
+        if lse is None:
+            lse = torch.empty((n, self.n_head), dtype=_F32, device=device)
+        lp = _vector(lse, "lse", device, _F32, n * self.n_head)
+        need = self.tree_attention_workspace(rows.n_seq, n, max_rows, max_len, device)
+        if workspace is None and need:
+            workspace = torch.empty(need, dtype=_U8, device=device)
+        wp, have = (None, 0) if workspace is None else (_vector(workspace, "workspace", device, _U8), workspace.numel())
+        self._call(self.lib.wf_tree_attention, device, stream, c, rows, qp, qs, self.d_head ** -0.5 if scale is None else scale, TAILS[tail],
+                   mp, words, max_rows, max_len, op, os_, lp, wp, have, self._status(status, device))
+        return out, lse
+
+    def tree_attention_workspace(self, n_seq: int, n_rows: int, max_rows: int, max_len: int, device="cuda") -> int:
+        """Bytes of workspace of ``wf_tree_attention`` for these sizes (a function of them and the device alone)."""
+        key = (n_seq, n_rows, max_rows, max_len, device)
+        if key not in self._workspace_bytes:
+            n = C.c_size_t()
+            with torch.cuda.device(device):
+                self._check(self.lib.wf_tree_attention_workspace(self.handle, n_seq, n_rows, max_rows, max_len, C.byref(n)))
+            if len(self._workspace_bytes) > 4096:
+                self._workspace_bytes.clear()
+            self._workspace_bytes[key] = n.value
+        return self._workspace_bytes[key]
 
     def wf_beam_reorder(self, parents: torch.Tensor, states=(), caches=(), page_table=None, lengths=None, status=None, stream=None):
         """Moves every beam's states to the beams that grew from it, in place.  parents: [B, n_beam] (negative: stays).

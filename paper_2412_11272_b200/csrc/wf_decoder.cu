@@ -138,6 +138,98 @@ wf_status wf_cache_read(wf_decoder* d, const wf_cache* cache, const wf_rows* row
                                        v_stride, status, (cudaStream_t)stream));
 }
 
+namespace {
+// Number of SMs of the current device (asked once per device; the same for every thread that asks).
+wf_status sm_count(wf_decoder* d, int* n) {
+  static int known[64] = {0};
+  int dev = 0;
+  cudaError_t e = cudaGetDevice(&dev);
+  if (e == cudaSuccess && dev < 64 && known[dev] > 0) {
+    *n = known[dev];
+    return WF_OK;
+  }
+  if (e == cudaSuccess) e = cudaDeviceGetAttribute(n, cudaDevAttrMultiProcessorCount, dev);
+  if (e != cudaSuccess) return cuda_result(d, "device query", e);
+  if (dev < 64) known[dev] = *n;
+  return WF_OK;
+}
+wf_status check_attention_sizes(wf_decoder* d, int n_seq, int n_rows, int max_rows, int max_len) {
+  if (n_seq < 0 || n_rows < 0 || max_rows < 0 || max_len < 0)
+    return fail(d, WF_ERR_INVALID_ARG, "wf_tree_attention: a negative size");
+  if (n_seq > 65535) return fail(d, WF_ERR_CAPACITY, "wf_tree_attention: more than 65535 sequences");
+  if (n_rows > (1 << 27) || max_rows > (1 << 16)) return fail(d, WF_ERR_CAPACITY, "wf_tree_attention: more than 2^27 rows, or 2^16 in a sequence");
+  return WF_OK;
+}
+}  // namespace
+
+wf_status wf_tree_attention_workspace(wf_decoder* d, int n_seq, int n_rows, int max_rows, int max_len, size_t* bytes) {
+  if (!d) return WF_ERR_INVALID_ARG;
+  if (!bytes) return fail(d, WF_ERR_INVALID_ARG, "wf_tree_attention_workspace: NULL argument");
+  *bytes = 0;
+  wf_status st = check_attention_sizes(d, n_seq, n_rows, max_rows, max_len);
+  if (st != WF_OK || n_seq == 0 || n_rows == 0 || max_rows == 0) return st;
+  int sms = 0;
+  st = sm_count(d, &sms);
+  if (st != WF_OK) return st;
+  const wf_decoder_config& c = d->cfg;
+  *bytes = plan_tree_attention(c.dtype, c.d_head, c.n_head, c.n_kv_head, n_seq, n_rows, max_rows, max_len, sms).bytes;
+  return WF_OK;
+}
+
+wf_status wf_tree_attention(wf_decoder* d, const wf_cache* cache, const wf_rows* rows, const void* q, long q_stride, float scale,
+                            int tail, const unsigned* mask, int mask_words, int max_rows, int max_len, void* out, long out_stride,
+                            float* lse, void* workspace, size_t workspace_bytes, int* status, void* stream) {
+  if (!d) return WF_ERR_INVALID_ARG;
+  wf_status st = check_rows(d, "wf_tree_attention", rows);
+  if (st != WF_OK) return st;
+  st = check_cache(d, "wf_tree_attention", cache);
+  if (st != WF_OK) return st;
+  st = check_attention_sizes(d, rows->n_seq, rows->n_rows, max_rows, max_len);
+  if (st != WF_OK) return st;
+  if (tail < WF_TAIL_NONE || tail > WF_TAIL_MASK) return fail(d, WF_ERR_INVALID_ARG, "wf_tree_attention: unknown tail %d", tail);
+  if (tail == WF_TAIL_MASK && (mask_words < 0 || (long)mask_words * 32 < max_rows || (max_rows > 0 && !mask)))
+    return fail(d, WF_ERR_INVALID_ARG, "wf_tree_attention: WF_TAIL_MASK needs a mask of at least max_rows bits per row");
+  if (!(scale == scale) || scale - scale != 0.f) return fail(d, WF_ERR_INVALID_ARG, "wf_tree_attention: scale must be finite");
+  if (rows->n_seq == 0 || rows->n_rows == 0 || max_rows == 0) return WF_OK;
+  const wf_decoder_config& c = d->cfg;
+  if ((long)max_len > (long)rows->table_stride * c.page_size)
+    return fail(d, WF_ERR_INVALID_ARG, "wf_tree_attention: max_len %d exceeds the page table (%d pages of %d)", max_len,
+                rows->table_stride, c.page_size);
+  const int esz = path_bytes(c);
+  const long row = (long)c.n_head * c.d_head;
+  if (!q || !out) return fail(d, WF_ERR_INVALID_ARG, "wf_tree_attention: NULL queries or output");
+  if (!aligned16(q) || !aligned16(out) || q_stride * esz % 16 || out_stride * esz % 16 || q_stride < row || out_stride < row)
+    return fail(d, WF_ERR_INVALID_ARG, "wf_tree_attention: queries and outputs need 16-byte aligned pointers and row strides of at least %ld elements", row);
+  int sms = 0;
+  st = sm_count(d, &sms);
+  if (st != WF_OK) return st;
+  const TreeAttnPlan plan = plan_tree_attention(c.dtype, c.d_head, c.n_head, c.n_kv_head, rows->n_seq, rows->n_rows, max_rows, max_len, sms);
+  if (plan.bytes > 0 && (!workspace || workspace_bytes < plan.bytes || !aligned16(workspace)))
+    return fail(d, WF_ERR_INVALID_ARG, "wf_tree_attention: needs %zu bytes of 16-byte aligned workspace, got %zu", plan.bytes, workspace_bytes);
+  TreeAttnParams p{};
+  p.cache = view_of(d, cache);
+  p.rows = view_of(rows);
+  p.q = q;
+  p.out = out;
+  p.q_stride = q_stride;
+  p.out_stride = out_stride;
+  p.lse = lse;
+  p.mask = mask;
+  p.mask_words = mask_words;
+  p.tail = tail;
+  p.max_rows = max_rows;
+  p.max_len = max_len;
+  p.n_head = c.n_head;
+  p.group = c.n_head / c.n_kv_head;
+  p.scale = scale;
+  p.n_splits = plan.n_splits;
+  p.chunk = plan.chunk;
+  p.part_o = (float*)workspace;
+  p.part_ml = plan.bytes ? (float2*)((float*)workspace + (size_t)rows->n_rows * c.n_head * plan.n_splits * c.d_head) : nullptr;
+  p.status = status;
+  return cuda_result(d, "wf_tree_attention", launch_tree_attention(p, c.d_head, c.dtype, c.cache_format, (cudaStream_t)stream));
+}
+
 wf_status wf_beam_reorder(wf_decoder* d, const int* parents, int B, int n_beam, const wf_beam_state* states, int n_states,
                           const wf_cache* caches, int n_caches, int* page_table, int table_stride, const int* lengths, int* status,
                           void* stream) {

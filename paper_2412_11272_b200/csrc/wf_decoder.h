@@ -58,6 +58,34 @@ cudaError_t launch_cache_write(const CacheView& c, const RowsView& r, int d_head
 cudaError_t launch_cache_read(const CacheView& c, const RowsView& r, int d_head, int dtype, int format, void* k,
                               long k_stride, void* v, long v_stride, int* status, cudaStream_t s);
 
+// ---- attention over the paged cache (wf_tree_attention.cu)
+struct TreeAttnParams {
+  CacheView cache;
+  RowsView rows;
+  const void* q;
+  void* out;
+  long q_stride, out_stride;  // elements
+  float* lse;
+  const unsigned* mask;
+  int mask_words, tail;
+  int max_rows, max_len;
+  int n_head, group;  // group = n_head / n_kv_head
+  float scale;
+  // split of the positions: split i of a sequence has [i chunk, (i + 1) chunk); with more than one split the
+  // unnormalised sums go to part_o [n_rows][n_head][n_splits][d_head] and (maximum, sum) to part_ml
+  int n_splits, chunk;
+  float* part_o;
+  float2* part_ml;
+  int* status;
+};
+struct TreeAttnPlan {
+  int n_splits, chunk;
+  size_t bytes;
+};
+TreeAttnPlan plan_tree_attention(int dtype, int d_head, int n_head, int n_kv_head, int n_seq, int n_rows, int max_rows, int max_len,
+                                 int num_sms);
+cudaError_t launch_tree_attention(const TreeAttnParams& p, int d_head, int dtype, int format, cudaStream_t s);
+
 // An item of the reorder kernel: a contiguous state, one side (keys or values) of a paged cache, or the
 // page table itself.
 struct ReorderItem {
