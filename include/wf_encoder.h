@@ -459,6 +459,27 @@ wf_status wf_tree_attention(wf_decoder *dec, const wf_cache *cache, const wf_row
                             void *out, long out_stride, float *lse, void *workspace, size_t workspace_bytes,
                             int *status, void *stream);
 
+/* wf_beam_select: one round of beam search.  Of all continuations of the live beams of a sequence the
+ * `keep` best: c_wv = score_w + x_wv - log sum_u exp(x_wu), in descending order, ties to the lower w, then the
+ * lower v.  The logarithm of the sum and c are float64 (the exponentials and their first partial sums float32), so
+ * that beams are told apart where they nearly tie.
+ *   logits     dev   float32 or bfloat16 (logits_dtype, a wf_dtype) [B * n_beam][vocab], rows `ld` elements apart
+ *   scores     dev   float32 [B][n_beam] sums of log probabilities so far; -infinity: an unused beam
+ *   beams      dev   int [B]: beams live in this round (what wf_beam_pruner_step said), or NULL: all.  Values outside
+ *                    [0, n_beam] are cut to it and reported in `status` (bit 2)
+ *   finished   dev   uint8 [B][n_beam] or NULL: a beam with a non-zero flag has ended; it offers one continuation, end_token
+ *                    at its own score, and its logits are not read
+ *   end_token  host  the token that ends a text, or -1: none
+ *   suppress   dev   uint32 [(vocab + 31) / 32] or NULL: tokens whose bit is set count as -infinity, before the softmax
+ *   out_*      dev   [B][keep]: float32 scores, int parents and tokens, uint8 flags (1: ended by this token or before; may be
+ *                    NULL).  With fewer continuations the rest is -infinity, -1, -1, 0
+ * A beam whose logits hold a NaN or +infinity, or nothing but -infinity, offers no continuation.
+ * n_beam <= 16, keep <= 32, vocab <= 2^28, n_beam * vocab < 2^31. */
+wf_status wf_beam_select(wf_decoder *dec, const void *logits, int logits_dtype, long ld, int B, int n_beam, int vocab,
+                         const float *scores, const int *beams, const unsigned char *finished, int end_token,
+                         const unsigned *suppress, int keep, float *out_scores, int *out_parents, int *out_tokens,
+                         unsigned char *out_finished, int *status, void *stream);
+
 /* wf_beam_reorder: after a selection every beam takes over the states of the beam it grew from:
  * new[b][w] = old[b][parents[b][w]], in place; a negative parent leaves the row as it is.  One pass
  * that moves only rows whose parent is another beam.

@@ -76,7 +76,7 @@ EXPORTS = ("wf_encoder_create", "wf_logmel", "wf_encode", "wf_encode_raw_hush", 
            "wf_streams_create", "wf_streams_destroy", "wf_streams_length", "wf_streams_push", "wf_encode_streams", "wf_attention_f32_static",
            "wf_beam_pruner_create", "wf_beam_pruner_step", "wf_beam_pruner_state", "wf_beam_pruner_destroy",
            "wf_decoder_create", "wf_decoder_destroy", "wf_decoder_last_error", "wf_cache_write", "wf_cache_read",
-           "wf_tree_attention_workspace", "wf_tree_attention", "wf_beam_reorder")
+           "wf_tree_attention_workspace", "wf_tree_attention", "wf_beam_select", "wf_beam_reorder")
 
 _lib = None
 
@@ -133,6 +133,7 @@ def load_library() -> C.CDLL:
     lib.wf_tree_attention_workspace.argtypes = [vp, C.c_int, C.c_int, C.c_int, C.c_int, C.POINTER(C.c_size_t)]
     lib.wf_tree_attention.argtypes = [vp, cp, rp, vp, C.c_long, C.c_float, C.c_int, vp, C.c_int, C.c_int, C.c_int, vp, C.c_long, vp, vp,
                                       C.c_size_t, vp, vp]
+    lib.wf_beam_select.argtypes = [vp, vp, C.c_int, C.c_long, C.c_int, C.c_int, C.c_int, vp, vp, vp, C.c_int, vp, C.c_int, vp, vp, vp, vp, vp, vp]
     lib.wf_beam_reorder.argtypes = [vp, vp, C.c_int, C.c_int, C.POINTER(wf_beam_state), C.c_int, cp, C.c_int, vp, C.c_int, vp, vp, vp]
     for name in EXPORTS:
         if name not in ("wf_last_error", "wf_decoder_last_error"):
@@ -728,6 +729,33 @@ class Decoder:
                 self._workspace_bytes.clear()
             self._workspace_bytes[key] = n.value
         return self._workspace_bytes[key]
+
+    def wf_beam_select(self, logits: torch.Tensor, scores: torch.Tensor, keep: int, beams=None, finished=None, end_token: int = -1,
+                       suppress=None, status=None, stream=None):
+        """One round of beam search: the ``keep`` best continuations of every sequence.  logits [B * n_beam, vocab] float32 or
+        bfloat16 (row stride free), scores float32 [B, n_beam]; beams [B] live beams, finished uint8 or bool [B, n_beam], suppress int32
+        or uint32 bit words of tokens that are never chosen.  Returns (scores float32, parents int32, tokens int32, finished uint8),
+        each [B, keep]; places without a continuation hold (-inf, -1, -1, 0)."""
+        device = logits.device
+        if device.type != "cuda" or logits.dim() != 2 or logits.dtype not in (_F32, _BF16) or logits.stride(1) != 1:
+            _refuse("logits must be float32 or bfloat16 [B * n_beam, vocab] in device memory, a row's elements contiguous")
+        if scores.dim() != 2 or logits.shape[0] != scores.numel():
+            _refuse("scores must be [B, n_beam] for the B * n_beam rows of logits")
+        (B, W), V = scores.shape, logits.shape[1]
+        sp = _vector(scores, "scores", device, _F32)
+        bp = None if beams is None else _vector(beams, "beams", device, n=B)
+        fp = None if finished is None else _vector(finished, "finished", device, torch.bool if finished.dtype == torch.bool else _U8, B * W)
+        up = None
+        if suppress is not None:
+            up = _vector(suppress, "suppress", device, suppress.dtype if suppress.dtype in (_INT, torch.uint32) else _INT, -(-V // 32))
+        out = torch.empty((B, keep), dtype=_F32, device=device)
+        both = torch.empty((2, B, keep), dtype=_INT, device=device)
+        done = torch.empty((B, keep), dtype=_U8, device=device)
+        ints = both.data_ptr()
+        ld = logits.stride(0) if logits.shape[0] > 1 else max(logits.stride(0), V)
+        self._call(self.lib.wf_beam_select, device, stream, logits.data_ptr(), WF_BF16 if logits.dtype == _BF16 else WF_F32, ld, B, W, V, sp, bp, fp,
+                   end_token, up, keep, out.data_ptr(), ints, ints + 4 * B * keep, done.data_ptr(), self._status(status, device))
+        return out, both[0], both[1], done
 
     def wf_beam_reorder(self, parents: torch.Tensor, states=(), caches=(), page_table=None, lengths=None, status=None, stream=None):
         """Moves every beam's states to the beams that grew from it, in place.  parents: [B, n_beam] (negative: stays).

@@ -230,6 +230,43 @@ wf_status wf_tree_attention(wf_decoder* d, const wf_cache* cache, const wf_rows*
   return cuda_result(d, "wf_tree_attention", launch_tree_attention(p, c.d_head, c.dtype, c.cache_format, (cudaStream_t)stream));
 }
 
+wf_status wf_beam_select(wf_decoder* d, const void* logits, int logits_dtype, long ld, int B, int n_beam, int vocab, const float* scores,
+                         const int* beams, const unsigned char* finished, int end_token, const unsigned* suppress, int keep,
+                         float* out_scores, int* out_parents, int* out_tokens, unsigned char* out_finished, int* status, void* stream) {
+  if (!d) return WF_ERR_INVALID_ARG;
+  if (B < 0 || n_beam < 1 || n_beam > kMaxBeams || keep < 1 || keep > kMaxKeep || vocab < 1 || (long)vocab * n_beam >= (1L << 31))
+    return fail(d, WF_ERR_INVALID_ARG, "wf_beam_select: needs 1 .. %d beams, 1 .. %d to keep and a vocabulary below 2^31 / n_beam", kMaxBeams, kMaxKeep);
+  if (B > (1 << 24) || vocab > (1 << 28)) return fail(d, WF_ERR_CAPACITY, "wf_beam_select: more than 2^24 sequences or 2^28 tokens");
+  const int esz = logits_dtype == WF_BF16 ? 2 : 4;
+  if ((logits_dtype != WF_F32 && logits_dtype != WF_BF16) || ld < vocab)
+    return fail(d, WF_ERR_INVALID_ARG, "wf_beam_select: unknown logits type, or rows shorter than the vocabulary");
+  if (end_token < -1 || end_token >= vocab || (finished && end_token < 0))
+    return fail(d, WF_ERR_INVALID_ARG, "wf_beam_select: end_token %d outside the vocabulary (finished beams need one)", end_token);
+  if (B == 0) return WF_OK;
+  if (!logits || !scores || !out_scores || !out_parents || !out_tokens) return fail(d, WF_ERR_INVALID_ARG, "wf_beam_select: NULL argument");
+  if ((uintptr_t)logits % esz) return fail(d, WF_ERR_INVALID_ARG, "wf_beam_select: logits are not aligned to their type");
+  int sms = 0;
+  const wf_status st = sm_count(d, &sms);
+  if (st != WF_OK) return st;
+  BeamSelectParams p{};
+  p.logits = logits;
+  p.ld = ld;
+  p.n_beam = n_beam;
+  p.vocab = vocab;
+  p.keep = keep;
+  p.scores = scores;
+  p.beams = beams;
+  p.finished = finished;
+  p.end_token = end_token;
+  p.suppress = suppress;
+  p.out_scores = out_scores;
+  p.out_parents = out_parents;
+  p.out_tokens = out_tokens;
+  p.out_finished = out_finished;
+  p.status = status;
+  return cuda_result(d, "wf_beam_select", launch_beam_select(p, B, logits_dtype, sms, (cudaStream_t)stream));
+}
+
 wf_status wf_beam_reorder(wf_decoder* d, const int* parents, int B, int n_beam, const wf_beam_state* states, int n_states,
                           const wf_cache* caches, int n_caches, int* page_table, int table_stride, const int* lengths, int* status,
                           void* stream) {

@@ -86,6 +86,27 @@ TreeAttnPlan plan_tree_attention(int dtype, int d_head, int n_head, int n_kv_hea
                                  int num_sms);
 cudaError_t launch_tree_attention(const TreeAttnParams& p, int d_head, int dtype, int format, cudaStream_t s);
 
+// ---- beam selection (wf_beam_search.cu)
+constexpr int kMaxKeep = 32;
+struct BeamSelectParams {
+  const void* logits;
+  long ld;
+  int n_beam, vocab, keep;
+  const float* scores;
+  const int* beams;
+  const unsigned char* finished;
+  int end_token;
+  const unsigned* suppress;
+  float* out_scores;
+  int *out_parents, *out_tokens;
+  unsigned char* out_finished;
+  int* status;
+  int slice;   // elements of a row per block of the cluster (a multiple of 8)
+  int groups;  // items that a block makes of its slice of a row
+  int tiles;   // tiles of an item
+};
+cudaError_t launch_beam_select(BeamSelectParams p, int B, int dtype, int num_sms, cudaStream_t s);
+
 // An item of the reorder kernel: a contiguous state, one side (keys or values) of a paged cache, or the
 // page table itself.
 struct ReorderItem {
