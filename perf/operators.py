@@ -279,7 +279,8 @@ def _decoder(s):
     """The framework's handle for these heads and this cache, kept as a program keeps it."""
     from paper_2412_11272_b200.binding import Decoder
     heads = s.get("heads") or 1
-    key = (heads, s.get("kv_heads") or heads, s.get("dim") or 64, s.get("dtype") or "bf16", s.get("fmt") or "bf16", s.get("page") or 16)
+    dtype = s.get("dtype") or "bf16"
+    key = (heads, s.get("kv_heads") or heads, s.get("dim") or 64, dtype, s.get("fmt") or dtype, s.get("page") or 16)
     if key not in _kept:
         _kept[key] = Decoder(n_head=key[0], n_kv_head=key[1], d_head=key[2], dtype=key[3], cache_format="path" if key[4] == key[3] else key[4],
                              page_size=key[5])
