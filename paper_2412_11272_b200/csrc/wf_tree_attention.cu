@@ -7,54 +7,11 @@
 // Splits are joined by a second kernel in split order, so results do not depend on scheduling.
 #include <algorithm>
 
-#include "wf_decoder.h"
+#include "wf_tree_attention.cuh"
 
 namespace wf {
 
 namespace {
-
-// What a block needs to know about its sequence.
-struct Sequence {
-  int first_row, n_rows;  // rows of the batch
-  int start;              // committed positions
-  int len;                // positions to look at, the rows' own included
-};
-
-// The same for every thread of the block.
-__device__ __forceinline__ Sequence load_sequence(const TreeAttnParams& p, int seq, bool reporter) {
-  Sequence s;
-  s.first_row = __ldg(p.rows.cu_rows + seq);
-  s.n_rows = __ldg(p.rows.cu_rows + seq + 1) - s.first_row;
-  s.start = __ldg(p.rows.start + seq);
-  bool bad = s.first_row < 0 || s.n_rows < 0 || (long)s.first_row + s.n_rows > p.rows.n_rows || s.start < 0;
-  if (bad) s.n_rows = 0, s.start = 0;
-  long len = (long)s.start + (p.tail == WF_TAIL_NONE ? 0 : s.n_rows);
-  if (s.n_rows > 0 && len > p.max_len) {
-    bad = true;
-    len = p.max_len;
-  }
-  if (s.n_rows > p.max_rows) bad = true;
-  s.len = (int)len;
-  if (bad && reporter) report(p.status, kBadRows);
-  return s;
-}
-
-// Whether batch row i of the sequence sees position start + t (t >= 0).
-__device__ __forceinline__ bool sees_tail(const TreeAttnParams& p, const Sequence& s, int i, int t) {
-  if (p.tail == WF_TAIL_CAUSAL) return t <= i;
-  const int w = t >> 5;
-  if (w >= p.mask_words) return false;
-  return (__ldg(p.mask + (long)(s.first_row + i) * p.mask_words + w) >> (t & 31)) & 1;
-}
-
-__device__ __forceinline__ int page_of(const TreeAttnParams& p, int seq, int pos) {
-  const int page = __ldg(p.rows.page_table + (long)seq * p.rows.table_stride + (pos >> p.cache.page_shift));
-  if (page < 0 || page >= p.cache.n_pages) {
-    report(p.status, kBadPage);
-    return -1;
-  }
-  return page;
-}
 
 // 16 bytes of stored elements as float32.
 template <typename T, int kFormat>
@@ -286,10 +243,14 @@ cudaError_t launch_simt(const TreeAttnParams& p, cudaStream_t s) {
   return e;
 }
 
+// Rows of one tile of the tensor-core kernel.
+int tc_rows(int d_head, long rows) { return rows <= 8 ? 8 : rows <= 16 || d_head == 128 ? 16 : 32; }
+
 template <typename T, int kDim>
 cudaError_t launch_format(const TreeAttnParams& p, int format, cudaStream_t s) {
   cudaError_t e;
-  if (format == WF_CACHE_PATH) e = launch_simt<T, WF_CACHE_PATH, kDim>(p, s);
+  if constexpr (sizeof(T) == 2) e = launch_tree_attention_tc(p, kDim, format, tc_rows(kDim, (long)p.max_rows * p.group), s);
+  else if (format == WF_CACHE_PATH) e = launch_simt<T, WF_CACHE_PATH, kDim>(p, s);
   else if (format == WF_CACHE_E4M3) e = launch_simt<T, WF_CACHE_E4M3, kDim>(p, s);
   else e = launch_simt<T, WF_CACHE_INT8, kDim>(p, s);
   if (e == cudaSuccess && p.n_splits > 1)
@@ -302,7 +263,9 @@ cudaError_t launch_format(const TreeAttnParams& p, int format, cudaStream_t s) {
 TreeAttnPlan plan_tree_attention(int dtype, int d_head, int n_head, int n_kv_head, int n_seq, int n_rows, int max_rows, int max_len,
                                  int num_sms) {
   TreeAttnPlan plan{};
-  const long tiles = ((long)max_rows * (n_head / n_kv_head) + kSimtRows - 1) / kSimtRows;
+  const long rows = (long)max_rows * (n_head / n_kv_head);
+  const int tile = dtype == WF_BF16 ? tc_rows(d_head, rows) : kSimtRows;
+  const long tiles = (rows + tile - 1) / tile;
   const long blocks = tiles * n_kv_head * n_seq;
   // as many splits as fill the SMs four times over, of at least 256 positions each
   long splits = blocks >= 4L * num_sms ? 1 : (4L * num_sms + blocks - 1) / blocks;
@@ -310,8 +273,8 @@ TreeAttnPlan plan_tree_attention(int dtype, int d_head, int n_head, int n_kv_hea
   if (splits > longest) splits = longest;
   if (splits < 1) splits = 1;
   long chunk = ((long)max_len + splits - 1) / splits;
-  chunk = (chunk + kSimtKeys - 1) / kSimtKeys * kSimtKeys;
-  if (chunk < kSimtKeys) chunk = kSimtKeys;
+  const int step = dtype == WF_BF16 ? 256 : kSimtKeys;
+  chunk = std::max((chunk + step - 1) / step * step, (long)step);
   plan.chunk = (int)chunk;
   plan.n_splits = (int)std::max(1L, ((long)max_len + chunk - 1) / chunk);
   plan.bytes = plan.n_splits > 1 ? (size_t)n_rows * n_head * plan.n_splits * (d_head * sizeof(float) + sizeof(float2)) : 0;

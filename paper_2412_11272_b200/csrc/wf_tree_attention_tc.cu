@@ -1,0 +1,528 @@
+// Attention over the paged cache on the tensor cores, for few query rows per key/value head.
+//
+// The cache is read once and everything else is small, so the kernel is built around the loads: the scores
+// are computed transposed, S^T = K Q^T, with the keys as the 16-row operand and 8 query rows as the columns.  A
+// lane then needs whole 16-byte pieces of a key (the sum over channels may run in any order, so a lane's piece
+// serves several steps of the product) and loads them from the pages straight into registers: no shared memory, no barrier, every
+// byte used once.  The output is transposed as well, O^T = V^T P^T; the value operand's pairs of neighbouring keys are
+// made by byte permutation of two lanes' rows, and P^T comes from S^T by one 8 x 8 transposition in registers.
+// The four warps of a block take blocks of keys in turn, each with its own running maximum and sums, and are joined at the end.
+//
+// Quantised caches: a code is exact in float16 and in bfloat16.  Scores: codes as float16 times the queries
+// scaled by a power of two per row into float16 (exact up to 2^-24 of the row's largest element), the vector's scale
+// multiplies the float32 score.  Values: codes as bfloat16, and the probability times the vector's scale rounded once
+// to bfloat16, whose range holds any scale.  Unquantised: bfloat16 throughout, the probability rounded to it.
+#include "wf_ptx.cuh"
+#include "wf_tree_attention.cuh"
+
+namespace wf {
+
+namespace {
+
+constexpr int kWarps = 4, kThreads = kWarps * 32;
+constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+
+__device__ __forceinline__ void mma_f16(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+  asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+               : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+               : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ void mma_bf16(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+  asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+               : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+               : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ uint32_t transpose8x8(uint32_t x) {
+  uint32_t y;
+  asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
+  return y;
+}
+__device__ __forceinline__ void ldg16(const void* p, uint32_t* r) {
+  asm volatile("ld.global.nc.L1::no_allocate.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "l"(p));
+}
+__device__ __forceinline__ void ldg8(const void* p, uint32_t* r) {
+  asm volatile("ld.global.nc.L1::no_allocate.v2.u32 {%0, %1}, [%2];" : "=r"(r[0]), "=r"(r[1]) : "l"(p));
+}
+__device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
+  const __nv_bfloat162 h = __floats2bfloat162_rn(lo, hi);
+  return *reinterpret_cast<const uint32_t*>(&h);
+}
+__device__ __forceinline__ uint32_t pack_f16(float lo, float hi) {
+  const __half2 h = __floats2half2_rn(lo, hi);
+  return *reinterpret_cast<const uint32_t*>(&h);
+}
+
+// Four codes (bytes 0..3 of w) as float16 pairs (0, 1) and (2, 3), exactly.
+template <int kFormat>
+__device__ __forceinline__ void codes_f16(uint32_t w, uint32_t& lo, uint32_t& hi) {
+  if (kFormat == WF_CACHE_E4M3) {
+    asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(lo) : "h"((unsigned short)(w & 0xffffu)));
+    asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(hi) : "h"((unsigned short)(w >> 16)));
+  } else {
+    // 1024 + (code + 128) is a float16 whose low mantissa byte is the biased code
+    const uint32_t u = w ^ 0x80808080u, bias = 0x64806480u;
+    const uint32_t a = __byte_perm(u, 0x64646464u, 0x4140), b = __byte_perm(u, 0x64646464u, 0x4342);
+    asm("sub.rn.f16x2 %0, %1, %2;" : "=r"(lo) : "r"(a), "r"(bias));
+    asm("sub.rn.f16x2 %0, %1, %2;" : "=r"(hi) : "r"(b), "r"(bias));
+  }
+}
+// Codes in two bytes of w (kSel 0: bytes 0 and 1, 1: bytes 2 and 3) as a bfloat16 pair, exactly.
+template <int kFormat, int kSel>
+__device__ __forceinline__ uint32_t codes_bf16(uint32_t w) {
+  uint32_t r;
+  if (kFormat == WF_CACHE_E4M3) {
+    // sign, then the seven other bits where bfloat16 has its low exponent bits: the value times 2^-120
+    const uint32_t x = __byte_perm(w, 0, kSel == 0 ? 0x1404 : 0x3424);
+    const uint32_t y = ((x >> 4) & 0x07f007f0u) | (x & 0x80008000u);
+    asm("mul.rn.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(y), "r"(0x7b807b80u));
+  } else {
+    // (128 + low seven bits) - (128, or 256 for a negative code)
+    const uint32_t x = __byte_perm(w, 0x43434343u, kSel == 0 ? 0x4140 : 0x4342);
+    asm("sub.rn.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(x & 0xff7fff7fu), "r"(x & 0xff80ff80u));
+  }
+  return r;
+}
+
+template <int kFormat, int kDim>
+struct Layout {
+  static constexpr int kEsz = kFormat == WF_CACHE_PATH ? 2 : 1;
+  static constexpr int kVecBytes = kDim * kEsz;
+  static constexpr int kTiles = kVecBytes == 64 ? 2 : 1;  // 16-key tiles of a block of keys
+  static constexpr int kKeys = 16 * kTiles;           // 32 or 16
+  static constexpr int kKChunks = kVecBytes / 64;     // 16-byte pieces of a key per lane
+  static constexpr int kVWords = kVecBytes / 32;      // 32-bit words of a value per lane
+  static constexpr int kSteps = kDim / 16;            // steps of S^T's product = 16-channel tiles of O^T
+  // channel of element e (0 .. 3) of the lane's share of step s
+  static __device__ __forceinline__ int key_channel(int s, int t) {
+    return kEsz == 2 ? 32 * (s / 2) + 8 * t + 4 * (s % 2) : 64 * (s / 4) + 16 * t + 4 * (s % 4);
+  }
+  // channel of rows g and g + 8 (the next one) of 16-channel tile j
+  static __device__ __forceinline__ int value_channel(int j, int g) {
+    return kVecBytes == 256 ? 64 * (j / 4) + 8 * g + 2 * (j % 4) : kDim / 8 * g + 2 * j;
+  }
+};
+
+template <int kFormat, int kDim, int kNT>
+constexpr size_t tc_smem() {
+  return (size_t)kWarps * 8 * kNT * (kDim + 4) * sizeof(float) + (size_t)2 * kWarps * 8 * kNT * sizeof(float);
+}
+
+template <int kFormat, int kDim, int kNT>
+__global__ void __launch_bounds__(kThreads, kNT == 1 ? 4 : kNT == 2 ? 3 : 2) tree_attention_tc_kernel(const __grid_constant__ TreeAttnParams p) {
+  using L = Layout<kFormat, kDim>;
+  constexpr bool kQuant = kFormat != WF_CACHE_PATH;
+  constexpr int kRows = 8 * kNT;
+  extern __shared__ __align__(16) float smem[];
+  float* part = smem;                                   // [warp][row][kDim + 4]
+  float* part_m = part + kWarps * kRows * (kDim + 4);   // [warp][row]
+  float* part_l = part_m + kWarps * kRows;
+
+  const int seq = blockIdx.z, kvh = blockIdx.y;
+  const int split = blockIdx.x % p.n_splits, tile = blockIdx.x / p.n_splits;
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, t = lane & 3;
+  const Sequence s = load_sequence(p, seq, tid == 0 && blockIdx.x == 0 && kvh == 0);
+  const int rows = min(s.n_rows, p.max_rows) * p.group;
+  const int r0 = tile * kRows;
+  if (r0 >= rows) return;
+  const int begin = split * p.chunk, end = min(s.len, begin + p.chunk);
+  if (split > 0 && begin >= s.len) return;
+  const int shift = p.cache.page_shift;
+
+  // ---- queries: the second operand of S^T, element pairs matching the lane's pieces of a key
+  uint32_t qf[kNT][L::kSteps][2];
+  float factor[kNT][2];  // of the scores of rows 2t and 2t + 1: scale * log2(e), and the row's power of two
+#pragma unroll
+  for (int nt = 0; nt < kNT; ++nt) {
+    const int r = r0 + nt * 8 + g;
+    uint2 raw[L::kSteps];
+    const __nv_bfloat16* q = reinterpret_cast<const __nv_bfloat16*>(p.q) + (long)(s.first_row + r / p.group) * p.q_stride +
+                             (long)(kvh * p.group + r % p.group) * kDim;
+#pragma unroll
+    for (int i = 0; i < L::kSteps; ++i)
+      raw[i] = r < rows ? __ldg(reinterpret_cast<const uint2*>(q + L::key_channel(i, t))) : make_uint2(0, 0);
+    if constexpr (kQuant) {
+      uint32_t top = 0;
+#pragma unroll
+      for (int i = 0; i < L::kSteps; ++i)
+        top = max(max(top, max(raw[i].x << 16 & 0x7fff0000u, raw[i].x & 0x7fff0000u)), max(raw[i].y << 16 & 0x7fff0000u, raw[i].y & 0x7fff0000u));
+      top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
+      top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
+      // the row's largest element becomes 1 .. 2; exponents at either end of the range stay within normal floats
+      const int e = min(max((int)(top >> 23), 2), 252);
+      const float down = __uint_as_float((uint32_t)(254 - e) << 23), up = __uint_as_float((uint32_t)e << 23);  // 2^(127 - e), 2^(e - 127)
+#pragma unroll
+      for (int i = 0; i < L::kSteps; ++i) {
+        qf[nt][i][0] = pack_f16(__uint_as_float(raw[i].x << 16) * down, __uint_as_float(raw[i].x & 0xffff0000u) * down);
+        qf[nt][i][1] = pack_f16(__uint_as_float(raw[i].y << 16) * down, __uint_as_float(raw[i].y & 0xffff0000u) * down);
+      }
+      factor[nt][0] = __shfl_sync(0xffffffffu, up, 8 * t) * (p.scale * kLog2e);
+      factor[nt][1] = __shfl_sync(0xffffffffu, up, 8 * t + 4) * (p.scale * kLog2e);
+    } else {
+#pragma unroll
+      for (int i = 0; i < L::kSteps; ++i) qf[nt][i][0] = raw[i].x, qf[nt][i][1] = raw[i].y;
+      factor[nt][0] = factor[nt][1] = p.scale * kLog2e;
+    }
+  }
+
+  float o[kNT][L::kSteps][4];
+  float m[kNT][2], l[kNT][2];
+#pragma unroll
+  for (int nt = 0; nt < kNT; ++nt) {
+#pragma unroll
+    for (int j = 0; j < L::kSteps; ++j)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) o[nt][j][i] = 0.f;
+    m[nt][0] = m[nt][1] = -INFINITY;
+    l[nt][0] = l[nt][1] = 0.f;
+  }
+
+  // ---- loads: one block of keys is in registers, the next one's keys are on their way while its values are used and
+  // the other way round; page numbers run one block further ahead
+  uint32_t kreg[L::kTiles][2][L::kKChunks][4], vreg[L::kTiles][4][L::kVWords];
+  unsigned short sreg[L::kTiles];  // lanes 0 .. 15: scales of the tile's keys; 16 .. 31: of its values
+  int page[L::kTiles], page_next[L::kTiles];
+  auto load_pages = [&](int pos, int (&id)[L::kTiles]) {
+#pragma unroll
+    for (int i = 0; i < L::kTiles; ++i) {
+      const int at = pos + 16 * i;
+      id[i] = -1;
+      if (at < end) {
+        const int x = __ldg(p.rows.page_table + (long)seq * p.rows.table_stride + (at >> shift));
+        if (x >= 0 && x < p.cache.n_pages) id[i] = x;
+        else if (lane == 0) report(p.status, kBadPage);
+      }
+    }
+  };
+  auto first_vector = [&](int id, int pos) {  // index of the tile's first vector
+    return (((long)id * p.cache.n_kv_head + kvh) << shift) + (pos & ((1 << shift) - 1));
+  };
+  auto load_keys = [&](int pos, const int (&id)[L::kTiles]) {
+#pragma unroll
+    for (int i = 0; i < L::kTiles; ++i) {
+      const char* base = reinterpret_cast<const char*>(p.cache.k) + first_vector(id[i], pos + 16 * i) * L::kVecBytes;
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+#pragma unroll
+        for (int c = 0; c < L::kKChunks; ++c) {
+          if (id[i] >= 0) ldg16(base + (g + 8 * h) * L::kVecBytes + c * 64 + t * 16, kreg[i][h][c]);
+          else kreg[i][h][c][0] = kreg[i][h][c][1] = kreg[i][h][c][2] = kreg[i][h][c][3] = 0;
+        }
+    }
+  };
+  auto load_scales = [&](int pos, const int (&id)[L::kTiles]) {
+    if constexpr (kQuant) {
+#pragma unroll
+      for (int i = 0; i < L::kTiles; ++i) {
+        const __nv_bfloat16* from = (lane < 16 ? p.cache.k_scale : p.cache.v_scale) + first_vector(id[i], pos + 16 * i) + (lane & 15);
+        sreg[i] = id[i] >= 0 ? __ldg(reinterpret_cast<const unsigned short*>(from)) : (unsigned short)0;
+      }
+    }
+  };
+  auto load_values = [&](int pos, const int (&id)[L::kTiles]) {
+#pragma unroll
+    for (int i = 0; i < L::kTiles; ++i) {
+      const char* base = reinterpret_cast<const char*>(p.cache.v) + first_vector(id[i], pos + 16 * i) * L::kVecBytes;
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const char* at = base + (2 * t + (k & 1) + 8 * (k >> 1)) * L::kVecBytes;
+        if (id[i] < 0) {
+#pragma unroll
+          for (int w = 0; w < L::kVWords; ++w) vreg[i][k][w] = 0;
+        } else if constexpr (L::kVWords == 2) {
+          ldg8(at + g * 8, vreg[i][k]);
+        } else {
+#pragma unroll
+          for (int c = 0; c < L::kVWords / 4; ++c) ldg16(at + c * 128 + g * 16, vreg[i][k] + 4 * c);
+        }
+      }
+    }
+  };
+
+  constexpr int kStride = kWarps * L::kKeys;
+  int pos = begin + warp * L::kKeys;
+  if (pos < end) {
+    load_pages(pos, page);
+    load_keys(pos, page);
+    load_scales(pos, page);
+    load_values(pos, page);
+    load_pages(pos + kStride, page_next);
+  }
+  for (; pos < end; pos += kStride) {
+    const int next = pos + kStride;
+    // ---- S^T
+    float sc[L::kTiles][kNT][4];
+#pragma unroll
+    for (int i = 0; i < L::kTiles; ++i) {
+#pragma unroll
+      for (int nt = 0; nt < kNT; ++nt) sc[i][nt][0] = sc[i][nt][1] = sc[i][nt][2] = sc[i][nt][3] = 0.f;
+#pragma unroll
+      for (int st = 0; st < L::kSteps; ++st) {
+        uint32_t a[4];
+        if constexpr (kQuant) {
+          codes_f16<kFormat>(kreg[i][0][st / 4][st % 4], a[0], a[2]);
+          codes_f16<kFormat>(kreg[i][1][st / 4][st % 4], a[1], a[3]);
+        } else {
+          a[0] = kreg[i][0][st / 2][(st % 2) * 2];
+          a[1] = kreg[i][1][st / 2][(st % 2) * 2];
+          a[2] = kreg[i][0][st / 2][(st % 2) * 2 + 1];
+          a[3] = kreg[i][1][st / 2][(st % 2) * 2 + 1];
+        }
+#pragma unroll
+        for (int nt = 0; nt < kNT; ++nt) {
+          if constexpr (kQuant) mma_f16(sc[i][nt], a, qf[nt][st][0], qf[nt][st][1]);
+          else mma_bf16(sc[i][nt], a, qf[nt][st][0], qf[nt][st][1]);
+        }
+      }
+    }
+    float kscale[L::kTiles][2], vscale[L::kTiles][2];  // of keys g and g + 8 of each tile
+    if constexpr (kQuant) {
+#pragma unroll
+      for (int i = 0; i < L::kTiles; ++i) {
+        const uint32_t mine = (uint32_t)sreg[i] << 16;
+        kscale[i][0] = __uint_as_float(__shfl_sync(0xffffffffu, mine, g));
+        kscale[i][1] = __uint_as_float(__shfl_sync(0xffffffffu, mine, g + 8));
+        vscale[i][0] = __uint_as_float(__shfl_sync(0xffffffffu, mine, g + 16));
+        vscale[i][1] = __uint_as_float(__shfl_sync(0xffffffffu, mine, g + 24));
+      }
+    }
+    bool clean = pos + L::kKeys <= min(end, s.start);
+#pragma unroll
+    for (int i = 0; i < L::kTiles; ++i) clean = clean && page[i] >= 0;
+    if (next < end) {
+      load_keys(next, page_next);
+      load_scales(next, page_next);
+    }
+
+    // ---- softmax over the keys (rows of S^T: lanes with the same t hold the same query rows)
+#pragma unroll
+    for (int i = 0; i < L::kTiles; ++i)
+#pragma unroll
+      for (int nt = 0; nt < kNT; ++nt)
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+          sc[i][nt][c] *= factor[nt][c & 1];
+          if constexpr (kQuant) sc[i][nt][c] *= kscale[i][c >> 1];
+        }
+    if (!clean) {
+#pragma unroll
+      for (int i = 0; i < L::kTiles; ++i)
+#pragma unroll
+        for (int nt = 0; nt < kNT; ++nt)
+#pragma unroll
+          for (int c = 0; c < 4; ++c) {
+            const int at = pos + 16 * i + g + 8 * (c >> 1), r = r0 + nt * 8 + 2 * t + (c & 1);
+            const bool see = page[i] >= 0 && at < end && r < rows && (at < s.start || sees_tail(p, s, r / p.group, at - s.start));
+            if (!see) sc[i][nt][c] = -INFINITY;
+          }
+    }
+    bool grew = false;
+    float m_new[kNT][2];
+#pragma unroll
+    for (int nt = 0; nt < kNT; ++nt)
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        float x = m[nt][h];
+#pragma unroll
+        for (int i = 0; i < L::kTiles; ++i) x = fmaxf(x, fmaxf(sc[i][nt][h], sc[i][nt][h + 2]));
+        x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 4));
+        x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 8));
+        x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 16));
+        m_new[nt][h] = x;
+        grew |= x != m[nt][h];
+      }
+    if (__any_sync(0xffffffffu, grew)) {
+#pragma unroll
+      for (int nt = 0; nt < kNT; ++nt)
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          const float f = m_new[nt][h] == -INFINITY ? 1.f : exp2f(m[nt][h] - m_new[nt][h]);
+          m[nt][h] = m_new[nt][h];
+          l[nt][h] *= f;
+#pragma unroll
+          for (int j = 0; j < L::kSteps; ++j) o[nt][j][h] *= f, o[nt][j][h + 2] *= f;
+        }
+    }
+    uint32_t pf[L::kTiles][kNT][2];
+#pragma unroll
+    for (int nt = 0; nt < kNT; ++nt) {
+      const float base0 = m[nt][0] == -INFINITY ? 0.f : m[nt][0], base1 = m[nt][1] == -INFINITY ? 0.f : m[nt][1];
+#pragma unroll
+      for (int i = 0; i < L::kTiles; ++i) {
+        float w[4];
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+          const float x = sc[i][nt][c];
+          w[c] = ptx::ex2_approx(x - ((c & 1) ? base1 : base0));
+          l[nt][c & 1] += w[c];
+          if constexpr (kQuant) w[c] = x == -INFINITY ? 0.f : w[c] * vscale[i][c >> 1];  // a masked vector's scale may be NaN
+        }
+        pf[i][nt][0] = transpose8x8(pack_bf16(w[0], w[1]));
+        pf[i][nt][1] = transpose8x8(pack_bf16(w[2], w[3]));
+      }
+    }
+
+    // ---- O^T
+    if constexpr (!kQuant) {
+      if (!clean) {
+        // Values behind the end are not the sequence's, and a batch row's value that is not finite must not reach rows that do not
+        // see it through 0 * inf: such elements are taken out here and added to the rows that see them.
+#pragma unroll
+        for (int i = 0; i < L::kTiles; ++i) {
+          bool odd = false;
+#pragma unroll
+          for (int k = 0; k < 4; ++k) {
+            const bool in = pos + 16 * i + 2 * t + (k & 1) + 8 * (k >> 1) < end;
+#pragma unroll
+            for (int w = 0; w < L::kVWords; ++w) {
+              if (!in) vreg[i][k][w] = 0;
+              odd |= (vreg[i][k][w] & 0x7f80u) == 0x7f80u || (vreg[i][k][w] & 0x7f800000u) == 0x7f800000u;
+            }
+          }
+          if (!__any_sync(0xffffffffu, odd)) continue;
+#pragma unroll
+          for (int k = 0; k < 4; ++k)
+            for (int owner = 0; owner < 4; ++owner) {
+              const int at = pos + 16 * i + 2 * owner + (k & 1) + 8 * (k >> 1);
+#pragma unroll
+              for (int j = 0; j < L::kVWords; ++j) {
+                const uint32_t w = __shfl_sync(0xffffffffu, vreg[i][k][j], (lane & ~3) | owner);
+#pragma unroll
+                for (int half = 0; half < 2; ++half) {
+                  const uint32_t bits = half == 0 ? w << 16 : w & 0xffff0000u;
+                  if ((bits & 0x7f800000u) != 0x7f800000u) continue;
+#pragma unroll
+                  for (int nt = 0; nt < kNT; ++nt)
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {
+                      const int r = r0 + nt * 8 + 2 * t + h;
+                      if (at < end && r < rows && (at < s.start || sees_tail(p, s, r / p.group, at - s.start)))
+                        o[nt][j][2 * half + h] += __uint_as_float(bits);
+                    }
+                }
+              }
+            }
+#pragma unroll
+          for (int k = 0; k < 4; ++k)
+#pragma unroll
+            for (int w = 0; w < L::kVWords; ++w) {
+              if ((vreg[i][k][w] & 0x7f80u) == 0x7f80u) vreg[i][k][w] &= 0xffff0000u;
+              if ((vreg[i][k][w] & 0x7f800000u) == 0x7f800000u) vreg[i][k][w] &= 0x0000ffffu;
+            }
+        }
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < L::kTiles; ++i)
+#pragma unroll
+      for (int j = 0; j < L::kSteps; ++j) {
+        uint32_t a[4];
+        if constexpr (kQuant) {
+          const uint32_t x = __byte_perm(vreg[i][0][j / 2], vreg[i][1][j / 2], j % 2 == 0 ? 0x5140 : 0x7362);
+          const uint32_t y = __byte_perm(vreg[i][2][j / 2], vreg[i][3][j / 2], j % 2 == 0 ? 0x5140 : 0x7362);
+          a[0] = codes_bf16<kFormat, 0>(x);
+          a[1] = codes_bf16<kFormat, 1>(x);
+          a[2] = codes_bf16<kFormat, 0>(y);
+          a[3] = codes_bf16<kFormat, 1>(y);
+        } else {
+          a[0] = __byte_perm(vreg[i][0][j], vreg[i][1][j], 0x5410);
+          a[1] = __byte_perm(vreg[i][0][j], vreg[i][1][j], 0x7632);
+          a[2] = __byte_perm(vreg[i][2][j], vreg[i][3][j], 0x5410);
+          a[3] = __byte_perm(vreg[i][2][j], vreg[i][3][j], 0x7632);
+        }
+#pragma unroll
+        for (int nt = 0; nt < kNT; ++nt) mma_bf16(o[nt][j], a, pf[i][nt][0], pf[i][nt][1]);
+      }
+    if (next < end) load_values(next, page_next);
+#pragma unroll
+    for (int i = 0; i < L::kTiles; ++i) page[i] = page_next[i];
+    load_pages(next + kStride, page_next);
+  }
+
+  // ---- join the warps
+#pragma unroll
+  for (int nt = 0; nt < kNT; ++nt)
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      float x = l[nt][h];
+      x += __shfl_xor_sync(0xffffffffu, x, 4);
+      x += __shfl_xor_sync(0xffffffffu, x, 8);
+      x += __shfl_xor_sync(0xffffffffu, x, 16);
+      const int r = nt * 8 + 2 * t + h;
+      if (g == 0) part_m[warp * kRows + r] = m[nt][h], part_l[warp * kRows + r] = x;
+#pragma unroll
+      for (int j = 0; j < L::kSteps; ++j)
+        *reinterpret_cast<float2*>(part + (warp * kRows + r) * (kDim + 4) + L::value_channel(j, g)) = make_float2(o[nt][j][h], o[nt][j][h + 2]);
+    }
+  __syncthreads();
+  constexpr int kUnits = kRows * kDim / 8;  // 8 channels of a row
+  for (int u = tid; u < kUnits; u += kThreads) {
+    const int rr = u / (kDim / 8), ch = u % (kDim / 8) * 8, r = r0 + rr;
+    if (r >= rows) break;
+    float top = -INFINITY;
+#pragma unroll
+    for (int w = 0; w < kWarps; ++w) top = fmaxf(top, part_m[w * kRows + rr]);
+    const float base = top == -INFINITY ? 0.f : top;
+    float sum = 0.f, x[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) x[e] = 0.f;
+#pragma unroll
+    for (int w = 0; w < kWarps; ++w) {
+      const float f = exp2f(part_m[w * kRows + rr] - base);
+      sum += part_l[w * kRows + rr] * f;
+      const float* from = part + (w * kRows + rr) * (kDim + 4) + ch;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) x[e] += from[e] * f;
+    }
+    const long row = s.first_row + r / p.group;
+    const int head = kvh * p.group + r % p.group;
+    if (p.n_splits > 1) {
+      const long at = (row * p.n_head + head) * p.n_splits + split;
+      float4* to = reinterpret_cast<float4*>(p.part_o + at * kDim + ch);
+      to[0] = make_float4(x[0], x[1], x[2], x[3]);
+      to[1] = make_float4(x[4], x[5], x[6], x[7]);
+      if (ch == 0) p.part_ml[at] = make_float2(top * kLn2, sum);
+    } else {
+      const float inv = sum == 0.f ? 0.f : 1.f / sum;
+      uint4 out;
+      out.x = pack_bf16(x[0] * inv, x[1] * inv);
+      out.y = pack_bf16(x[2] * inv, x[3] * inv);
+      out.z = pack_bf16(x[4] * inv, x[5] * inv);
+      out.w = pack_bf16(x[6] * inv, x[7] * inv);
+      *reinterpret_cast<uint4*>(reinterpret_cast<__nv_bfloat16*>(p.out) + row * p.out_stride + (long)head * kDim + ch) = out;
+      if (ch == 0 && p.lse) p.lse[row * p.n_head + head] = sum == 0.f ? -INFINITY : (top + log2f(sum)) * kLn2;
+    }
+  }
+}
+
+template <int kFormat, int kDim, int kNT>
+cudaError_t launch_tile(const TreeAttnParams& p, cudaStream_t s) {
+  const long rows = (long)p.max_rows * p.group;
+  const int tiles = (int)((rows + 8 * kNT - 1) / (8 * kNT));
+  const dim3 grid((unsigned)(tiles * p.n_splits), (unsigned)p.cache.n_kv_head, (unsigned)p.rows.n_seq);
+  auto kernel = tree_attention_tc_kernel<kFormat, kDim, kNT>;
+  constexpr size_t smem = tc_smem<kFormat, kDim, kNT>();
+  cudaError_t e = cudaSuccess;
+  if (smem > 48 * 1024) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+  if (e != cudaSuccess) return e;
+  return launch_dependent(kernel, grid, dim3(kThreads), smem, s, 1, false, p);
+}
+
+template <int kFormat>
+cudaError_t launch_dim(const TreeAttnParams& p, int d_head, int rows_tile, cudaStream_t s) {
+  if (d_head == 64) {
+    if (rows_tile == 8) return launch_tile<kFormat, 64, 1>(p, s);
+    if (rows_tile == 16) return launch_tile<kFormat, 64, 2>(p, s);
+    return launch_tile<kFormat, 64, 4>(p, s);
+  }
+  return rows_tile == 8 ? launch_tile<kFormat, 128, 1>(p, s) : launch_tile<kFormat, 128, 2>(p, s);
+}
+
+}  // namespace
+
+cudaError_t launch_tree_attention_tc(const TreeAttnParams& p, int d_head, int format, int rows_tile, cudaStream_t s) {
+  if (format == WF_CACHE_PATH) return launch_dim<WF_CACHE_PATH>(p, d_head, rows_tile, s);
+  if (format == WF_CACHE_E4M3) return launch_dim<WF_CACHE_E4M3>(p, d_head, rows_tile, s);
+  return launch_dim<WF_CACHE_INT8>(p, d_head, rows_tile, s);
+}
+
+}  // namespace wf

@@ -144,8 +144,9 @@ class Case:
         most e times the sum of p |v|, so errors are counted against B = max |v| of the sequence.
         float32: scores are sums of d products (relative 2^-24 each step, |q||k| scale <= 60 here): absolute error under
         60 d 2^-24 / 8 in a score (random signs; 5e-5 for d = 128), the same relative error in p; sums and products add less.
-        bf16: the weight is rounded to bfloat16 (2^-9 B at most: half a step, 2^-8 / 2) and the output once more (2^-9 |o|);
-        both together stay under 2^-8 B + the float32 part.  lse is never rounded to 16 bits: the score's error alone."""
+        bf16: bfloat16 has 8 significant bits, half a step is at most eps / 2 = 2^-8 of the value (the step of [1, 2) is 2^-7).  The
+        weight is rounded once (2^-8 B at most) and the output once (2^-8 |o|, |o| <= B): 2^-7 B + the float32 part.  lse is never
+        rounded to 16 bits: the score's error alone."""
         (out, lse), (wo, wl) = got, want
         out, lse = out[:self.n].double().cpu().numpy(), lse[:self.n].double().cpu().numpy()
         assert np.array_equal(np.isneginf(lse), np.isneginf(wl)), "empty rows"
@@ -154,9 +155,10 @@ class Case:
         if fin.any():
             assert np.abs(lse[fin] - wl[fin]).max() <= 1e-4
         B = float(self.v.double().abs().max()) if len(self.v) else 1.0
-        tol = (2.0 ** -8 + 1e-4) * B if self.dec.dtype == "bf16" else 1e-4 * B
+        tol = (2.0 ** -7 + 1e-4) * B if self.dec.dtype == "bf16" else 1e-4 * B
         assert np.abs(out - wo).max() <= tol
-        # on the whole the rounding is much smaller: 2^-9 relative, uniform: 2^-9 / sqrt(3) of the output's own size twice over
+        # on the whole the rounding is smaller: uniform within half a step, 2^-8 / sqrt(3) in the root mean square, for the output and for the
+        # weights (where few carry the sum): together at most 2^-8 sqrt(2 / 3)
         if fin.any():
             rel = np.linalg.norm(out - wo) / np.linalg.norm(wo)
             assert rel <= (2.0 ** -8 if self.dec.dtype == "bf16" else 2e-5)
@@ -279,11 +281,11 @@ def test_vectors_of_very_different_sizes(fmt, where):
     out, lse = c.run()
     wo, wl = c.want()
     assert np.abs(lse.cpu().double().numpy() - wl).max() <= 1e-4
-    # against the sum of p |v| of each row and channel: 2^-8 for the weight's and the output's rounding
+    # against the sum of p |v| of each row and channel: half a step, 2^-8, for the weight's rounding and as much for the output's
     see = O.visible(T - 3, 3, "causal")
     ks, vs = (O.stored(x.double().numpy(), fmt) for x in (k, v))
     bound, _ = O.attend(c.q.double().numpy(), ks, np.abs(vs), see, 0.125)
-    assert (np.abs(out.double().cpu().numpy() - wo) <= (2.0 ** -8 + 1e-4) * bound).all()
+    assert (np.abs(out.double().cpu().numpy() - wo) <= (2.0 ** -7 + 1e-4) * bound).all()
     # a large value that a row gives almost no weight must not drown the rest: one key far below the others
     if where == "values":
         k2, v2 = torch.zeros(T, 1, 64, dtype=torch.bfloat16), torch.ones(T, 1, 64, dtype=torch.bfloat16)
@@ -293,7 +295,7 @@ def test_vectors_of_very_different_sizes(fmt, where):
         c.q = torch.zeros(1, 1, 64, dtype=torch.bfloat16)
         c.q[0, 0, 0] = 10.0
         out, _ = c.run()                                         # weight of key 5: exp(-110) = 2e-48, times 1e20 is nothing
-        assert (out.float() - 1).abs().max() <= 2.0 ** -8
+        assert (out.float() - 1).abs().max() <= 2.0 ** -7       # half a step for the weights (all alike), half a step for the output
 
 
 @pytest.mark.gpu
@@ -311,7 +313,7 @@ def test_scores_of_any_size(dtype, fmt):
     c.q[:, :, 0] = torch.tensor([800.0, -800.0, 8.0, -0.5])[:, None].to(dec.torch_dtype)
     (out, lse), (wo, wl) = c.run(), c.want()
     assert (np.abs(lse.cpu().double().numpy() - wl) <= 1e-4 + 2.0 ** -22 * np.abs(wl)).all()
-    assert np.abs(out.cpu().double().numpy() - wo).max() <= (2.0 ** -8 if dtype == "bf16" else 1e-2) * float(v.abs().max())
+    assert np.abs(out.cpu().double().numpy() - wo).max() <= (2.0 ** -7 if dtype == "bf16" else 1e-2) * float(v.abs().max())
 
 
 @pytest.mark.gpu
@@ -422,4 +424,4 @@ def test_offsets_beyond_32_bits():
     q = torch.randn(1, 1, 128, device="cuda").bfloat16()
     out, _ = dec.wf_tree_attention(cache, table, _dev([0, 1]), _dev([700]), q, 1, 700, tail="none")
     p = torch.softmax((k[:, 0].double() @ q[0, 0].double()) * 128 ** -0.5, 0)
-    assert (out[0, 0].double() - p @ k[:, 0].double()).abs().max() <= 2.0 ** -8 * float(k.abs().max())
+    assert (out[0, 0].double() - p @ k[:, 0].double()).abs().max() <= (2.0 ** -7 + 1e-4) * float(k.abs().max())
