@@ -646,13 +646,11 @@ class Decoder:
 
     def _call(self, fn, device, stream, *args):
         """Runs one entry point with the tensors' device current, on its stream."""
-        if torch.cuda.current_device() == device.index:
-            s = stream if stream is not None else torch.cuda.current_stream()
-            st = fn(self.handle, *args, s.cuda_stream)
-        else:
+        index = device.index
+        if torch._C._cuda_getDevice() != index:
             with torch.cuda.device(device):
-                s = stream if stream is not None else torch.cuda.current_stream()
-                st = fn(self.handle, *args, s.cuda_stream)
+                return self._call(fn, device, stream, *args)
+        st = fn(self.handle, *args, stream.cuda_stream if stream is not None else torch._C._cuda_getCurrentRawStream(index))
         if st != 0:
             self._check(st)
 

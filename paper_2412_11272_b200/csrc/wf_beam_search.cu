@@ -14,26 +14,26 @@ namespace {
 
 // ---------------------------------------------------------------------------------------------
 // Selection.  One cluster of blocks per sequence; a block has one slice of the vocabulary of all its beams, cut
-// into items (one beam, up to `tiles` tiles of 1024 elements) that its warps take in turn.  A warp holds a tile in
-// registers (32 elements a lane) and makes, in one pass over the logits:
-//   * the running maximum and sum of exponentials of its lanes;
-//   * the item's best `keep` elements: the keep-th largest of the 32 lane maxima is a lower bound of the
-//     keep-th largest element, few elements reach it (the bound's own lanes and little more), those are collected and
-//     ranked by (value, index).
-// After a cluster barrier every block knows every beam's log-sum (partial sums joined in a fixed order, in
-// float64), turns its items' elements into float64 scores and keeps the best; the first block joins the blocks'
-// lists.  No workspace, no atomics that decide an order, one launch.
+// into items (one beam, up to `tiles` tiles) that its warps take in turn, loading the next tile while they work on
+// one.  The pass over the logits only keeps, per lane, the maximum and the sum of exponentials: a lane's
+// maximum stands for its 32 (float32: 16) elements of every tile.  Then
+//   * the blocks exchange the beams' partial sums (through distributed shared memory) and know every log-sum;
+//   * the keep-th largest of lane maxima, turned into scores, bounds the keep-th best score from below; only the few lanes
+//     whose maximum reaches the bound can hold one of the best: their elements are read once more and ranked by
+//     (score, index) in float64;
+//   * the first block joins the blocks' lists.
+// Where many elements tie at the bound, the lists overflow and the block picks its best one by one instead.  No workspace
+// and one launch; sums are joined in a fixed order and a shared list's order decides nothing, so results are reproducible.
 
 constexpr int kSelThreads = 256, kSelWarps = kSelThreads / 32;
-constexpr int kPerLane = 32, kTile = 32 * kPerLane;
-constexpr int kRanked = 64;  // elements a warp collects and ranks at once; more (many ties) are picked one by one
+constexpr int kMaxCluster = 8;
+constexpr int kVecs = 4;            // 16-byte vectors of a lane per tile
+constexpr int kMaxGroups = 16;      // items of one beam in a block
+constexpr int kLaneList = 1024;     // lanes that reach the first bound
+constexpr int kCandidates = 512;    // elements that reach the second
+constexpr int kRanked = 64;         // entries that are ranked at once, each against all others
 
-struct Pick {  // an element with its place in the order: larger value first, then lower index
-  float x;
-  int v;
-};
-
-// Order-preserving map of a float to an unsigned integer above 0 (NaN excluded).
+// Order-preserving maps to unsigned integers above 0 (NaN excluded).
 __device__ __forceinline__ uint32_t ordered(float x) {
   const uint32_t b = __float_as_uint(x + 0.f);  // -0 counts as 0
   return b & 0x80000000u ? ~b : b | 0x80000000u;
@@ -43,6 +43,13 @@ __device__ __forceinline__ uint64_t ordered(double x) {
   const uint64_t b = (uint64_t)__double_as_longlong(x + 0.0);
   return b >> 63 ? ~b : b | (1ull << 63);
 }
+
+struct Ranked {
+  uint64_t key;   // ordered score; 0: none
+  uint32_t flat;  // beam * vocab + token
+  uint32_t pad;
+  __device__ __forceinline__ bool before(const Ranked& o) const { return key > o.key || (key == o.key && flat < o.flat); }
+};
 
 // keep-th largest of the lanes' keys (0 counts as none; 0 if there are fewer).
 __device__ __forceinline__ uint32_t kth_lane_key(uint32_t key, int keep) {
@@ -55,370 +62,356 @@ __device__ __forceinline__ uint32_t kth_lane_key(uint32_t key, int keep) {
   return top;
 }
 
-// The best `keep` of n entries by (key descending, tie ascending), found by one warp; entries with key 0 are absent.
-// emit(rank, i) is called once for each of them, by one lane.  `found` is the warp's list of n indexes.
-template <typename Key, typename Tie, typename Emit>
-__device__ void warp_best(int n, int keep, Key key, Tie tie, unsigned short* found, Emit emit) {
-  const int lane = threadIdx.x & 31;
-  uint32_t high = 0;
-  for (int i = lane; i < n; i += 32) high = max(high, (uint32_t)(key(i) >> 32));
-  const uint32_t bound = max(kth_lane_key(high, keep), 1u);  // present keys have a high half above 0
-  int c = 0;
-  for (int i0 = 0; i0 < n; i0 += 32) {
-    const int i = i0 + lane;
-    const bool in = i < n && (uint32_t)(key(i) >> 32) >= bound;
-    const unsigned who = __ballot_sync(0xffffffffu, in);
-    if (in) found[c + __popc(who & ((1u << lane) - 1))] = (unsigned short)i;
-    c += __popc(who);
-  }
-  __syncwarp();
-  if (c <= kRanked) {
-    for (int a = lane; a < c; a += 32) {
-      const int i = found[a];
-      const uint64_t ki = key(i);
-      const uint32_t ti = tie(i);
-      int rank = 0;
-      for (int b = 0; b < c; ++b) {
-        const int j = found[b];
-        const uint64_t kj = key(j);
-        rank += kj > ki || (kj == ki && tie(j) < ti);
-      }
-      if (rank < keep) emit(rank, i);
-    }
-  } else {  // many ties: one after the other, each the best of what comes after the one before
-    uint64_t last_k = ~0ull;
-    uint32_t last_t = 0;
-    for (int r = 0; r < keep; ++r) {
-      uint64_t bk = 0;
-      uint32_t bt = 0xffffffffu;
-      int bi = -1;
-      for (int a = lane; a < c; a += 32) {
-        const int i = found[a];
-        const uint64_t k = key(i);
-        const uint32_t t = tie(i);
-        const bool after = r == 0 || k < last_k || (k == last_k && t > last_t);
-        if (after && (k > bk || (k == bk && t < bt))) bk = k, bt = t, bi = i;
-      }
-      const uint32_t h = __reduce_max_sync(0xffffffffu, (uint32_t)(bk >> 32));
-      const uint32_t l = __reduce_max_sync(0xffffffffu, (uint32_t)(bk >> 32) == h ? (uint32_t)bk : 0u);
-      const uint64_t k = ((uint64_t)h << 32) | l;
-      if (k == 0) break;
-      const uint32_t t = __reduce_min_sync(0xffffffffu, bk == k ? bt : 0xffffffffu);
-      if (bk == k && bt == t && bi >= 0) emit(r, bi);
-      last_k = k;
-      last_t = t;
-    }
-  }
-  __syncwarp();
-}
-
-template <typename T>
-struct Vec;
-template <>
-struct Vec<float> {
-  static constexpr int n = 4;
-  static __device__ __forceinline__ void load(const float* p, float* x) {
-    const float4 r = __ldcs(reinterpret_cast<const float4*>(p));
-    x[0] = r.x; x[1] = r.y; x[2] = r.z; x[3] = r.w;
-  }
-};
-template <>
-struct Vec<__nv_bfloat16> {
-  static constexpr int n = 8;
-  static __device__ __forceinline__ void load(const __nv_bfloat16* p, float* x) {
-    const uint4 r = __ldcs(reinterpret_cast<const uint4*>(p));
-    const uint32_t w[4] = {r.x, r.y, r.z, r.w};
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      x[2 * i] = __uint_as_float(w[i] << 16);
-      x[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
-    }
-  }
-};
-__device__ __forceinline__ float one(const float* p) { return __ldg(p); }
-__device__ __forceinline__ float one(const __nv_bfloat16* p) { return __bfloat162float(*p); }
-
-// Best `keep` elements of a tile held in registers (element (j, e) of a lane has index first + (j * 32 + lane) * n + e),
-// joined with the `have` elements that the item's earlier tiles left in out[]; returns how many there are now.
-template <int kVec>
-__device__ int best_of_tile(const float (&x)[kPerLane], float lane_max, int first, int keep, Pick* buf, Pick* out, int have) {
-  const int lane = threadIdx.x & 31;
-  uint32_t bound = kth_lane_key(lane_max > -INFINITY ? ordered(lane_max) : 0u, keep);
-  if (have == keep) bound = max(bound, ordered(out[keep - 1].x));  // the list is full: its last element is a bound too
-  const float least = bound ? from_ordered(bound) : -INFINITY;
-  int mine = 0;
-#pragma unroll
-  for (int i = 0; i < kPerLane; ++i) mine += x[i] >= least && x[i] > -INFINITY;
-  int before = mine;  // inclusive prefix sum over the lanes
-#pragma unroll
-  for (int o = 1; o < 32; o <<= 1) {
-    const int y = __shfl_up_sync(0xffffffffu, before, o);
-    if (lane >= o) before += y;
-  }
-  const int c = __shfl_sync(0xffffffffu, before, 31);
-  if (c == 0) return have;
-  if (c + have <= kRanked) {
-    int at = before - mine;
-    if (mine) {
-#pragma unroll
-      for (int i = 0; i < kPerLane; ++i)
-        if (x[i] >= least && x[i] > -INFINITY) buf[at++] = Pick{x[i], first + ((i / kVec) * 32 + lane) * kVec + i % kVec};
-    }
-    for (int i = lane; i < have; i += 32) buf[c + i] = out[i];
-    __syncwarp();
-    const int total = c + have;
-    Pick p[2];
-    int rank[2];
-#pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      const int i = h * 32 + lane;
-      rank[h] = keep;
-      if (i < total) {
-        p[h] = buf[i];
-        rank[h] = 0;
-        for (int j = 0; j < total; ++j) {
-          const Pick q = buf[j];
-          rank[h] += q.x > p[h].x || (q.x == p[h].x && q.v < p[h].v);
-        }
-      }
-    }
-    __syncwarp();
-#pragma unroll
-    for (int h = 0; h < 2; ++h)
-      if (rank[h] < keep) out[rank[h]] = p[h];
-    __syncwarp();
-    return min(total, keep);
-  }
-  // many elements reach the bound: pick the best one by one, from the registers and the old list alike
-  for (int i = lane; i < have; i += 32) buf[i] = out[i];
-  __syncwarp();
-  float last_x = INFINITY;
-  int last_v = -1, r = 0;
-  for (; r < keep; ++r) {
-    float bx = -INFINITY;
-    int bv = 0x7fffffff;
-    auto consider = [&](float y, int v) {
-      const bool after = r == 0 || y < last_x || (y == last_x && v > last_v);
-      if (after && y > -INFINITY && (y > bx || (y == bx && v < bv))) bx = y, bv = v;
-    };
-#pragma unroll
-    for (int i = 0; i < kPerLane; ++i) consider(x[i], first + ((i / kVec) * 32 + lane) * kVec + i % kVec);
-    for (int i = lane; i < have; i += 32) consider(buf[i].x, buf[i].v);
-    const uint32_t k = __reduce_max_sync(0xffffffffu, bx > -INFINITY ? ordered(bx) : 0u);
-    if (k == 0) break;
-    last_x = from_ordered(k);
-    last_v = (int)__reduce_min_sync(0xffffffffu, bx > -INFINITY && ordered(bx) == k ? (unsigned)bv : 0xffffffffu);
-    if (lane == 0) out[r] = Pick{last_x, last_v};
-  }
-  __syncwarp();
+// The best of the lanes' entries, in every lane.
+__device__ __forceinline__ Ranked warp_first(Ranked x) {
+  const uint32_t h = __reduce_max_sync(0xffffffffu, (uint32_t)(x.key >> 32));
+  const uint32_t l = __reduce_max_sync(0xffffffffu, (uint32_t)(x.key >> 32) == h ? (uint32_t)x.key : 0u);
+  Ranked r;
+  r.key = ((uint64_t)h << 32) | l;
+  r.flat = __reduce_min_sync(0xffffffffu, x.key == r.key ? x.flat : 0xffffffffu);
+  r.pad = 0;
   return r;
 }
 
-static_assert(kSelWarps >= 8, "the join of a cluster's lists uses the warps' lists");
-struct SelectShared {  // sizes of the dynamic shared memory's parts
-  int items, entries;
-  size_t pick, stat, rows, found, best, total;
-};
-__host__ __device__ inline SelectShared select_shared(int n_beam, int groups, int keep) {
-  SelectShared s;
-  s.items = n_beam * groups;
-  s.entries = s.items * keep + n_beam;
-  size_t at = 0;
-  s.best = at; at += (size_t)kSelWarps * keep * 16;                 // per warp: (key, tie, -); the first `keep` also: the block's list
-  s.pick = at; at += (size_t)s.entries * sizeof(Pick);
-  s.stat = at; at += (size_t)s.items * 8;
-  s.rows = at; at += (size_t)((s.entries + 15) / 16 * 16);          // beam of each entry
-  s.found = at; at += (size_t)(s.entries + 8 * kMaxKeep) * 2 + 16;  // index lists of all warps, or of one
-  s.total = (at + 15) / 16 * 16;
-  return s;
+// Writes the best `keep` of n entries to out(rank, entry), best first, by one warp; fewer if fewer have a key.
+template <typename Emit>
+__device__ __forceinline__ void warp_best(const Ranked* from, int n, int keep, Emit out) {
+  const int lane = threadIdx.x & 31;
+  if (n <= kRanked) {
+    for (int i = lane; i < n; i += 32) {
+      const Ranked x = from[i];
+      if (x.key == 0) continue;
+      int rank = 0;
+      for (int j = 0; j < n; ++j) rank += from[j].before(x);
+      if (rank < keep) out(rank, x);
+    }
+  } else {  // one after the other, each the best of what comes after the one before
+    Ranked last{~0ull, 0, 0};
+    for (int r = 0; r < keep; ++r) {
+      Ranked mine{0, 0xffffffffu, 0};
+      for (int i = lane; i < n; i += 32) {
+        const Ranked x = from[i];
+        if ((r == 0 || last.before(x)) && x.before(mine)) mine = x;
+      }
+      last = warp_first(mine);
+      if (last.key == 0) break;
+      if (lane == 0) out(r, last);
+    }
+  }
+  __syncwarp();
 }
 
-struct Ranked {
-  uint64_t key;
-  uint32_t flat;
-  uint32_t unused;
+template <typename T>
+struct Vec {  // 16 bytes of logits
+  static constexpr int n = 16 / (int)sizeof(T);
+  static constexpr int tile = kVecs * 32 * n;
+  static __device__ __forceinline__ void unpack(const uint4& r, float* x) {
+    const uint32_t w[4] = {r.x, r.y, r.z, r.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      if constexpr (sizeof(T) == 4) {
+        x[i] = __uint_as_float(w[i]);
+      } else {
+        x[2 * i] = __uint_as_float(w[i] << 16);
+        x[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+      }
+    }
+  }
 };
+__device__ __forceinline__ uint32_t bits_of(float x) { return __float_as_uint(x); }
+__device__ __forceinline__ uint32_t bits_of(__nv_bfloat16 x) { return (uint32_t)__bfloat16_as_ushort(x); }
+__device__ __forceinline__ float to_f32(float x) { return x; }
+__device__ __forceinline__ float to_f32(__nv_bfloat16 x) { return __bfloat162float(x); }
+
+__device__ __forceinline__ bool suppressed(const BeamSelectParams& p, int v) { return p.suppress && ((__ldg(p.suppress + (v >> 5)) >> (v & 31)) & 1); }
+
+// Elements v .. v + n - 1 of a row; those outside [0, end) are -infinity.
+template <typename T>
+__device__ __forceinline__ uint4 load_vec(const T* row, int v, int end) {
+  constexpr int n = Vec<T>::n;
+  if (v >= 0 && v + n <= end) return __ldcs(reinterpret_cast<const uint4*>(row + v));
+  uint32_t w[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    w[i] = sizeof(T) == 4 ? 0xff800000u : 0xff80ff80u;
+    if constexpr (sizeof(T) == 4) {
+      if (v + i >= 0 && v + i < end) w[i] = bits_of(row[v + i]);
+    } else {
+      if (v + 2 * i >= 0 && v + 2 * i < end) w[i] = (w[i] & 0xffff0000u) | bits_of(row[v + 2 * i]);
+      if (v + 2 * i + 1 >= 0 && v + 2 * i + 1 < end) w[i] = (w[i] & 0x0000ffffu) | (bits_of(row[v + 2 * i + 1]) << 16);
+    }
+  }
+  return make_uint4(w[0], w[1], w[2], w[3]);
+}
+// Sets suppressed elements to -infinity.
+template <int n>
+__device__ __forceinline__ void suppress_vec(const BeamSelectParams& p, int v, int end, float* x) {
+  if (v + n <= 0 || v >= end) return;
+  const unsigned char* bytes = reinterpret_cast<const unsigned char*>(p.suppress);
+  const int from = max(v, 0), at = from >> 3;
+  unsigned word = __ldg(bytes + at);
+  if (at + 1 < (p.vocab + 31) / 32 * 4) word |= (unsigned)__ldg(bytes + at + 1) << 8;
+  word = (word >> (from & 7)) << (from - v);
+  if (word & ((1u << n) - 1)) {
+#pragma unroll
+    for (int e = 0; e < n; ++e)
+      if ((word >> e) & 1) x[e] = -INFINITY;
+  }
+}
+
+__device__ __forceinline__ float exp_diff(float x, float base) { return ptx::ex2_approx((x - base) * 1.4426950408889634f); }
 
 template <typename T>
-__global__ void __launch_bounds__(kSelThreads) beam_select_kernel(const __grid_constant__ BeamSelectParams p, int cluster) {
-  extern __shared__ __align__(16) unsigned char dyn[];
-  __shared__ Pick buf[kSelWarps][kRanked];
+__global__ void __launch_bounds__(kSelThreads, 3) beam_select_kernel(const __grid_constant__ BeamSelectParams p, int cluster) {
+  extern __shared__ __align__(16) uint32_t lane_key[];  // [item][lane]: the lane's maximum, later its ordered score's high half
+  __shared__ float2 stat[kMaxBeams * kMaxGroups];       // (maximum, sum) of an item
+  __shared__ float2 part[kMaxCluster][kMaxBeams];       // of a beam, from every block
+  __shared__ Ranked gather[kMaxCluster * kMaxKeep];     // first block: the blocks' lists
+  __shared__ Ranked cand[kCandidates + kMaxBeams];
+  __shared__ unsigned short lanes[kLaneList], few[kRanked];
+  __shared__ Ranked warp_top[kSelWarps];
+  __shared__ double lse[kMaxBeams];
   __shared__ int live_row[kMaxBeams];  // beams whose logits are read
-  __shared__ int n_live, n_done;
-  __shared__ double block_l[kMaxBeams], lse[kMaxBeams];
-  __shared__ float block_m[kMaxBeams];
-  __shared__ Ranked list[kMaxKeep];
-  const SelectShared sh = select_shared(p.n_beam, p.groups, p.keep);
-  Ranked* best = reinterpret_cast<Ranked*>(dyn + sh.best);
-  Pick* pick = reinterpret_cast<Pick*>(dyn + sh.pick);
-  float2* stat = reinterpret_cast<float2*>(dyn + sh.stat);
-  unsigned char* beam_of = dyn + sh.rows;
-  unsigned short* found = reinterpret_cast<unsigned short*>(dyn + sh.found);
+  __shared__ int n_live, n_done, n_lanes, n_few, n_cand;
+  __shared__ unsigned bound, bound2;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int rank = (int)blockIdx.x % cluster, b = (int)blockIdx.x / cluster;
-  constexpr int kVec = Vec<T>::n;
+  constexpr int kVec = Vec<T>::n, kTile = Vec<T>::tile, kPerTile = kVecs * kVec;
+  ptx::cluster_arrive();
 
-  if (tid == 0) {
+  if (warp == 0) {
     int live = p.n_beam;
     if (p.beams) {
       const int asked = __ldg(p.beams + b);
       live = min(max(asked, 0), p.n_beam);
-      if (live != asked && rank == 0) report(p.status, kBadRows);
+      if (live != asked && rank == 0 && lane == 0) report(p.status, kBadRows);
     }
-    int n = 0, done = 0;
-    for (int w = 0; w < live; ++w) {
-      if (p.finished && p.finished[(long)b * p.n_beam + w]) {
-        if (rank == 0) {  // the one continuation of a finished beam, behind the items' entries
-          pick[sh.items * p.keep + done] = Pick{0.f, p.end_token};
-          beam_of[sh.items * p.keep + done] = (unsigned char)w;
-          ++done;
-        }
-        lse[w] = 0.0;
-      } else {
-        live_row[n++] = w;
-      }
+    const bool done = lane < live && p.finished && p.finished[(long)b * p.n_beam + lane];
+    const unsigned ended = __ballot_sync(0xffffffffu, done), open = __ballot_sync(0xffffffffu, lane < live && !done);
+    if (lane < live && !done) live_row[__popc(open & ((1u << lane) - 1))] = lane;
+    if (done && rank == 0) {  // the one continuation of a finished beam
+      const double c = (double)__ldg(p.scores + (long)b * p.n_beam + lane);
+      cand[__popc(ended & ((1u << lane) - 1))] = Ranked{c > -INFINITY ? ordered(c) : 0, (uint32_t)lane * (uint32_t)p.vocab + (uint32_t)p.end_token, 0};
     }
-    n_live = n;
-    n_done = done;
+    if (lane == 0) {
+      n_live = __popc(open);
+      n_done = rank == 0 ? __popc(ended) : 0;
+      n_cand = n_done;
+      n_lanes = n_few = 0;
+      bound = bound2 = 0;
+    }
   }
   __syncthreads();
   const int n_items = n_live * p.groups;
 
-  // ---- items: statistics and best elements
-  for (int item = warp; item < n_items; item += kSelWarps) {
-    const int w = live_row[item / p.groups], g = item % p.groups;
-    const T* row = reinterpret_cast<const T*>(p.logits) + ((long)b * p.n_beam + w) * p.ld;
-    const int shift = (int)(((uintptr_t)row / sizeof(T)) % kVec);  // windows start at 16-byte borders
-    const int slice_end = min(p.vocab, (rank + 1) * p.slice - shift);
-    float m = -INFINITY, l = 0.f;
-    int have = 0;
-    Pick* out = pick + item * p.keep;
-    for (int t = 0; t < p.tiles; ++t) {
-      const int first = rank * p.slice - shift + (g * p.tiles + t) * kTile;
-      if (first >= slice_end) break;
-      float x[kPerLane];
+  // ---- one pass over the logits
+  struct Place {
+    const T* row;
+    int first, end;  // first element of the item's first tile, end of the slice
+  };
+  auto place = [&](int item) {
+    Place x;
+    x.row = reinterpret_cast<const T*>(p.logits) + ((long)b * p.n_beam + live_row[item / p.groups]) * p.ld;
+    const int shift = (int)(((uintptr_t)x.row / sizeof(T)) % kVec);  // vectors start at 16-byte borders
+    x.first = rank * p.slice - shift + item % p.groups * p.tiles * kTile;
+    x.end = min(p.vocab, (rank + 1) * p.slice - shift);
+    return x;
+  };
+  uint4 raw[kVecs];
+  Place at{};
+  int item = warp, tile = 0;
+  if (item < n_items) {
+    at = place(item);
 #pragma unroll
-      for (int j = 0; j < kPerLane / kVec; ++j) {
-        const int v = first + (j * 32 + lane) * kVec;
-        if (v >= 0 && v + kVec <= slice_end) {
-          Vec<T>::load(row + v, x + j * kVec);
-        } else {
+    for (int j = 0; j < kVecs; ++j) raw[j] = load_vec(at.row, at.first + (j * 32 + lane) * kVec, at.end);
+  }
+  float m = -INFINITY, l = 0.f;
+  while (item < n_items) {
+    const Place now = at;
+    const int now_item = item, now_first = at.first + tile * kTile;
+    // the next tile
+    if (++tile == p.tiles) {
+      tile = 0;
+      item += kSelWarps;
+      if (item < n_items) at = place(item);
+    }
+    uint4 next[kVecs];
+    if (item < n_items) {
 #pragma unroll
-          for (int e = 0; e < kVec; ++e) x[j * kVec + e] = v + e >= 0 && v + e < slice_end ? one(row + v + e) : -INFINITY;
+      for (int j = 0; j < kVecs; ++j) next[j] = load_vec(at.row, at.first + tile * kTile + (j * 32 + lane) * kVec, at.end);
+    }
+    float x[kPerTile];
+#pragma unroll
+    for (int j = 0; j < kVecs; ++j) Vec<T>::unpack(raw[j], x + j * kVec);
+    if (p.suppress) {
+#pragma unroll
+      for (int j = 0; j < kVecs; ++j) suppress_vec<kVec>(p, now_first + (j * 32 + lane) * kVec, now.end, x + j * kVec);
+    }
+    float top = x[0];
+#pragma unroll
+    for (int i = 1; i < kPerTile; ++i) top = fmaxf(top, x[i]);
+    top = fmaxf(top, m);
+    const float base = top > -INFINITY ? top : 0.f;  // an all-NaN lane has top = NaN: base 0, the sum is NaN
+    float sum[4] = {l * exp_diff(m, base), 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int i = 0; i < kPerTile; ++i) sum[i % 4] += exp_diff(x[i], base);
+    l = (sum[0] + sum[1]) + (sum[2] + sum[3]);
+    m = fmaxf(top, -INFINITY);
+    if (tile == 0) {  // the item is complete
+      lane_key[now_item * 32 + lane] = __float_as_uint(m);
+      const float wm = from_ordered(__reduce_max_sync(0xffffffffu, ordered(m)));
+      float wl = l * exp_diff(m, wm > -INFINITY ? wm : 0.f);
+#pragma unroll
+      for (int o = 16; o > 0; o >>= 1) wl += __shfl_xor_sync(0xffffffffu, wl, o);
+      if (lane == 0) stat[now_item] = make_float2(wm, wl);
+      m = -INFINITY;
+      l = 0.f;
+    }
+#pragma unroll
+    for (int j = 0; j < kVecs; ++j) raw[j] = next[j];
+  }
+  __syncthreads();
+
+  // ---- the beams' log-sums: items of a block, then blocks of the cluster, in order
+  ptx::cluster_wait();  // every block of the cluster runs
+  for (int i = warp; i < n_live; i += kSelWarps) {
+    const float2 s = lane < p.groups ? stat[i * p.groups + lane] : make_float2(-INFINITY, 0.f);
+    const float wm = from_ordered(__reduce_max_sync(0xffffffffu, ordered(s.x)));
+    float wl = s.y == 0.f ? 0.f : s.y * exp_diff(s.x, wm);
+#pragma unroll
+    for (int o = 8; o > 0; o >>= 1) wl += __shfl_xor_sync(0xffffffffu, wl, o);
+    if (lane < cluster) ptx::st_cluster_v2(ptx::map_to_cta(ptx::smem_u32(&part[rank][i]), lane), __float_as_uint(wm), __float_as_uint(wl));
+  }
+  __syncwarp();
+  ptx::cluster_arrive();
+  ptx::cluster_wait();
+  for (int i = warp; i < n_live; i += kSelWarps) {
+    const float2 s = lane < cluster ? part[lane][i] : make_float2(-INFINITY, 0.f);
+    const float wm = from_ordered(__reduce_max_sync(0xffffffffu, ordered(s.x)));
+    double wl = s.y == 0.f ? 0.0 : (double)(s.y * exp_diff(s.x, wm));
+#pragma unroll
+    for (int o = 4; o > 0; o >>= 1) wl += __shfl_xor_sync(0xffffffffu, wl, o);
+    if (lane == 0) lse[live_row[i]] = (double)wm + log(wl);  // NaN if the row holds one, or +infinity; all -infinity: no score
+  }
+  __syncthreads();
+
+  const float* scores = p.scores + (long)b * p.n_beam;
+  auto key_of = [&](int w, float x) -> uint64_t {
+    const double c = (double)__ldg(scores + w) + ((double)x - lse[w]);
+    return x > -INFINITY && c > -INFINITY ? ordered(c) : 0;  // false for NaN
+  };
+  // ---- the lanes that can hold one of the best
+  const int n_entries = n_items * 32;
+  uint32_t high = 0;
+  for (int e = tid; e < n_entries; e += kSelThreads) {
+    const uint32_t k = (uint32_t)(key_of(live_row[(e >> 5) / p.groups], __uint_as_float(lane_key[e])) >> 32);
+    lane_key[e] = k;
+    high = max(high, k);
+  }
+  const uint32_t mine = kth_lane_key(high, p.keep);
+  if (lane == 0) atomicMax(&bound, mine);
+  __syncthreads();
+  {
+    const uint32_t least = max(bound, 1u);
+    for (int e = tid; e < n_entries; e += kSelThreads)
+      if (lane_key[e] >= least) {
+        const int i = atomicAdd(&n_lanes, 1);
+        if (i < kLaneList) lanes[i] = (unsigned short)e;
+      }
+  }
+  __syncthreads();
+  if (warp == 0 && n_lanes <= kLaneList) {
+    uint32_t h = 0;
+    for (int i = lane; i < n_lanes; i += 32) h = max(h, lane_key[lanes[i]]);
+    const uint32_t least = max(max(kth_lane_key(h, p.keep), bound), 1u);
+    int n = 0;
+    for (int i0 = 0; i0 < n_lanes; i0 += 32) {
+      const bool in = i0 + lane < n_lanes && lane_key[lanes[i0 + lane]] >= least;
+      const unsigned who = __ballot_sync(0xffffffffu, in);
+      const int to = n + __popc(who & ((1u << lane) - 1));
+      if (in && to < kRanked) few[to] = lanes[i0 + lane];
+      n += __popc(who);
+    }
+    if (lane == 0) n_few = n, bound2 = least;
+  }
+  __syncthreads();
+  bool fits = n_lanes <= kLaneList && n_few <= kRanked;
+  if (fits) {
+    // ---- their elements once more
+    for (int q = warp; q < n_few; q += kSelWarps) {
+      const int e = few[q], w = live_row[(e >> 5) / p.groups], L = e & 31;
+      const Place x = place(e >> 5);
+      for (int k = lane; k < p.tiles * kPerTile; k += 32) {
+        const int within = k % kPerTile, v = x.first + k / kPerTile * kTile + (within / kVec * 32 + L) * kVec + within % kVec;
+        if (v < 0 || v >= x.end || suppressed(p, v)) continue;
+        const uint64_t key = key_of(w, to_f32(x.row[v]));
+        if ((uint32_t)(key >> 32) >= bound2) {
+          const int i = atomicAdd(&n_cand, 1);
+          if (i < kCandidates) cand[i] = Ranked{key, (uint32_t)w * (uint32_t)p.vocab + (uint32_t)v, 0};
         }
       }
-      if (p.suppress) {
-        const unsigned char* bits = reinterpret_cast<const unsigned char*>(p.suppress);
-        const int n_bytes = (p.vocab + 31) / 32 * 4;
+    }
+    __syncthreads();
+    fits = n_cand <= kCandidates;
+  }
+  const uint32_t to_first = ptx::map_to_cta(ptx::smem_u32(gather + rank * p.keep), 0);
+  auto send = [&](int r, const Ranked& x) {
+    ptx::st_cluster_v4(to_first + r * 16, (uint32_t)x.key, (uint32_t)(x.key >> 32), x.flat, 0);
+  };
+  if (fits) {
+    if (warp == 0) {
+      const int n = n_cand;  // a finished beam of score -infinity has no key
+      const int keyless = __popc(__ballot_sync(0xffffffffu, lane < n_done && cand[lane].key == 0));
+      for (int r = n - keyless + lane; r < p.keep; r += 32) send(r, Ranked{0, 0, 0});
+      warp_best(cand, n, p.keep, send);
+    }
+  } else {
+    // ---- many ties: one by one, each the best element of the slice behind the one before
+    Ranked last{~0ull, 0, 0};
+    const int done = n_done;
+    for (int r = 0; r < p.keep; ++r) {
+      Ranked best{0, 0xffffffffu, 0};
+      for (int i = warp; i < n_items; i += kSelWarps) {
+        const Place x = place(i);
+        const int w = live_row[i / p.groups];
+        for (int k = 0; k < p.tiles * kVecs; ++k) {
+          const int v = x.first + k / kVecs * kTile + (k % kVecs * 32 + lane) * kVec;
+          float y[kVec];
+          Vec<T>::unpack(load_vec(x.row, v, x.end), y);
+          if (p.suppress) suppress_vec<kVec>(p, v, x.end, y);
 #pragma unroll
-        for (int j = 0; j < kPerLane / kVec; ++j) {
-          const int v = first + (j * 32 + lane) * kVec;
-          if (v + kVec <= 0 || v >= slice_end) continue;
-          const int at = max(v, 0) >> 3, off = max(v, 0) & 7;
-          unsigned word = __ldg(bits + at);
-          if (at + 1 < n_bytes) word |= (unsigned)__ldg(bits + at + 1) << 8;
-          word = (word >> off) << (max(v, 0) - v);
-          if (word & ((1u << kVec) - 1)) {
-#pragma unroll
-            for (int e = 0; e < kVec; ++e)
-              if ((word >> e) & 1) x[j * kVec + e] = -INFINITY;
+          for (int e = 0; e < kVec; ++e) {
+            const Ranked z{key_of(w, y[e]), (uint32_t)w * (uint32_t)p.vocab + (uint32_t)(v + e), 0};
+            if ((r == 0 || last.before(z)) && z.before(best)) best = z;
           }
         }
       }
-      float top = -INFINITY;
+      if (tid < done) {
+        const Ranked z = cand[tid];
+        if ((r == 0 || last.before(z)) && z.before(best)) best = z;
+      }
+      best = warp_first(best);
+      if (lane == 0) warp_top[warp] = best;
+      __syncthreads();
+      last = warp_top[0];
 #pragma unroll
-      for (int i = 0; i < kPerLane; ++i) top = fmaxf(top, x[i]);
-      const float m_new = fmaxf(m, top);
-      const float base = m_new == -INFINITY ? 0.f : m_new;
-      l *= exp2f((m - base) * 1.4426950408889634f);
-#pragma unroll
-      for (int i = 0; i < kPerLane; ++i) l += exp2f((x[i] - base) * 1.4426950408889634f);
-      m = m_new;
-      have = best_of_tile<kVec>(x, top, first, p.keep, buf[warp], out, have);
+      for (int i = 1; i < kSelWarps; ++i)
+        if (warp_top[i].before(last)) last = warp_top[i];
+      __syncthreads();
+      if (tid == 0) send(r, last);
+      if (last.key == 0) {
+        for (int q = r + 1 + tid; q < p.keep; q += kSelThreads) send(q, Ranked{0, 0, 0});
+        break;
+      }
     }
-    float wm = m;
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) wm = fmaxf(wm, __shfl_xor_sync(0xffffffffu, wm, o));
-    float wl = l * exp2f((m - (wm == -INFINITY ? 0.f : wm)) * 1.4426950408889634f);
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) wl += __shfl_xor_sync(0xffffffffu, wl, o);
-    if (lane == 0) stat[item] = make_float2(wm, wl);
-    for (int i = lane; i < p.keep; i += 32) {
-      if (i >= have) out[i].v = -1;
-      beam_of[item * p.keep + i] = (unsigned char)w;
-    }
-  }
-  __syncthreads();
-  if (tid < n_live) {
-    float m = -INFINITY;
-    for (int g = 0; g < p.groups; ++g) m = fmaxf(m, stat[tid * p.groups + g].x);
-    double l = 0.0;
-    for (int g = 0; g < p.groups; ++g) {
-      const float2 s = stat[tid * p.groups + g];
-      if (s.y != 0.f) l += (double)s.y * exp((double)s.x - (double)m);
-    }
-    block_m[tid] = m;
-    block_l[tid] = l;
   }
   __syncwarp();
-  ptx::cluster_sync_all();
-  if (tid < n_live) {  // log-sum of a beam from all blocks' parts, in rank order
-    const uint32_t am = ptx::smem_u32(block_m + tid), al = ptx::smem_u32(block_l + tid);
-    float m = -INFINITY;
-    for (int r = 0; r < cluster; ++r) m = fmaxf(m, ptx::ld_cluster_f32(ptx::map_to_cta(am, r)));
-    double l = 0.0;
-    for (int r = 0; r < cluster; ++r) {
-      const double lr = ptx::ld_cluster_f64(ptx::map_to_cta(al, r));
-      const float mr = ptx::ld_cluster_f32(ptx::map_to_cta(am, r));
-      if (lr != 0.0) l += lr * exp((double)mr - (double)m);
-    }
-    lse[live_row[tid]] = (double)m + log(l);  // NaN if the row holds one, or +infinity
-  }
-  __syncthreads();
-
-  // ---- the block's best: every warp of a share of the entries, then the first warp of the warps' lists
-  const float* scores = p.scores + (long)b * p.n_beam;
-  auto key_of = [&](int e) -> uint64_t {
-    const Pick q = pick[e];
-    if (q.v < 0) return 0;
-    const int w = beam_of[e];
-    const double c = (double)__ldg(scores + w) + ((double)q.x - lse[w]);
-    return c > -INFINITY ? ordered(c) : 0;  // false for NaN
-  };
-  auto flat_of = [&](int e) -> uint32_t { return (uint32_t)beam_of[e] * (uint32_t)p.vocab + (uint32_t)pick[e].v; };
-  const int n_entries = n_items * p.keep;
-  {
-    const int share = (n_entries + kSelWarps - 1) / kSelWarps, e0 = min(warp * share, n_entries), n = min(share, n_entries - e0);
-    for (int i = lane; i < p.keep; i += 32) best[warp * p.keep + i].key = 0;
-    __syncwarp();
-    warp_best(n, p.keep, [&](int i) { return key_of(e0 + i); }, [&](int i) { return flat_of(e0 + i); }, found + e0, [&](int r, int i) {
-      best[warp * p.keep + r].key = key_of(e0 + i);
-      best[warp * p.keep + r].flat = flat_of(e0 + i);
-    });
-  }
-  __syncthreads();
-  if (warp == 0) {
-    const int done0 = sh.items * p.keep, n = kSelWarps * p.keep + n_done;
-    auto key = [&](int i) { return i < kSelWarps * p.keep ? best[i].key : key_of(done0 + i - kSelWarps * p.keep); };
-    auto flat = [&](int i) { return i < kSelWarps * p.keep ? best[i].flat : flat_of(done0 + i - kSelWarps * p.keep); };
-    for (int i = lane; i < p.keep; i += 32) list[i].key = 0;
-    __syncwarp();
-    warp_best(n, p.keep, key, flat, found, [&](int r, int i) {
-      list[r].key = key(i);
-      list[r].flat = flat(i);
-    });
-  }
-  __syncwarp();
-  ptx::cluster_sync_all();
+  ptx::cluster_arrive();
+  if (rank != 0) return;
 
   // ---- the sequence's best
-  if (rank == 0 && warp == 0) {
-    for (int i = lane; i < cluster * p.keep; i += 32) {
-      const uint32_t a = ptx::map_to_cta(ptx::smem_u32(list + i % p.keep), i / p.keep);
-      best[i].key = ptx::ld_cluster_u64(a);
-      best[i].flat = ptx::ld_cluster_u32(a + 8);
-    }
-    __syncwarp();
+  ptx::cluster_wait();
+  if (warp == 0) {
     const long o = (long)b * p.keep;
     for (int i = lane; i < p.keep; i += 32) {
       p.out_scores[o + i] = -INFINITY;
@@ -426,18 +419,15 @@ __global__ void __launch_bounds__(kSelThreads) beam_select_kernel(const __grid_c
       if (p.out_finished) p.out_finished[o + i] = 0;
     }
     __syncwarp();
-    warp_best(cluster * p.keep, p.keep, [&](int i) { return best[i].key; }, [&](int i) { return best[i].flat; }, found, [&](int r, int i) {
-      const uint64_t k = best[i].key;
-      const double c = __longlong_as_double((long long)(k >> 63 ? k & ~(1ull << 63) : ~k));
-      const int w = (int)(best[i].flat / (uint32_t)p.vocab), v = (int)(best[i].flat % (uint32_t)p.vocab);
+    warp_best(gather, cluster * p.keep, p.keep, [&](int r, const Ranked& x) {
+      const double c = __longlong_as_double((long long)(x.key >> 63 ? x.key & ~(1ull << 63) : ~x.key));
+      const int w = (int)(x.flat / (uint32_t)p.vocab), v = (int)(x.flat % (uint32_t)p.vocab);
       p.out_scores[o + r] = (float)c;
       p.out_parents[o + r] = w;
       p.out_tokens[o + r] = v;
       if (p.out_finished) p.out_finished[o + r] = v == p.end_token || (p.finished && p.finished[(long)b * p.n_beam + w]);
     });
   }
-  __syncwarp();
-  ptx::cluster_sync_all();  // the lists stay until they have been read
 }
 
 // ---------------------------------------------------------------------------------------------
@@ -550,17 +540,18 @@ __global__ void __launch_bounds__(kReorderThreads) beam_reorder_kernel(const __g
 }  // namespace
 
 cudaError_t launch_beam_select(BeamSelectParams p, int B, int dtype, int num_sms, cudaStream_t s) {
+  const int tile = dtype == WF_BF16 ? Vec<__nv_bfloat16>::tile : Vec<float>::tile;
   // enough blocks for two on every SM, at least one tile of every row each, at most the 8 of a portable cluster
   int cluster = 1;
-  while (cluster < 8 && (long)B * cluster < 2L * num_sms && p.vocab > cluster * kTile) cluster *= 2;
+  while (cluster < kMaxCluster && (long)B * cluster < 2L * num_sms && p.vocab > cluster * tile) cluster *= 2;
   p.slice = ((p.vocab + 8 + cluster - 1) / cluster + 7) / 8 * 8;
-  const int n_tiles = (p.slice + kTile - 1) / kTile;
-  p.tiles = (n_tiles + 15) / 16;  // at most 16 items of a row in a block
+  const int n_tiles = (p.slice + tile - 1) / tile;
+  p.tiles = (n_tiles + kMaxGroups - 1) / kMaxGroups;
   p.groups = (n_tiles + p.tiles - 1) / p.tiles;
-  const size_t smem = select_shared(p.n_beam, p.groups, p.keep).total;
+  const size_t smem = (size_t)p.n_beam * p.groups * 32 * sizeof(uint32_t);  // at most 32 KB
   auto kernel = dtype == WF_BF16 ? beam_select_kernel<__nv_bfloat16> : beam_select_kernel<float>;
   cudaError_t e = cudaSuccess;
-  if (smem > 40 * 1024) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+  if (smem > 16 * 1024) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
   if (e != cudaSuccess) return e;
   return launch_dependent(kernel, dim3((unsigned)(B * cluster)), dim3(kSelThreads), smem, s, cluster, false, p, cluster);
 }
