@@ -25,13 +25,13 @@ namespace {
 // Where many elements tie at the bound, the lists overflow and the block picks its best one by one instead.  No workspace
 // and one launch; sums are joined in a fixed order and a shared list's order decides nothing, so results are reproducible.
 
-constexpr int kSelThreads = 256, kSelWarps = kSelThreads / 32;
+constexpr int kSelThreads = 512, kSelWarps = kSelThreads / 32;
 constexpr int kMaxCluster = 8;
 constexpr int kVecs = 4;            // 16-byte vectors of a lane per tile
 constexpr int kMaxGroups = 16;      // items of one beam in a block
 constexpr int kLaneList = 1024;     // lanes that reach the first bound
 constexpr int kCandidates = 512;    // elements that reach the second
-constexpr int kRanked = 64;         // entries that are ranked at once, each against all others
+constexpr int kFewLanes = 64;       // lanes that reach the second bound
 
 // Order-preserving maps to unsigned integers above 0 (NaN excluded).
 __device__ __forceinline__ uint32_t ordered(float x) {
@@ -73,32 +73,17 @@ __device__ __forceinline__ Ranked warp_first(Ranked x) {
   return r;
 }
 
-// Writes the best `keep` of n entries to out(rank, entry), best first, by one warp; fewer if fewer have a key.
+// Gives the best `keep` of n entries to out(rank, entry), by all threads of the block: every entry against all others.
 template <typename Emit>
-__device__ __forceinline__ void warp_best(const Ranked* from, int n, int keep, Emit out) {
-  const int lane = threadIdx.x & 31;
-  if (n <= kRanked) {
-    for (int i = lane; i < n; i += 32) {
-      const Ranked x = from[i];
-      if (x.key == 0) continue;
-      int rank = 0;
-      for (int j = 0; j < n; ++j) rank += from[j].before(x);
-      if (rank < keep) out(rank, x);
-    }
-  } else {  // one after the other, each the best of what comes after the one before
-    Ranked last{~0ull, 0, 0};
-    for (int r = 0; r < keep; ++r) {
-      Ranked mine{0, 0xffffffffu, 0};
-      for (int i = lane; i < n; i += 32) {
-        const Ranked x = from[i];
-        if ((r == 0 || last.before(x)) && x.before(mine)) mine = x;
-      }
-      last = warp_first(mine);
-      if (last.key == 0) break;
-      if (lane == 0) out(r, last);
-    }
+__device__ __forceinline__ void block_best(const Ranked* from, int n, int keep, Emit out) {
+  for (int i = threadIdx.x; i < n; i += kSelThreads) {
+    const Ranked x = from[i];
+    if (x.key == 0) continue;
+    int rank = 0;
+#pragma unroll 8
+    for (int j = 0; j < n; ++j) rank += from[j].before(x);
+    if (rank < keep) out(rank, x);
   }
-  __syncwarp();
 }
 
 template <typename T>
@@ -162,16 +147,17 @@ __device__ __forceinline__ void suppress_vec(const BeamSelectParams& p, int v, i
 __device__ __forceinline__ float exp_diff(float x, float base) { return ptx::ex2_approx((x - base) * 1.4426950408889634f); }
 
 template <typename T>
-__global__ void __launch_bounds__(kSelThreads, 3) beam_select_kernel(const __grid_constant__ BeamSelectParams p, int cluster) {
-  extern __shared__ __align__(16) uint32_t lane_key[];  // [item][lane]: the lane's maximum, later its ordered score's high half
-  __shared__ float2 stat[kMaxBeams * kMaxGroups];       // (maximum, sum) of an item
+__global__ void __launch_bounds__(kSelThreads, 2) beam_select_kernel(const __grid_constant__ BeamSelectParams p, int cluster) {
+  // [item][lane]: (maximum, sum) of the lane's elements; later .x is the high half of its ordered best score
+  extern __shared__ __align__(16) float2 lane_stat[];
   __shared__ float2 part[kMaxCluster][kMaxBeams];       // of a beam, from every block
   __shared__ Ranked gather[kMaxCluster * kMaxKeep];     // first block: the blocks' lists
   __shared__ Ranked cand[kCandidates + kMaxBeams];
-  __shared__ unsigned short lanes[kLaneList], few[kRanked];
+  __shared__ unsigned short lanes[kLaneList], few[kFewLanes];
   __shared__ Ranked warp_top[kSelWarps];
   __shared__ double lse[kMaxBeams];
   __shared__ int live_row[kMaxBeams];  // beams whose logits are read
+  __shared__ unsigned char row_of[kMaxBeams * kMaxGroups], group_of[kMaxBeams * kMaxGroups];  // of an item: index into live_row, share of the slice
   __shared__ int n_live, n_done, n_lanes, n_few, n_cand;
   __shared__ unsigned bound, bound2;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
@@ -201,6 +187,11 @@ __global__ void __launch_bounds__(kSelThreads, 3) beam_select_kernel(const __gri
       bound = bound2 = 0;
     }
   }
+  for (int i = tid; i < p.n_beam * p.groups; i += kSelThreads) {
+    const int r = i / p.groups;
+    row_of[i] = (unsigned char)r;
+    group_of[i] = (unsigned char)(i - r * p.groups);
+  }
   __syncthreads();
   const int n_items = n_live * p.groups;
 
@@ -211,9 +202,9 @@ __global__ void __launch_bounds__(kSelThreads, 3) beam_select_kernel(const __gri
   };
   auto place = [&](int item) {
     Place x;
-    x.row = reinterpret_cast<const T*>(p.logits) + ((long)b * p.n_beam + live_row[item / p.groups]) * p.ld;
+    x.row = reinterpret_cast<const T*>(p.logits) + ((long)b * p.n_beam + live_row[row_of[item]]) * p.ld;
     const int shift = (int)(((uintptr_t)x.row / sizeof(T)) % kVec);  // vectors start at 16-byte borders
-    x.first = rank * p.slice - shift + item % p.groups * p.tiles * kTile;
+    x.first = rank * p.slice - shift + group_of[item] * p.tiles * kTile;
     x.end = min(p.vocab, (rank + 1) * p.slice - shift);
     return x;
   };
@@ -258,12 +249,7 @@ __global__ void __launch_bounds__(kSelThreads, 3) beam_select_kernel(const __gri
     l = (sum[0] + sum[1]) + (sum[2] + sum[3]);
     m = fmaxf(top, -INFINITY);
     if (tile == 0) {  // the item is complete
-      lane_key[now_item * 32 + lane] = __float_as_uint(m);
-      const float wm = from_ordered(__reduce_max_sync(0xffffffffu, ordered(m)));
-      float wl = l * exp_diff(m, wm > -INFINITY ? wm : 0.f);
-#pragma unroll
-      for (int o = 16; o > 0; o >>= 1) wl += __shfl_xor_sync(0xffffffffu, wl, o);
-      if (lane == 0) stat[now_item] = make_float2(wm, wl);
+      lane_stat[now_item * 32 + lane] = make_float2(m, l);
       m = -INFINITY;
       l = 0.f;
     }
@@ -272,14 +258,20 @@ __global__ void __launch_bounds__(kSelThreads, 3) beam_select_kernel(const __gri
   }
   __syncthreads();
 
-  // ---- the beams' log-sums: items of a block, then blocks of the cluster, in order
+  // ---- the beams' log-sums: lanes of a block, then blocks of the cluster, in a fixed order; one warp per beam
   ptx::cluster_wait();  // every block of the cluster runs
   for (int i = warp; i < n_live; i += kSelWarps) {
-    const float2 s = lane < p.groups ? stat[i * p.groups + lane] : make_float2(-INFINITY, 0.f);
-    const float wm = from_ordered(__reduce_max_sync(0xffffffffu, ordered(s.x)));
-    float wl = s.y == 0.f ? 0.f : s.y * exp_diff(s.x, wm);
+    const float2* from = lane_stat + i * p.groups * 32 + lane;
+    float top = -INFINITY;
+    for (int g = 0; g < p.groups; ++g) top = fmaxf(top, from[g * 32].x);
+    const float wm = from_ordered(__reduce_max_sync(0xffffffffu, ordered(top)));
+    float wl = 0.f;
+    for (int g = 0; g < p.groups; ++g) {
+      const float2 s = from[g * 32];
+      if (s.y != 0.f) wl += s.y * exp_diff(s.x, wm > -INFINITY ? wm : 0.f);
+    }
 #pragma unroll
-    for (int o = 8; o > 0; o >>= 1) wl += __shfl_xor_sync(0xffffffffu, wl, o);
+    for (int o = 16; o > 0; o >>= 1) wl += __shfl_xor_sync(0xffffffffu, wl, o);
     if (lane < cluster) ptx::st_cluster_v2(ptx::map_to_cta(ptx::smem_u32(&part[rank][i]), lane), __float_as_uint(wm), __float_as_uint(wl));
   }
   __syncwarp();
@@ -288,10 +280,14 @@ __global__ void __launch_bounds__(kSelThreads, 3) beam_select_kernel(const __gri
   for (int i = warp; i < n_live; i += kSelWarps) {
     const float2 s = lane < cluster ? part[lane][i] : make_float2(-INFINITY, 0.f);
     const float wm = from_ordered(__reduce_max_sync(0xffffffffu, ordered(s.x)));
-    double wl = s.y == 0.f ? 0.0 : (double)(s.y * exp_diff(s.x, wm));
+    float wl = s.y == 0.f ? 0.f : s.y * exp_diff(s.x, wm > -INFINITY ? wm : 0.f);
 #pragma unroll
     for (int o = 4; o > 0; o >>= 1) wl += __shfl_xor_sync(0xffffffffu, wl, o);
-    if (lane == 0) lse[live_row[i]] = (double)wm + log(wl);  // NaN if the row holds one, or +infinity; all -infinity: no score
+    // log of 2^e f as e log 2 + log f: the float32 logarithm of 1 <= f < 2 is off by 2^-24 at most
+    const uint32_t bits = __float_as_uint(wl);
+    const double log_l = wl > 0.f && wl < INFINITY ? (double)((int)(bits >> 23) - 127) * 0.6931471805599453 + (double)logf(__uint_as_float((bits & 0x7fffffu) | 0x3f800000u))
+                                                   : (double)logf(wl);
+    if (lane == 0) lse[live_row[i]] = (double)wm + log_l;  // NaN if the row holds one, or +infinity; all -infinity: no score
   }
   __syncthreads();
 
@@ -303,18 +299,20 @@ __global__ void __launch_bounds__(kSelThreads, 3) beam_select_kernel(const __gri
   // ---- the lanes that can hold one of the best
   const int n_entries = n_items * 32;
   uint32_t high = 0;
-  for (int e = tid; e < n_entries; e += kSelThreads) {
-    const uint32_t k = (uint32_t)(key_of(live_row[(e >> 5) / p.groups], __uint_as_float(lane_key[e])) >> 32);
-    lane_key[e] = k;
+  for (int i = warp; i < n_items; i += kSelWarps) {
+    const int e = i * 32 + lane;
+    const uint32_t k = (uint32_t)(key_of(live_row[row_of[i]], lane_stat[e].x) >> 32);
+    lane_stat[e].x = __uint_as_float(k);
     high = max(high, k);
   }
   const uint32_t mine = kth_lane_key(high, p.keep);
   if (lane == 0) atomicMax(&bound, mine);
+  auto lane_key = [&](int e) { return __float_as_uint(lane_stat[e].x); };
   __syncthreads();
   {
     const uint32_t least = max(bound, 1u);
     for (int e = tid; e < n_entries; e += kSelThreads)
-      if (lane_key[e] >= least) {
+      if (lane_key(e) >= least) {
         const int i = atomicAdd(&n_lanes, 1);
         if (i < kLaneList) lanes[i] = (unsigned short)e;
       }
@@ -322,24 +320,24 @@ __global__ void __launch_bounds__(kSelThreads, 3) beam_select_kernel(const __gri
   __syncthreads();
   if (warp == 0 && n_lanes <= kLaneList) {
     uint32_t h = 0;
-    for (int i = lane; i < n_lanes; i += 32) h = max(h, lane_key[lanes[i]]);
+    for (int i = lane; i < n_lanes; i += 32) h = max(h, lane_key(lanes[i]));
     const uint32_t least = max(max(kth_lane_key(h, p.keep), bound), 1u);
     int n = 0;
     for (int i0 = 0; i0 < n_lanes; i0 += 32) {
-      const bool in = i0 + lane < n_lanes && lane_key[lanes[i0 + lane]] >= least;
+      const bool in = i0 + lane < n_lanes && lane_key(lanes[i0 + lane]) >= least;
       const unsigned who = __ballot_sync(0xffffffffu, in);
       const int to = n + __popc(who & ((1u << lane) - 1));
-      if (in && to < kRanked) few[to] = lanes[i0 + lane];
+      if (in && to < kFewLanes) few[to] = lanes[i0 + lane];
       n += __popc(who);
     }
     if (lane == 0) n_few = n, bound2 = least;
   }
   __syncthreads();
-  bool fits = n_lanes <= kLaneList && n_few <= kRanked;
+  bool fits = n_lanes <= kLaneList && n_few <= kFewLanes;
   if (fits) {
     // ---- their elements once more
     for (int q = warp; q < n_few; q += kSelWarps) {
-      const int e = few[q], w = live_row[(e >> 5) / p.groups], L = e & 31;
+      const int e = few[q], w = live_row[row_of[e >> 5]], L = e & 31;
       const Place x = place(e >> 5);
       for (int k = lane; k < p.tiles * kPerTile; k += 32) {
         const int within = k % kPerTile, v = x.first + k / kPerTile * kTile + (within / kVec * 32 + L) * kVec + within % kVec;
@@ -359,11 +357,10 @@ __global__ void __launch_bounds__(kSelThreads, 3) beam_select_kernel(const __gri
     ptx::st_cluster_v4(to_first + r * 16, (uint32_t)x.key, (uint32_t)(x.key >> 32), x.flat, 0);
   };
   if (fits) {
-    if (warp == 0) {
-      const int n = n_cand;  // a finished beam of score -infinity has no key
+    block_best(cand, n_cand, p.keep, send);
+    if (warp == 0) {  // a finished beam of score -infinity has no key
       const int keyless = __popc(__ballot_sync(0xffffffffu, lane < n_done && cand[lane].key == 0));
-      for (int r = n - keyless + lane; r < p.keep; r += 32) send(r, Ranked{0, 0, 0});
-      warp_best(cand, n, p.keep, send);
+      for (int r = n_cand - keyless + lane; r < p.keep; r += 32) send(r, Ranked{0, 0, 0});
     }
   } else {
     // ---- many ties: one by one, each the best element of the slice behind the one before
@@ -373,7 +370,7 @@ __global__ void __launch_bounds__(kSelThreads, 3) beam_select_kernel(const __gri
       Ranked best{0, 0xffffffffu, 0};
       for (int i = warp; i < n_items; i += kSelWarps) {
         const Place x = place(i);
-        const int w = live_row[i / p.groups];
+        const int w = live_row[row_of[i]];
         for (int k = 0; k < p.tiles * kVecs; ++k) {
           const int v = x.first + k / kVecs * kTile + (k % kVecs * 32 + lane) * kVec;
           float y[kVec];
@@ -411,22 +408,24 @@ __global__ void __launch_bounds__(kSelThreads, 3) beam_select_kernel(const __gri
 
   // ---- the sequence's best
   ptx::cluster_wait();
-  if (warp == 0) {
-    const long o = (long)b * p.keep;
-    for (int i = lane; i < p.keep; i += 32) {
+  const long o = (long)b * p.keep;
+  const int n = cluster * p.keep;
+  block_best(gather, n, p.keep, [&](int r, const Ranked& x) {
+    const double c = __longlong_as_double((long long)(x.key >> 63 ? x.key & ~(1ull << 63) : ~x.key));
+    const int w = (int)(x.flat / (uint32_t)p.vocab), v = (int)(x.flat - (uint32_t)w * (uint32_t)p.vocab);
+    p.out_scores[o + r] = (float)c;
+    p.out_parents[o + r] = w;
+    p.out_tokens[o + r] = v;
+    if (p.out_finished) p.out_finished[o + r] = v == p.end_token;  // what a finished beam offers is end_token
+  });
+  if (warp == kSelWarps - 1) {  // places without a continuation
+    int found = 0;
+    for (int i0 = 0; i0 < n; i0 += 32) found += __popc(__ballot_sync(0xffffffffu, i0 + lane < n && gather[i0 + lane].key != 0));
+    for (int i = found + lane; i < p.keep; i += 32) {
       p.out_scores[o + i] = -INFINITY;
       p.out_parents[o + i] = p.out_tokens[o + i] = -1;
       if (p.out_finished) p.out_finished[o + i] = 0;
     }
-    __syncwarp();
-    warp_best(gather, cluster * p.keep, p.keep, [&](int r, const Ranked& x) {
-      const double c = __longlong_as_double((long long)(x.key >> 63 ? x.key & ~(1ull << 63) : ~x.key));
-      const int w = (int)(x.flat / (uint32_t)p.vocab), v = (int)(x.flat % (uint32_t)p.vocab);
-      p.out_scores[o + r] = (float)c;
-      p.out_parents[o + r] = w;
-      p.out_tokens[o + r] = v;
-      if (p.out_finished) p.out_finished[o + r] = v == p.end_token || (p.finished && p.finished[(long)b * p.n_beam + w]);
-    });
   }
 }
 
@@ -541,14 +540,15 @@ __global__ void __launch_bounds__(kReorderThreads) beam_reorder_kernel(const __g
 
 cudaError_t launch_beam_select(BeamSelectParams p, int B, int dtype, int num_sms, cudaStream_t s) {
   const int tile = dtype == WF_BF16 ? Vec<__nv_bfloat16>::tile : Vec<float>::tile;
-  // enough blocks for two on every SM, at least one tile of every row each, at most the 8 of a portable cluster
+  // up to two blocks on every SM (what their registers allow), at least one tile of every row each, at most the 8 of a
+  // portable cluster
   int cluster = 1;
-  while (cluster < kMaxCluster && (long)B * cluster < 2L * num_sms && p.vocab > cluster * tile) cluster *= 2;
+  while (cluster < kMaxCluster && (long)B * cluster <= num_sms && p.vocab > cluster * tile) cluster *= 2;
   p.slice = ((p.vocab + 8 + cluster - 1) / cluster + 7) / 8 * 8;
   const int n_tiles = (p.slice + tile - 1) / tile;
   p.tiles = (n_tiles + kMaxGroups - 1) / kMaxGroups;
   p.groups = (n_tiles + p.tiles - 1) / p.tiles;
-  const size_t smem = (size_t)p.n_beam * p.groups * 32 * sizeof(uint32_t);  // at most 32 KB
+  const size_t smem = (size_t)p.n_beam * p.groups * 32 * sizeof(float2);  // at most 64 KB
   auto kernel = dtype == WF_BF16 ? beam_select_kernel<__nv_bfloat16> : beam_select_kernel<float>;
   cudaError_t e = cudaSuccess;
   if (smem > 16 * 1024) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
