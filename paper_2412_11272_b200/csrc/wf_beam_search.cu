@@ -44,11 +44,11 @@ __device__ __forceinline__ uint64_t ordered(double x) {
   return b >> 63 ? ~b : b | (1ull << 63);
 }
 
-struct Ranked {
+struct __align__(16) Ranked {
   uint64_t key;   // ordered score; 0: none
   uint32_t flat;  // beam * vocab + token
   uint32_t pad;
-  __device__ __forceinline__ bool before(const Ranked& o) const { return key > o.key || (key == o.key && flat < o.flat); }
+  __device__ __forceinline__ bool before(const Ranked& o) const { return (key > o.key) | ((key == o.key) & (flat < o.flat)); }
 };
 
 // keep-th largest of the lanes' keys (0 counts as none; 0 if there are fewer).
@@ -81,7 +81,10 @@ __device__ __forceinline__ void block_best(const Ranked* from, int n, int keep, 
     if (x.key == 0) continue;
     int rank = 0;
 #pragma unroll 8
-    for (int j = 0; j < n; ++j) rank += from[j].before(x);
+    for (int j = 0; j < n; ++j) {
+      const uint4 r = *reinterpret_cast<const uint4*>(from + j);  // one load, no branch
+      rank += Ranked{((uint64_t)r.y << 32) | r.x, r.z, 0}.before(x);
+    }
     if (rank < keep) out(rank, x);
   }
 }
@@ -128,19 +131,20 @@ __device__ __forceinline__ uint4 load_vec(const T* row, int v, int end) {
   }
   return make_uint4(w[0], w[1], w[2], w[3]);
 }
-// Sets suppressed elements to -infinity.
-template <int n>
-__device__ __forceinline__ void suppress_vec(const BeamSelectParams& p, int v, int end, float* x) {
-  if (v + n <= 0 || v >= end) return;
+// Bits of elements v .. v + n - 1 (bit e: element v + e is suppressed); those outside [0, end) are anything.
+__device__ __forceinline__ unsigned suppress_bits(const BeamSelectParams& p, int v, int end) {
+  if (!p.suppress || v >= end || v <= -8) return 0;
   const unsigned char* bytes = reinterpret_cast<const unsigned char*>(p.suppress);
   const int from = max(v, 0), at = from >> 3;
-  unsigned word = __ldg(bytes + at);
-  if (at + 1 < (p.vocab + 31) / 32 * 4) word |= (unsigned)__ldg(bytes + at + 1) << 8;
-  word = (word >> (from & 7)) << (from - v);
-  if (word & ((1u << n) - 1)) {
+  const unsigned lo = __ldg(bytes + at), hi = __ldg(bytes + min(at + 1, (p.vocab - 1) >> 3));
+  return ((lo | (hi << 8)) >> (from & 7)) << (from - v);
+}
+template <int n>
+__device__ __forceinline__ void suppress_vec(unsigned bits, float* x) {
+  if (bits & ((1u << n) - 1)) {
 #pragma unroll
     for (int e = 0; e < n; ++e)
-      if ((word >> e) & 1) x[e] = -INFINITY;
+      if ((bits >> e) & 1) x[e] = -INFINITY;
   }
 }
 
@@ -156,6 +160,7 @@ __global__ void __launch_bounds__(kSelThreads, 2) beam_select_kernel(const __gri
   __shared__ unsigned short lanes[kLaneList], few[kFewLanes];
   __shared__ Ranked warp_top[kSelWarps];
   __shared__ double lse[kMaxBeams];
+  __shared__ float score[kMaxBeams];
   __shared__ int live_row[kMaxBeams];  // beams whose logits are read
   __shared__ unsigned char row_of[kMaxBeams * kMaxGroups], group_of[kMaxBeams * kMaxGroups];  // of an item: index into live_row, share of the slice
   __shared__ int n_live, n_done, n_lanes, n_few, n_cand;
@@ -166,17 +171,17 @@ __global__ void __launch_bounds__(kSelThreads, 2) beam_select_kernel(const __gri
   ptx::cluster_arrive();
 
   if (warp == 0) {
-    int live = p.n_beam;
-    if (p.beams) {
-      const int asked = __ldg(p.beams + b);
-      live = min(max(asked, 0), p.n_beam);
-      if (live != asked && rank == 0 && lane == 0) report(p.status, kBadRows);
-    }
-    const bool done = lane < live && p.finished && p.finished[(long)b * p.n_beam + lane];
+    const int asked = p.beams ? __ldg(p.beams + b) : p.n_beam;
+    const bool flag = p.finished && lane < p.n_beam && __ldg(p.finished + (long)b * p.n_beam + lane);
+    const float mine = lane < p.n_beam ? __ldg(p.scores + (long)b * p.n_beam + lane) : 0.f;
+    if (lane < p.n_beam) score[lane] = mine;
+    const int live = min(max(asked, 0), p.n_beam);
+    if (live != asked && rank == 0 && lane == 0) report(p.status, kBadRows);
+    const bool done = lane < live && flag;
     const unsigned ended = __ballot_sync(0xffffffffu, done), open = __ballot_sync(0xffffffffu, lane < live && !done);
     if (lane < live && !done) live_row[__popc(open & ((1u << lane) - 1))] = lane;
     if (done && rank == 0) {  // the one continuation of a finished beam
-      const double c = (double)__ldg(p.scores + (long)b * p.n_beam + lane);
+      const double c = (double)mine;
       cand[__popc(ended & ((1u << lane) - 1))] = Ranked{c > -INFINITY ? ordered(c) : 0, (uint32_t)lane * (uint32_t)p.vocab + (uint32_t)p.end_token, 0};
     }
     if (lane == 0) {
@@ -209,17 +214,21 @@ __global__ void __launch_bounds__(kSelThreads, 2) beam_select_kernel(const __gri
     return x;
   };
   uint4 raw[kVecs];
+  unsigned off[kVecs];
   Place at{};
   int item = warp, tile = 0;
   if (item < n_items) {
     at = place(item);
 #pragma unroll
-    for (int j = 0; j < kVecs; ++j) raw[j] = load_vec(at.row, at.first + (j * 32 + lane) * kVec, at.end);
+    for (int j = 0; j < kVecs; ++j) {
+      const int v = at.first + (j * 32 + lane) * kVec;
+      raw[j] = load_vec(at.row, v, at.end);
+      off[j] = suppress_bits(p, v, at.end);
+    }
   }
   float m = -INFINITY, l = 0.f;
   while (item < n_items) {
-    const Place now = at;
-    const int now_item = item, now_first = at.first + tile * kTile;
+    const int now_item = item;
     // the next tile
     if (++tile == p.tiles) {
       tile = 0;
@@ -227,17 +236,20 @@ __global__ void __launch_bounds__(kSelThreads, 2) beam_select_kernel(const __gri
       if (item < n_items) at = place(item);
     }
     uint4 next[kVecs];
+    unsigned next_off[kVecs];
     if (item < n_items) {
 #pragma unroll
-      for (int j = 0; j < kVecs; ++j) next[j] = load_vec(at.row, at.first + tile * kTile + (j * 32 + lane) * kVec, at.end);
+      for (int j = 0; j < kVecs; ++j) {
+        const int v = at.first + tile * kTile + (j * 32 + lane) * kVec;
+        next[j] = load_vec(at.row, v, at.end);
+        next_off[j] = suppress_bits(p, v, at.end);
+      }
     }
     float x[kPerTile];
 #pragma unroll
     for (int j = 0; j < kVecs; ++j) Vec<T>::unpack(raw[j], x + j * kVec);
-    if (p.suppress) {
 #pragma unroll
-      for (int j = 0; j < kVecs; ++j) suppress_vec<kVec>(p, now_first + (j * 32 + lane) * kVec, now.end, x + j * kVec);
-    }
+    for (int j = 0; j < kVecs; ++j) suppress_vec<kVec>(off[j], x + j * kVec);
     float top = x[0];
 #pragma unroll
     for (int i = 1; i < kPerTile; ++i) top = fmaxf(top, x[i]);
@@ -254,7 +266,7 @@ __global__ void __launch_bounds__(kSelThreads, 2) beam_select_kernel(const __gri
       l = 0.f;
     }
 #pragma unroll
-    for (int j = 0; j < kVecs; ++j) raw[j] = next[j];
+    for (int j = 0; j < kVecs; ++j) raw[j] = next[j], off[j] = next_off[j];
   }
   __syncthreads();
 
@@ -291,9 +303,8 @@ __global__ void __launch_bounds__(kSelThreads, 2) beam_select_kernel(const __gri
   }
   __syncthreads();
 
-  const float* scores = p.scores + (long)b * p.n_beam;
   auto key_of = [&](int w, float x) -> uint64_t {
-    const double c = (double)__ldg(scores + w) + ((double)x - lse[w]);
+    const double c = (double)score[w] + ((double)x - lse[w]);
     return x > -INFINITY && c > -INFINITY ? ordered(c) : 0;  // false for NaN
   };
   // ---- the lanes that can hold one of the best
@@ -341,8 +352,9 @@ __global__ void __launch_bounds__(kSelThreads, 2) beam_select_kernel(const __gri
       const Place x = place(e >> 5);
       for (int k = lane; k < p.tiles * kPerTile; k += 32) {
         const int within = k % kPerTile, v = x.first + k / kPerTile * kTile + (within / kVec * 32 + L) * kVec + within % kVec;
-        if (v < 0 || v >= x.end || suppressed(p, v)) continue;
-        const uint64_t key = key_of(w, to_f32(x.row[v]));
+        if (v < 0 || v >= x.end) continue;
+        const float y = to_f32(x.row[v]);
+        const uint64_t key = suppressed(p, v) ? 0 : key_of(w, y);
         if ((uint32_t)(key >> 32) >= bound2) {
           const int i = atomicAdd(&n_cand, 1);
           if (i < kCandidates) cand[i] = Ranked{key, (uint32_t)w * (uint32_t)p.vocab + (uint32_t)v, 0};
@@ -375,7 +387,7 @@ __global__ void __launch_bounds__(kSelThreads, 2) beam_select_kernel(const __gri
           const int v = x.first + k / kVecs * kTile + (k % kVecs * 32 + lane) * kVec;
           float y[kVec];
           Vec<T>::unpack(load_vec(x.row, v, x.end), y);
-          if (p.suppress) suppress_vec<kVec>(p, v, x.end, y);
+          suppress_vec<kVec>(suppress_bits(p, v, x.end), y);
 #pragma unroll
           for (int e = 0; e < kVec; ++e) {
             const Ranked z{key_of(w, y[e]), (uint32_t)w * (uint32_t)p.vocab + (uint32_t)(v + e), 0};
