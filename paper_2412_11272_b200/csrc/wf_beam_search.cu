@@ -27,6 +27,7 @@ namespace {
 
 constexpr int kSelThreads = 512, kSelWarps = kSelThreads / 32;
 constexpr int kMaxCluster = 8;
+constexpr float kLog2e = 1.4426950408889634f;
 constexpr int kVecs = 4;            // 16-byte vectors of a lane per tile
 constexpr int kMaxGroups = 16;      // items of one beam in a block
 constexpr int kLaneList = 1024;     // lanes that reach the first bound
@@ -51,15 +52,24 @@ struct __align__(16) Ranked {
   __device__ __forceinline__ bool before(const Ranked& o) const { return (key > o.key) | ((key == o.key) & (flat < o.flat)); }
 };
 
-// keep-th largest of the lanes' keys (0 counts as none; 0 if there are fewer).
-__device__ __forceinline__ uint32_t kth_lane_key(uint32_t key, int keep) {
-  uint32_t top = 0;
-  for (int i = 0; i < keep; ++i) {
-    top = __reduce_max_sync(0xffffffffu, key);
-    const unsigned who = __ballot_sync(0xffffffffu, key == top);
-    if ((threadIdx.x & 31) == __ffs(who) - 1) key = 0;
+// keep-th largest of the lanes' keys (0 if fewer lanes have one), by counting for every lane the keys before its own;
+// `space`: 32 words of shared memory of the warp's own.
+__device__ __forceinline__ uint32_t kth_lane_key(uint32_t key, int keep, uint32_t* space) {
+  const int lane = threadIdx.x & 31;
+  space[lane] = key;
+  __syncwarp();
+  int before = 0;
+#pragma unroll
+  for (int i = 0; i < 32; i += 4) {
+    const uint4 k = *reinterpret_cast<const uint4*>(space + i);
+    before += (k.x > key) | ((k.x == key) & (i < lane));
+    before += (k.y > key) | ((k.y == key) & (i + 1 < lane));
+    before += (k.z > key) | ((k.z == key) & (i + 2 < lane));
+    before += (k.w > key) | ((k.w == key) & (i + 3 < lane));
   }
-  return top;
+  __syncwarp();
+  const unsigned who = __ballot_sync(0xffffffffu, before == keep - 1);  // one lane: the places are 0 .. 31
+  return __shfl_sync(0xffffffffu, key, __ffs(who) - 1);
 }
 
 // The best of the lanes' entries, in every lane.
@@ -93,6 +103,18 @@ template <typename T>
 struct Vec {  // 16 bytes of logits
   static constexpr int n = 16 / (int)sizeof(T);
   static constexpr int tile = kVecs * 32 * n;
+  // largest element; NaN counts as nothing
+  static __device__ __forceinline__ float max(const uint4& r) {
+    if constexpr (sizeof(T) == 4) {
+      return fmaxf(fmaxf(fmaxf(__uint_as_float(r.x), __uint_as_float(r.y)), fmaxf(__uint_as_float(r.z), __uint_as_float(r.w))), -INFINITY);
+    } else {
+      uint32_t a, b;
+      asm("max.bf16x2 %0, %1, %2;" : "=r"(a) : "r"(r.x), "r"(r.y));
+      asm("max.bf16x2 %0, %1, %2;" : "=r"(b) : "r"(r.z), "r"(r.w));
+      asm("max.bf16x2 %0, %1, %2;" : "=r"(a) : "r"(a), "r"(b));
+      return fmaxf(fmaxf(__uint_as_float(a << 16), __uint_as_float(a & 0xffff0000u)), -INFINITY);
+    }
+  }
   static __device__ __forceinline__ void unpack(const uint4& r, float* x) {
     const uint32_t w[4] = {r.x, r.y, r.z, r.w};
 #pragma unroll
@@ -139,16 +161,23 @@ __device__ __forceinline__ unsigned suppress_bits(const BeamSelectParams& p, int
   const unsigned lo = __ldg(bytes + at), hi = __ldg(bytes + min(at + 1, (p.vocab - 1) >> 3));
   return ((lo | (hi << 8)) >> (from & 7)) << (from - v);
 }
-template <int n>
-__device__ __forceinline__ void suppress_vec(unsigned bits, float* x) {
-  if (bits & ((1u << n) - 1)) {
+template <typename T>
+__device__ __forceinline__ void suppress_vec(unsigned bits, uint4& r) {
+  if (bits & ((1u << Vec<T>::n) - 1)) {
+    uint32_t* w = &r.x;
 #pragma unroll
-    for (int e = 0; e < n; ++e)
-      if ((bits >> e) & 1) x[e] = -INFINITY;
+    for (int i = 0; i < 4; ++i) {
+      if constexpr (sizeof(T) == 4) {
+        if ((bits >> i) & 1) w[i] = 0xff800000u;
+      } else {
+        if ((bits >> (2 * i)) & 1) w[i] = (w[i] & 0xffff0000u) | 0xff80u;
+        if ((bits >> (2 * i)) & 2) w[i] = (w[i] & 0x0000ffffu) | 0xff800000u;
+      }
+    }
   }
 }
 
-__device__ __forceinline__ float exp_diff(float x, float base) { return ptx::ex2_approx((x - base) * 1.4426950408889634f); }
+__device__ __forceinline__ float exp_diff(float x, float base) { return ptx::ex2_approx((x - base) * kLog2e); }
 
 template <typename T>
 __global__ void __launch_bounds__(kSelThreads, 2) beam_select_kernel(const __grid_constant__ BeamSelectParams p, int cluster) {
@@ -159,6 +188,7 @@ __global__ void __launch_bounds__(kSelThreads, 2) beam_select_kernel(const __gri
   __shared__ Ranked cand[kCandidates + kMaxBeams];
   __shared__ unsigned short lanes[kLaneList], few[kFewLanes];
   __shared__ Ranked warp_top[kSelWarps];
+  __shared__ __align__(16) uint32_t space[kSelWarps][32];
   __shared__ double lse[kMaxBeams];
   __shared__ float score[kMaxBeams];
   __shared__ int live_row[kMaxBeams];  // beams whose logits are read
@@ -245,21 +275,31 @@ __global__ void __launch_bounds__(kSelThreads, 2) beam_select_kernel(const __gri
         next_off[j] = suppress_bits(p, v, at.end);
       }
     }
-    float x[kPerTile];
 #pragma unroll
-    for (int j = 0; j < kVecs; ++j) Vec<T>::unpack(raw[j], x + j * kVec);
+    for (int j = 0; j < kVecs; ++j) suppress_vec<T>(off[j], raw[j]);
+    float top = m;
 #pragma unroll
-    for (int j = 0; j < kVecs; ++j) suppress_vec<kVec>(off[j], x + j * kVec);
-    float top = x[0];
+    for (int j = 0; j < kVecs; ++j) top = fmaxf(top, Vec<T>::max(raw[j]));
+    const float base = top > -INFINITY ? top : 0.f;  // an all-NaN lane has top = -infinity: base 0, the sum is NaN
+    // sum of exp(x - base), two elements per arithmetic instruction
+    const uint64_t minus = ptx::pack_f32x2(-base, -base), log2e = ptx::pack_f32x2(kLog2e, kLog2e);
+    uint64_t sum[2] = {ptx::pack_f32x2(l * exp_diff(m, base), 0.f), 0ull};
 #pragma unroll
-    for (int i = 1; i < kPerTile; ++i) top = fmaxf(top, x[i]);
-    top = fmaxf(top, m);
-    const float base = top > -INFINITY ? top : 0.f;  // an all-NaN lane has top = NaN: base 0, the sum is NaN
-    float sum[4] = {l * exp_diff(m, base), 0.f, 0.f, 0.f};
+    for (int j = 0; j < kVecs; ++j) {
+      float x[kVec];
+      Vec<T>::unpack(raw[j], x);
 #pragma unroll
-    for (int i = 0; i < kPerTile; ++i) sum[i % 4] += exp_diff(x[i], base);
-    l = (sum[0] + sum[1]) + (sum[2] + sum[3]);
-    m = fmaxf(top, -INFINITY);
+      for (int e = 0; e < kVec; e += 2) {
+        float lo, hi;
+        ptx::unpack_f32x2(ptx::mul_f32x2(ptx::add_f32x2(ptx::pack_f32x2(x[e], x[e + 1]), minus), log2e), lo, hi);
+        sum[(e / 2) % 2] = ptx::add_f32x2(sum[(e / 2) % 2], ptx::pack_f32x2(ptx::ex2_approx(lo), ptx::ex2_approx(hi)));
+      }
+    }
+    float s0, s1, s2, s3;
+    ptx::unpack_f32x2(sum[0], s0, s1);
+    ptx::unpack_f32x2(sum[1], s2, s3);
+    l = (s0 + s1) + (s2 + s3);
+    m = top;
     if (tile == 0) {  // the item is complete
       lane_stat[now_item * 32 + lane] = make_float2(m, l);
       m = -INFINITY;
@@ -308,7 +348,6 @@ __global__ void __launch_bounds__(kSelThreads, 2) beam_select_kernel(const __gri
     return x > -INFINITY && c > -INFINITY ? ordered(c) : 0;  // false for NaN
   };
   // ---- the lanes that can hold one of the best
-  const int n_entries = n_items * 32;
   uint32_t high = 0;
   for (int i = warp; i < n_items; i += kSelWarps) {
     const int e = i * 32 + lane;
@@ -316,23 +355,28 @@ __global__ void __launch_bounds__(kSelThreads, 2) beam_select_kernel(const __gri
     lane_stat[e].x = __uint_as_float(k);
     high = max(high, k);
   }
-  const uint32_t mine = kth_lane_key(high, p.keep);
+  const uint32_t mine = kth_lane_key(high, p.keep, space[warp]);
   if (lane == 0) atomicMax(&bound, mine);
   auto lane_key = [&](int e) { return __float_as_uint(lane_stat[e].x); };
   __syncthreads();
   {
     const uint32_t least = max(bound, 1u);
-    for (int e = tid; e < n_entries; e += kSelThreads)
-      if (lane_key(e) >= least) {
-        const int i = atomicAdd(&n_lanes, 1);
-        if (i < kLaneList) lanes[i] = (unsigned short)e;
-      }
+    for (int i = warp; i < n_items; i += kSelWarps) {
+      const int e = i * 32 + lane;
+      const bool in = lane_key(e) >= least;
+      const unsigned who = __ballot_sync(0xffffffffu, in);
+      if (who == 0) continue;
+      int to = 0;
+      if (lane == 0) to = atomicAdd(&n_lanes, __popc(who));
+      to = __shfl_sync(0xffffffffu, to, 0) + __popc(who & ((1u << lane) - 1));
+      if (in && to < kLaneList) lanes[to] = (unsigned short)e;
+    }
   }
   __syncthreads();
   if (warp == 0 && n_lanes <= kLaneList) {
     uint32_t h = 0;
     for (int i = lane; i < n_lanes; i += 32) h = max(h, lane_key(lanes[i]));
-    const uint32_t least = max(max(kth_lane_key(h, p.keep), bound), 1u);
+    const uint32_t least = max(max(kth_lane_key(h, p.keep, space[0]), bound), 1u);
     int n = 0;
     for (int i0 = 0; i0 < n_lanes; i0 += 32) {
       const bool in = i0 + lane < n_lanes && lane_key(lanes[i0 + lane]) >= least;
@@ -386,8 +430,9 @@ __global__ void __launch_bounds__(kSelThreads, 2) beam_select_kernel(const __gri
         for (int k = 0; k < p.tiles * kVecs; ++k) {
           const int v = x.first + k / kVecs * kTile + (k % kVecs * 32 + lane) * kVec;
           float y[kVec];
-          Vec<T>::unpack(load_vec(x.row, v, x.end), y);
-          suppress_vec<kVec>(suppress_bits(p, v, x.end), y);
+          uint4 bits = load_vec(x.row, v, x.end);
+          suppress_vec<T>(suppress_bits(p, v, x.end), bits);
+          Vec<T>::unpack(bits, y);
 #pragma unroll
           for (int e = 0; e < kVec; ++e) {
             const Ranked z{key_of(w, y[e]), (uint32_t)w * (uint32_t)p.vocab + (uint32_t)(v + e), 0};
