@@ -130,6 +130,12 @@ struct Vec {  // 16 bytes of logits
 };
 __device__ __forceinline__ uint32_t bits_of(float x) { return __float_as_uint(x); }
 __device__ __forceinline__ uint32_t bits_of(__nv_bfloat16 x) { return (uint32_t)__bfloat16_as_ushort(x); }
+template <typename T>
+__device__ __forceinline__ T minus_infinity();
+template <>
+__device__ __forceinline__ float minus_infinity<float>() { return -INFINITY; }
+template <>
+__device__ __forceinline__ __nv_bfloat16 minus_infinity<__nv_bfloat16>() { return __ushort_as_bfloat16(0xff80); }
 __device__ __forceinline__ float to_f32(float x) { return x; }
 __device__ __forceinline__ float to_f32(__nv_bfloat16 x) { return __bfloat162float(x); }
 
@@ -179,10 +185,23 @@ __device__ __forceinline__ void suppress_vec(unsigned bits, uint4& r) {
 
 __device__ __forceinline__ float exp_diff(float x, float base) { return ptx::ex2_approx((x - base) * kLog2e); }
 
+// Starts the copy of elements v .. v + n - 1 of a row to 16 bytes of shared memory; those outside [0, end) are not read and
+// anything there.
 template <typename T>
+__device__ __forceinline__ void copy_vec(const T* row, int v, int end, uint4* to) {
+  constexpr int n = Vec<T>::n;
+  if (v >= 0) {
+    if (v < end) ptx::cp_async_16_partial(ptx::smem_u32(to), row + v, (uint32_t)min(n, end - v) * (uint32_t)sizeof(T));
+  } else if (v > -n) {
+    *to = load_vec(row, v, end);
+  }
+}
+
+template <typename T, int kStages>
 __global__ void __launch_bounds__(kSelThreads, 2) beam_select_kernel(const __grid_constant__ BeamSelectParams p, int cluster) {
   // [item][lane]: (maximum, sum) of the lane's elements; later .x is the high half of its ordered best score
   extern __shared__ __align__(16) float2 lane_stat[];
+  uint4* ring = reinterpret_cast<uint4*>(lane_stat + p.n_beam * p.groups * 32) + (threadIdx.x >> 5) * (kStages * kVecs * 32);  // the warp's tiles in flight
   __shared__ float2 part[kMaxCluster][kMaxBeams];       // of a beam, from every block
   __shared__ Ranked gather[kMaxCluster * kMaxKeep];     // first block: the blocks' lists
   __shared__ Ranked cand[kCandidates + kMaxBeams];
@@ -192,7 +211,12 @@ __global__ void __launch_bounds__(kSelThreads, 2) beam_select_kernel(const __gri
   __shared__ double lse[kMaxBeams];
   __shared__ float score[kMaxBeams];
   __shared__ int live_row[kMaxBeams];  // beams whose logits are read
-  __shared__ unsigned char row_of[kMaxBeams * kMaxGroups], group_of[kMaxBeams * kMaxGroups];  // of an item: index into live_row, share of the slice
+  struct Place {
+    const T* row;
+    int first, end;  // first element of the item's first tile, end of the slice
+  };
+  __shared__ __align__(16) Place place[kMaxBeams * kMaxGroups];   // of an item
+  __shared__ unsigned char beam_of[kMaxBeams * kMaxGroups];
   __shared__ int n_live, n_done, n_lanes, n_few, n_cand;
   __shared__ unsigned bound, bound2;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
@@ -222,61 +246,92 @@ __global__ void __launch_bounds__(kSelThreads, 2) beam_select_kernel(const __gri
       bound = bound2 = 0;
     }
   }
-  for (int i = tid; i < p.n_beam * p.groups; i += kSelThreads) {
-    const int r = i / p.groups;
-    row_of[i] = (unsigned char)r;
-    group_of[i] = (unsigned char)(i - r * p.groups);
-  }
   __syncthreads();
   const int n_items = n_live * p.groups;
+  for (int i = tid; i < n_items; i += kSelThreads) {
+    const int r = i / p.groups, w = live_row[r];
+    const T* row = reinterpret_cast<const T*>(p.logits) + ((long)b * p.n_beam + w) * p.ld;
+    const int shift = (int)(((uintptr_t)row / sizeof(T)) % kVec);  // vectors start at 16-byte borders
+    place[i] = Place{row, rank * p.slice - shift + (i - r * p.groups) * p.tiles * kTile, min(p.vocab, (rank + 1) * p.slice - shift)};
+    beam_of[i] = (unsigned char)w;
+  }
+  __syncthreads();
 
   // ---- one pass over the logits
-  struct Place {
-    const T* row;
-    int first, end;  // first element of the item's first tile, end of the slice
-  };
-  auto place = [&](int item) {
-    Place x;
-    x.row = reinterpret_cast<const T*>(p.logits) + ((long)b * p.n_beam + live_row[row_of[item]]) * p.ld;
-    const int shift = (int)(((uintptr_t)x.row / sizeof(T)) % kVec);  // vectors start at 16-byte borders
-    x.first = rank * p.slice - shift + group_of[item] * p.tiles * kTile;
-    x.end = min(p.vocab, (rank + 1) * p.slice - shift);
-    return x;
-  };
-  uint4 raw[kVecs];
-  unsigned off[kVecs];
-  Place at{};
-  int item = warp, tile = 0;
-  if (item < n_items) {
-    at = place(item);
+  // A warp's tiles are copied to shared memory kStages ahead; every lane copies and reads its own pieces, so no barrier is
+  // needed.  (Held in registers instead, one tile ahead, the compiler waited for each tile at the end of the one before.)
+  int ahead_item = warp, ahead_tile = 0;
+  auto start_next = [&](int stage) {
+    if (ahead_item < n_items) {
+      const Place x = place[ahead_item];
+      const int v = x.first + ahead_tile * kTile + lane * kVec;
+      uint4* to = ring + stage * (kVecs * 32) + lane;
+      if (v - lane * kVec >= 0 && v - lane * kVec + kTile <= x.end) {
+        const uint32_t at = ptx::smem_u32(to);
+        const T* from = x.row + v;
 #pragma unroll
-    for (int j = 0; j < kVecs; ++j) {
-      const int v = at.first + (j * 32 + lane) * kVec;
-      raw[j] = load_vec(at.row, v, at.end);
-      off[j] = suppress_bits(p, v, at.end);
+        for (int j = 0; j < kVecs; ++j) ptx::cp_async_16(at + j * 512, from + j * 32 * kVec, true);
+      } else {
+#pragma unroll
+        for (int j = 0; j < kVecs; ++j) copy_vec(x.row, v + j * 32 * kVec, x.end, to + j * 32);
+      }
+      if (++ahead_tile == p.tiles) {
+        ahead_tile = 0;
+        ahead_item += kSelWarps;
+      }
     }
-  }
+    ptx::cp_async_commit();
+  };
+#pragma unroll
+  for (int i = 0; i < kStages; ++i) start_next(i);
+  int stage = 0;
   float m = -INFINITY, l = 0.f;
-  while (item < n_items) {
-    const int now_item = item;
-    // the next tile
+  for (int item = warp, tile = 0; item < n_items;) {
+    const Place at = place[item];
+    const int first = at.first + tile * kTile, now_item = item;
     if (++tile == p.tiles) {
       tile = 0;
       item += kSelWarps;
-      if (item < n_items) at = place(item);
     }
-    uint4 next[kVecs];
-    unsigned next_off[kVecs];
-    if (item < n_items) {
+    // words of suppression bits of the tile: lane i has the i-th, lane 0 also the one behind the lanes'
+    unsigned word = 0, word_end = 0;
+    if (p.suppress) {
+      const int w = (max(first, 0) >> 5) + lane, last = (p.vocab - 1) >> 5;
+      if (w <= last && lane <= kTile / 32) word = __ldg(p.suppress + w);
+      if (kTile == 1024 && lane == 0 && w + 32 <= last) word_end = __ldg(p.suppress + w + 32);
+    }
+    ptx::cp_async_wait<kStages - 1>();
+    uint4* mine = ring + stage * (kVecs * 32);
+    if (__any_sync(0xffffffffu, (word | word_end) != 0)) {  // suppressed elements become -infinity
+      __syncwarp();
+      const int base = (max(first, 0) >> 5) * 32;
+      auto poke = [&](unsigned bits, int at) {
+        while (bits) {
+          const int v = base + at * 32 + __ffs(bits) - 1;
+          bits &= bits - 1;
+          if (v >= first && v < first + kTile) reinterpret_cast<T*>(mine)[v - first] = minus_infinity<T>();
+        }
+      };
+      poke(word, lane);
+      poke(word_end, 32);
+      __syncwarp();
+    }
+    uint4 raw[kVecs];
+#pragma unroll
+    for (int j = 0; j < kVecs; ++j) raw[j] = mine[j * 32 + lane];
+    __syncwarp();  // other lanes' pieces may have been written above: all are read before the next copies land
+    start_next(stage);
+    stage = stage + 1 == kStages ? 0 : stage + 1;
+    if (first < 0 || first + kTile > at.end) {  // elements outside the slice are -infinity too
 #pragma unroll
       for (int j = 0; j < kVecs; ++j) {
-        const int v = at.first + tile * kTile + (j * 32 + lane) * kVec;
-        next[j] = load_vec(at.row, v, at.end);
-        next_off[j] = suppress_bits(p, v, at.end);
+        const int v = first + (j * 32 + lane) * kVec;
+        unsigned off = 0;
+        if (v < 0) off |= (1u << min(-v, kVec)) - 1;
+        if (v + kVec > at.end) off |= ~0u << min(max(at.end - v, 0), 31);
+        suppress_vec<T>(off, raw[j]);
       }
     }
-#pragma unroll
-    for (int j = 0; j < kVecs; ++j) suppress_vec<T>(off[j], raw[j]);
     float top = m;
 #pragma unroll
     for (int j = 0; j < kVecs; ++j) top = fmaxf(top, Vec<T>::max(raw[j]));
@@ -305,8 +360,6 @@ __global__ void __launch_bounds__(kSelThreads, 2) beam_select_kernel(const __gri
       m = -INFINITY;
       l = 0.f;
     }
-#pragma unroll
-    for (int j = 0; j < kVecs; ++j) raw[j] = next[j], off[j] = next_off[j];
   }
   __syncthreads();
 
@@ -351,7 +404,7 @@ __global__ void __launch_bounds__(kSelThreads, 2) beam_select_kernel(const __gri
   uint32_t high = 0;
   for (int i = warp; i < n_items; i += kSelWarps) {
     const int e = i * 32 + lane;
-    const uint32_t k = (uint32_t)(key_of(live_row[row_of[i]], lane_stat[e].x) >> 32);
+    const uint32_t k = (uint32_t)(key_of(beam_of[i], lane_stat[e].x) >> 32);
     lane_stat[e].x = __uint_as_float(k);
     high = max(high, k);
   }
@@ -392,8 +445,8 @@ __global__ void __launch_bounds__(kSelThreads, 2) beam_select_kernel(const __gri
   if (fits) {
     // ---- their elements once more
     for (int q = warp; q < n_few; q += kSelWarps) {
-      const int e = few[q], w = live_row[row_of[e >> 5]], L = e & 31;
-      const Place x = place(e >> 5);
+      const int e = few[q], w = beam_of[e >> 5], L = e & 31;
+      const Place x = place[e >> 5];
       for (int k = lane; k < p.tiles * kPerTile; k += 32) {
         const int within = k % kPerTile, v = x.first + k / kPerTile * kTile + (within / kVec * 32 + L) * kVec + within % kVec;
         if (v < 0 || v >= x.end) continue;
@@ -425,8 +478,8 @@ __global__ void __launch_bounds__(kSelThreads, 2) beam_select_kernel(const __gri
     for (int r = 0; r < p.keep; ++r) {
       Ranked best{0, 0xffffffffu, 0};
       for (int i = warp; i < n_items; i += kSelWarps) {
-        const Place x = place(i);
-        const int w = live_row[row_of[i]];
+        const Place x = place[i];
+        const int w = beam_of[i];
         for (int k = 0; k < p.tiles * kVecs; ++k) {
           const int v = x.first + k / kVecs * kTile + (k % kVecs * 32 + lane) * kVec;
           float y[kVec];
@@ -605,10 +658,12 @@ cudaError_t launch_beam_select(BeamSelectParams p, int B, int dtype, int num_sms
   const int n_tiles = (p.slice + tile - 1) / tile;
   p.tiles = (n_tiles + kMaxGroups - 1) / kMaxGroups;
   p.groups = (n_tiles + p.tiles - 1) / p.tiles;
-  const size_t smem = (size_t)p.n_beam * p.groups * 32 * sizeof(float2);  // at most 64 KB
-  auto kernel = dtype == WF_BF16 ? beam_select_kernel<__nv_bfloat16> : beam_select_kernel<float>;
-  cudaError_t e = cudaSuccess;
-  if (smem > 16 * 1024) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+  // with a block or less per SM there is room for four tiles of every warp in flight, else for two
+  const bool alone = (long)B * cluster <= num_sms;
+  const size_t smem = (size_t)p.n_beam * p.groups * 32 * sizeof(float2) + (size_t)(alone ? 4 : 2) * kSelWarps * kVecs * 32 * sizeof(uint4);  // at most 192 KB
+  auto kernel = dtype == WF_BF16 ? (alone ? beam_select_kernel<__nv_bfloat16, 4> : beam_select_kernel<__nv_bfloat16, 2>)
+                                 : (alone ? beam_select_kernel<float, 4> : beam_select_kernel<float, 2>);
+  cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
   if (e != cudaSuccess) return e;
   return launch_dependent(kernel, dim3((unsigned)(B * cluster)), dim3(kSelThreads), smem, s, cluster, false, p, cluster);
 }
