@@ -41,6 +41,8 @@ wf_status cuda_result(wf_decoder* d, const char* what, cudaError_t e) {
 // The checks that every cache operator makes.
 wf_status check_cache(wf_decoder* d, const char* what, const wf_cache* c) {
   if (!c || !c->k || !c->v || c->n_pages < 1) return fail(d, WF_ERR_INVALID_ARG, "%s: NULL cache or no pages", what);
+  if ((long)c->n_pages * d->cfg.n_kv_head * d->cfg.page_size >= (1L << 32) - 1)
+    return fail(d, WF_ERR_CAPACITY, "%s: more than 2^32 vectors in a cache", what);
   if (!aligned16(c->k) || !aligned16(c->v)) return fail(d, WF_ERR_INVALID_ARG, "%s: cache pages must be 16-byte aligned", what);
   if (d->cfg.cache_format != WF_CACHE_PATH) {
     if (!c->k_scale || !c->v_scale) return fail(d, WF_ERR_INVALID_ARG, "%s: a quantised cache needs scales", what);
@@ -224,6 +226,7 @@ wf_status wf_tree_attention(wf_decoder* d, const wf_cache* cache, const wf_rows*
   p.scale = scale;
   p.n_splits = plan.n_splits;
   p.chunk = plan.chunk;
+  p.unit_warps = plan.unit_warps;
   p.part_o = (float*)workspace;
   p.part_ml = plan.bytes ? (float2*)((float*)workspace + (size_t)rows->n_rows * c.n_head * plan.n_splits * c.d_head) : nullptr;
   p.status = status;

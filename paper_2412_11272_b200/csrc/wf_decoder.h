@@ -74,12 +74,13 @@ struct TreeAttnParams {
   // split of the positions: split i of a sequence has [i chunk, (i + 1) chunk); with more than one split the
   // unnormalised sums go to part_o [n_rows][n_head][n_splits][d_head] and (maximum, sum) to part_ml
   int n_splits, chunk;
+  int unit_warps;  // tensor-core kernel: warps that share a tile of rows (1, 2 or 4)
   float* part_o;
   float2* part_ml;
   int* status;
 };
 struct TreeAttnPlan {
-  int n_splits, chunk;
+  int n_splits, chunk, unit_warps;
   size_t bytes;
 };
 TreeAttnPlan plan_tree_attention(int dtype, int d_head, int n_head, int n_kv_head, int n_seq, int n_rows, int max_rows, int max_len,

@@ -266,17 +266,22 @@ TreeAttnPlan plan_tree_attention(int dtype, int d_head, int n_head, int n_kv_hea
   const long rows = (long)max_rows * (n_head / n_kv_head);
   const int tile = dtype == WF_BF16 ? tc_rows(d_head, rows) : kSimtRows;
   const long tiles = (rows + tile - 1) / tile;
-  const long blocks = tiles * n_kv_head * n_seq;
-  // as many splits as fill the SMs four times over, of at least 256 positions each
-  long splits = blocks >= 4L * num_sms ? 1 : (4L * num_sms + blocks - 1) / blocks;
-  const long longest = ((long)max_len + 255) / 256;
-  if (splits > longest) splits = longest;
-  if (splits < 1) splits = 1;
-  long chunk = ((long)max_len + splits - 1) / splits;
-  const int step = dtype == WF_BF16 ? 256 : kSimtKeys;
-  chunk = std::max((chunk + step - 1) / step * step, (long)step);
-  plan.chunk = (int)chunk;
-  plan.n_splits = (int)std::max(1L, ((long)max_len + chunk - 1) / chunk);
+  const long units = tiles * n_kv_head * n_seq;
+  if (dtype == WF_BF16) {
+    // Warps that the registers let reside: 16, 12 or 8 per SM.  A unit is shared by as few warps as fill them (each one has
+    // a start and an end to pay for), and cut into splits, all of one wave, where four are not enough.
+    const long resident = (long)num_sms * (tile == 8 ? 16 : tile == 16 && d_head == 64 ? 12 : 8);
+    plan.unit_warps = units >= resident ? 1 : 2 * units >= resident ? 2 : 4;
+    const long splits = std::max(1L, std::min(resident / (4 * units), ((long)max_len + 255) / 256));
+    plan.chunk = (int)(((long)max_len + splits * 64 - 1) / (splits * 64) * 64);
+  } else {
+    // as many splits as fill the SMs four times over, of at least 256 positions each
+    const long splits = std::max(1L, std::min((4L * num_sms + units - 1) / units, ((long)max_len + 255) / 256));
+    plan.unit_warps = 4;
+    plan.chunk = (int)(((long)max_len + splits * kSimtKeys - 1) / (splits * kSimtKeys) * kSimtKeys);
+  }
+  if (plan.chunk < 64) plan.chunk = 64;
+  plan.n_splits = (int)std::max(1L, ((long)max_len + plan.chunk - 1) / plan.chunk);
   plan.bytes = plan.n_splits > 1 ? (size_t)n_rows * n_head * plan.n_splits * (d_head * sizeof(float) + sizeof(float2)) : 0;
   return plan;
 }

@@ -19,7 +19,7 @@ namespace wf {
 
 namespace {
 
-constexpr int kWarps = 4, kThreads = kWarps * 32;
+constexpr int kThreads = 128;  // four warps
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 
 __device__ __forceinline__ void mma_f16(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
@@ -102,31 +102,31 @@ struct Layout {
   }
 };
 
-template <int kFormat, int kDim, int kNT>
+// A unit of work is one tile of query rows of one key/value head over one split of the positions; kW warps share it.
+template <int kDim, int kNT, int kW>
 constexpr size_t tc_smem() {
-  return (size_t)kWarps * 8 * kNT * (kDim + 4) * sizeof(float) + (size_t)2 * kWarps * 8 * kNT * sizeof(float);
+  return kW == 1 ? 0 : (size_t)4 * 8 * kNT * (kDim + 4) * sizeof(float) + (size_t)2 * 4 * 8 * kNT * sizeof(float);
 }
 
-template <int kFormat, int kDim, int kNT>
-__global__ void __launch_bounds__(kThreads, kNT == 1 ? 4 : kNT == 2 ? 3 : 2) tree_attention_tc_kernel(const __grid_constant__ TreeAttnParams p) {
+template <int kFormat, int kDim, int kNT, int kW>
+__global__ void __launch_bounds__(kThreads, kNT == 1 ? 4 : kNT == 2 && kDim == 64 ? 3 : 2) tree_attention_tc_kernel(const __grid_constant__ TreeAttnParams p, int tiles) {
   using L = Layout<kFormat, kDim>;
   constexpr bool kQuant = kFormat != WF_CACHE_PATH;
   constexpr int kRows = 8 * kNT;
   extern __shared__ __align__(16) float smem[];
-  float* part = smem;                                   // [warp][row][kDim + 4]
-  float* part_m = part + kWarps * kRows * (kDim + 4);   // [warp][row]
-  float* part_l = part_m + kWarps * kRows;
-
-  const int seq = blockIdx.z, kvh = blockIdx.y;
-  const int split = blockIdx.x % p.n_splits, tile = blockIdx.x / p.n_splits;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, t = lane & 3;
-  const Sequence s = load_sequence(p, seq, tid == 0 && blockIdx.x == 0 && kvh == 0);
+  const int seq = blockIdx.y;
+  const int unit = (int)blockIdx.x * (4 / kW) + warp / kW, rest = unit / p.n_splits;
+  const int split = unit - rest * p.n_splits, kvh = rest / tiles, tile = rest - kvh * tiles;
+  if (kvh >= p.cache.n_kv_head) return;
+  const Sequence s = load_sequence(p, seq, tid == 0 && blockIdx.x == 0);
   const int rows = min(s.n_rows, p.max_rows) * p.group;
   const int r0 = tile * kRows;
   if (r0 >= rows) return;
   const int begin = split * p.chunk, end = min(s.len, begin + p.chunk);
   if (split > 0 && begin >= s.len) return;
   const int shift = p.cache.page_shift;
+  const int* table = p.rows.page_table + (long)seq * p.rows.table_stride;
 
   // ---- queries: the second operand of S^T, element pairs matching the lane's pieces of a key
   uint32_t qf[kNT][L::kSteps][2];
@@ -180,72 +180,65 @@ __global__ void __launch_bounds__(kThreads, kNT == 1 ? 4 : kNT == 2 ? 3 : 2) tre
   // the other way round; page numbers run one block further ahead
   uint32_t kreg[L::kTiles][2][L::kKChunks][4], vreg[L::kTiles][4][L::kVWords];
   unsigned short sreg[L::kTiles];  // lanes 0 .. 15: scales of the tile's keys; 16 .. 31: of its values
-  int page[L::kTiles], page_next[L::kTiles];
-  auto load_pages = [&](int pos, int (&id)[L::kTiles]) {
+  // index of each tile's first vector in the cache, kAbsent where there is none (at most 2^32 vectors of 64 bytes or more fit a GPU)
+  constexpr uint32_t kAbsent = 0xffffffffu;
+  uint32_t vec[L::kTiles], vec_next[L::kTiles];
+  auto load_pages = [&](int pos, uint32_t (&id)[L::kTiles]) {
 #pragma unroll
     for (int i = 0; i < L::kTiles; ++i) {
       const int at = pos + 16 * i;
-      id[i] = -1;
+      id[i] = kAbsent;
       if (at < end) {
-        const int x = __ldg(p.rows.page_table + (long)seq * p.rows.table_stride + (at >> shift));
-        if (x >= 0 && x < p.cache.n_pages) id[i] = x;
+        const uint32_t x = (uint32_t)__ldg(table + (at >> shift));
+        if (x < (uint32_t)p.cache.n_pages) id[i] = ((x * (uint32_t)p.cache.n_kv_head + (uint32_t)kvh) << shift) + (uint32_t)(at & ((1 << shift) - 1));
         else if (lane == 0) report(p.status, kBadPage);
       }
     }
   };
-  auto first_vector = [&](int id, int pos) {  // index of the tile's first vector
-    return (((long)id * p.cache.n_kv_head + kvh) << shift) + (pos & ((1 << shift) - 1));
-  };
-  auto load_keys = [&](int pos, const int (&id)[L::kTiles]) {
+  const char* const key_base = reinterpret_cast<const char*>(p.cache.k) + g * L::kVecBytes + t * 16;
+  const char* const value_base = reinterpret_cast<const char*>(p.cache.v) + 2 * t * L::kVecBytes + g * (L::kVWords == 2 ? 8 : 16);
+  const unsigned short* const scale_base = reinterpret_cast<const unsigned short*>(lane < 16 ? p.cache.k_scale : p.cache.v_scale) + (lane & 15);
+  auto load_keys = [&](const uint32_t (&id)[L::kTiles]) {
 #pragma unroll
     for (int i = 0; i < L::kTiles; ++i) {
-      const char* base = reinterpret_cast<const char*>(p.cache.k) + first_vector(id[i], pos + 16 * i) * L::kVecBytes;
+      const char* base = key_base + (uint64_t)id[i] * L::kVecBytes;
 #pragma unroll
       for (int h = 0; h < 2; ++h)
 #pragma unroll
         for (int c = 0; c < L::kKChunks; ++c) {
-          if (id[i] >= 0) ldg16(base + (g + 8 * h) * L::kVecBytes + c * 64 + t * 16, kreg[i][h][c]);
+          if (id[i] != kAbsent) ldg16(base + 8 * h * L::kVecBytes + c * 64, kreg[i][h][c]);
           else kreg[i][h][c][0] = kreg[i][h][c][1] = kreg[i][h][c][2] = kreg[i][h][c][3] = 0;
         }
+      if constexpr (kQuant) sreg[i] = id[i] != kAbsent ? __ldg(scale_base + id[i]) : (unsigned short)0;
     }
   };
-  auto load_scales = [&](int pos, const int (&id)[L::kTiles]) {
-    if constexpr (kQuant) {
-#pragma unroll
-      for (int i = 0; i < L::kTiles; ++i) {
-        const __nv_bfloat16* from = (lane < 16 ? p.cache.k_scale : p.cache.v_scale) + first_vector(id[i], pos + 16 * i) + (lane & 15);
-        sreg[i] = id[i] >= 0 ? __ldg(reinterpret_cast<const unsigned short*>(from)) : (unsigned short)0;
-      }
-    }
-  };
-  auto load_values = [&](int pos, const int (&id)[L::kTiles]) {
+  auto load_values = [&](const uint32_t (&id)[L::kTiles]) {
 #pragma unroll
     for (int i = 0; i < L::kTiles; ++i) {
-      const char* base = reinterpret_cast<const char*>(p.cache.v) + first_vector(id[i], pos + 16 * i) * L::kVecBytes;
+      const char* base = value_base + (uint64_t)id[i] * L::kVecBytes;
 #pragma unroll
       for (int k = 0; k < 4; ++k) {
-        const char* at = base + (2 * t + (k & 1) + 8 * (k >> 1)) * L::kVecBytes;
-        if (id[i] < 0) {
+        const char* at = base + ((k & 1) + 8 * (k >> 1)) * L::kVecBytes;
+        if (id[i] == kAbsent) {
 #pragma unroll
           for (int w = 0; w < L::kVWords; ++w) vreg[i][k][w] = 0;
         } else if constexpr (L::kVWords == 2) {
-          ldg8(at + g * 8, vreg[i][k]);
+          ldg8(at, vreg[i][k]);
         } else {
 #pragma unroll
-          for (int c = 0; c < L::kVWords / 4; ++c) ldg16(at + c * 128 + g * 16, vreg[i][k] + 4 * c);
+          for (int c = 0; c < L::kVWords / 4; ++c) ldg16(at + c * 128, vreg[i][k] + 4 * c);
         }
       }
     }
   };
 
-  constexpr int kStride = kWarps * L::kKeys;
-  int pos = begin + warp * L::kKeys;
+  constexpr int kStride = kW * L::kKeys;
+  int pos = begin + (warp % kW) * L::kKeys;
   if (pos < end) {
-    load_pages(pos, page);
-    load_keys(pos, page);
-    load_scales(pos, page);
-    load_values(pos, page);
-    load_pages(pos + kStride, page_next);
+    load_pages(pos, vec);
+    load_keys(vec);
+    load_values(vec);
+    load_pages(pos + kStride, vec_next);
   }
   for (; pos < end; pos += kStride) {
     const int next = pos + kStride;
@@ -287,11 +280,8 @@ __global__ void __launch_bounds__(kThreads, kNT == 1 ? 4 : kNT == 2 ? 3 : 2) tre
     }
     bool clean = pos + L::kKeys <= min(end, s.start);
 #pragma unroll
-    for (int i = 0; i < L::kTiles; ++i) clean = clean && page[i] >= 0;
-    if (next < end) {
-      load_keys(next, page_next);
-      load_scales(next, page_next);
-    }
+    for (int i = 0; i < L::kTiles; ++i) clean = clean && vec[i] != kAbsent;
+    if (next < end) load_keys(vec_next);
 
     // ---- softmax over the keys (rows of S^T: lanes with the same t hold the same query rows)
 #pragma unroll
@@ -299,9 +289,10 @@ __global__ void __launch_bounds__(kThreads, kNT == 1 ? 4 : kNT == 2 ? 3 : 2) tre
 #pragma unroll
       for (int nt = 0; nt < kNT; ++nt)
 #pragma unroll
-        for (int c = 0; c < 4; ++c) {
-          sc[i][nt][c] *= factor[nt][c & 1];
-          if constexpr (kQuant) sc[i][nt][c] *= kscale[i][c >> 1];
+        for (int h = 0; h < 2; ++h) {  // key g + 8 h, rows 2t and 2t + 1
+          uint64_t f = ptx::pack_f32x2(factor[nt][0], factor[nt][1]);
+          if constexpr (kQuant) f = ptx::mul_f32x2(f, ptx::pack_f32x2(kscale[i][h], kscale[i][h]));
+          ptx::unpack_f32x2(ptx::mul_f32x2(ptx::pack_f32x2(sc[i][nt][2 * h], sc[i][nt][2 * h + 1]), f), sc[i][nt][2 * h], sc[i][nt][2 * h + 1]);
         }
     if (!clean) {
 #pragma unroll
@@ -311,7 +302,7 @@ __global__ void __launch_bounds__(kThreads, kNT == 1 ? 4 : kNT == 2 ? 3 : 2) tre
 #pragma unroll
           for (int c = 0; c < 4; ++c) {
             const int at = pos + 16 * i + g + 8 * (c >> 1), r = r0 + nt * 8 + 2 * t + (c & 1);
-            const bool see = page[i] >= 0 && at < end && r < rows && (at < s.start || sees_tail(p, s, r / p.group, at - s.start));
+            const bool see = vec[i] != kAbsent && at < end && r < rows && (at < s.start || sees_tail(p, s, r / p.group, at - s.start));
             if (!see) sc[i][nt][c] = -INFINITY;
           }
     }
@@ -346,19 +337,28 @@ __global__ void __launch_bounds__(kThreads, kNT == 1 ? 4 : kNT == 2 ? 3 : 2) tre
 #pragma unroll
     for (int nt = 0; nt < kNT; ++nt) {
       const float base0 = m[nt][0] == -INFINITY ? 0.f : m[nt][0], base1 = m[nt][1] == -INFINITY ? 0.f : m[nt][1];
+      const uint64_t minus = ptx::pack_f32x2(-base0, -base1);
+      uint64_t sum = ptx::pack_f32x2(l[nt][0], l[nt][1]);
 #pragma unroll
-      for (int i = 0; i < L::kTiles; ++i) {
-        float w[4];
+      for (int i = 0; i < L::kTiles; ++i)
 #pragma unroll
-        for (int c = 0; c < 4; ++c) {
-          const float x = sc[i][nt][c];
-          w[c] = ptx::ex2_approx(x - ((c & 1) ? base1 : base0));
-          l[nt][c & 1] += w[c];
-          if constexpr (kQuant) w[c] = x == -INFINITY ? 0.f : w[c] * vscale[i][c >> 1];  // a masked vector's scale may be NaN
+        for (int h = 0; h < 2; ++h) {
+          float w0, w1;
+          ptx::unpack_f32x2(ptx::add_f32x2(ptx::pack_f32x2(sc[i][nt][2 * h], sc[i][nt][2 * h + 1]), minus), w0, w1);
+          w0 = ptx::ex2_approx(w0);
+          w1 = ptx::ex2_approx(w1);
+          const uint64_t w = ptx::pack_f32x2(w0, w1);
+          sum = ptx::add_f32x2(sum, w);
+          if constexpr (kQuant) {
+            ptx::unpack_f32x2(ptx::mul_f32x2(w, ptx::pack_f32x2(vscale[i][h], vscale[i][h])), w0, w1);
+            if (!clean) {  // a masked vector's scale may be NaN
+              if (sc[i][nt][2 * h] == -INFINITY) w0 = 0.f;
+              if (sc[i][nt][2 * h + 1] == -INFINITY) w1 = 0.f;
+            }
+          }
+          pf[i][nt][h] = transpose8x8(pack_bf16(w0, w1));
         }
-        pf[i][nt][0] = transpose8x8(pack_bf16(w[0], w[1]));
-        pf[i][nt][1] = transpose8x8(pack_bf16(w[2], w[3]));
-      }
+      ptx::unpack_f32x2(sum, l[nt][0], l[nt][1]);
     }
 
     // ---- O^T
@@ -432,47 +432,25 @@ __global__ void __launch_bounds__(kThreads, kNT == 1 ? 4 : kNT == 2 ? 3 : 2) tre
 #pragma unroll
         for (int nt = 0; nt < kNT; ++nt) mma_bf16(o[nt][j], a, pf[i][nt][0], pf[i][nt][1]);
       }
-    if (next < end) load_values(next, page_next);
+    if (next < end) load_values(vec_next);
 #pragma unroll
-    for (int i = 0; i < L::kTiles; ++i) page[i] = page_next[i];
-    load_pages(next + kStride, page_next);
+    for (int i = 0; i < L::kTiles; ++i) vec[i] = vec_next[i];
+    load_pages(next + kStride, vec_next);
   }
 
-  // ---- join the warps
+  // ---- output
 #pragma unroll
   for (int nt = 0; nt < kNT; ++nt)
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
+    for (int h = 0; h < 2; ++h) {  // the lanes' shares of a row's sum
       float x = l[nt][h];
       x += __shfl_xor_sync(0xffffffffu, x, 4);
       x += __shfl_xor_sync(0xffffffffu, x, 8);
       x += __shfl_xor_sync(0xffffffffu, x, 16);
-      const int r = nt * 8 + 2 * t + h;
-      if (g == 0) part_m[warp * kRows + r] = m[nt][h], part_l[warp * kRows + r] = x;
-#pragma unroll
-      for (int j = 0; j < L::kSteps; ++j)
-        *reinterpret_cast<float2*>(part + (warp * kRows + r) * (kDim + 4) + L::value_channel(j, g)) = make_float2(o[nt][j][h], o[nt][j][h + 2]);
+      l[nt][h] = x;
     }
-  __syncthreads();
-  constexpr int kUnits = kRows * kDim / 8;  // 8 channels of a row
-  for (int u = tid; u < kUnits; u += kThreads) {
-    const int rr = u / (kDim / 8), ch = u % (kDim / 8) * 8, r = r0 + rr;
-    if (r >= rows) break;
-    float top = -INFINITY;
-#pragma unroll
-    for (int w = 0; w < kWarps; ++w) top = fmaxf(top, part_m[w * kRows + rr]);
-    const float base = top == -INFINITY ? 0.f : top;
-    float sum = 0.f, x[8];
-#pragma unroll
-    for (int e = 0; e < 8; ++e) x[e] = 0.f;
-#pragma unroll
-    for (int w = 0; w < kWarps; ++w) {
-      const float f = exp2f(part_m[w * kRows + rr] - base);
-      sum += part_l[w * kRows + rr] * f;
-      const float* from = part + (w * kRows + rr) * (kDim + 4) + ch;
-#pragma unroll
-      for (int e = 0; e < 8; ++e) x[e] += from[e] * f;
-    }
+  // eight neighbouring channels of a row
+  auto finish = [&](int r, int ch, float top, float sum, const float (&x)[8], bool first) {
     const long row = s.first_row + r / p.group;
     const int head = kvh * p.group + r % p.group;
     if (p.n_splits > 1) {
@@ -480,7 +458,7 @@ __global__ void __launch_bounds__(kThreads, kNT == 1 ? 4 : kNT == 2 ? 3 : 2) tre
       float4* to = reinterpret_cast<float4*>(p.part_o + at * kDim + ch);
       to[0] = make_float4(x[0], x[1], x[2], x[3]);
       to[1] = make_float4(x[4], x[5], x[6], x[7]);
-      if (ch == 0) p.part_ml[at] = make_float2(top * kLn2, sum);
+      if (first) p.part_ml[at] = make_float2(top * kLn2, sum);
     } else {
       const float inv = sum == 0.f ? 0.f : 1.f / sum;
       uint4 out;
@@ -489,32 +467,94 @@ __global__ void __launch_bounds__(kThreads, kNT == 1 ? 4 : kNT == 2 ? 3 : 2) tre
       out.z = pack_bf16(x[4] * inv, x[5] * inv);
       out.w = pack_bf16(x[6] * inv, x[7] * inv);
       *reinterpret_cast<uint4*>(reinterpret_cast<__nv_bfloat16*>(p.out) + row * p.out_stride + (long)head * kDim + ch) = out;
-      if (ch == 0 && p.lse) p.lse[row * p.n_head + head] = sum == 0.f ? -INFINITY : (top + log2f(sum)) * kLn2;
+      if (first && p.lse) p.lse[row * p.n_head + head] = sum == 0.f ? -INFINITY : (top + log2f(sum)) * kLn2;
+    }
+  };
+  if constexpr (kW == 1) {
+#pragma unroll
+    for (int nt = 0; nt < kNT; ++nt)
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const int r = r0 + nt * 8 + 2 * t + h;
+        if (r >= rows) continue;
+#pragma unroll
+        for (int j = 0; j < L::kSteps; j += 4) {
+          float x[8];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) x[2 * e] = o[nt][j + e][h], x[2 * e + 1] = o[nt][j + e][h + 2];
+          finish(r, L::value_channel(j, g), m[nt][h], l[nt][h], x, j == 0 && g == 0);
+        }
+      }
+  } else {
+    // join the unit's warps
+    float* part = smem;                        // [warp][row][kDim + 4]
+    float* part_m = part + 4 * kRows * (kDim + 4);  // [warp][row]
+    float* part_l = part_m + 4 * kRows;
+#pragma unroll
+    for (int nt = 0; nt < kNT; ++nt)
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const int r = nt * 8 + 2 * t + h;
+        if (g == 0) part_m[warp * kRows + r] = m[nt][h], part_l[warp * kRows + r] = l[nt][h];
+#pragma unroll
+        for (int j = 0; j < L::kSteps; ++j)
+          *reinterpret_cast<float2*>(part + (warp * kRows + r) * (kDim + 4) + L::value_channel(j, g)) = make_float2(o[nt][j][h], o[nt][j][h + 2]);
+      }
+    const int w0 = warp / kW * kW;
+    asm volatile("bar.sync %0, %1;" ::"r"(1 + w0 / kW), "n"(kW * 32) : "memory");
+    constexpr int kUnits = kRows * kDim / 8;
+    for (int u = tid - w0 * 32; u < kUnits; u += kW * 32) {
+      const int rr = u / (kDim / 8), ch = u % (kDim / 8) * 8;
+      if (r0 + rr >= rows) break;
+      float top = -INFINITY;
+#pragma unroll
+      for (int w = 0; w < kW; ++w) top = fmaxf(top, part_m[(w0 + w) * kRows + rr]);
+      const float base = top == -INFINITY ? 0.f : top;
+      float sum = 0.f, x[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) x[e] = 0.f;
+#pragma unroll
+      for (int w = 0; w < kW; ++w) {
+        const float f = exp2f(part_m[(w0 + w) * kRows + rr] - base);
+        sum += part_l[(w0 + w) * kRows + rr] * f;
+        const float* from = part + ((w0 + w) * kRows + rr) * (kDim + 4) + ch;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x[e] += from[e] * f;
+      }
+      finish(r0 + rr, ch, top, sum, x, ch == 0);
     }
   }
 }
 
-template <int kFormat, int kDim, int kNT>
+template <int kFormat, int kDim, int kNT, int kW>
 cudaError_t launch_tile(const TreeAttnParams& p, cudaStream_t s) {
   const long rows = (long)p.max_rows * p.group;
   const int tiles = (int)((rows + 8 * kNT - 1) / (8 * kNT));
-  const dim3 grid((unsigned)(tiles * p.n_splits), (unsigned)p.cache.n_kv_head, (unsigned)p.rows.n_seq);
-  auto kernel = tree_attention_tc_kernel<kFormat, kDim, kNT>;
-  constexpr size_t smem = tc_smem<kFormat, kDim, kNT>();
+  const long units = (long)tiles * p.n_splits * p.cache.n_kv_head;
+  const dim3 grid((unsigned)((units + 4 / kW - 1) / (4 / kW)), (unsigned)p.rows.n_seq);
+  auto kernel = tree_attention_tc_kernel<kFormat, kDim, kNT, kW>;
+  constexpr size_t smem = tc_smem<kDim, kNT, kW>();
   cudaError_t e = cudaSuccess;
   if (smem > 48 * 1024) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
   if (e != cudaSuccess) return e;
-  return launch_dependent(kernel, grid, dim3(kThreads), smem, s, 1, false, p);
+  return launch_dependent(kernel, grid, dim3(kThreads), smem, s, 1, false, p, tiles);
+}
+
+template <int kFormat, int kDim, int kNT>
+cudaError_t launch_warps(const TreeAttnParams& p, cudaStream_t s) {
+  if (p.unit_warps == 1) return launch_tile<kFormat, kDim, kNT, 1>(p, s);
+  if (p.unit_warps == 2) return launch_tile<kFormat, kDim, kNT, 2>(p, s);
+  return launch_tile<kFormat, kDim, kNT, 4>(p, s);
 }
 
 template <int kFormat>
 cudaError_t launch_dim(const TreeAttnParams& p, int d_head, int rows_tile, cudaStream_t s) {
   if (d_head == 64) {
-    if (rows_tile == 8) return launch_tile<kFormat, 64, 1>(p, s);
-    if (rows_tile == 16) return launch_tile<kFormat, 64, 2>(p, s);
-    return launch_tile<kFormat, 64, 4>(p, s);
+    if (rows_tile == 8) return launch_warps<kFormat, 64, 1>(p, s);
+    if (rows_tile == 16) return launch_warps<kFormat, 64, 2>(p, s);
+    return launch_warps<kFormat, 64, 4>(p, s);
   }
-  return rows_tile == 8 ? launch_tile<kFormat, 128, 1>(p, s) : launch_tile<kFormat, 128, 2>(p, s);
+  return rows_tile == 8 ? launch_warps<kFormat, 128, 1>(p, s) : launch_warps<kFormat, 128, 2>(p, s);
 }
 
 }  // namespace
