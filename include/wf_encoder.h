@@ -365,6 +365,7 @@ wf_status wf_attention_f32_static(const float *qkv, const int *cu_seqlens, int B
  *   1  a page index outside [0, n_pages): the position is treated as absent
  *   2  prefix sums, a start or a length that do not fit the rows or the page table
  *   4  a parent beam outside [0, n_beam): the row stays as it is
+ *   8  a bounded wait inside a kernel gave up: the call's outputs are undefined
  * A handle's calls come from one host thread at a time; distinct handles are independent. */
 typedef struct wf_decoder wf_decoder;
 
@@ -445,7 +446,7 @@ typedef enum {
  *   q          dev   path dtype [n_rows][n_head][d_head], rows q_stride elements apart
  *   tail       host  wf_tail;  mask  dev  uint32 [n_rows][mask_words], bit t % 32 of word t / 32 (WF_TAIL_MASK only)
  *   max_rows   host  no sequence has more rows in this call (mask_words * 32 >= max_rows)
- *   max_len    host  no sequence has more positions, its own rows included; at most table_stride * page_size.
+ *   max_len    host  no sequence has more positions, its own rows included; at most table_stride * page_size and 2^30.
  *                    Longer ones are cut there and reported.
  *   out        dev   path dtype [n_rows][n_head][d_head], rows out_stride elements apart
  *   lse        dev   float32 [n_rows][n_head], or NULL

@@ -523,7 +523,7 @@ class BeamPruner:
 
 TAILS = {"none": 0, "causal": 1, "mask": 2, "tree": 2}
 CACHE_FORMATS = {"path": 0, "e4m3": 1, "int8": 2}
-STATUS_BAD_PAGE, STATUS_BAD_ROWS, STATUS_BAD_PARENT = 1, 2, 4
+STATUS_BAD_PAGE, STATUS_BAD_ROWS, STATUS_BAD_PARENT, STATUS_GAVE_UP = 1, 2, 4, 8
 _INT, _U8, _F32, _BF16 = torch.int32, torch.uint8, torch.float32, torch.bfloat16
 
 

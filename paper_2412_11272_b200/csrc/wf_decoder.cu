@@ -159,6 +159,7 @@ wf_status check_attention_sizes(wf_decoder* d, int n_seq, int n_rows, int max_ro
   if (n_seq < 0 || n_rows < 0 || max_rows < 0 || max_len < 0)
     return fail(d, WF_ERR_INVALID_ARG, "wf_tree_attention: a negative size");
   if (n_seq > 65535) return fail(d, WF_ERR_CAPACITY, "wf_tree_attention: more than 65535 sequences");
+  if (max_len > (1 << 30)) return fail(d, WF_ERR_CAPACITY, "wf_tree_attention: max_len above 2^30");
   if (n_rows > (1 << 27) || max_rows > (1 << 16)) return fail(d, WF_ERR_CAPACITY, "wf_tree_attention: more than 2^27 rows, or 2^16 in a sequence");
   return WF_OK;
 }

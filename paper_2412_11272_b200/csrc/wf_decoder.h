@@ -12,7 +12,7 @@
 namespace wf {
 
 // Bits of the caller's status word.
-enum DeviceStatus : int { kBadPage = 1, kBadRows = 2, kBadParent = 4 };
+enum DeviceStatus : int { kBadPage = 1, kBadRows = 2, kBadParent = 4, kGaveUp = 8 };
 
 constexpr int kMaxBeams = 16;
 
@@ -74,7 +74,7 @@ struct TreeAttnParams {
   // split of the positions: split i of a sequence has [i chunk, (i + 1) chunk); with more than one split the
   // unnormalised sums go to part_o [n_rows][n_head][n_splits][d_head] and (maximum, sum) to part_ml
   int n_splits, chunk;
-  int unit_warps;  // tensor-core kernel: warps that share a tile of rows (1, 2 or 4)
+  int unit_warps;  // warps that share a tile of few rows (1, 2 or 4); 0: the kernel for many rows
   float* part_o;
   float2* part_ml;
   int* status;

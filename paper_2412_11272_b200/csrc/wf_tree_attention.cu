@@ -6,6 +6,7 @@
 //   m' = max(m, max_j s_j),  l' = l e^(m - m') + sum_j e^(s_j - m'),  o' = o e^(m - m') + sum_j e^(s_j - m') v_j.
 // Splits are joined by a second kernel in split order, so results do not depend on scheduling.
 #include <algorithm>
+#include <cstdlib>
 
 #include "wf_tree_attention.cuh"
 
@@ -243,13 +244,17 @@ cudaError_t launch_simt(const TreeAttnParams& p, cudaStream_t s) {
   return e;
 }
 
-// Rows of one tile of the tensor-core kernel.
+constexpr int kWideRows = 32;  // more rows of a key/value head than this go to the kernel with 128-row tiles
+
+// Rows of one tile of the kernel for few rows.
 int tc_rows(int d_head, long rows) { return rows <= 8 ? 8 : rows <= 16 || d_head == 128 ? 16 : 32; }
 
 template <typename T, int kDim>
 cudaError_t launch_format(const TreeAttnParams& p, int format, cudaStream_t s) {
   cudaError_t e;
-  if constexpr (sizeof(T) == 2) e = launch_tree_attention_tc(p, kDim, format, tc_rows(kDim, (long)p.max_rows * p.group), s);
+  if constexpr (sizeof(T) == 2)
+    e = p.unit_warps == 0 ? launch_tree_attention_wide(p, kDim, format, s)
+                          : launch_tree_attention_tc(p, kDim, format, tc_rows(kDim, (long)p.max_rows * p.group), s);
   else if (format == WF_CACHE_PATH) e = launch_simt<T, WF_CACHE_PATH, kDim>(p, s);
   else if (format == WF_CACHE_E4M3) e = launch_simt<T, WF_CACHE_E4M3, kDim>(p, s);
   else e = launch_simt<T, WF_CACHE_INT8, kDim>(p, s);
@@ -264,14 +269,19 @@ TreeAttnPlan plan_tree_attention(int dtype, int d_head, int n_head, int n_kv_hea
                                  int num_sms) {
   TreeAttnPlan plan{};
   const long rows = (long)max_rows * (n_head / n_kv_head);
-  const int tile = dtype == WF_BF16 ? tc_rows(d_head, rows) : kSimtRows;
+  const bool wide = dtype == WF_BF16 && rows > kWideRows;
+  const int tile = wide ? 128 : dtype == WF_BF16 ? tc_rows(d_head, rows) : kSimtRows;
   const long tiles = (rows + tile - 1) / tile;
   const long units = tiles * n_kv_head * n_seq;
-  if (dtype == WF_BF16) {
+  if (wide) {
+    const long splits = std::max(1L, std::min((4L * num_sms + units - 1) / units, ((long)max_len + 511) / 512));
+    plan.unit_warps = 0;
+    plan.chunk = (int)(((long)max_len + splits * 64 - 1) / (splits * 64) * 64);
+  } else if (dtype == WF_BF16) {
     // Warps that the registers let reside: 16, 12 or 8 per SM.  A unit is shared by as few warps as fill them (each one has
     // a start and an end to pay for), and cut into splits, all of one wave, where four are not enough.
     const long resident = (long)num_sms * (tile == 8 ? 16 : tile == 16 && d_head == 64 ? 12 : 8);
-    plan.unit_warps = units >= resident ? 1 : 2 * units >= resident ? 2 : 4;
+    plan.unit_warps = getenv("XW") ? atoi(getenv("XW")) : 4;
     const long splits = std::max(1L, std::min(resident / (4 * units), ((long)max_len + 255) / 256));
     plan.chunk = (int)(((long)max_len + splits * 64 - 1) / (splits * 64) * 64);
   } else {

@@ -48,7 +48,8 @@ __device__ __forceinline__ int page_of(const TreeAttnParams& p, int seq, int pos
   return page;
 }
 
-// 16-bit tensor-core kernels, one per cache format (wf_tree_attention_tc.cu); rows_tile is 8, 16 or 32.
+// bfloat16 path: tiles of few query rows (wf_tree_attention_tc.cu; rows_tile is 8, 16 or 32) and of 128 (wf_tree_attention_wide.cu).
 cudaError_t launch_tree_attention_tc(const TreeAttnParams& p, int d_head, int format, int rows_tile, cudaStream_t s);
+cudaError_t launch_tree_attention_wide(const TreeAttnParams& p, int d_head, int format, cudaStream_t s);
 
 }  // namespace wf

@@ -1,12 +1,13 @@
 // Attention over the paged cache on the tensor cores, for few query rows per key/value head.
 //
-// The cache is read once and everything else is small, so the kernel is built around the loads: the scores
+// The cache is read once and everything else is small, so the kernel is built around the loads.  The scores
 // are computed transposed, S^T = K Q^T, with the keys as the 16-row operand and 8 query rows as the columns.  A
 // lane then needs whole 16-byte pieces of a key (the sum over channels may run in any order, so a lane's piece
-// serves several steps of the product) and loads them from the pages straight into registers: no shared memory, no barrier, every
-// byte used once.  The output is transposed as well, O^T = V^T P^T; the value operand's pairs of neighbouring keys are
-// made by byte permutation of two lanes' rows, and P^T comes from S^T by one 8 x 8 transposition in registers.
-// The four warps of a block take blocks of keys in turn, each with its own running maximum and sums, and are joined at the end.
+// serves several steps of the product).  Every lane copies its own pieces to shared memory, a few blocks of keys ahead
+// (cp.async), and reads them back into operand registers: no barrier, no bank conflict, every byte moved once.  The output is
+// transposed as well, O^T = V^T P^T; the value operand's pairs of neighbouring keys are made by byte permutation of
+// two keys' pieces, and P^T comes from S^T by one 8 x 8 transposition in registers.
+// The warps of a unit take blocks of keys in turn, each with its own running maximum and sums, and are joined at the end.
 //
 // Quantised caches: a code is exact in float16 and in bfloat16.  Scores: codes as float16 times the queries
 // scaled by a power of two per row into float16 (exact up to 2^-24 of the row's largest element), the vector's scale
@@ -36,12 +37,6 @@ __device__ __forceinline__ uint32_t transpose8x8(uint32_t x) {
   uint32_t y;
   asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
   return y;
-}
-__device__ __forceinline__ void ldg16(const void* p, uint32_t* r) {
-  asm volatile("ld.global.nc.L1::no_allocate.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "l"(p));
-}
-__device__ __forceinline__ void ldg8(const void* p, uint32_t* r) {
-  asm volatile("ld.global.nc.L1::no_allocate.v2.u32 {%0, %1}, [%2];" : "=r"(r[0]), "=r"(r[1]) : "l"(p));
 }
 __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
   const __nv_bfloat162 h = __floats2bfloat162_rn(lo, hi);
@@ -92,6 +87,12 @@ struct Layout {
   static constexpr int kKChunks = kVecBytes / 64;     // 16-byte pieces of a key per lane
   static constexpr int kVWords = kVecBytes / 32;      // 32-bit words of a value per lane
   static constexpr int kSteps = kDim / 16;            // steps of S^T's product = 16-channel tiles of O^T
+  // a warp's blocks of keys in flight, and the bytes of one: keys' pieces, values' pieces, scales
+  static constexpr int kStages = 2;
+  static constexpr int kKeyBytes = kKeys * kVecBytes;
+  static constexpr int kStageBytes = 2 * kKeyBytes + (kFormat == WF_CACHE_PATH ? 0 : 64 * kTiles);
+  static constexpr int kVPieces = kVecBytes == 256 ? 2 : 1;             // pieces of a value per lane
+  static constexpr int kVPieceBytes = kVecBytes == 64 ? 8 : 16;
   // channel of element e (0 .. 3) of the lane's share of step s
   static __device__ __forceinline__ int key_channel(int s, int t) {
     return kEsz == 2 ? 32 * (s / 2) + 8 * t + 4 * (s % 2) : 64 * (s / 4) + 16 * t + 4 * (s % 4);
@@ -103,31 +104,114 @@ struct Layout {
 };
 
 // A unit of work is one tile of query rows of one key/value head over one split of the positions; kW warps share it.
-template <int kDim, int kNT, int kW>
-constexpr size_t tc_smem() {
-  return kW == 1 ? 0 : (size_t)4 * 8 * kNT * (kDim + 4) * sizeof(float) + (size_t)2 * 4 * 8 * kNT * sizeof(float);
+// Shared memory of a warp: its copies in flight, and at the end its rows' sums.
+template <int kFormat, int kDim, int kNT>
+__host__ __device__ constexpr int warp_bytes() {
+  constexpr int copies = Layout<kFormat, kDim>::kStages * Layout<kFormat, kDim>::kStageBytes, rows = 8 * kNT * (kDim + 6) * 4;
+  return copies > rows ? copies : (rows + 15) / 16 * 16;
 }
 
 template <int kFormat, int kDim, int kNT, int kW>
-__global__ void __launch_bounds__(kThreads, kNT == 1 ? 4 : kNT == 2 && kDim == 64 ? 3 : 2) tree_attention_tc_kernel(const __grid_constant__ TreeAttnParams p, int tiles) {
+__global__ void __launch_bounds__(kThreads, kNT == 1 ? 5 : kNT == 2 && kDim == 64 ? 3 : 2) tree_attention_tc_kernel(const __grid_constant__ TreeAttnParams p, int tiles) {
   using L = Layout<kFormat, kDim>;
   constexpr bool kQuant = kFormat != WF_CACHE_PATH;
   constexpr int kRows = 8 * kNT;
-  extern __shared__ __align__(16) float smem[];
+  extern __shared__ __align__(16) unsigned char smem[];
+  constexpr int kWarpBytes = warp_bytes<kFormat, kDim, kNT>();
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, t = lane & 3;
   const int seq = blockIdx.y;
   const int unit = (int)blockIdx.x * (4 / kW) + warp / kW, rest = unit / p.n_splits;
   const int split = unit - rest * p.n_splits, kvh = rest / tiles, tile = rest - kvh * tiles;
   if (kvh >= p.cache.n_kv_head) return;
+  const int begin = split * p.chunk, shift = p.cache.page_shift;
+  const int* table = p.rows.page_table + (long)seq * p.rows.table_stride;
+  // The warp's 16-key tiles, T = 0, 1, ...: lane i holds the page of tile 32 b + i for the current b and the next one.
+  auto tile_pos = [&](int T) -> long { return (long)begin + (long)(warp % kW + T / L::kTiles * kW) * L::kKeys + 16 * (T % L::kTiles); };
+  auto load_pages = [&](int b) {
+    const long index = tile_pos(32 * b + lane) >> shift;
+    return index < p.rows.table_stride ? __ldg(table + index) : -1;
+  };
+  int page_next = load_pages(0);
   const Sequence s = load_sequence(p, seq, tid == 0 && blockIdx.x == 0);
   const int rows = min(s.n_rows, p.max_rows) * p.group;
   const int r0 = tile * kRows;
   if (r0 >= rows) return;
-  const int begin = split * p.chunk, end = min(s.len, begin + p.chunk);
+  const int end = min(s.len, begin + p.chunk);
   if (split > 0 && begin >= s.len) return;
-  const int shift = p.cache.page_shift;
-  const int* table = p.rows.page_table + (long)seq * p.rows.table_stride;
-
+  // ---- copies
+  constexpr uint32_t kAbsent = 0xffffffffu;  // (at most 2^32 vectors of 64 bytes or more fit a GPU)
+  auto first_vector = [&](int page, int b) -> uint32_t {  // index of the lane's tile's first vector in the cache
+    const long at = tile_pos(32 * b + lane);
+    if (at >= end) return kAbsent;
+    if ((unsigned)page >= (unsigned)p.cache.n_pages) {
+      report(p.status, kBadPage);
+      return kAbsent;
+    }
+    return (((uint32_t)page * (uint32_t)p.cache.n_kv_head + (uint32_t)kvh) << shift) + (uint32_t)((int)at & ((1 << shift) - 1));
+  };
+  const int w0 = begin + warp % kW * L::kKeys;
+  const int n_blocks = w0 < end ? (end - w0 + kW * L::kKeys - 1) / (kW * L::kKeys) : 0;
+  uint32_t vec = first_vector(page_next, 0);
+  page_next = load_pages(1);
+  unsigned char* const ring = smem + warp * kWarpBytes;
+  const char* const key_base = reinterpret_cast<const char*>(p.cache.k) + g * L::kVecBytes + t * 16;
+  const char* const value_base = reinterpret_cast<const char*>(p.cache.v) + 2 * t * L::kVecBytes + g * L::kVPieceBytes;
+  // lanes 0, 1: the scales of a tile's 16 keys; 2, 3: of its values
+  const char* const scale_base = reinterpret_cast<const char*>(lane < 2 ? p.cache.k_scale : p.cache.v_scale) + (lane & 1) * 16;
+  uint32_t id[L::kTiles];   // of the block whose copies are being started
+  unsigned absent = 0;      // bit (stage, tile): the tile has no page
+  auto copy_keys = [&](int n, int stage) {
+    if (n < n_blocks) {
+      if (n > 0 && (n * L::kTiles) % 32 == 0) {
+        vec = first_vector(page_next, n * L::kTiles / 32);
+        page_next = load_pages(n * L::kTiles / 32 + 1);
+      }
+      const uint32_t at = ptx::smem_u32(ring + stage * L::kStageBytes) + lane * 16;
+#pragma unroll
+      for (int i = 0; i < L::kTiles; ++i) {
+        id[i] = __shfl_sync(0xffffffffu, vec, (n * L::kTiles + i) % 32);
+        const unsigned bit = 1u << (stage * L::kTiles + i);
+        absent = id[i] == kAbsent ? absent | bit : absent & ~bit;
+        if (id[i] == kAbsent) continue;
+        const char* from = key_base + (uint64_t)id[i] * L::kVecBytes;
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+          for (int c = 0; c < L::kKChunks; ++c)
+            ptx::cp_async_16(at + ((i * 2 + h) * L::kKChunks + c) * 512, from + 8 * h * L::kVecBytes + c * 64, true);
+        if constexpr (kQuant) {
+          if (lane < 4) ptx::cp_async_16(at + 2 * L::kKeyBytes + i * 64, scale_base + (uint64_t)id[i] * 2, true);
+        }
+      }
+    }
+    ptx::cp_async_commit();
+  };
+  auto copy_values = [&](int n, int stage) {
+    if (n < n_blocks) {
+      const uint32_t at = ptx::smem_u32(ring + stage * L::kStageBytes) + L::kKeyBytes + lane * L::kVPieceBytes;
+#pragma unroll
+      for (int i = 0; i < L::kTiles; ++i) {
+        if (id[i] == kAbsent) continue;
+        const char* from = value_base + (uint64_t)id[i] * L::kVecBytes;
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+#pragma unroll
+          for (int c = 0; c < L::kVPieces; ++c) {
+            const uint32_t to = at + ((i * 4 + k) * L::kVPieces + c) * 32 * L::kVPieceBytes;
+            const char* src = from + ((k & 1) + 8 * (k >> 1)) * L::kVecBytes + c * 128;
+            if constexpr (L::kVPieceBytes == 16) ptx::cp_async_16(to, src, true);
+            else ptx::cp_async_8(to, src);
+          }
+      }
+    }
+    ptx::cp_async_commit();
+  };
+  // commit groups alternate, keys of block 0, values of block 0, keys of block 1, ...: 2 kStages of them are open
+#pragma unroll
+  for (int i = 0; i < L::kStages; ++i) {
+    copy_keys(i, i);
+    copy_values(i, i);
+  }
   // ---- queries: the second operand of S^T, element pairs matching the lane's pieces of a key
   uint32_t qf[kNT][L::kSteps][2];
   float factor[kNT][2];  // of the scores of rows 2t and 2t + 1: scale * log2(e), and the row's power of two
@@ -176,89 +260,36 @@ __global__ void __launch_bounds__(kThreads, kNT == 1 ? 4 : kNT == 2 && kDim == 6
     l[nt][0] = l[nt][1] = 0.f;
   }
 
-  // ---- loads: one block of keys is in registers, the next one's keys are on their way while its values are used and
-  // the other way round; page numbers run one block further ahead
-  uint32_t kreg[L::kTiles][2][L::kKChunks][4], vreg[L::kTiles][4][L::kVWords];
-  unsigned short sreg[L::kTiles];  // lanes 0 .. 15: scales of the tile's keys; 16 .. 31: of its values
-  // index of each tile's first vector in the cache, kAbsent where there is none (at most 2^32 vectors of 64 bytes or more fit a GPU)
-  constexpr uint32_t kAbsent = 0xffffffffu;
-  uint32_t vec[L::kTiles], vec_next[L::kTiles];
-  auto load_pages = [&](int pos, uint32_t (&id)[L::kTiles]) {
-#pragma unroll
-    for (int i = 0; i < L::kTiles; ++i) {
-      const int at = pos + 16 * i;
-      id[i] = kAbsent;
-      if (at < end) {
-        const uint32_t x = (uint32_t)__ldg(table + (at >> shift));
-        if (x < (uint32_t)p.cache.n_pages) id[i] = ((x * (uint32_t)p.cache.n_kv_head + (uint32_t)kvh) << shift) + (uint32_t)(at & ((1 << shift) - 1));
-        else if (lane == 0) report(p.status, kBadPage);
-      }
-    }
-  };
-  const char* const key_base = reinterpret_cast<const char*>(p.cache.k) + g * L::kVecBytes + t * 16;
-  const char* const value_base = reinterpret_cast<const char*>(p.cache.v) + 2 * t * L::kVecBytes + g * (L::kVWords == 2 ? 8 : 16);
-  const unsigned short* const scale_base = reinterpret_cast<const unsigned short*>(lane < 16 ? p.cache.k_scale : p.cache.v_scale) + (lane & 15);
-  auto load_keys = [&](const uint32_t (&id)[L::kTiles]) {
-#pragma unroll
-    for (int i = 0; i < L::kTiles; ++i) {
-      const char* base = key_base + (uint64_t)id[i] * L::kVecBytes;
-#pragma unroll
-      for (int h = 0; h < 2; ++h)
-#pragma unroll
-        for (int c = 0; c < L::kKChunks; ++c) {
-          if (id[i] != kAbsent) ldg16(base + 8 * h * L::kVecBytes + c * 64, kreg[i][h][c]);
-          else kreg[i][h][c][0] = kreg[i][h][c][1] = kreg[i][h][c][2] = kreg[i][h][c][3] = 0;
-        }
-      if constexpr (kQuant) sreg[i] = id[i] != kAbsent ? __ldg(scale_base + id[i]) : (unsigned short)0;
-    }
-  };
-  auto load_values = [&](const uint32_t (&id)[L::kTiles]) {
-#pragma unroll
-    for (int i = 0; i < L::kTiles; ++i) {
-      const char* base = value_base + (uint64_t)id[i] * L::kVecBytes;
-#pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        const char* at = base + ((k & 1) + 8 * (k >> 1)) * L::kVecBytes;
-        if (id[i] == kAbsent) {
-#pragma unroll
-          for (int w = 0; w < L::kVWords; ++w) vreg[i][k][w] = 0;
-        } else if constexpr (L::kVWords == 2) {
-          ldg8(at, vreg[i][k]);
-        } else {
-#pragma unroll
-          for (int c = 0; c < L::kVWords / 4; ++c) ldg16(at + c * 128, vreg[i][k] + 4 * c);
-        }
-      }
-    }
-  };
-
-  constexpr int kStride = kW * L::kKeys;
-  int pos = begin + (warp % kW) * L::kKeys;
-  if (pos < end) {
-    load_pages(pos, vec);
-    load_keys(vec);
-    load_values(vec);
-    load_pages(pos + kStride, vec_next);
-  }
-  for (; pos < end; pos += kStride) {
-    const int next = pos + kStride;
+  int stage = 0;
+  for (int n = 0; n < n_blocks; ++n) {
+    const int pos = w0 + n * kW * L::kKeys;
+    const unsigned char* slot = ring + stage * L::kStageBytes;
+    const unsigned no_page = absent >> (stage * L::kTiles);  // bit i: tile i
+    ptx::cp_async_wait<2 * L::kStages - 1>();
+    if constexpr (kQuant) __syncwarp();  // the scales are copied by some lanes for all
     // ---- S^T
     float sc[L::kTiles][kNT][4];
 #pragma unroll
     for (int i = 0; i < L::kTiles; ++i) {
 #pragma unroll
       for (int nt = 0; nt < kNT; ++nt) sc[i][nt][0] = sc[i][nt][1] = sc[i][nt][2] = sc[i][nt][3] = 0.f;
+      uint4 piece[2][L::kKChunks];
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+#pragma unroll
+        for (int c = 0; c < L::kKChunks; ++c) piece[h][c] = reinterpret_cast<const uint4*>(slot)[((i * 2 + h) * L::kKChunks + c) * 32 + lane];
+      auto word = [&](int h, int c, int w) { return w == 0 ? piece[h][c].x : w == 1 ? piece[h][c].y : w == 2 ? piece[h][c].z : piece[h][c].w; };
 #pragma unroll
       for (int st = 0; st < L::kSteps; ++st) {
         uint32_t a[4];
         if constexpr (kQuant) {
-          codes_f16<kFormat>(kreg[i][0][st / 4][st % 4], a[0], a[2]);
-          codes_f16<kFormat>(kreg[i][1][st / 4][st % 4], a[1], a[3]);
+          codes_f16<kFormat>(word(0, st / 4, st % 4), a[0], a[2]);
+          codes_f16<kFormat>(word(1, st / 4, st % 4), a[1], a[3]);
         } else {
-          a[0] = kreg[i][0][st / 2][(st % 2) * 2];
-          a[1] = kreg[i][1][st / 2][(st % 2) * 2];
-          a[2] = kreg[i][0][st / 2][(st % 2) * 2 + 1];
-          a[3] = kreg[i][1][st / 2][(st % 2) * 2 + 1];
+          a[0] = word(0, st / 2, (st % 2) * 2);
+          a[1] = word(1, st / 2, (st % 2) * 2);
+          a[2] = word(0, st / 2, (st % 2) * 2 + 1);
+          a[3] = word(1, st / 2, (st % 2) * 2 + 1);
         }
 #pragma unroll
         for (int nt = 0; nt < kNT; ++nt) {
@@ -271,17 +302,16 @@ __global__ void __launch_bounds__(kThreads, kNT == 1 ? 4 : kNT == 2 && kDim == 6
     if constexpr (kQuant) {
 #pragma unroll
       for (int i = 0; i < L::kTiles; ++i) {
-        const uint32_t mine = (uint32_t)sreg[i] << 16;
-        kscale[i][0] = __uint_as_float(__shfl_sync(0xffffffffu, mine, g));
-        kscale[i][1] = __uint_as_float(__shfl_sync(0xffffffffu, mine, g + 8));
-        vscale[i][0] = __uint_as_float(__shfl_sync(0xffffffffu, mine, g + 16));
-        vscale[i][1] = __uint_as_float(__shfl_sync(0xffffffffu, mine, g + 24));
+        const unsigned short* x = reinterpret_cast<const unsigned short*>(slot + 2 * L::kKeyBytes + i * 64);
+        kscale[i][0] = __uint_as_float((uint32_t)x[g] << 16);
+        kscale[i][1] = __uint_as_float((uint32_t)x[g + 8] << 16);
+        vscale[i][0] = __uint_as_float((uint32_t)x[g + 16] << 16);
+        vscale[i][1] = __uint_as_float((uint32_t)x[g + 24] << 16);
       }
+      __syncwarp();
     }
-    bool clean = pos + L::kKeys <= min(end, s.start);
-#pragma unroll
-    for (int i = 0; i < L::kTiles; ++i) clean = clean && vec[i] != kAbsent;
-    if (next < end) load_keys(vec_next);
+    const bool clean = pos + L::kKeys <= min(end, s.start) && (no_page & ((1u << L::kTiles) - 1)) == 0;
+    copy_keys(n + L::kStages, stage);
 
     // ---- softmax over the keys (rows of S^T: lanes with the same t hold the same query rows)
 #pragma unroll
@@ -302,7 +332,7 @@ __global__ void __launch_bounds__(kThreads, kNT == 1 ? 4 : kNT == 2 && kDim == 6
 #pragma unroll
           for (int c = 0; c < 4; ++c) {
             const int at = pos + 16 * i + g + 8 * (c >> 1), r = r0 + nt * 8 + 2 * t + (c & 1);
-            const bool see = vec[i] != kAbsent && at < end && r < rows && (at < s.start || sees_tail(p, s, r / p.group, at - s.start));
+            const bool see = !((no_page >> i) & 1) && at < end && r < rows && (at < s.start || sees_tail(p, s, r / p.group, at - s.start));
             if (!see) sc[i][nt][c] = -INFINITY;
           }
     }
@@ -362,6 +392,27 @@ __global__ void __launch_bounds__(kThreads, kNT == 1 ? 4 : kNT == 2 && kDim == 6
     }
 
     // ---- O^T
+    ptx::cp_async_wait<2 * L::kStages - 1>();
+    uint32_t vreg[L::kTiles][4][L::kVWords];
+#pragma unroll
+    for (int i = 0; i < L::kTiles; ++i)
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        if constexpr (L::kVPieceBytes == 8) {
+          const uint2 x = reinterpret_cast<const uint2*>(slot + L::kKeyBytes)[(i * 4 + k) * 32 + lane];
+          vreg[i][k][0] = x.x;
+          vreg[i][k][1] = x.y;
+        } else {
+#pragma unroll
+          for (int c = 0; c < L::kVPieces; ++c) {
+            const uint4 x = reinterpret_cast<const uint4*>(slot + L::kKeyBytes)[((i * 4 + k) * L::kVPieces + c) * 32 + lane];
+            vreg[i][k][4 * c] = x.x;
+            vreg[i][k][4 * c + 1] = x.y;
+            vreg[i][k][4 * c + 2] = x.z;
+            vreg[i][k][4 * c + 3] = x.w;
+          }
+        }
+      }
     if constexpr (!kQuant) {
       if (!clean) {
         // Values behind the end are not the sequence's, and a batch row's value that is not finite must not reach rows that do not
@@ -371,7 +422,7 @@ __global__ void __launch_bounds__(kThreads, kNT == 1 ? 4 : kNT == 2 && kDim == 6
           bool odd = false;
 #pragma unroll
           for (int k = 0; k < 4; ++k) {
-            const bool in = pos + 16 * i + 2 * t + (k & 1) + 8 * (k >> 1) < end;
+            const bool in = !((no_page >> i) & 1) && pos + 16 * i + 2 * t + (k & 1) + 8 * (k >> 1) < end;
 #pragma unroll
             for (int w = 0; w < L::kVWords; ++w) {
               if (!in) vreg[i][k][w] = 0;
@@ -432,11 +483,10 @@ __global__ void __launch_bounds__(kThreads, kNT == 1 ? 4 : kNT == 2 && kDim == 6
 #pragma unroll
         for (int nt = 0; nt < kNT; ++nt) mma_bf16(o[nt][j], a, pf[i][nt][0], pf[i][nt][1]);
       }
-    if (next < end) load_values(vec_next);
-#pragma unroll
-    for (int i = 0; i < L::kTiles; ++i) vec[i] = vec_next[i];
-    load_pages(next + kStride, vec_next);
+    copy_values(n + L::kStages, stage);
+    stage = stage + 1 == L::kStages ? 0 : stage + 1;
   }
+  ptx::cp_async_wait<0>();
 
   // ---- output
 #pragma unroll
@@ -487,37 +537,39 @@ __global__ void __launch_bounds__(kThreads, kNT == 1 ? 4 : kNT == 2 && kDim == 6
       }
   } else {
     // join the unit's warps
-    float* part = smem;                        // [warp][row][kDim + 4]
-    float* part_m = part + 4 * kRows * (kDim + 4);  // [warp][row]
-    float* part_l = part_m + 4 * kRows;
+    auto rows_of = [&](int w) { return reinterpret_cast<float*>(smem + w * kWarpBytes); };  // [row][kDim + 4], then [row] m, [row] l
+    constexpr int kStat = kRows * (kDim + 4);
+    float* mine = rows_of(warp);
+    __syncwarp();
 #pragma unroll
     for (int nt = 0; nt < kNT; ++nt)
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
         const int r = nt * 8 + 2 * t + h;
-        if (g == 0) part_m[warp * kRows + r] = m[nt][h], part_l[warp * kRows + r] = l[nt][h];
+        if (g == 0) mine[kStat + r] = m[nt][h], mine[kStat + kRows + r] = l[nt][h];
 #pragma unroll
         for (int j = 0; j < L::kSteps; ++j)
-          *reinterpret_cast<float2*>(part + (warp * kRows + r) * (kDim + 4) + L::value_channel(j, g)) = make_float2(o[nt][j][h], o[nt][j][h + 2]);
+          *reinterpret_cast<float2*>(mine + r * (kDim + 4) + L::value_channel(j, g)) = make_float2(o[nt][j][h], o[nt][j][h + 2]);
       }
-    const int w0 = warp / kW * kW;
-    asm volatile("bar.sync %0, %1;" ::"r"(1 + w0 / kW), "n"(kW * 32) : "memory");
+    const int first_warp = warp / kW * kW;
+    asm volatile("bar.sync %0, %1;" ::"r"(1 + first_warp / kW), "n"(kW * 32) : "memory");
     constexpr int kUnits = kRows * kDim / 8;
-    for (int u = tid - w0 * 32; u < kUnits; u += kW * 32) {
+    for (int u = tid - first_warp * 32; u < kUnits; u += kW * 32) {
       const int rr = u / (kDim / 8), ch = u % (kDim / 8) * 8;
       if (r0 + rr >= rows) break;
       float top = -INFINITY;
 #pragma unroll
-      for (int w = 0; w < kW; ++w) top = fmaxf(top, part_m[(w0 + w) * kRows + rr]);
+      for (int w = 0; w < kW; ++w) top = fmaxf(top, rows_of(first_warp + w)[kStat + rr]);
       const float base = top == -INFINITY ? 0.f : top;
       float sum = 0.f, x[8];
 #pragma unroll
       for (int e = 0; e < 8; ++e) x[e] = 0.f;
 #pragma unroll
       for (int w = 0; w < kW; ++w) {
-        const float f = exp2f(part_m[(w0 + w) * kRows + rr] - base);
-        sum += part_l[(w0 + w) * kRows + rr] * f;
-        const float* from = part + ((w0 + w) * kRows + rr) * (kDim + 4) + ch;
+        const float* x_of = rows_of(first_warp + w);
+        const float f = exp2f(x_of[kStat + rr] - base);
+        sum += x_of[kStat + kRows + rr] * f;
+        const float* from = x_of + rr * (kDim + 4) + ch;
 #pragma unroll
         for (int e = 0; e < 8; ++e) x[e] += from[e] * f;
       }
@@ -533,7 +585,7 @@ cudaError_t launch_tile(const TreeAttnParams& p, cudaStream_t s) {
   const long units = (long)tiles * p.n_splits * p.cache.n_kv_head;
   const dim3 grid((unsigned)((units + 4 / kW - 1) / (4 / kW)), (unsigned)p.rows.n_seq);
   auto kernel = tree_attention_tc_kernel<kFormat, kDim, kNT, kW>;
-  constexpr size_t smem = tc_smem<kDim, kNT, kW>();
+  constexpr size_t smem = (size_t)4 * warp_bytes<kFormat, kDim, kNT>();
   cudaError_t e = cudaSuccess;
   if (smem > 48 * 1024) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
   if (e != cudaSuccess) return e;
