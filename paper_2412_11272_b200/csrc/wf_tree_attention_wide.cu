@@ -13,6 +13,8 @@
 // instructions, a code is converted once per 128 rows and the products cost no register traffic.
 // Two blocks run per SM (256 tensor-memory columns each: S [0, 64), P [64, 96) and [96, 128), O [128, 128 + d)), so that one
 // computes while the other waits.  Every wait is bounded; one that gives up reports in the caller's status word.
+#include <type_traits>
+
 #include "wf_ptx.cuh"
 #include "wf_tree_attention.cuh"
 
@@ -129,13 +131,24 @@ __global__ void __launch_bounds__(kThreads, 2) tree_attention_wide_kernel(const 
     tmem_relinquish();
   }
   // ---- the query tile, rows behind the last one as zeros
-  for (int i = tid; i < kTileRows * (kDim / 8); i += kThreads) {
-    const int rr = i / (kDim / 8), c = i % (kDim / 8), r = r0 + rr;
-    uint4 x = make_uint4(0, 0, 0, 0);
-    if (r < rows)
-      x = __ldg(reinterpret_cast<const uint4*>(reinterpret_cast<const __nv_bfloat16*>(p.q) + (long)(s.first_row + r / p.group) * p.q_stride +
-                                               (long)(kvh * p.group + r % p.group) * kDim) + c);
-    st_shared_v4(sbase + S::kQ + (c / 8) * (kTileRows * 128) + swizzled(rr, c % 8), x.x, x.y, x.z, x.w);
+  {
+    constexpr int kEach = kTileRows * (kDim / 8) / kThreads;  // 16-byte pieces per thread
+    uint4 x[kEach];
+#pragma unroll
+    for (int k = 0; k < kEach; ++k) {
+      const int i = k * kThreads + tid, rr = i / (kDim / 8), c = i % (kDim / 8), r = r0 + rr;
+      x[k] = make_uint4(0, 0, 0, 0);
+      if (r < rows) {
+        const int row = r / p.group;
+        x[k] = __ldg(reinterpret_cast<const uint4*>(reinterpret_cast<const __nv_bfloat16*>(p.q) + (long)(s.first_row + row) * p.q_stride +
+                                                    (long)(kvh * p.group + r - row * p.group) * kDim) + c);
+      }
+    }
+#pragma unroll
+    for (int k = 0; k < kEach; ++k) {
+      const int i = k * kThreads + tid, rr = i / (kDim / 8), c = i % (kDim / 8);
+      st_shared_v4(sbase + S::kQ + (c / 8) * (kTileRows * 128) + swizzled(rr, c % 8), x[k].x, x[k].y, x[k].z, x[k].w);
+    }
   }
   fence_proxy_async_smem();
   tc_fence_before();
@@ -152,31 +165,46 @@ __global__ void __launch_bounds__(kThreads, 2) tree_attention_wide_kernel(const 
     const int* table = p.rows.page_table + (long)seq * p.rows.table_stride;
     constexpr uint32_t kAbsent = 0xffffffffu;
     uint4 kraw[kPasses], vraw[kPasses];
-    float scale_raw = 0.f;
-    bool there = false;  // of key lt % 64
-    auto vector_of = [&](int pos) -> uint32_t {
+    unsigned short scale_raw = 0;  // bfloat16 bits of key lt % 64
+    bool there = false;
+    auto vector_of = [&](int pos, uint32_t page) -> uint32_t {
       if (pos >= end) return kAbsent;
-      const uint32_t page = (uint32_t)__ldg(table + (pos >> shift));
       if (page >= (uint32_t)p.cache.n_pages) {
         report(p.status, kBadPage);
         return kAbsent;
       }
       return ((page * (uint32_t)p.cache.n_kv_head + (uint32_t)kvh) << shift) + (uint32_t)(pos & ((1 << shift) - 1));
     };
-    auto load = [&](int j) {
-      const int pos0 = begin + j * kStep;
+    // pages, then vectors, of this thread's pieces and of key lt % 64; pages are looked up a step before their vectors are loaded
+    uint32_t page[kPasses + 1], vec[kPasses], own = kAbsent;
+    auto position = [&](int j, int i) { return begin + j * kStep + (i < kPasses ? i * kKeysPerPass + key0 : lt % kStep); };
+    auto look_up = [&](int j) {
+#pragma unroll
+      for (int i = 0; i <= kPasses; ++i) {
+        const int pos = position(j, i);
+        page[i] = pos < end ? (uint32_t)__ldg(table + (pos >> shift)) : 0u;
+      }
+    };
+    auto find = [&](int j) {
+#pragma unroll
+      for (int i = 0; i < kPasses; ++i) vec[i] = vector_of(position(j, i), page[i]);
+      own = vector_of(position(j, kPasses), page[kPasses]);
+    };
+    auto load_keys = [&]() {
 #pragma unroll
       for (int i = 0; i < kPasses; ++i) {
-        const uint32_t v = vector_of(pos0 + i * kKeysPerPass + key0);
-        kraw[i] = vraw[i] = make_uint4(0, 0, 0, 0);
-        if (v != kAbsent) {
-          kraw[i] = __ldcs(reinterpret_cast<const uint4*>(p.cache.k) + (uint64_t)v * kPieces + piece);
-          vraw[i] = __ldcs(reinterpret_cast<const uint4*>(p.cache.v) + (uint64_t)v * kPieces + piece);
-        }
+        kraw[i] = make_uint4(0, 0, 0, 0);
+        if (vec[i] != kAbsent) kraw[i] = __ldcs(reinterpret_cast<const uint4*>(p.cache.k) + (uint64_t)vec[i] * kPieces + piece);
       }
-      const uint32_t v = vector_of(pos0 + lt % kStep);
-      there = v != kAbsent;
-      if constexpr (kQuant) scale_raw = there ? __bfloat162float((lt < kStep ? p.cache.k_scale : p.cache.v_scale)[v]) : 0.f;
+    };
+    auto load_values = [&]() {
+#pragma unroll
+      for (int i = 0; i < kPasses; ++i) {
+        vraw[i] = make_uint4(0, 0, 0, 0);
+        if (vec[i] != kAbsent) vraw[i] = __ldcs(reinterpret_cast<const uint4*>(p.cache.v) + (uint64_t)vec[i] * kPieces + piece);
+      }
+      there = own != kAbsent;
+      if constexpr (kQuant) scale_raw = there ? __ldg(reinterpret_cast<const unsigned short*>(lt < kStep ? p.cache.k_scale : p.cache.v_scale) + own) : (unsigned short)0;
     };
     auto put = [&](uint32_t base, const uint4 (&raw)[kPasses]) {
 #pragma unroll
@@ -239,7 +267,13 @@ __global__ void __launch_bounds__(kThreads, 2) tree_attention_wide_kernel(const 
       __syncwarp();
       return true;
     };
-    if (n_steps > 0) load(0);
+    if (n_steps > 0) {
+      look_up(0);
+      find(0);
+      load_keys();
+      load_values();
+      look_up(1);
+    }
     for (int j = 0; j < n_steps; ++j) {
       const int st = j & 1;
       const uint32_t parity = ((j >> 1) & 1u) ^ 1u;
@@ -247,6 +281,12 @@ __global__ void __launch_bounds__(kThreads, 2) tree_attention_wide_kernel(const 
       put(sbase + S::kK + st * S::kHalves * kHalfBytes, kraw);
       fence_proxy_async_smem();
       mbar_arrive(k_full(st));
+      if (j + 1 < n_steps) {
+        find(j + 1);
+        load_keys();
+        look_up(j + 2);
+      }
+      if (issuer && !issue_scores(j)) { ok = false; break; }
       if (!__all_sync(0xffffffffu, mbar_wait(v_free(st), parity, abort_flag))) { ok = false; break; }
       if constexpr (!kQuant) {
         // A batch row's value that is not finite must not reach rows that do not see it through 0 * inf: it is left out here
@@ -267,13 +307,13 @@ __global__ void __launch_bounds__(kThreads, 2) tree_attention_wide_kernel(const 
         }
       }
       put(sbase + S::kV + st * S::kHalves * kHalfBytes, vraw);
-      if constexpr (kQuant) scales[st * 2 * kStep + lt] = lt < kStep ? scale_raw * (p.scale * kLog2e) : scale_raw;
+      if constexpr (kQuant) scales[st * 2 * kStep + lt] = __uint_as_float((uint32_t)scale_raw << 16) * (lt < kStep ? p.scale * kLog2e : 1.f);
       const unsigned exists = __ballot_sync(0xffffffffu, there);
       if (lt < kStep && lane == 0) valid[st * 2 + lt / 32] = exists;
       fence_proxy_async_smem();
       mbar_arrive(v_full(st));
-      if (j + 1 < n_steps) load(j + 1);
-      if (issuer && (!issue_scores(j) || (j > 0 && !issue_output(j - 1)))) { ok = false; break; }
+      if (j + 1 < n_steps) load_values();
+      if (issuer && j > 0 && !issue_output(j - 1)) { ok = false; break; }
     }
     if (ok && issuer && n_steps > 0) ok = issue_output(n_steps - 1);
   } else {
@@ -366,7 +406,8 @@ __global__ void __launch_bounds__(kThreads, 2) tree_attention_wide_kernel(const 
           if (m == -INFINITY) m = top;  // nothing has been added up yet
         }
         float sum;
-        auto exponentials = [&]() {
+        auto exponentials_of = [&](auto clean_tag) {
+          constexpr bool kClean = decltype(clean_tag)::value;
           const float base = m == -INFINITY ? 0.f : m;
           const uint64_t minus = pack_f32x2(-base, -base);
           uint64_t s0 = 0, s1 = 0;
@@ -389,7 +430,7 @@ __global__ void __launch_bounds__(kThreads, 2) tree_attention_wide_kernel(const 
               }
               unpack_f32x2(wa, a0, a1);
               unpack_f32x2(wb, b0, b1);
-              if (kQuant && !clean) {  // a vector that the row does not see may have any scale, NaN too
+              if constexpr (kQuant && !kClean) {  // a vector that the row does not see may have any scale, NaN too
                 if (!((see[c] >> (2 * i)) & 1)) a0 = 0.f;
                 if (!((see[c] >> (2 * i)) & 2)) a1 = 0.f;
                 if (!((see[c] >> (2 * i)) & 4)) b0 = 0.f;
@@ -405,6 +446,10 @@ __global__ void __launch_bounds__(kThreads, 2) tree_attention_wide_kernel(const 
           unpack_f32x2(s0, q0, q1);
           unpack_f32x2(s1, q2, q3);
           sum = (q0 + q1) + (q2 + q3);
+        };
+        auto exponentials = [&]() {
+          if (!kQuant || clean) exponentials_of(std::true_type{});
+          else exponentials_of(std::false_type{});
         };
         // The buffer of these probabilities was last read by the product of two steps ago, which had landed when this step's
         // scores came (its issue precedes theirs in the same thread, and their commit covers it).
