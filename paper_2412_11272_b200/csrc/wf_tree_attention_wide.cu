@@ -5,10 +5,10 @@
 //   warps 0-3   softmax, one thread per query row: scores from tensor memory, probabilities back to it as packed bfloat16
 //               (two buffers), the running maximum raised (and the accumulator rescaled in place) only when it is exceeded
 //               by more than 2^8;
-//   warps 4-7   load keys and values from their pages into registers one step ahead, turn codes into bfloat16 (exact, so a
+//   warps 5-7   load keys and values from their pages into registers one step ahead, turn codes into bfloat16 (exact, so a
 //               scale multiplies the float32 score or the float32 probability, never a key or value) and write them to shared
 //               memory in the swizzled layout the tensor core reads;
-//   warp 4      also issues S = Q K^T (128 x 64 x d) and O += P V (128 x d x 64), O staying in tensor memory.
+//   warp 4      issues S = Q K^T (128 x 64 x d) and O += P V (128 x d x 64), O staying in tensor memory.
 // Against the kernel for few rows, which converts every code once per 8 .. 32 query rows and feeds the legacy matrix
 // instructions, a code is converted once per 128 rows and the products cost no register traffic.
 // Two blocks run per SM (256 tensor-memory columns each: S [0, 64), P [64, 96) and [96, 128), O [128, 128 + d)), so that one
@@ -25,7 +25,7 @@ using namespace ptx;
 namespace {
 
 constexpr int kTileRows = 128, kStep = 64;
-constexpr int kThreads = 256;
+constexpr int kThreads = 256, kLoaders = 96;
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 constexpr int kHalfBytes = kStep * 128;  // 64 keys x 64 channels of bfloat16
 
@@ -81,7 +81,7 @@ __global__ void __launch_bounds__(kThreads, 2) tree_attention_wide_kernel(const 
   constexpr bool kQuant = kFormat != WF_CACHE_PATH;
   constexpr int kVecBytes = kDim * (kQuant ? 1 : 2);
   constexpr int kPieces = kVecBytes / 16;          // 16-byte pieces of a vector
-  constexpr int kPasses = kStep * kPieces / 128;   // pieces per loading thread and step
+  constexpr int kPasses = (kStep * kPieces + kLoaders - 1) / kLoaders;  // pieces per loading thread and step
   extern __shared__ unsigned char smem_raw[];
 
   const int seq = blockIdx.z, kvh = blockIdx.y;
@@ -113,9 +113,9 @@ __global__ void __launch_bounds__(kThreads, 2) tree_attention_wide_kernel(const 
 
   if (tid == 0) {
     for (int i = 0; i < 2; ++i) {
-      mbar_init(k_full(i), 128);
+      mbar_init(k_full(i), kLoaders);
       mbar_init(k_free(i), 1);
-      mbar_init(v_full(i), 128);
+      mbar_init(v_full(i), kLoaders);
       mbar_init(v_free(i), 1);
       mbar_init(p_full(i), 128);
       mbar_init(o_full(i), 1);
@@ -157,15 +157,18 @@ __global__ void __launch_bounds__(kThreads, 2) tree_attention_wide_kernel(const 
   const uint32_t tmem = *tmem_slot;
   bool ok = true;
 
-  if (warp >= 4) {
+  if (warp > 4) {
     // ------------------------------------------------------------------ loads and conversion
-    const int lt = tid - 128, piece = lt % kPieces, key0 = lt / kPieces;
-    constexpr int kKeysPerPass = 128 / kPieces;
+    const int lt = tid - (kThreads - kLoaders);
+    // this thread's i-th piece of a step: piece `piece_of(i)` of key `key_of(i)`; the last pass may have none for it
+    auto key_of = [&](int i) { return (i * kLoaders + lt) / kPieces; };
+    auto piece_of = [&](int i) { return (i * kLoaders + lt) % kPieces; };
+    auto has = [&](int i) { return (i + 1) * kLoaders <= kStep * kPieces || i * kLoaders + lt < kStep * kPieces; };
     const int shift = p.cache.page_shift;
     const int* table = p.rows.page_table + (long)seq * p.rows.table_stride;
     constexpr uint32_t kAbsent = 0xffffffffu;
     uint4 kraw[kPasses], vraw[kPasses];
-    unsigned short scale_raw = 0;  // bfloat16 bits of key lt % 64
+    unsigned short kscale = 0, vscale = 0;  // bfloat16 bits, of key lt
     bool there = false;
     auto vector_of = [&](int pos, uint32_t page) -> uint32_t {
       if (pos >= end) return kAbsent;
@@ -175,9 +178,10 @@ __global__ void __launch_bounds__(kThreads, 2) tree_attention_wide_kernel(const 
       }
       return ((page * (uint32_t)p.cache.n_kv_head + (uint32_t)kvh) << shift) + (uint32_t)(pos & ((1 << shift) - 1));
     };
-    // pages, then vectors, of this thread's pieces and of key lt % 64; pages are looked up a step before their vectors are loaded
+    // pages, then vectors, of this thread's pieces and of key lt (of the first 64 threads), whose scales it loads; pages are
+    // looked up a step before their vectors are loaded
     uint32_t page[kPasses + 1], vec[kPasses], own = kAbsent;
-    auto position = [&](int j, int i) { return begin + j * kStep + (i < kPasses ? i * kKeysPerPass + key0 : lt % kStep); };
+    auto position = [&](int j, int i) { return begin + j * kStep + (i < kPasses ? (has(i) ? key_of(i) : kStep - 1) : min(lt, kStep - 1)); };
     auto look_up = [&](int j) {
 #pragma unroll
       for (int i = 0; i <= kPasses; ++i) {
@@ -194,22 +198,26 @@ __global__ void __launch_bounds__(kThreads, 2) tree_attention_wide_kernel(const 
 #pragma unroll
       for (int i = 0; i < kPasses; ++i) {
         kraw[i] = make_uint4(0, 0, 0, 0);
-        if (vec[i] != kAbsent) kraw[i] = __ldcs(reinterpret_cast<const uint4*>(p.cache.k) + (uint64_t)vec[i] * kPieces + piece);
+        if (vec[i] != kAbsent) kraw[i] = __ldcs(reinterpret_cast<const uint4*>(p.cache.k) + (uint64_t)vec[i] * kPieces + piece_of(i));
       }
     };
     auto load_values = [&]() {
 #pragma unroll
       for (int i = 0; i < kPasses; ++i) {
         vraw[i] = make_uint4(0, 0, 0, 0);
-        if (vec[i] != kAbsent) vraw[i] = __ldcs(reinterpret_cast<const uint4*>(p.cache.v) + (uint64_t)vec[i] * kPieces + piece);
+        if (vec[i] != kAbsent) vraw[i] = __ldcs(reinterpret_cast<const uint4*>(p.cache.v) + (uint64_t)vec[i] * kPieces + piece_of(i));
       }
       there = own != kAbsent;
-      if constexpr (kQuant) scale_raw = there ? __ldg(reinterpret_cast<const unsigned short*>(lt < kStep ? p.cache.k_scale : p.cache.v_scale) + own) : (unsigned short)0;
+      if constexpr (kQuant) {
+        kscale = there ? __ldg(reinterpret_cast<const unsigned short*>(p.cache.k_scale) + own) : (unsigned short)0;
+        vscale = there ? __ldg(reinterpret_cast<const unsigned short*>(p.cache.v_scale) + own) : (unsigned short)0;
+      }
     };
     auto put = [&](uint32_t base, const uint4 (&raw)[kPasses]) {
 #pragma unroll
       for (int i = 0; i < kPasses; ++i) {
-        const int key = i * kKeysPerPass + key0;
+        if (!has(i)) continue;
+        const int key = key_of(i), piece = piece_of(i);
         const uint4 x = raw[i];
         if constexpr (kQuant) {
           uint32_t a[4], b[4];
@@ -225,9 +233,58 @@ __global__ void __launch_bounds__(kThreads, 2) tree_attention_wide_kernel(const 
         }
       }
     };
-    // Warp 4 also issues the matrix products: of step j the scores' as soon as all loading warps have written the keys, of
-    // step j - 1 the output's when the probabilities are there.
-    const bool issuer = warp == 4, leader = issuer && elect_one();
+    if (n_steps > 0) {
+      look_up(0);
+      find(0);
+      load_keys();
+      load_values();
+      look_up(1);
+    }
+    for (int j = 0; j < n_steps; ++j) {
+      const int st = j & 1;
+      const uint32_t parity = ((j >> 1) & 1u) ^ 1u;
+      if (!__all_sync(0xffffffffu, mbar_wait(k_free(st), parity, abort_flag))) { ok = false; break; }
+      put(sbase + S::kK + st * S::kHalves * kHalfBytes, kraw);
+      fence_proxy_async_smem();
+      mbar_arrive(k_full(st));
+      if (j + 1 < n_steps) {
+        find(j + 1);
+        load_keys();
+        look_up(j + 2);
+      }
+      if (!__all_sync(0xffffffffu, mbar_wait(v_free(st), parity, abort_flag))) { ok = false; break; }
+      if constexpr (!kQuant) {
+        // A batch row's value that is not finite must not reach rows that do not see it through 0 * inf: it is left out here
+        // and added, at the end, to the rows that see it.
+        if (begin + (j + 1) * kStep > s.start) {
+#pragma unroll
+          for (int i = 0; i < kPasses; ++i) {
+            uint32_t* w = &vraw[i].x;
+            const bool batch_row = begin + j * kStep + key_of(i) >= s.start;
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+              if (batch_row && odd_bf16x2(w[e])) {
+                *odd_values = 1;
+                if ((w[e] & 0x7f80u) == 0x7f80u) w[e] &= 0xffff0000u;
+                if ((w[e] & 0x7f800000u) == 0x7f800000u) w[e] &= 0x0000ffffu;
+              }
+          }
+        }
+      }
+      put(sbase + S::kV + st * S::kHalves * kHalfBytes, vraw);
+      if (kQuant && lt < kStep) {
+        scales[st * 2 * kStep + lt] = __uint_as_float((uint32_t)kscale << 16) * (p.scale * kLog2e);
+        scales[st * 2 * kStep + kStep + lt] = __uint_as_float((uint32_t)vscale << 16);
+      }
+      const unsigned exists = __ballot_sync(0xffffffffu, there);
+      if (lt < kStep && lane == 0) valid[st * 2 + lt / 32] = exists;
+      fence_proxy_async_smem();
+      mbar_arrive(v_full(st));
+      if (j + 1 < n_steps) load_values();
+    }
+  } else if (warp == 4) {
+    // ------------------------------------------------------------------ matrix products
+    const bool leader = elect_one();
     constexpr uint32_t idesc_s = umma_idesc_bf16(kTileRows, kStep, 0, 0);
     constexpr uint32_t idesc_o = umma_idesc_bf16(kTileRows, 64, 0, 1);
     auto wait_all = [&](uint32_t b, uint32_t parity) -> bool { return __all_sync(0xffffffffu, mbar_wait(b, parity, abort_flag)); };
@@ -267,55 +324,9 @@ __global__ void __launch_bounds__(kThreads, 2) tree_attention_wide_kernel(const 
       __syncwarp();
       return true;
     };
-    if (n_steps > 0) {
-      look_up(0);
-      find(0);
-      load_keys();
-      load_values();
-      look_up(1);
-    }
-    for (int j = 0; j < n_steps; ++j) {
-      const int st = j & 1;
-      const uint32_t parity = ((j >> 1) & 1u) ^ 1u;
-      if (!__all_sync(0xffffffffu, mbar_wait(k_free(st), parity, abort_flag))) { ok = false; break; }
-      put(sbase + S::kK + st * S::kHalves * kHalfBytes, kraw);
-      fence_proxy_async_smem();
-      mbar_arrive(k_full(st));
-      if (j + 1 < n_steps) {
-        find(j + 1);
-        load_keys();
-        look_up(j + 2);
-      }
-      if (issuer && !issue_scores(j)) { ok = false; break; }
-      if (!__all_sync(0xffffffffu, mbar_wait(v_free(st), parity, abort_flag))) { ok = false; break; }
-      if constexpr (!kQuant) {
-        // A batch row's value that is not finite must not reach rows that do not see it through 0 * inf: it is left out here
-        // and added, at the end, to the rows that see it.
-        if (begin + (j + 1) * kStep > s.start) {
-#pragma unroll
-          for (int i = 0; i < kPasses; ++i) {
-            uint32_t* w = &vraw[i].x;
-            const bool batch_row = begin + j * kStep + i * kKeysPerPass + key0 >= s.start;
-#pragma unroll
-            for (int e = 0; e < 4; ++e)
-              if (batch_row && odd_bf16x2(w[e])) {
-                *odd_values = 1;
-                if ((w[e] & 0x7f80u) == 0x7f80u) w[e] &= 0xffff0000u;
-                if ((w[e] & 0x7f800000u) == 0x7f800000u) w[e] &= 0x0000ffffu;
-              }
-          }
-        }
-      }
-      put(sbase + S::kV + st * S::kHalves * kHalfBytes, vraw);
-      if constexpr (kQuant) scales[st * 2 * kStep + lt] = __uint_as_float((uint32_t)scale_raw << 16) * (lt < kStep ? p.scale * kLog2e : 1.f);
-      const unsigned exists = __ballot_sync(0xffffffffu, there);
-      if (lt < kStep && lane == 0) valid[st * 2 + lt / 32] = exists;
-      fence_proxy_async_smem();
-      mbar_arrive(v_full(st));
-      if (j + 1 < n_steps) load_values();
-      if (issuer && j > 0 && !issue_output(j - 1)) { ok = false; break; }
-    }
-    if (ok && issuer && n_steps > 0) ok = issue_output(n_steps - 1);
+    // the scores of a step run while the softmax works on those of the step before
+    if (n_steps > 0) ok = issue_scores(0);
+    for (int j = 0; ok && j < n_steps; ++j) ok = (j + 1 >= n_steps || issue_scores(j + 1)) && issue_output(j);
   } else {
     // ------------------------------------------------------------------ softmax, one query row per thread
     const int r = r0 + tid;
