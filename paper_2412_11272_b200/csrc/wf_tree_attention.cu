@@ -274,7 +274,7 @@ TreeAttnPlan plan_tree_attention(int dtype, int d_head, int n_head, int n_kv_hea
   const long tiles = (rows + tile - 1) / tile;
   const long units = tiles * n_kv_head * n_seq;
   if (wide) {
-    const long splits = std::max(1L, std::min((4L * num_sms + units - 1) / units, ((long)max_len + 511) / 512));
+    const long splits = getenv("XC") ? ((long)max_len + atoi(getenv("XC")) - 1) / atoi(getenv("XC")) : std::max(1L, std::min((4L * num_sms + units - 1) / units, ((long)max_len + 511) / 512));
     plan.unit_warps = 0;
     plan.chunk = (int)(((long)max_len + splits * 64 - 1) / (splits * 64) * 64);
   } else if (dtype == WF_BF16) {

@@ -170,47 +170,45 @@ __global__ void __launch_bounds__(kThreads, 2) tree_attention_wide_kernel(const 
     uint4 kraw[kPasses], vraw[kPasses];
     unsigned short kscale = 0, vscale = 0;  // bfloat16 bits, of key lt
     bool there = false;
-    auto vector_of = [&](int pos, uint32_t page) -> uint32_t {
-      if (pos >= end) return kAbsent;
-      if (page >= (uint32_t)p.cache.n_pages) {
-        report(p.status, kBadPage);
-        return kAbsent;
-      }
-      return ((page * (uint32_t)p.cache.n_kv_head + (uint32_t)kvh) << shift) + (uint32_t)(pos & ((1 << shift) - 1));
-    };
-    // pages, then vectors, of this thread's pieces and of key lt (of the first 64 threads), whose scales it loads; pages are
-    // looked up a step before their vectors are loaded
-    uint32_t page[kPasses + 1], vec[kPasses], own = kAbsent;
-    auto position = [&](int j, int i) { return begin + j * kStep + (i < kPasses ? (has(i) ? key_of(i) : kStep - 1) : min(lt, kStep - 1)); };
+    // Lanes 0 .. 3 of a warp look up the pages of the step's four 16-key tiles, a step before their vectors are loaded.
+    uint32_t page = 0, tile = kAbsent, vtile = kAbsent;  // vtile: of the values in registers
     auto look_up = [&](int j) {
-#pragma unroll
-      for (int i = 0; i <= kPasses; ++i) {
-        const int pos = position(j, i);
-        page[i] = pos < end ? (uint32_t)__ldg(table + (pos >> shift)) : 0u;
+      const int pos = begin + j * kStep + 16 * (lane & 3);
+      page = pos < end ? (uint32_t)__ldg(table + (pos >> shift)) : 0u;
+    };
+    auto find = [&](int j) {  // index of the lane's tile's first vector in the cache
+      const int pos = begin + j * kStep + 16 * (lane & 3);
+      tile = kAbsent;
+      if (pos < end) {
+        if (page < (uint32_t)p.cache.n_pages) tile = ((page * (uint32_t)p.cache.n_kv_head + (uint32_t)kvh) << shift) + (uint32_t)(pos & ((1 << shift) - 1));
+        else report(p.status, kBadPage);
       }
     };
-    auto find = [&](int j) {
-#pragma unroll
-      for (int i = 0; i < kPasses; ++i) vec[i] = vector_of(position(j, i), page[i]);
-      own = vector_of(position(j, kPasses), page[kPasses]);
+    // vector of a key of the step; an absent one's place is taken by the cache's first (it is masked)
+    auto vector_of = [&](int key) -> uint32_t {
+      const uint32_t first = __shfl_sync(0xffffffffu, tile, key >> 4);
+      return first == kAbsent ? 0u : first + (uint32_t)(key & 15);
     };
     auto load_keys = [&]() {
 #pragma unroll
       for (int i = 0; i < kPasses; ++i) {
-        kraw[i] = make_uint4(0, 0, 0, 0);
-        if (vec[i] != kAbsent) kraw[i] = __ldcs(reinterpret_cast<const uint4*>(p.cache.k) + (uint64_t)vec[i] * kPieces + piece_of(i));
+        const uint32_t v = vector_of(min(key_of(i), kStep - 1));
+        kraw[i] = __ldcs(reinterpret_cast<const uint4*>(p.cache.k) + (uint64_t)v * kPieces + piece_of(i));
       }
     };
-    auto load_values = [&]() {
+    auto load_values = [&](int j) {
+      vtile = tile;
 #pragma unroll
       for (int i = 0; i < kPasses; ++i) {
-        vraw[i] = make_uint4(0, 0, 0, 0);
-        if (vec[i] != kAbsent) vraw[i] = __ldcs(reinterpret_cast<const uint4*>(p.cache.v) + (uint64_t)vec[i] * kPieces + piece_of(i));
+        const uint32_t v = vector_of(min(key_of(i), kStep - 1));
+        vraw[i] = __ldcs(reinterpret_cast<const uint4*>(p.cache.v) + (uint64_t)v * kPieces + piece_of(i));
       }
-      there = own != kAbsent;
+      const int key = min(lt, kStep - 1);
+      const uint32_t v = vector_of(key);
+      there = __shfl_sync(0xffffffffu, tile, key >> 4) != kAbsent && begin + j * kStep + key < end;
       if constexpr (kQuant) {
-        kscale = there ? __ldg(reinterpret_cast<const unsigned short*>(p.cache.k_scale) + own) : (unsigned short)0;
-        vscale = there ? __ldg(reinterpret_cast<const unsigned short*>(p.cache.v_scale) + own) : (unsigned short)0;
+        kscale = __ldg(reinterpret_cast<const unsigned short*>(p.cache.k_scale) + v);
+        vscale = __ldg(reinterpret_cast<const unsigned short*>(p.cache.v_scale) + v);
       }
     };
     auto put = [&](uint32_t base, const uint4 (&raw)[kPasses]) {
@@ -237,7 +235,7 @@ __global__ void __launch_bounds__(kThreads, 2) tree_attention_wide_kernel(const 
       look_up(0);
       find(0);
       load_keys();
-      load_values();
+      load_values(0);
       look_up(1);
     }
     for (int j = 0; j < n_steps; ++j) {
@@ -256,11 +254,15 @@ __global__ void __launch_bounds__(kThreads, 2) tree_attention_wide_kernel(const 
       if constexpr (!kQuant) {
         // A batch row's value that is not finite must not reach rows that do not see it through 0 * inf: it is left out here
         // and added, at the end, to the rows that see it.
-        if (begin + (j + 1) * kStep > s.start) {
+        // (Positions behind the end and absent ones are zeros.)
+        const unsigned pages = __ballot_sync(0xffffffffu, vtile != kAbsent) & 15u;
+        if (begin + (j + 1) * kStep > min(s.start, end) || pages != 15u) {
 #pragma unroll
           for (int i = 0; i < kPasses; ++i) {
             uint32_t* w = &vraw[i].x;
-            const bool batch_row = begin + j * kStep + key_of(i) >= s.start;
+            const int pos = begin + j * kStep + key_of(i);
+            const bool batch_row = pos >= s.start;
+            if (pos >= end || !((pages >> (key_of(i) >> 4 & 3)) & 1)) vraw[i] = make_uint4(0, 0, 0, 0);
 #pragma unroll
             for (int e = 0; e < 4; ++e)
               if (batch_row && odd_bf16x2(w[e])) {
@@ -280,7 +282,7 @@ __global__ void __launch_bounds__(kThreads, 2) tree_attention_wide_kernel(const 
       if (lt < kStep && lane == 0) valid[st * 2 + lt / 32] = exists;
       fence_proxy_async_smem();
       mbar_arrive(v_full(st));
-      if (j + 1 < n_steps) load_values();
+      if (j + 1 < n_steps) load_values(j + 1);
     }
   } else if (warp == 4) {
     // ------------------------------------------------------------------ matrix products
