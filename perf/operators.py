@@ -396,8 +396,10 @@ def _reorder(s):
     if own:
         caches = _caches(s) if s["page"] else []
         states = [s["history"]] if s["page"] else [s["history"]] + [r[:, :s["live"] // 4] for r in s["rows"].unbind(0)]
-        _decoder(s).wf_beam_reorder(s["parents"], states=states, caches=caches, page_table=s["table"] if s["page"] else None,
-                                    lengths=s["lengths"] if s["page"] else None)
+        table = s["table"].contiguous() if s["page"] else None  # (of a single sequence it lies column by column)
+        _decoder(s).wf_beam_reorder(s["parents"], states=states, caches=caches, page_table=table, lengths=s["lengths"] if s["page"] else None)
+        if s["page"] and table is not s["table"]:
+            s["table"].copy_(table)
         return _moved(s)
     source = (s["parents"].long() + W * torch.arange(B, device=DEVICE)[:, None]).view(-1)  # the row whose state each row takes
     s["history"].copy_(s["history"][source])
