@@ -8,6 +8,7 @@
 #include <algorithm>
 #include <type_traits>
 
+#include "wf_ptx.cuh"
 #include "wf_tree_attention.cuh"
 
 namespace wf {
@@ -232,10 +233,17 @@ __global__ void __launch_bounds__(kSimtThreads, 2) tree_attention_simt_kernel(co
   }
 }
 
-// Joins the splits of a row: one block per (row, head), one thread per channel.
-template <typename T, int kDim>
-__global__ void __launch_bounds__(kDim) tree_attention_join_kernel(const __grid_constant__ TreeAttnParams p) {
-  const int row = blockIdx.x, head = blockIdx.y, ch = threadIdx.x;
+// Joins the splits of a row: one block per (row, head).  The splits' weights e^(m_i - m) first, all at once, then a sum over
+// the splits by groups of kDim threads, whose parts are added in group order.  Bound by latency (the partial sums are in the L2):
+// with many splits 256 threads (139 splits of 64 channels: 30 -> 13 us with the kernel before it), with few one group, as there
+// are many rows then (5 splits, 12,800 rows and heads: 124 -> 107 us with the kernel before it).
+template <typename T, int kDim, int kJoinThreads>
+__global__ void __launch_bounds__(kJoinThreads) tree_attention_join_kernel(const __grid_constant__ TreeAttnParams p) {
+  extern __shared__ __align__(16) float weight[];  // [n_splits]
+  __shared__ float red_m[kJoinThreads / 32], red_l[kJoinThreads / 32], part[kJoinThreads];
+  constexpr int kGroups = kJoinThreads / kDim;
+  const int row = blockIdx.x, head = blockIdx.y, tid = threadIdx.x, ch = tid % kDim, group = tid / kDim;
+  ptx::griddep_wait();  // the partial sums are the kernel's before this one
   const int seq = warp_find_sequence(p.rows.cu_rows, p.rows.n_seq, row);
   const Sequence s = load_sequence(p, seq, false);
   if (row < s.first_row || row - s.first_row >= min(s.n_rows, p.max_rows)) return;
@@ -243,21 +251,45 @@ __global__ void __launch_bounds__(kDim) tree_attention_join_kernel(const __grid_
   const long at = ((long)row * p.n_head + head) * p.n_splits;
   float m = -INFINITY;
   bool nan = false;
-  for (int i = 0; i < n; ++i) {
+  for (int i = tid; i < n; i += kJoinThreads) {
     const float mi = p.part_ml[at + i].x;
     nan |= mi != mi;
     m = fmaxf(m, mi);
   }
-  if (nan) m = __int_as_float(0x7fc00000);
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
+  if (__any_sync(0xffffffffu, nan)) m = __int_as_float(0x7fc00000);
+  if (tid % 32 == 0) red_m[tid / 32] = m;
+  __syncthreads();
+#pragma unroll
+  for (int w = 0; w < kJoinThreads / 32; ++w) m = (m != m || red_m[w] != red_m[w]) ? __int_as_float(0x7fc00000) : fmaxf(m, red_m[w]);
   const float base = m == -INFINITY ? 0.f : m;
-  float l = 0.f, o = 0.f;
-  for (int i = 0; i < n; ++i) {
+  float l = 0.f;
+  for (int i = tid; i < n; i += kJoinThreads) {
     const float2 ml = p.part_ml[at + i];
     const float f = expf(ml.x - base);
+    weight[i] = ml.y != 0.f ? f : 0.f;
     l += ml.y * f;
-    const float x = p.part_o[(at + i) * kDim + ch];
-    if (ml.y != 0.f) o += x * f;
   }
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) l += __shfl_xor_sync(0xffffffffu, l, o);
+  if (tid % 32 == 0) red_l[tid / 32] = l;
+  __syncthreads();
+  l = 0.f;
+#pragma unroll
+  for (int w = 0; w < kJoinThreads / 32; ++w) l += red_l[w];
+  float o = 0.f;
+#pragma unroll 8
+  for (int i = group; i < n; i += kGroups) {
+    const float f = weight[i], x = p.part_o[(at + i) * kDim + ch];
+    if (f != 0.f) o = fmaf(x, f, o);
+  }
+  part[tid] = o;
+  __syncthreads();
+  if (group != 0) return;
+  o = part[ch];
+#pragma unroll
+  for (int w = 1; w < kGroups; ++w) o += part[w * kDim + ch];
   put(reinterpret_cast<T*>(p.out) + (long)row * p.out_stride + (long)head * kDim + ch, l == 0.f ? 0.f : o / l);
   if (ch == 0 && p.lse) p.lse[(long)row * p.n_head + head] = l == 0.f ? -INFINITY : m + logf(l);
 }
@@ -294,7 +326,9 @@ cudaError_t launch_format(const TreeAttnParams& p, int format, cudaStream_t s) {
         : format == WF_CACHE_E4M3 ? launch_simt<WF_CACHE_E4M3, kDim>(p, s)
                                   : launch_simt<WF_CACHE_INT8, kDim>(p, s);
   if (e == cudaSuccess && p.n_splits > 1)
-    e = launch_dependent(tree_attention_join_kernel<T, kDim>, dim3((unsigned)p.rows.n_rows, (unsigned)p.n_head), dim3(kDim), 0, s, 1, false, p);
+    e = launch_dependent(p.n_splits > 16 ? tree_attention_join_kernel<T, kDim, 256> : tree_attention_join_kernel<T, kDim, kDim>,
+                         dim3((unsigned)p.rows.n_rows, (unsigned)p.n_head), dim3(p.n_splits > 16 ? 256 : kDim), p.n_splits * sizeof(float), s, 1,
+                         true, p);
   return e;
 }
 
