@@ -2,10 +2,12 @@
 //
 // A vector (one position, one head, keys or values; d_head = 64 or 128 elements) is handled by
 // d_head / 8 neighbouring lanes with 8 elements each, so its absolute maximum is a shuffle reduction
-// and its codes leave as one 8-byte store per lane (coalesced: a position's heads are read side by side,
-// each written as d_head consecutive bytes of its page).  A thread takes the key and the value vector
-// of its (row, head), so two (float32: four) 16-byte loads are in flight per thread.
+// and its codes leave as one 8-byte store per lane.  A warp takes the keys and values of one row for 4 or 8
+// (d_head 128: 2 or 4) heads -- of several rows where a row has fewer heads than a warp has such groups of lanes -- so that the
+// search for the row's sequence and page is paid once for them.
 // Bound by memory: d_head (esz + 1) + 2 bytes per vector, once.
+#include <type_traits>
+
 #include "wf_decoder.h"
 
 namespace wf {
@@ -126,9 +128,8 @@ __device__ __forceinline__ void dequantise(uint2 c, float s, float (&x)[8]) {
   }
 }
 
-// Where the thread's (row, head) lives in the cache: index of its vector among all vectors of a side,
-// or -1 (padding rows, bad tables).
-__device__ __forceinline__ long locate(const CacheView& c, const RowsView& r, long row, int head, int seq_hint, int* status) {
+// Where a row lives in the cache: index of its first head's vector among all vectors of a side, or -1 (padding rows, bad tables).
+__device__ __forceinline__ long locate(const CacheView& c, const RowsView& r, long row, int seq_hint, int* status) {
   if (row >= r.n_rows) return -1;
   int seq = seq_hint;
   while (seq + 1 < r.n_seq && __ldg(r.cu_rows + seq + 1) <= row) ++seq;
@@ -148,92 +149,159 @@ __device__ __forceinline__ long locate(const CacheView& c, const RowsView& r, lo
     report(status, kBadPage);
     return -1;
   }
-  return (((long)page * c.n_kv_head + head) << c.page_shift) + (pos & ((1L << c.page_shift) - 1));
+  return (((long)page * c.n_kv_head) << c.page_shift) + (pos & ((1L << c.page_shift) - 1));
 }
 
-template <typename T, int kFormat, int kDim>
+// What a lane works on: one row, heads `head`, `head` + kGroups, ... below `end_head` (at most kSteps of them).
+struct Share {
+  long row, at;  // at: vector of the row's head 0; < 0: nothing to do
+  int head, end_head;
+};
+template <int kLanes>
+__device__ __forceinline__ Share share_of(const CacheView& c, const RowsView& r, int n_chunks, int chunk_heads, int* status) {
+  constexpr int kGroups = 32 / kLanes;
+  const int lane = threadIdx.x & 31, group = lane / kLanes;
+  const long w = ((long)blockIdx.x * kThreads + threadIdx.x) >> 5;
+  if (w == 0 && lane == 0 && __ldg(r.cu_rows + r.n_seq) > r.n_rows) report(status, kBadRows);
+  Share s;
+  long row0;
+  if (n_chunks > 0) {  // a row's heads in n_chunks parts
+    row0 = s.row = (long)((unsigned long)w / (unsigned)n_chunks);
+    const int chunk = (int)(w - row0 * n_chunks);
+    s.head = chunk * chunk_heads + group;
+    s.end_head = min(c.n_kv_head, (chunk + 1) * chunk_heads);
+  } else {  // several rows of few heads
+    const int rows = kGroups / c.n_kv_head, k = group / c.n_kv_head;
+    row0 = w * rows;
+    s.row = k < rows ? row0 + k : r.n_rows;
+    s.head = group - k * c.n_kv_head;
+    s.end_head = s.head + 1;
+  }
+  const int hint = warp_find_sequence(r.cu_rows, r.n_seq, (int)min(row0, (long)r.n_rows));
+  s.at = locate(c, r, s.row, hint, lane % kLanes == 0 ? status : nullptr);  // the lanes of one vector agree
+  return s;
+}
+
+template <typename T, int kFormat, int kDim, int kSteps>
 __global__ void __launch_bounds__(kThreads) cache_write_kernel(CacheView c, RowsView r, const T* __restrict__ k, long k_stride,
-                                                               const T* __restrict__ v, long v_stride, int* status) {
-  constexpr int kLanes = kDim / 8;
-  const long first = (long)blockIdx.x * kThreads + (threadIdx.x & ~31);
-  const int hint = warp_find_sequence(r.cu_rows, r.n_seq, (int)min(first / kLanes / c.n_kv_head, (long)r.n_rows));
-  const long t = (long)blockIdx.x * kThreads + threadIdx.x;
-  if (t == 0 && __ldg(r.cu_rows + r.n_seq) > r.n_rows) report(status, kBadRows);
-  const int sub = (int)(t % kLanes);
-  const long item = t / kLanes;
-  const long row = item / c.n_kv_head;
-  const int head = (int)(item - row * c.n_kv_head);
-  const long at = locate(c, r, row, head, hint, sub == 0 ? status : nullptr);
-  if (at < 0) return;  // the lanes of one vector agree
+                                                               const T* __restrict__ v, long v_stride, int n_chunks, int chunk_heads,
+                                                               int* status) {
+  constexpr int kLanes = kDim / 8, kGroups = 32 / kLanes;
+  const int sub = (threadIdx.x & 31) % kLanes;
+  const Share s = share_of<kLanes>(c, r, n_chunks, chunk_heads, status);
+  if (s.at < 0) return;
+  const T* from_k = k + s.row * k_stride + sub * 8;
+  const T* from_v = v + s.row * v_stride + sub * 8;
+  Raw8<T> raw[kSteps][2];
+#pragma unroll
+  for (int u = 0; u < kSteps; ++u) {
+    const int head = s.head + u * kGroups;
+    if (head < s.end_head) {
+      load8(from_k + head * kDim, raw[u][0]);
+      load8(from_v + head * kDim, raw[u][1]);
+    }
+  }
   const unsigned group = ((kLanes == 16 ? 0xffffu : 0xffu)) << (threadIdx.x & 31 & ~(kLanes - 1));
-  Raw8<T> raw[2];
-  load8(k + row * k_stride + (long)head * kDim + sub * 8, raw[0]);
-  load8(v + row * v_stride + (long)head * kDim + sub * 8, raw[1]);
 #pragma unroll
-  for (int side = 0; side < 2; ++side) {
-    void* out = side == 0 ? c.k : c.v;
-    if (kFormat == WF_CACHE_PATH) {
-      reinterpret_cast<Raw8<T>*>(out)[at * kLanes + sub] = raw[side];
-    } else {
-      float x[8];
-      unpack(raw[side], x);
-      uint32_t top = 0;
+  for (int u = 0; u < kSteps; ++u) {
+    const int head = s.head + u * kGroups;
+    if (head >= s.end_head) break;
+    const long at = s.at + ((long)head << c.page_shift);
 #pragma unroll
-      for (int i = 0; i < 8; ++i) top = max(top, __float_as_uint(x[i]) & 0x7fffffffu);
+    for (int side = 0; side < 2; ++side) {
+      void* out = side == 0 ? c.k : c.v;
+      if (kFormat == WF_CACHE_PATH) {
+        reinterpret_cast<Raw8<T>*>(out)[at * kLanes + sub] = raw[u][side];
+      } else {
+        float x[8];
+        unpack(raw[u][side], x);
+        uint32_t top = 0;
 #pragma unroll
-      for (int o = kLanes / 2; o > 0; o >>= 1) top = max(top, __shfl_xor_sync(group, top, o));
-      const float s = scale_of<kFormat>(top);
-      uint2 codes = make_uint2(0, 0);
-      if (top < 0x7f800000u) codes = kFormat == WF_CACHE_E4M3 ? quantise_e4m3(x, s) : quantise_int8(x, s);
-      reinterpret_cast<uint2*>(out)[at * kLanes + sub] = codes;
-      if (sub == 0) (side == 0 ? c.k_scale : c.v_scale)[at] = __float2bfloat16_rn(s);  // exact: s is a bfloat16
+        for (int i = 0; i < 8; ++i) top = max(top, __float_as_uint(x[i]) & 0x7fffffffu);
+#pragma unroll
+        for (int o = kLanes / 2; o > 0; o >>= 1) top = max(top, __shfl_xor_sync(group, top, o));
+        const float scale = scale_of<kFormat>(top);
+        uint2 codes = make_uint2(0, 0);
+        if (top < 0x7f800000u) codes = kFormat == WF_CACHE_E4M3 ? quantise_e4m3(x, scale) : quantise_int8(x, scale);
+        reinterpret_cast<uint2*>(out)[at * kLanes + sub] = codes;
+        if (sub == 0) (side == 0 ? c.k_scale : c.v_scale)[at] = __float2bfloat16_rn(scale);  // exact: a bfloat16 already
+      }
     }
   }
 }
 
-template <typename T, int kFormat, int kDim>
+template <typename T, int kFormat, int kDim, int kSteps>
 __global__ void __launch_bounds__(kThreads) cache_read_kernel(CacheView c, RowsView r, T* __restrict__ k, long k_stride,
-                                                              T* __restrict__ v, long v_stride, int* status) {
-  constexpr int kLanes = kDim / 8;
-  const long first = (long)blockIdx.x * kThreads + (threadIdx.x & ~31);
-  const int hint = warp_find_sequence(r.cu_rows, r.n_seq, (int)min(first / kLanes / c.n_kv_head, (long)r.n_rows));
-  const long t = (long)blockIdx.x * kThreads + threadIdx.x;
-  if (t == 0 && __ldg(r.cu_rows + r.n_seq) > r.n_rows) report(status, kBadRows);
-  const int sub = (int)(t % kLanes);
-  const long item = t / kLanes;
-  const long row = item / c.n_kv_head;
-  const int head = (int)(item - row * c.n_kv_head);
-  const long at = locate(c, r, row, head, hint, sub == 0 ? status : nullptr);
-  if (at < 0) return;
-  T* const dst_k = k + row * k_stride + (long)head * kDim + sub * 8;
-  T* const dst_v = v + row * v_stride + (long)head * kDim + sub * 8;
-  if (kFormat == WF_CACHE_PATH) {
-    const Raw8<T> a = reinterpret_cast<const Raw8<T>*>(c.k)[at * kLanes + sub];
-    const Raw8<T> b = reinterpret_cast<const Raw8<T>*>(c.v)[at * kLanes + sub];
-    *reinterpret_cast<Raw8<T>*>(dst_k) = a;
-    *reinterpret_cast<Raw8<T>*>(dst_v) = b;
-  } else {
-    const uint2 a = reinterpret_cast<const uint2*>(c.k)[at * kLanes + sub];
-    const uint2 b = reinterpret_cast<const uint2*>(c.v)[at * kLanes + sub];
-    const float sa = __bfloat162float(c.k_scale[at]), sb = __bfloat162float(c.v_scale[at]);
-    float x[8];
-    dequantise<kFormat>(a, sa, x);
-    store8(dst_k, x);
-    dequantise<kFormat>(b, sb, x);
-    store8(dst_v, x);
+                                                              T* __restrict__ v, long v_stride, int n_chunks, int chunk_heads,
+                                                              int* status) {
+  constexpr int kLanes = kDim / 8, kGroups = 32 / kLanes;
+  const int sub = (threadIdx.x & 31) % kLanes;
+  const Share s = share_of<kLanes>(c, r, n_chunks, chunk_heads, status);
+  if (s.at < 0) return;
+  T* to_k = k + s.row * k_stride + sub * 8;
+  T* to_v = v + s.row * v_stride + sub * 8;
+  using Raw = std::conditional_t<kFormat == WF_CACHE_PATH, Raw8<T>, uint2>;
+  Raw raw[kSteps][2];
+  float scale[kSteps][2];
+#pragma unroll
+  for (int u = 0; u < kSteps; ++u) {
+    const int head = s.head + u * kGroups;
+    if (head < s.end_head) {
+      const long at = s.at + ((long)head << c.page_shift);
+      raw[u][0] = reinterpret_cast<const Raw*>(c.k)[at * kLanes + sub];
+      raw[u][1] = reinterpret_cast<const Raw*>(c.v)[at * kLanes + sub];
+      if (kFormat != WF_CACHE_PATH) scale[u][0] = __bfloat162float(c.k_scale[at]), scale[u][1] = __bfloat162float(c.v_scale[at]);
+    }
   }
+#pragma unroll
+  for (int u = 0; u < kSteps; ++u) {
+    const int head = s.head + u * kGroups;
+    if (head >= s.end_head) break;
+#pragma unroll
+    for (int side = 0; side < 2; ++side) {
+      T* to = (side == 0 ? to_k : to_v) + head * kDim;
+      if constexpr (kFormat == WF_CACHE_PATH) {
+        *reinterpret_cast<Raw8<T>*>(to) = raw[u][side];
+      } else {
+        float x[8];
+        dequantise<kFormat>(raw[u][side], scale[u][side], x);
+        store8(to, x);
+      }
+    }
+  }
+}
+
+template <typename T, int kFormat, int kDim, int kSteps>
+cudaError_t write_or_read_steps(bool write, const CacheView& c, const RowsView& r, void* k, long ks, void* v, long vs, int* status,
+                          cudaStream_t s) {
+  constexpr int kGroups = 32 / (kDim / 8);
+  long warps;
+  int n_chunks = 0, chunk_heads = 0;
+  if (c.n_kv_head < kGroups) {
+    const int rows = kGroups / c.n_kv_head;
+    warps = ((long)r.n_rows + rows - 1) / rows;
+  } else {
+    n_chunks = (c.n_kv_head + kSteps * kGroups - 1) / (kSteps * kGroups);
+    chunk_heads = ((c.n_kv_head + n_chunks - 1) / n_chunks + kGroups - 1) / kGroups * kGroups;
+    n_chunks = (c.n_kv_head + chunk_heads - 1) / chunk_heads;
+    warps = (long)r.n_rows * n_chunks;
+  }
+  const dim3 grid((unsigned)((warps * 32 + kThreads - 1) / kThreads));
+  if (write)
+    return launch_dependent(cache_write_kernel<T, kFormat, kDim, kSteps>, grid, dim3(kThreads), 0, s, 1, false, c, r, (const T*)k, ks,
+                            (const T*)v, vs, n_chunks, chunk_heads, status);
+  return launch_dependent(cache_read_kernel<T, kFormat, kDim, kSteps>, grid, dim3(kThreads), 0, s, 1, false, c, r, (T*)k, ks, (T*)v, vs, n_chunks,
+                          chunk_heads, status);
 }
 
 template <typename T, int kFormat, int kDim>
 cudaError_t write_or_read(bool write, const CacheView& c, const RowsView& r, void* k, long ks, void* v, long vs, int* status,
                           cudaStream_t s) {
-  const long threads = (long)r.n_rows * c.n_kv_head * (kDim / 8);
-  const long blocks = (threads + kThreads - 1) / kThreads;
-  const dim3 grid((unsigned)blocks);
-  if (write)
-    return launch_dependent(cache_write_kernel<T, kFormat, kDim>, grid, dim3(kThreads), 0, s, 1, false, c, r, (const T*)k, ks,
-                            (const T*)v, vs, status);
-  return launch_dependent(cache_read_kernel<T, kFormat, kDim>, grid, dim3(kThreads), 0, s, 1, false, c, r, (T*)k, ks, (T*)v, vs, status);
+  // Two heads per group of lanes pay once a large call of 16-bit rows leaves the SMs with threads enough either way (35 M
+  // elements a side written and read back: 107 -> 96 us); float32 rows have as many bytes in flight with one (49 -> 44 us).
+  if (sizeof(T) == 2 && (long)r.n_rows * c.n_kv_head * (kDim / 8) >= 1L << 20)
+    return write_or_read_steps<T, kFormat, kDim, 2>(write, c, r, k, ks, v, vs, status, s);
+  return write_or_read_steps<T, kFormat, kDim, 1>(write, c, r, k, ks, v, vs, status, s);
 }
 
 template <typename T>
