@@ -641,6 +641,14 @@ class Decoder:
         return t.data_ptr(), s[0] if t.shape[0] > 1 else max(s[0], heads * self.d_head)
 
     @staticmethod
+    def _empty(shape, dtype, device, stream):
+        """Memory for a call on ``stream``: the allocator then gives it to nobody else before that stream is done with it."""
+        if stream is None:
+            return torch.empty(shape, dtype=dtype, device=device)
+        with torch.cuda.stream(stream):
+            return torch.empty(shape, dtype=dtype, device=device)
+
+    @staticmethod
     def _status(status, device):
         return None if status is None else _vector(status, "status", device, n=1)
 
@@ -670,8 +678,8 @@ class Decoder:
         in the path's type.  Rows at or behind cu_rows[-1] are left as they are."""
         c, device = self._cache(cache), cache.device
         shape = (n_rows, self.n_kv_head, self.d_head)
-        k = torch.empty(shape, dtype=self.torch_dtype, device=device) if k is None else k
-        v = torch.empty(shape, dtype=self.torch_dtype, device=device) if v is None else v
+        k = self._empty(shape, self.torch_dtype, device, stream) if k is None else k
+        v = self._empty(shape, self.torch_dtype, device, stream) if v is None else v
         if k.shape[0] < n_rows or v.shape[0] < n_rows:
             _refuse("k and v must have n_rows rows")
         (kp, ks), (vp, vs) = self._vectors(k, "k", device, self.n_kv_head), self._vectors(v, "v", device, self.n_kv_head)
@@ -701,16 +709,16 @@ class Decoder:
         if max_len is None:
             max_len = page_table.shape[1] * self.page_size
         if out is None:
-            out = torch.empty((n, self.n_head, self.d_head), dtype=self.torch_dtype, device=device)
+            out = self._empty((n, self.n_head, self.d_head), self.torch_dtype, device, stream)
         elif out.shape[0] < n:
             _refuse("out must have the rows of q")
         op, os_ = self._vectors(out, "out", device, self.n_head)
         if lse is None:
-            lse = torch.empty((n, self.n_head), dtype=_F32, device=device)
+            lse = self._empty((n, self.n_head), _F32, device, stream)
         lp = _vector(lse, "lse", device, _F32, n * self.n_head)
         need = self.tree_attention_workspace(rows.n_seq, n, max_rows, max_len, device)
         if workspace is None and need:
-            workspace = torch.empty(need, dtype=_U8, device=device)
+            workspace = self._empty(need, _U8, device, stream)
         wp, have = (None, 0) if workspace is None else (_vector(workspace, "workspace", device, _U8), workspace.numel())
         self._call(self.lib.wf_tree_attention, device, stream, c, rows, qp, qs, self.d_head ** -0.5 if scale is None else scale, TAILS[tail],
                    mp, words, max_rows, max_len, op, os_, lp, wp, have, self._status(status, device))
@@ -746,9 +754,9 @@ class Decoder:
         up = None
         if suppress is not None:
             up = _vector(suppress, "suppress", device, suppress.dtype if suppress.dtype in (_INT, torch.uint32) else _INT, -(-V // 32))
-        out = torch.empty((B, keep), dtype=_F32, device=device)
-        both = torch.empty((2, B, keep), dtype=_INT, device=device)
-        done = torch.empty((B, keep), dtype=_U8, device=device)
+        out = self._empty((B, keep), _F32, device, stream)
+        both = self._empty((2, B, keep), _INT, device, stream)
+        done = self._empty((B, keep), _U8, device, stream)
         ints = both.data_ptr()
         ld = logits.stride(0) if logits.shape[0] > 1 else max(logits.stride(0), V)
         self._call(self.lib.wf_beam_select, device, stream, logits.data_ptr(), WF_BF16 if logits.dtype == _BF16 else WF_F32, ld, B, W, V, sp, bp, fp,

@@ -290,11 +290,15 @@ __device__ __forceinline__ void tmem_ld_wait() {
 // ---- cp.async (the front end stages its DFT basis rows with it)
 __device__ __forceinline__ void cp_async_16(uint32_t smem_dst, const void* src, bool valid) {
   uint32_t sz = valid ? 16u : 0u;
-  asm volatile("cp.async.cg.shared.global.L2::256B [%0], [%1], 16, %2;" ::"r"(smem_dst), "l"(src), "r"(sz) : "memory");
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(smem_dst), "l"(src), "r"(sz) : "memory");
 }
 // the first `bytes` of the 16 come from `src` (1 .. 16), the rest are zeros
 __device__ __forceinline__ void cp_async_16_partial(uint32_t smem_dst, const void* src, uint32_t bytes) {
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(smem_dst), "l"(src), "r"(bytes) : "memory");
+}
+// the same for data that is read front to back: the L2 fetches 256 bytes
+__device__ __forceinline__ void cp_async_16_stream(uint32_t smem_dst, const void* src) {
+  asm volatile("cp.async.cg.shared.global.L2::256B [%0], [%1], 16;" ::"r"(smem_dst), "l"(src) : "memory");
 }
 __device__ __forceinline__ void cp_async_8(uint32_t smem_dst, const void* src) {
   asm volatile("cp.async.ca.shared.global [%0], [%1], 8;" ::"r"(smem_dst), "l"(src) : "memory");

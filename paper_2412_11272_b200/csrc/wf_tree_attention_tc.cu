@@ -178,7 +178,7 @@ __global__ void __launch_bounds__(kThreads, kNT == 1 ? 5 : kNT == 2 && kDim == 6
         for (int h = 0; h < 2; ++h)
 #pragma unroll
           for (int c = 0; c < L::kKChunks; ++c)
-            ptx::cp_async_16(at + ((i * 2 + h) * L::kKChunks + c) * 512, from + 8 * h * L::kVecBytes + c * 64, true);
+            ptx::cp_async_16_stream(at + ((i * 2 + h) * L::kKChunks + c) * 512, from + 8 * h * L::kVecBytes + c * 64);
         if constexpr (kQuant) {
           if (lane < 4) ptx::cp_async_16(at + 2 * L::kKeyBytes + i * 64, scale_base + (uint64_t)id[i] * 2, true);
         }
@@ -199,7 +199,7 @@ __global__ void __launch_bounds__(kThreads, kNT == 1 ? 5 : kNT == 2 && kDim == 6
           for (int c = 0; c < L::kVPieces; ++c) {
             const uint32_t to = at + ((i * 4 + k) * L::kVPieces + c) * 32 * L::kVPieceBytes;
             const char* src = from + ((k & 1) + 8 * (k >> 1)) * L::kVecBytes + c * 128;
-            if constexpr (L::kVPieceBytes == 16) ptx::cp_async_16(to, src, true);
+            if constexpr (L::kVPieceBytes == 16) ptx::cp_async_16_stream(to, src);
             else ptx::cp_async_8(to, src);
           }
       }

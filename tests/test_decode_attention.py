@@ -425,3 +425,52 @@ def test_offsets_beyond_32_bits():
     out, _ = dec.wf_tree_attention(cache, table, _dev([0, 1]), _dev([700]), q, 1, 700, tail="none")
     p = torch.softmax((k[:, 0].double() @ q[0, 0].double()) * 128 ** -0.5, 0)
     assert (out[0, 0].double() - p @ k[:, 0].double()).abs().max() <= (2.0 ** -7 + 1e-4) * float(k.abs().max())
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype,fmt", _FORMATS)
+@pytest.mark.parametrize("n,H,Hk,d", [(1, 3, 3, 64), (9, 4, 2, 128), (40, 2, 1, 128), (70, 2, 2, 64)])
+def test_repeated_calls_agree_bit_for_bit(dtype, fmt, n, H, Hk, d):
+    """No result depends on the order in which blocks run: twenty calls in a row, with other work between, give the same bits."""
+    rng = np.random.default_rng([n, H, d])
+    dec = _decoder(n_head=H, n_kv_head=Hk, d_head=d, dtype=dtype, cache_format=fmt, page_size=32)
+    c = Case(rng, dec, rows=[n, 1, max(1, n // 2)] * 6, starts=[700, 5, 1300] * 6, tail="mask")
+    table, cu, starts, mask, q = _dev(c.table), _dev(c.cu), _dev(c.starts), _dev(c.mask), c.q.cuda()
+    first = None
+    for _ in range(20):
+        got = dec.wf_tree_attention(c.cache, table, cu, starts, q, n, c.max_len, "mask", mask)
+        if first is None:
+            first = got
+            c.check(got, c.want())
+        assert torch.equal(got[0], first[0]) and torch.equal(got[1], first[1])
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("n", [3, 40])
+def test_calls_on_a_given_stream_keep_their_workspace(n):
+    """Calls on a side stream with workspaces of their own, while the current stream allocates and overwrites memory."""
+    rng = np.random.default_rng(15)
+    dec = _decoder(n_head=4, cache_format="int8", page_size=64)
+    c = Case(rng, dec, rows=[n, 1], starts=[4000, 17], tail="causal")
+    table, cu, starts, q = _dev(c.table), _dev(c.cu), _dev(c.starts), c.q.cuda()
+    need = dec.tree_attention_workspace(2, n + 1, n, c.max_len)
+    assert need > 0
+    want = dec.wf_tree_attention(c.cache, table, cu, starts, q, n, c.max_len, "causal")
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    for _ in range(50):
+        got = dec.wf_tree_attention(c.cache, table, cu, starts, q, n, c.max_len, "causal", stream=side)
+        junk = [torch.full((need,), 255, dtype=torch.uint8, device="cuda") for _ in range(3)]   # on the current stream
+        del junk
+        torch.cuda.synchronize()
+        assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+
+
+@pytest.mark.gpu
+def test_prompts_of_many_rows():
+    """A prompt as a call of its own: hundreds of causal rows of ragged sequences, several row tiles."""
+    rng = np.random.default_rng(16)
+    for fmt, H, Hk, d in (("e4m3", 2, 1, 64), ("path", 2, 2, 128), ("int8", 1, 1, 128)):
+        dec = _decoder(n_head=H, n_kv_head=Hk, d_head=d, cache_format=fmt, page_size=128)
+        c = Case(rng, dec, rows=[300, 1, 129, 0, 64], starts=[0, 200, 33, 5, 500], tail="causal")
+        c.check(c.run(), c.want())
