@@ -533,7 +533,7 @@ def _refuse(message: str):
 
 def _vector(t, name: str, device, dtype=_INT, n: int | None = None):
     """Checks a contiguous device array of one type (and at least ``n`` elements); returns its address."""
-    if not isinstance(t, torch.Tensor) or t.dtype != dtype or t.device != device or not t.is_contiguous():
+    if not isinstance(t, torch.Tensor) or t.dtype is not dtype or not t.is_contiguous() or t.device != device:
         _refuse(f"{name} must be a contiguous {dtype} tensor on {device}")
     if n is not None and t.numel() < n:
         _refuse(f"{name} has {t.numel()} elements, {n} are needed")
@@ -625,28 +625,32 @@ class Decoder:
         return cache.c
 
     def _rows(self, page_table, cu_rows, start, n_rows, device):
-        n_seq = cu_rows.numel() - 1
-        if n_seq < 0 or page_table.dim() != 2 or page_table.shape[0] < n_seq:
+        n_seq, shape = cu_rows.numel() - 1, page_table.shape
+        if n_seq < 0 or len(shape) != 2 or shape[0] < n_seq:
             _refuse("cu_rows has n_seq + 1 entries, page_table [n_seq, pages]")
         return wf_rows(n_seq, n_rows, _vector(cu_rows, "cu_rows", device), _vector(start, "start", device, n=n_seq),
-                       _vector(page_table, "page_table", device), page_table.shape[1])
+                       _vector(page_table, "page_table", device), shape[1])
 
     def _vectors(self, t, name, device, heads):
         """A [n, heads, d_head] tensor with contiguous rows: (address, row stride)."""
-        if t.dtype != self.torch_dtype or t.device != device or t.dim() != 3 or t.shape[1] != heads or t.shape[2] != self.d_head:
-            _refuse(f"{name} must be {self.torch_dtype} [rows, {heads}, {self.d_head}] on {device}")
+        shape, d = t.shape, self.d_head
+        if len(shape) != 3 or t.dtype is not self.torch_dtype or shape[1] != heads or shape[2] != d or t.device != device:
+            _refuse(f"{name} must be {self.torch_dtype} [rows, {heads}, {d}] on {device}")
+        if t.is_contiguous():
+            return t.data_ptr(), heads * d
         s = t.stride()
-        if s[2] != 1 or (heads > 1 and s[1] != self.d_head):
+        if s[2] != 1 or (heads > 1 and s[1] != d):
             _refuse(f"{name}: the heads of a row must lie one after the other")
-        return t.data_ptr(), s[0] if t.shape[0] > 1 else max(s[0], heads * self.d_head)
+        return t.data_ptr(), s[0] if shape[0] > 1 else max(s[0], heads * d)
 
     @staticmethod
-    def _empty(shape, dtype, device, stream):
-        """Memory for a call on ``stream``: the allocator then gives it to nobody else before that stream is done with it."""
+    def _empty(like, shape, dtype, stream):
+        """Memory beside ``like`` for a call on ``stream``: the allocator then gives it to nobody else before that stream is
+        done with it."""
         if stream is None:
-            return torch.empty(shape, dtype=dtype, device=device)
+            return like.new_empty(shape, dtype=dtype)
         with torch.cuda.stream(stream):
-            return torch.empty(shape, dtype=dtype, device=device)
+            return like.new_empty(shape, dtype=dtype)
 
     @staticmethod
     def _status(status, device):
@@ -678,8 +682,8 @@ class Decoder:
         in the path's type.  Rows at or behind cu_rows[-1] are left as they are."""
         c, device = self._cache(cache), cache.device
         shape = (n_rows, self.n_kv_head, self.d_head)
-        k = self._empty(shape, self.torch_dtype, device, stream) if k is None else k
-        v = self._empty(shape, self.torch_dtype, device, stream) if v is None else v
+        k = self._empty(cache.k, shape, self.torch_dtype, stream) if k is None else k
+        v = self._empty(cache.k, shape, self.torch_dtype, stream) if v is None else v
         if k.shape[0] < n_rows or v.shape[0] < n_rows:
             _refuse("k and v must have n_rows rows")
         (kp, ks), (vp, vs) = self._vectors(k, "k", device, self.n_kv_head), self._vectors(v, "v", device, self.n_kv_head)
@@ -709,16 +713,16 @@ class Decoder:
         if max_len is None:
             max_len = page_table.shape[1] * self.page_size
         if out is None:
-            out = self._empty((n, self.n_head, self.d_head), self.torch_dtype, device, stream)
+            out = self._empty(q, q.shape, self.torch_dtype, stream)
         elif out.shape[0] < n:
             _refuse("out must have the rows of q")
         op, os_ = self._vectors(out, "out", device, self.n_head)
         if lse is None:
-            lse = self._empty((n, self.n_head), _F32, device, stream)
+            lse = self._empty(q, (n, self.n_head), _F32, stream)
         lp = _vector(lse, "lse", device, _F32, n * self.n_head)
         need = self.tree_attention_workspace(rows.n_seq, n, max_rows, max_len, device)
         if workspace is None and need:
-            workspace = self._empty(need, _U8, device, stream)
+            workspace = self._empty(q, need, _U8, stream)
         wp, have = (None, 0) if workspace is None else (_vector(workspace, "workspace", device, _U8), workspace.numel())
         self._call(self.lib.wf_tree_attention, device, stream, c, rows, qp, qs, self.d_head ** -0.5 if scale is None else scale, TAILS[tail],
                    mp, words, max_rows, max_len, op, os_, lp, wp, have, self._status(status, device))
@@ -754,14 +758,13 @@ class Decoder:
         up = None
         if suppress is not None:
             up = _vector(suppress, "suppress", device, suppress.dtype if suppress.dtype in (_INT, torch.uint32) else _INT, -(-V // 32))
-        out = self._empty((B, keep), _F32, device, stream)
-        both = self._empty((2, B, keep), _INT, device, stream)
-        done = self._empty((B, keep), _U8, device, stream)
-        ints = both.data_ptr()
+        out = self._empty(logits, (B, keep), _F32, stream)
+        parents, tokens = self._empty(logits, (B, keep), _INT, stream), self._empty(logits, (B, keep), _INT, stream)
+        done = self._empty(logits, (B, keep), _U8, stream)
         ld = logits.stride(0) if logits.shape[0] > 1 else max(logits.stride(0), V)
         self._call(self.lib.wf_beam_select, device, stream, logits.data_ptr(), WF_BF16 if logits.dtype == _BF16 else WF_F32, ld, B, W, V, sp, bp, fp,
-                   end_token, up, keep, out.data_ptr(), ints, ints + 4 * B * keep, done.data_ptr(), self._status(status, device))
-        return out, both[0], both[1], done
+                   end_token, up, keep, out.data_ptr(), parents.data_ptr(), tokens.data_ptr(), done.data_ptr(), self._status(status, device))
+        return out, parents, tokens, done
 
     def wf_beam_reorder(self, parents: torch.Tensor, states=(), caches=(), page_table=None, lengths=None, status=None, stream=None):
         """Moves every beam's states to the beams that grew from it, in place.  parents: [B, n_beam] (negative: stays).
