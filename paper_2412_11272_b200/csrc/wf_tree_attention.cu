@@ -82,12 +82,20 @@ __global__ void __launch_bounds__(kSimtThreads, 2) tree_attention_simt_kernel(co
   uint4 kraw[kEach], vraw[kEach];
   unsigned short kscale[kEach], vscale[kEach];
   bool there[kEach];
+  int page_at[kEach];  // pages are looked up a step before what lies in them is loaded
+  auto look_up = [&](int k0) {
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) {
+      const int pos = k0 + (i * kSimtThreads + tid) / kPieces;
+      page_at[i] = pos < end ? __ldg(p.rows.page_table + (long)seq * p.rows.table_stride + (pos >> p.cache.page_shift)) : -1;
+    }
+  };
   auto load = [&](int k0) {
 #pragma unroll
     for (int i = 0; i < kEach; ++i) {
-      const int u = i * kSimtThreads + tid, pos = k0 + u / kPieces;
-      const int page = pos < end ? page_of(p, seq, pos) : -1;
-      there[i] = page >= 0;
+      const int u = i * kSimtThreads + tid, pos = k0 + u / kPieces, page = page_at[i];
+      there[i] = page >= 0 && page < p.cache.n_pages;
+      if (pos < end && !there[i]) report(p.status, kBadPage);
       kraw[i] = vraw[i] = make_uint4(0, 0, 0, 0);
       kscale[i] = vscale[i] = 0;
       if (there[i]) {
@@ -100,8 +108,12 @@ __global__ void __launch_bounds__(kSimtThreads, 2) tree_attention_simt_kernel(co
         }
       }
     }
+    look_up(k0 + kSimtKeys);
   };
-  if (begin < end) load(begin);
+  if (begin < end) {
+    look_up(begin);
+    load(begin);
+  }
   const float* q = reinterpret_cast<const float*>(p.q);
   for (int i = tid; i < kRows * kDim / 4; i += kSimtThreads) {
     const int r = r0 + i / (kDim / 4), row = r / p.group;
@@ -356,8 +368,8 @@ TreeAttnPlan plan_tree_attention(int dtype, int d_head, int n_head, int n_kv_hea
     const long splits = std::max(1L, std::min(resident / (4 * units), ((long)max_len + 255) / 256));
     plan.chunk = (int)(((long)max_len + splits * 64 - 1) / (splits * 64) * 64);
   } else {
-    // as many splits as fill the SMs four times over, of at least 128 positions each
-    const long splits = std::max(1L, std::min((4L * num_sms + units - 1) / units, ((long)max_len + 127) / 128));
+    // as many splits as fit the SMs at two blocks each, of at least 128 positions
+    const long splits = std::max(1L, std::min(2L * num_sms / units, ((long)max_len + 127) / 128));
     plan.unit_warps = 4;
     plan.chunk = (int)(((long)max_len + splits * kSimtKeys - 1) / (splits * kSimtKeys) * kSimtKeys);
   }
