@@ -713,7 +713,7 @@ class Decoder:
         if max_len is None:
             max_len = page_table.shape[1] * self.page_size
         if out is None:
-            out = self._empty(q, q.shape, self.torch_dtype, stream)
+            out = torch.empty_like(q) if stream is None and q.is_contiguous() else self._empty(q, q.shape, self.torch_dtype, stream)
         elif out.shape[0] < n:
             _refuse("out must have the rows of q")
         op, os_ = self._vectors(out, "out", device, self.n_head)

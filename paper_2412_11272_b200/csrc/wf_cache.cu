@@ -2,9 +2,9 @@
 //
 // A vector (one position, one head, keys or values; d_head = 64 or 128 elements) is handled by
 // d_head / 8 neighbouring lanes with 8 elements each, so its absolute maximum is a shuffle reduction
-// and its codes leave as one 8-byte store per lane.  A warp takes the keys and values of one row for 4 or 8
-// (d_head 128: 2 or 4) heads -- of several rows where a row has fewer heads than a warp has such groups of lanes -- so that the
-// search for the row's sequence and page is paid once for them.
+// and its codes leave as one 8-byte store per lane.  A warp takes four (d_head 128: two) consecutive rows and one or two
+// heads of them, so that the codes of neighbouring positions, and their two-byte scales, leave side by side (heads lie whole runs
+// of positions apart), and the search for a row's sequence and page is paid once for its keys and values.
 // Bound by memory: d_head (esz + 1) + 2 bytes per vector, once.
 #include <type_traits>
 
@@ -152,31 +152,22 @@ __device__ __forceinline__ long locate(const CacheView& c, const RowsView& r, lo
   return (((long)page * c.n_kv_head) << c.page_shift) + (pos & ((1L << c.page_shift) - 1));
 }
 
-// What a lane works on: one row, heads `head`, `head` + kGroups, ... below `end_head` (at most kSteps of them).
+// What a lane works on: one row, heads head .. head + kSteps - 1 (below n_kv_head).
 struct Share {
   long row, at;  // at: vector of the row's head 0; < 0: nothing to do
-  int head, end_head;
+  int head;
 };
-template <int kLanes>
-__device__ __forceinline__ Share share_of(const CacheView& c, const RowsView& r, int n_chunks, int chunk_heads, int* status) {
+template <int kLanes, int kSteps>
+__device__ __forceinline__ Share share_of(const CacheView& c, const RowsView& r, int n_chunks, int* status) {
   constexpr int kGroups = 32 / kLanes;
-  const int lane = threadIdx.x & 31, group = lane / kLanes;
+  const int lane = threadIdx.x & 31;
   const long w = ((long)blockIdx.x * kThreads + threadIdx.x) >> 5;
   if (w == 0 && lane == 0 && __ldg(r.cu_rows + r.n_seq) > r.n_rows) report(status, kBadRows);
   Share s;
-  long row0;
-  if (n_chunks > 0) {  // a row's heads in n_chunks parts
-    row0 = s.row = (long)((unsigned long)w / (unsigned)n_chunks);
-    const int chunk = (int)(w - row0 * n_chunks);
-    s.head = chunk * chunk_heads + group;
-    s.end_head = min(c.n_kv_head, (chunk + 1) * chunk_heads);
-  } else {  // several rows of few heads
-    const int rows = kGroups / c.n_kv_head, k = group / c.n_kv_head;
-    row0 = w * rows;
-    s.row = k < rows ? row0 + k : r.n_rows;
-    s.head = group - k * c.n_kv_head;
-    s.end_head = s.head + 1;
-  }
+  const long block = (long)((unsigned long)w / (unsigned)n_chunks);
+  s.head = (int)(w - block * n_chunks) * kSteps;
+  const long row0 = block * kGroups;
+  s.row = row0 + lane / kLanes;
   const int hint = warp_find_sequence(r.cu_rows, r.n_seq, (int)min(row0, (long)r.n_rows));
   s.at = locate(c, r, s.row, hint, lane % kLanes == 0 ? status : nullptr);  // the lanes of one vector agree
   return s;
@@ -184,19 +175,18 @@ __device__ __forceinline__ Share share_of(const CacheView& c, const RowsView& r,
 
 template <typename T, int kFormat, int kDim, int kSteps>
 __global__ void __launch_bounds__(kThreads) cache_write_kernel(CacheView c, RowsView r, const T* __restrict__ k, long k_stride,
-                                                               const T* __restrict__ v, long v_stride, int n_chunks, int chunk_heads,
-                                                               int* status) {
-  constexpr int kLanes = kDim / 8, kGroups = 32 / kLanes;
+                                                               const T* __restrict__ v, long v_stride, int n_chunks, int* status) {
+  constexpr int kLanes = kDim / 8;
   const int sub = (threadIdx.x & 31) % kLanes;
-  const Share s = share_of<kLanes>(c, r, n_chunks, chunk_heads, status);
+  const Share s = share_of<kLanes, kSteps>(c, r, n_chunks, status);
   if (s.at < 0) return;
   const T* from_k = k + s.row * k_stride + sub * 8;
   const T* from_v = v + s.row * v_stride + sub * 8;
   Raw8<T> raw[kSteps][2];
 #pragma unroll
   for (int u = 0; u < kSteps; ++u) {
-    const int head = s.head + u * kGroups;
-    if (head < s.end_head) {
+    const int head = s.head + u;
+    if (head < c.n_kv_head) {
       load8(from_k + head * kDim, raw[u][0]);
       load8(from_v + head * kDim, raw[u][1]);
     }
@@ -204,8 +194,8 @@ __global__ void __launch_bounds__(kThreads) cache_write_kernel(CacheView c, Rows
   const unsigned group = ((kLanes == 16 ? 0xffffu : 0xffu)) << (threadIdx.x & 31 & ~(kLanes - 1));
 #pragma unroll
   for (int u = 0; u < kSteps; ++u) {
-    const int head = s.head + u * kGroups;
-    if (head >= s.end_head) break;
+    const int head = s.head + u;
+    if (head >= c.n_kv_head) break;
     const long at = s.at + ((long)head << c.page_shift);
 #pragma unroll
     for (int side = 0; side < 2; ++side) {
@@ -232,11 +222,10 @@ __global__ void __launch_bounds__(kThreads) cache_write_kernel(CacheView c, Rows
 
 template <typename T, int kFormat, int kDim, int kSteps>
 __global__ void __launch_bounds__(kThreads) cache_read_kernel(CacheView c, RowsView r, T* __restrict__ k, long k_stride,
-                                                              T* __restrict__ v, long v_stride, int n_chunks, int chunk_heads,
-                                                              int* status) {
-  constexpr int kLanes = kDim / 8, kGroups = 32 / kLanes;
+                                                              T* __restrict__ v, long v_stride, int n_chunks, int* status) {
+  constexpr int kLanes = kDim / 8;
   const int sub = (threadIdx.x & 31) % kLanes;
-  const Share s = share_of<kLanes>(c, r, n_chunks, chunk_heads, status);
+  const Share s = share_of<kLanes, kSteps>(c, r, n_chunks, status);
   if (s.at < 0) return;
   T* to_k = k + s.row * k_stride + sub * 8;
   T* to_v = v + s.row * v_stride + sub * 8;
@@ -245,8 +234,8 @@ __global__ void __launch_bounds__(kThreads) cache_read_kernel(CacheView c, RowsV
   float scale[kSteps][2];
 #pragma unroll
   for (int u = 0; u < kSteps; ++u) {
-    const int head = s.head + u * kGroups;
-    if (head < s.end_head) {
+    const int head = s.head + u;
+    if (head < c.n_kv_head) {
       const long at = s.at + ((long)head << c.page_shift);
       raw[u][0] = reinterpret_cast<const Raw*>(c.k)[at * kLanes + sub];
       raw[u][1] = reinterpret_cast<const Raw*>(c.v)[at * kLanes + sub];
@@ -255,8 +244,8 @@ __global__ void __launch_bounds__(kThreads) cache_read_kernel(CacheView c, RowsV
   }
 #pragma unroll
   for (int u = 0; u < kSteps; ++u) {
-    const int head = s.head + u * kGroups;
-    if (head >= s.end_head) break;
+    const int head = s.head + u;
+    if (head >= c.n_kv_head) break;
 #pragma unroll
     for (int side = 0; side < 2; ++side) {
       T* to = (side == 0 ? to_k : to_v) + head * kDim;
@@ -275,23 +264,14 @@ template <typename T, int kFormat, int kDim, int kSteps>
 cudaError_t write_or_read_steps(bool write, const CacheView& c, const RowsView& r, void* k, long ks, void* v, long vs, int* status,
                           cudaStream_t s) {
   constexpr int kGroups = 32 / (kDim / 8);
-  long warps;
-  int n_chunks = 0, chunk_heads = 0;
-  if (c.n_kv_head < kGroups) {
-    const int rows = kGroups / c.n_kv_head;
-    warps = ((long)r.n_rows + rows - 1) / rows;
-  } else {
-    n_chunks = (c.n_kv_head + kSteps * kGroups - 1) / (kSteps * kGroups);
-    chunk_heads = ((c.n_kv_head + n_chunks - 1) / n_chunks + kGroups - 1) / kGroups * kGroups;
-    n_chunks = (c.n_kv_head + chunk_heads - 1) / chunk_heads;
-    warps = (long)r.n_rows * n_chunks;
-  }
+  const int n_chunks = (c.n_kv_head + kSteps - 1) / kSteps;
+  const long warps = ((long)r.n_rows + kGroups - 1) / kGroups * n_chunks;
   const dim3 grid((unsigned)((warps * 32 + kThreads - 1) / kThreads));
   if (write)
     return launch_dependent(cache_write_kernel<T, kFormat, kDim, kSteps>, grid, dim3(kThreads), 0, s, 1, false, c, r, (const T*)k, ks,
-                            (const T*)v, vs, n_chunks, chunk_heads, status);
-  return launch_dependent(cache_read_kernel<T, kFormat, kDim, kSteps>, grid, dim3(kThreads), 0, s, 1, false, c, r, (T*)k, ks, (T*)v, vs, n_chunks,
-                          chunk_heads, status);
+                            (const T*)v, vs, n_chunks, status);
+  return launch_dependent(cache_read_kernel<T, kFormat, kDim, kSteps>, grid, dim3(kThreads), 0, s, 1, false, c, r, (T*)k, ks, (T*)v, vs,
+                          n_chunks, status);
 }
 
 template <typename T, int kFormat, int kDim>
