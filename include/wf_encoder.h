@@ -396,7 +396,8 @@ const char *wf_decoder_last_error(const wf_decoder *dec);
 
 /* One layer's cache, caller-owned device memory, 16-byte aligned:
  *   k, v              [n_pages][n_kv_head][page_size][d_head] elements or codes
- *   k_scale, v_scale  bfloat16 [n_pages][n_kv_head][page_size]; NULL for WF_CACHE_PATH */
+ *   k_scale, v_scale  bfloat16 [n_pages][n_kv_head][page_size]; NULL for WF_CACHE_PATH
+ * n_pages * n_kv_head * page_size < 2^32 - 1. */
 typedef struct {
   void *k, *v;
   void *k_scale, *v_scale;
@@ -441,8 +442,8 @@ typedef enum {
  *   lse_ih = log sum_j exp(scale <q_ih, k_jg>)
  * A row that sees nothing gets out = 0 and lse = -infinity.  What a row does not see has no influence
  * on it, whatever it holds (NaN included).  Scores, softmax and sums are float32, keys and values are the stored ones
- * (code * s).  WF_BF16: the products run on the tensor cores; a probability is rounded once, to
- * bfloat16 (WF_CACHE_PATH) or to float16 after multiplication with its value's scale (quantised caches).
+ * (code * s).  WF_BF16: the products run on the tensor cores; a probability is rounded once to
+ * bfloat16, in the quantised caches after multiplication with its value's scale.
  *   q          dev   path dtype [n_rows][n_head][d_head], rows q_stride elements apart
  *   tail       host  wf_tail;  mask  dev  uint32 [n_rows][mask_words], bit t % 32 of word t / 32 (WF_TAIL_MASK only)
  *   max_rows   host  no sequence has more rows in this call (mask_words * 32 >= max_rows)

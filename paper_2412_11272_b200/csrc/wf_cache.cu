@@ -2,7 +2,7 @@
 //
 // A vector (one position, one head, keys or values; d_head = 64 or 128 elements) is handled by
 // d_head / 8 neighbouring lanes with 8 elements each, so its absolute maximum is a shuffle reduction
-// and its codes leave as one 8-byte store per lane.  A warp takes four (d_head 128: two) consecutive rows and one or two
+// and its codes leave as one 8-byte store per lane.  A warp takes four (d_head 128: two) consecutive rows and one to four
 // heads of them, so that the codes of neighbouring positions, and their two-byte scales, leave side by side (heads lie whole runs
 // of positions apart), and the search for a row's sequence and page is paid once for its keys and values.
 // Bound by memory: d_head (esz + 1) + 2 bytes per vector, once.
@@ -277,10 +277,12 @@ cudaError_t write_or_read_steps(bool write, const CacheView& c, const RowsView& 
 template <typename T, int kFormat, int kDim>
 cudaError_t write_or_read(bool write, const CacheView& c, const RowsView& r, void* k, long ks, void* v, long vs, int* status,
                           cudaStream_t s) {
-  // Two heads per group of lanes pay once a large call of 16-bit rows leaves the SMs with threads enough either way (35 M
-  // elements a side written and read back: 107 -> 96 us); float32 rows have as many bytes in flight with one (49 -> 44 us).
+  // Several heads per group of lanes pay once a large call of 16-bit rows leaves the SMs with threads enough either way: 35 M elements
+  // a side with one / two / four of them are written in 59 / 51 / 47 us and read back in 47 / 39 / 42 us; float32 rows have as many
+  // bytes in flight with one.
   if (sizeof(T) == 2 && (long)r.n_rows * c.n_kv_head * (kDim / 8) >= 1L << 20)
-    return write_or_read_steps<T, kFormat, kDim, 2>(write, c, r, k, ks, v, vs, status, s);
+    return write ? write_or_read_steps<T, kFormat, kDim, 4>(true, c, r, k, ks, v, vs, status, s)
+                 : write_or_read_steps<T, kFormat, kDim, 2>(false, c, r, k, ks, v, vs, status, s);
   return write_or_read_steps<T, kFormat, kDim, 1>(write, c, r, k, ks, v, vs, status, s);
 }
 
