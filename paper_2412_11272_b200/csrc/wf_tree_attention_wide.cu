@@ -174,7 +174,7 @@ __global__ void __launch_bounds__(kThreads, 2) tree_attention_wide_kernel(const 
     uint32_t page = 0, tile = kAbsent, vtile = kAbsent;  // vtile: of the values in registers
     auto look_up = [&](int j) {
       const int pos = begin + j * kStep + 16 * (lane & 3);
-      page = pos < end ? (uint32_t)__ldg(table + (pos >> shift)) : 0u;
+      page = (uint32_t)__ldg(table + (min(pos, end - 1) >> shift));
     };
     auto find = [&](int j) {  // index of the lane's tile's first vector in the cache
       const int pos = begin + j * kStep + 16 * (lane & 3);
@@ -245,11 +245,9 @@ __global__ void __launch_bounds__(kThreads, 2) tree_attention_wide_kernel(const 
       put(sbase + S::kK + st * S::kHalves * kHalfBytes, kraw);
       fence_proxy_async_smem();
       mbar_arrive(k_full(st));
-      if (j + 1 < n_steps) {
-        find(j + 1);
-        load_keys();
-        look_up(j + 2);
-      }
+      find(j + 1);
+      load_keys();
+      look_up(j + 2);
       if (!__all_sync(0xffffffffu, mbar_wait(v_free(st), parity, abort_flag))) { ok = false; break; }
       if constexpr (!kQuant) {
         // A batch row's value that is not finite must not reach rows that do not see it through 0 * inf: it is left out here
@@ -282,7 +280,7 @@ __global__ void __launch_bounds__(kThreads, 2) tree_attention_wide_kernel(const 
       if (lt < kStep && lane == 0) valid[st * 2 + lt / 32] = exists;
       fence_proxy_async_smem();
       mbar_arrive(v_full(st));
-      if (j + 1 < n_steps) load_values(j + 1);
+      load_values(j + 1);
     }
   } else if (warp == 4) {
     // ------------------------------------------------------------------ matrix products
