@@ -48,6 +48,7 @@ __device__ __forceinline__ void put(__nv_bfloat16* p, float x) { *p = __float2bf
 // float32 path: 8 or 16 query rows and 64 positions a step, dequantised into shared memory; the next step's 16-byte
 // pieces wait in registers meanwhile.  Products in float32 on the FMA pipe, whose rate (and shared memory's: a thread reads
 // one key piece per 2 or 4 query rows) is the bound for more than a few rows; a softmax row belongs to a warp.
+// 8 sequences of 301 .. 1508 positions, 6 heads of 64 channels, 3 .. 8 rows: 22 us with the join, 23.5 MB (1.07 TB/s).
 constexpr int kSimtKeys = 64, kSimtThreads = 256;
 
 template <int kDim, int kRows>
@@ -359,7 +360,7 @@ TreeAttnPlan plan_tree_attention(int dtype, int d_head, int n_head, int n_kv_hea
   const long units = tiles * n_kv_head * n_seq;
   if (wide) {
     // two blocks of an SM; sequences differ in length, so more blocks than fit at once even the load out, as long as a
-    // block's start (6 us of its 100 at 768 positions) stays small
+    // block's start (7 us of its 35 at 768 positions) stays small
     const long splits = std::max(1L, std::min((8L * num_sms + units - 1) / units, ((long)max_len + 767) / 768));
     plan.unit_warps = 0;
     plan.chunk = (int)(((long)max_len + splits * 64 - 1) / (splits * 64) * 64);
