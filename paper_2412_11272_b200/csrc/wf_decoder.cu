@@ -1,5 +1,6 @@
 // C entry points of the decoding-stage operators: argument checks and launches.
 #include <algorithm>
+#include <atomic>
 #include <cstdarg>
 #include <cstdio>
 #include <new>
@@ -143,16 +144,13 @@ wf_status wf_cache_read(wf_decoder* d, const wf_cache* cache, const wf_rows* row
 namespace {
 // Number of SMs of the current device (asked once per device; the same for every thread that asks).
 wf_status sm_count(wf_decoder* d, int* n) {
-  static int known[64] = {0};
+  static std::atomic<int> known[64];
   int dev = 0;
   cudaError_t e = cudaGetDevice(&dev);
-  if (e == cudaSuccess && dev < 64 && known[dev] > 0) {
-    *n = known[dev];
-    return WF_OK;
-  }
+  if (e == cudaSuccess && dev < 64 && (*n = known[dev].load(std::memory_order_relaxed)) > 0) return WF_OK;
   if (e == cudaSuccess) e = cudaDeviceGetAttribute(n, cudaDevAttrMultiProcessorCount, dev);
   if (e != cudaSuccess) return cuda_result(d, "device query", e);
-  if (dev < 64) known[dev] = *n;
+  if (dev < 64) known[dev].store(*n, std::memory_order_relaxed);
   return WF_OK;
 }
 wf_status check_attention_sizes(wf_decoder* d, int n_seq, int n_rows, int max_rows, int max_len) {
