@@ -323,10 +323,11 @@ cudaError_t launch_simt(const TreeAttnParams& p, cudaStream_t s) {
   return simt_rows((long)p.max_rows * p.group) == 8 ? launch_simt_rows<kFormat, kDim, 8>(p, s) : launch_simt_rows<kFormat, kDim, 16>(p, s);
 }
 
-// More rows of a key/value head than this go to the kernel with 128-row tiles.  Measured, that kernel / the one for few rows in
-// us: 8 sequences of 1000 positions, 8 heads of 64 channels: 24 rows 17.0 / 14.7, 40 rows 18.8 / 19.2, 100 rows 25 / 29; 32 sequences
-// of 300 positions, 128 channels int8: 12 rows 17.8 / 12.9, 24 rows 20 / 24, 40 rows 22 / 38, 160 rows 56 / 138.
-constexpr int kWideRows = 32;
+// More rows of a key/value head than fit one tile of the kernel for few rows go to the kernel with 128-row tiles.  Measured, that kernel /
+// the one for few rows in us: 8 sequences of 1000 positions, 8 heads of 64 channels, e4m3: 24 rows 17.4 / 16.2, 40 rows 18.7 / 22.7,
+// 100 rows 24 / 28; 32 sequences of 300 positions, 128 channels, int8: 12 rows 16.8 / 13.3, 24 rows 16.8 / 24.2, 40 rows 18.8 / 36, 160 rows
+// 41 / 125.
+int wide_rows(int d_head) { return d_head == 64 ? 32 : 16; }
 
 // Rows of one tile of the kernel for few rows.
 int tc_rows(int d_head, long rows) { return rows <= 8 ? 8 : rows <= 16 || d_head == 128 ? 16 : 32; }
@@ -354,7 +355,7 @@ TreeAttnPlan plan_tree_attention(int dtype, int d_head, int n_head, int n_kv_hea
                                  int num_sms) {
   TreeAttnPlan plan{};
   const long rows = (long)max_rows * (n_head / n_kv_head);
-  const bool wide = dtype == WF_BF16 && rows > kWideRows;
+  const bool wide = dtype == WF_BF16 && rows > wide_rows(d_head);
   const int tile = wide ? 128 : dtype == WF_BF16 ? tc_rows(d_head, rows) : simt_rows(rows);
   const long tiles = (rows + tile - 1) / tile;
   const long units = tiles * n_kv_head * n_seq;
