@@ -363,7 +363,8 @@ wf_status wf_attention_f32_static(const float *qkv, const int *cu_seqlens, int B
  * touching memory, and records in `status` (dev int, may be NULL; bits are or-ed into it, the
  * caller zeroes it):
  *   1  a page index outside [0, n_pages): the position is treated as absent
- *   2  prefix sums, a start or a length that do not fit the rows or the page table
+ *   2  prefix sums, a start or a length that do not fit the rows or the page table.  Where prefix sums decrease, which
+ *      of the sequences concerned has a row is not defined
  *   4  a parent beam outside [0, n_beam): the row stays as it is
  *   8  a bounded wait inside a kernel gave up: the call's outputs are undefined
  * A handle's calls come from one host thread at a time; distinct handles are independent. */

@@ -135,8 +135,8 @@ __device__ __forceinline__ long locate(const CacheView& c, const RowsView& r, lo
   int seq = seq_hint;
   while (seq + 1 < r.n_seq && __ldg(r.cu_rows + seq + 1) <= row) ++seq;
   const int first = __ldg(r.cu_rows + seq), next = __ldg(r.cu_rows + seq + 1);
-  if (row < first || row >= next) {
-    if (row < first || next < first) report(status, kBadRows);
+  if (row < first || row >= next || first < 0) {
+    if (row < first || next < first || first < 0) report(status, kBadRows);
     return -1;
   }
   const long pos = (long)__ldg(r.start + seq) + (row - first);
@@ -162,8 +162,13 @@ template <int kLanes, int kSteps>
 __device__ __forceinline__ Share share_of(const CacheView& c, const RowsView& r, int n_chunks, int* status) {
   constexpr int kGroups = 32 / kLanes;
   const int lane = threadIdx.x & 31;
-  const long w = ((long)blockIdx.x * kThreads + threadIdx.x) >> 5;
-  if (w == 0 && lane == 0 && __ldg(r.cu_rows + r.n_seq) > r.n_rows) report(status, kBadRows);
+  // The search below looks at a few sequences only: all prefix sums are checked by the launch's first threads, a pair each, loaded
+  // beside it.
+  const long thread = (long)blockIdx.x * kThreads + threadIdx.x;
+  const bool checks = thread < r.n_seq;
+  int lo = 0, hi = 0;
+  if (checks) lo = __ldg(r.cu_rows + thread), hi = __ldg(r.cu_rows + thread + 1);
+  const long w = thread >> 5;
   Share s;
   const long block = (long)((unsigned long)w / (unsigned)n_chunks);
   s.head = (int)(w - block * n_chunks) * kSteps;
@@ -171,6 +176,15 @@ __device__ __forceinline__ Share share_of(const CacheView& c, const RowsView& r,
   s.row = row0 + lane / kLanes;
   const int hint = warp_find_sequence(r.cu_rows, r.n_seq, (int)min(row0, (long)r.n_rows));
   s.at = locate(c, r, s.row, hint, lane % kLanes == 0 ? status : nullptr);  // the lanes of one vector agree
+  if (checks) {
+    bool bad = lo < 0 || hi < lo || hi > r.n_rows;
+    for (long i = thread + (long)gridDim.x * kThreads; i < r.n_seq; i += (long)gridDim.x * kThreads) {
+      lo = __ldg(r.cu_rows + i);
+      hi = __ldg(r.cu_rows + i + 1);
+      bad |= lo < 0 || hi < lo || hi > r.n_rows;
+    }
+    if (bad) report(status, kBadRows);
+  }
   return s;
 }
 

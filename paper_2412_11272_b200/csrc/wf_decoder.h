@@ -35,8 +35,9 @@ __device__ __forceinline__ void report(int* status, int bit) {
   if (status) atomicOr(status, bit);
 }
 
-// Sequence of a row, or -1 if no sequence has it: the largest s with cu[s] <= row, searched by a whole
-// warp 32 entries at a time (two dependent loads for up to 1024 sequences).  All lanes ask for one row.
+// Sequence that can have a row: the largest s with cu[s] <= row, searched by a whole warp 32 entries at a time (two
+// dependent loads for up to 1024 sequences).  All lanes ask for one row.  Always one of 0 .. n_seq - 1: whether the row lies
+// within it is the caller's to check (rows in front of the first sequence, rows behind the last one, sums that decrease).
 __device__ __forceinline__ int warp_find_sequence(const int* __restrict__ cu, int n_seq, int row) {
   const int lane = threadIdx.x & 31;
   int lo = 0, n = n_seq;  // the answer lies in [lo, lo + n)

@@ -1,0 +1,70 @@
+"""What the header of the decoding-stage operators promises about calls that are wrong: prefix sums that do not fit, messages of refusals,
+sizes that a launch cannot hold."""
+import ctypes as C
+
+import numpy as np
+import pytest
+
+torch = pytest.importorskip("torch")
+
+
+def _decoder(**kw):
+    from paper_2412_11272_b200.binding import Decoder
+    return Decoder(**{**dict(n_head=4, d_head=64, dtype="bf16", cache_format="e4m3", page_size=16), **kw})
+
+
+def _dev(a, dtype=torch.int32):
+    return torch.as_tensor(np.ascontiguousarray(a)).to("cuda:0", dtype)
+
+
+# ---- prefix sums
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_prefix_sums_that_do_not_fit_are_reported(dtype):
+    """Every cache call reports what wf_tree_attention reports, and writes no place outside the rows' own pages."""
+    from paper_2412_11272_b200.binding import STATUS_BAD_ROWS
+    dec = _decoder(n_head=1, dtype=dtype)
+    k = torch.ones(20, 1, 64, dtype=dec.torch_dtype, device="cuda")
+
+    def run(cu, call):
+        n = len(cu) - 1
+        cache = dec.cache(2 * n + 1)
+        status = torch.zeros(1, dtype=torch.int32, device="cuda")
+        args = (cache, _dev(np.arange(2 * n).reshape(n, 2)), _dev(cu), _dev(np.zeros(n)))
+        if call == "write":
+            dec.wf_cache_write(*args, k, k, status=status)
+        elif call == "read":
+            dec.wf_cache_read(*args, 20, status=status)
+        else:
+            dec.wf_tree_attention(*args, k, 20, 32, "none", status=status)
+        assert (cache.k[2 * n].float() == 0).all()                                    # no sequence has the last page
+        return int(status), (cache.k.float() != 0).any(-1).any(1)
+
+    many = np.concatenate([np.arange(0, 11).repeat(60), [20]])                        # hundreds of sequences, most of them empty
+    for cu, good in (([0, 5, 20], True), ([0, 0, 0, 7], True), (many, True), ([0, 5, 3, 8], False), ([0, 20, 18], False), ([0, 8, 8, 2, 8], False),
+                     ([-2, 3], False), ([0, 21], False), (np.concatenate([many[:400], [0], many[400:]]), False),
+                     ([0, 2 ** 31 - 1, -2 ** 31, 4], False)):
+        for call in ("write", "read", "attention"):
+            assert run(cu, call)[0] == (0 if good else STATUS_BAD_ROWS), (cu, call)
+    # a sequence whose rows begin before the first has no places: nothing of it is written
+    assert not run([-2, 3], "write")[1].any()
+
+
+# ---- refusals (no GPU is needed)
+def _message(d):
+    return d.lib.wf_decoder_last_error(d.handle).decode()
+
+
+def test_refusals_say_what_was_wrong():
+    from paper_2412_11272_b200 import binding as Bn
+    d = _decoder()
+    P = 1 << 20
+    cache, rows = Bn.wf_cache(P, P + 4096, P, P, 3), Bn.wf_rows(2, 8, P, P, P, 4)
+    for fn, name in ((d.lib.wf_cache_write, "wf_cache_write"), (d.lib.wf_cache_read, "wf_cache_read")):
+        assert fn(d.handle, cache, rows, P, 248, P, 256, None, None) == 1
+        assert _message(d).startswith(name) and "row stride is shorter than a row of 256" in _message(d)
+        assert fn(d.handle, cache, rows, P, 260, P, 256, None, None) == 1 and "16-byte aligned" in _message(d)
+        assert fn(d.handle, cache, Bn.wf_rows(2, (1 << 27) + 1, P, P, P, 4), P, 256, P, 256, None, None) == 4 and "2^27 rows" in _message(d)
+    with pytest.raises(Bn.WfError) as e:
+        _decoder(d_head=80)
+    assert "d_head must be 64 or 128" in str(e.value)
