@@ -454,7 +454,8 @@ typedef enum {
  *   out        dev   path dtype [n_rows][n_head][d_head], rows out_stride elements apart
  *   lse        dev   float32 [n_rows][n_head], or NULL
  *   workspace  dev   16-byte aligned, at least the bytes that wf_tree_attention_workspace gives for the same sizes (may be
- *                    0: then NULL).  Nothing in it has to be set and nothing is kept in it between calls.
+ *                    0: then NULL).  Nothing in it has to be set and nothing is kept in it between calls.  The bytes do not grow
+ *                    with every size (fewer sequences are split more): ask for the sizes of each call.
  * Pointers are 16-byte aligned and row strides whole multiples of 16 bytes.  Results do not depend on the
  * order in which blocks run.  n_seq <= 65535. */
 wf_status wf_tree_attention_workspace(wf_decoder *dec, int n_seq, int n_rows, int max_rows, int max_len, size_t *bytes);

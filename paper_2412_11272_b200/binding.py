@@ -729,11 +729,15 @@ class Decoder:
         return out, lse
 
     def tree_attention_workspace(self, n_seq: int, n_rows: int, max_rows: int, max_len: int, device="cuda") -> int:
-        """Bytes of workspace of ``wf_tree_attention`` for these sizes (a function of them and the device alone)."""
-        key = (n_seq, n_rows, max_rows, max_len, device)
+        """Bytes of workspace of ``wf_tree_attention`` for these sizes: a function of them and the device alone ("cuda": the current
+        one).  It does not grow with every size: fewer sequences are split more, and may need more than a larger batch."""
+        index = device.index if isinstance(device, torch.device) else device if isinstance(device, int) else torch.device(device).index
+        if index is None:
+            index = torch.cuda.current_device()
+        key = (n_seq, n_rows, max_rows, max_len, index)
         if key not in self._workspace_bytes:
             n = C.c_size_t()
-            with torch.cuda.device(device):
+            with torch.cuda.device(index):
                 self._check(self.lib.wf_tree_attention_workspace(self.handle, n_seq, n_rows, max_rows, max_len, C.byref(n)))
             if len(self._workspace_bytes) > 4096:
                 self._workspace_bytes.clear()

@@ -68,3 +68,36 @@ def test_refusals_say_what_was_wrong():
     with pytest.raises(Bn.WfError) as e:
         _decoder(d_head=80)
     assert "d_head must be 64 or 128" in str(e.value)
+
+
+def test_workspace_sizes_are_kept_per_device(monkeypatch):
+    """The size follows from the device's SMs: "cuda" stands for the device that is current when the question is asked, and one device
+    has one remembered size however it is named."""
+    import contextlib
+    import types
+    d = _decoder()
+    current, asked = [0], []
+
+    def fake_size(handle, n_seq, n_rows, max_rows, max_len, out):
+        asked.append(current[0])
+        out._obj.value = 1000 * (current[0] + 1)
+        return 0
+
+    @contextlib.contextmanager
+    def device(x):
+        index = x if isinstance(x, int) else torch.device(x).index
+        before, current[0] = current[0], current[0] if index is None else index
+        yield
+        current[0] = before
+
+    real = d.lib
+    d.lib = types.SimpleNamespace(wf_tree_attention_workspace=fake_size, wf_decoder_destroy=real.wf_decoder_destroy)
+    monkeypatch.setattr(torch.cuda, "device", device)
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: current[0])
+    sizes = (3, 9, 4, 5000)
+    assert d.tree_attention_workspace(*sizes) == 1000
+    current[0] = 1                                                                    # another device, with other SMs, is current now
+    assert d.tree_attention_workspace(*sizes) == 2000
+    assert d.tree_attention_workspace(*sizes, torch.device("cuda")) == 2000 and d.tree_attention_workspace(*sizes, "cuda:0") == 1000
+    assert d.tree_attention_workspace(*sizes, torch.device("cuda", 1)) == 2000 and d.tree_attention_workspace(*sizes, 0) == 1000
+    assert asked == [0, 1]
