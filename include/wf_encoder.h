@@ -366,7 +366,7 @@ wf_status wf_attention_f32_static(const float *qkv, const int *cu_seqlens, int B
  *   2  prefix sums, a start or a length that do not fit the rows or the page table.  Where prefix sums decrease, which
  *      of the sequences concerned has a row is not defined
  *   4  a parent beam outside [0, n_beam): the row stays as it is
- *   8  a bounded wait inside a kernel gave up: the call's outputs are undefined
+ *   8  a bounded wait inside a kernel gave up: the outputs of the rows concerned are NaN
  * A handle's calls come from one host thread at a time; distinct handles are independent. */
 typedef struct wf_decoder wf_decoder;
 
@@ -463,6 +463,11 @@ wf_status wf_tree_attention(wf_decoder *dec, const wf_cache *cache, const wf_row
                             float scale, int tail, const unsigned *mask, int mask_words, int max_rows, int max_len,
                             void *out, long out_stride, float *lse, void *workspace, size_t workspace_bytes,
                             int *status, void *stream);
+
+/* Exercises the failure path behind status bit 8 without any fault: while `on` is not 0, every bounded wait of the
+ * handle's following wf_tree_attention calls gives up at once (where the call runs on 128-row tiles, the only ones that wait).
+ * Such a call ends normally, its rows are NaN, and the handle stays usable; 0 restores the ordinary limit. */
+wf_status wf_selftest_attention_timeout(wf_decoder *dec, int on);
 
 /* wf_beam_select: one round of beam search.  Of all continuations of the live beams of a sequence the
  * `keep` best: c_wv = score_w + x_wv - log sum_u exp(x_wu), in descending order, ties to the lower w, then the

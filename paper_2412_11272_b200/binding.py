@@ -76,7 +76,7 @@ EXPORTS = ("wf_encoder_create", "wf_logmel", "wf_encode", "wf_encode_raw_hush", 
            "wf_streams_create", "wf_streams_destroy", "wf_streams_length", "wf_streams_push", "wf_encode_streams", "wf_attention_f32_static",
            "wf_beam_pruner_create", "wf_beam_pruner_step", "wf_beam_pruner_state", "wf_beam_pruner_destroy",
            "wf_decoder_create", "wf_decoder_destroy", "wf_decoder_last_error", "wf_cache_write", "wf_cache_read",
-           "wf_tree_attention_workspace", "wf_tree_attention", "wf_beam_select", "wf_beam_reorder")
+           "wf_tree_attention_workspace", "wf_tree_attention", "wf_selftest_attention_timeout", "wf_beam_select", "wf_beam_reorder")
 
 _lib = None
 
@@ -133,6 +133,7 @@ def load_library() -> C.CDLL:
     lib.wf_tree_attention_workspace.argtypes = [vp, C.c_int, C.c_int, C.c_int, C.c_int, C.POINTER(C.c_size_t)]
     lib.wf_tree_attention.argtypes = [vp, cp, rp, vp, C.c_long, C.c_float, C.c_int, vp, C.c_int, C.c_int, C.c_int, vp, C.c_long, vp, vp,
                                       C.c_size_t, vp, vp]
+    lib.wf_selftest_attention_timeout.argtypes = [vp, C.c_int]
     lib.wf_beam_select.argtypes = [vp, vp, C.c_int, C.c_long, C.c_int, C.c_int, C.c_int, vp, vp, vp, C.c_int, vp, C.c_int, vp, vp, vp, vp, vp, vp]
     lib.wf_beam_reorder.argtypes = [vp, vp, C.c_int, C.c_int, C.POINTER(wf_beam_state), C.c_int, cp, C.c_int, vp, C.c_int, vp, vp, vp]
     for name in EXPORTS:
@@ -743,6 +744,10 @@ class Decoder:
                 self._workspace_bytes.clear()
             self._workspace_bytes[key] = n.value
         return self._workspace_bytes[key]
+
+    def wf_selftest_attention_timeout(self, on: bool = True):
+        """While on, the bounded waits of ``wf_tree_attention`` on 128-row tiles give up at once: rows are NaN, status bit 8."""
+        self._check(self.lib.wf_selftest_attention_timeout(self.handle, int(on)))
 
     def wf_beam_select(self, logits: torch.Tensor, scores: torch.Tensor, keep: int, beams=None, finished=None, end_token: int = -1,
                        suppress=None, status=None, stream=None):

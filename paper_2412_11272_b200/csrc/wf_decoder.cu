@@ -6,11 +6,13 @@
 #include <new>
 
 #include "wf_decoder.h"
+#include "wf_ptx.cuh"
 
 using namespace wf;
 
 struct wf_decoder {
   wf_decoder_config cfg;
+  bool no_waits;  // wf_selftest_attention_timeout
   char err[512];
 };
 
@@ -90,6 +92,7 @@ wf_status wf_decoder_create(const wf_decoder_config* cfg, wf_decoder** out) {
   wf_decoder* d = new (std::nothrow) wf_decoder();
   if (!d) return WF_ERR_INVALID_ARG;
   d->cfg = *cfg;
+  d->no_waits = false;
   d->err[0] = 0;
   *out = d;  // returned even on failure so that the caller can read the message, then destroy
   const wf_decoder_config& c = d->cfg;
@@ -229,7 +232,14 @@ wf_status wf_tree_attention(wf_decoder* d, const wf_cache* cache, const wf_rows*
   p.part_o = (float*)workspace;
   p.part_ml = plan.bytes ? (float2*)((float*)workspace + (size_t)rows->n_rows * c.n_head * plan.n_splits * c.d_head) : nullptr;
   p.status = status;
+  p.wait_limit = d->no_waits ? 0 : ptx::kWaitLimit;
   return cuda_result(d, "wf_tree_attention", launch_tree_attention(p, c.d_head, c.dtype, c.cache_format, (cudaStream_t)stream));
+}
+
+wf_status wf_selftest_attention_timeout(wf_decoder* d, int on) {
+  if (!d) return WF_ERR_INVALID_ARG;
+  d->no_waits = on != 0;
+  return WF_OK;
 }
 
 wf_status wf_beam_select(wf_decoder* d, const void* logits, int logits_dtype, long ld, int B, int n_beam, int vocab, const float* scores,

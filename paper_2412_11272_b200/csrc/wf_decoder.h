@@ -79,6 +79,7 @@ struct TreeAttnParams {
   float* part_o;
   float2* part_ml;
   int* status;
+  unsigned wait_limit;  // polls of a wait of the 128-row kernel; 0: every wait gives up at once
 };
 struct TreeAttnPlan {
   int n_splits, chunk, unit_warps;

@@ -12,7 +12,7 @@
 // Against the kernel for few rows, which converts every code once per 8 .. 32 query rows and feeds the legacy matrix
 // instructions, a code is converted once per 128 rows and the products cost no register traffic.
 // Two blocks run per SM (256 tensor-memory columns each: S [0, 64), P [64, 96) and [96, 128), O [128, 128 + d)), so that one
-// computes while the other waits.  Every wait is bounded; one that gives up reports in the caller's status word.
+// computes while the other waits.  Every wait is bounded; where one gives up, the block's rows become NaN and the caller's status word says so.
 //
 // Bound by the loading warps, at 1.2 us per 64-key step of an SM (128 channels, int8): a step's keys and values are waited for
 // together, one step after their issue, and converted; the softmax waits for more than half of its time, the tensor cores and
@@ -43,8 +43,8 @@ struct Smem {  // offsets from a 1024-byte border
   static constexpr int kScale = kV + 2 * kHalves * kHalfBytes;             // [stage][keys: 64 factors, values: 64 scales] float32
   static constexpr int kValid = kScale + 2 * 2 * kStep * 4;                // [stage][2] words: the key exists
   static constexpr int kBars = kValid + 2 * 2 * 4;
-  // k_full, k_free, v_full, v_free (two each), s_full, s_free, p_full (2), o_full (2)
-  static constexpr int kNumBars = 14;
+  // k_full, k_free, v_full, v_free (two each), s_full, s_free, p_full (2), o_full (2), drain
+  static constexpr int kNumBars = 15;
   static constexpr int kSlot = kBars + 8 * kNumBars;                       // tensor memory address, abort flag, odd values
   // at least a third of an SM's shared memory and more: two blocks share the SM's 512 tensor-memory columns
   static constexpr int kTotal = kSlot + 16 + 1024 > 80 * 1024 ? kSlot + 16 + 1024 : 80 * 1024;
@@ -110,6 +110,7 @@ __global__ void __launch_bounds__(kThreads, 2) tree_attention_wide_kernel(const 
   const uint32_t s_full = bar(8), s_free = bar(9);
   auto p_full = [&](int b) { return bar(10 + b); };
   auto o_full = [&](int b) { return bar(12 + b); };
+  const uint32_t drain = bar(14);
   volatile uint32_t* tmem_slot = reinterpret_cast<volatile uint32_t*>(sgen + S::kSlot);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(sgen + S::kSlot + 4);
   volatile int* odd_values = reinterpret_cast<volatile int*>(sgen + S::kSlot + 8);
@@ -127,6 +128,7 @@ __global__ void __launch_bounds__(kThreads, 2) tree_attention_wide_kernel(const 
     }
     mbar_init(s_full, 1);
     mbar_init(s_free, 128);
+    mbar_init(drain, 1);
     *abort_flag = 0;
     *odd_values = 0;
     fence_mbar_init();
@@ -160,7 +162,7 @@ __global__ void __launch_bounds__(kThreads, 2) tree_attention_wide_kernel(const 
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem = *tmem_slot;
-  bool ok = true;
+  bool ok = true, issuer = false;  // issuer: the thread that starts the products
 
   if (warp > 4) {
     // ------------------------------------------------------------------ loads and conversion
@@ -249,11 +251,11 @@ __global__ void __launch_bounds__(kThreads, 2) tree_attention_wide_kernel(const 
     for (int j = 0; j < n_steps; ++j) {
       const int st = j & 1;
       const uint32_t parity = ((j >> 1) & 1u) ^ 1u;
-      if (!__all_sync(0xffffffffu, mbar_wait(k_free(st), parity, abort_flag))) { ok = false; break; }
+      if (!__all_sync(0xffffffffu, mbar_wait_limited(k_free(st), parity, abort_flag, p.wait_limit))) { ok = false; break; }
       put(sbase + S::kK + st * S::kHalves * kHalfBytes, kraw);
       fence_proxy_async_smem();
       mbar_arrive(k_full(st));
-      if (!__all_sync(0xffffffffu, mbar_wait(v_free(st), parity, abort_flag))) { ok = false; break; }
+      if (!__all_sync(0xffffffffu, mbar_wait_limited(v_free(st), parity, abort_flag, p.wait_limit))) { ok = false; break; }
       if constexpr (!kQuant) {
         // A batch row's value that is not finite must not reach rows that do not see it through 0 * inf: it is left out here
         // and added, at the end, to the rows that see it.
@@ -292,10 +294,10 @@ __global__ void __launch_bounds__(kThreads, 2) tree_attention_wide_kernel(const 
     }
   } else if (warp == 4) {
     // ------------------------------------------------------------------ matrix products
-    const bool leader = elect_one();
+    const bool leader = issuer = elect_one();
     constexpr uint32_t idesc_s = umma_idesc_bf16(kTileRows, kStep, 0, 0);
     constexpr uint32_t idesc_o = umma_idesc_bf16(kTileRows, 64, 0, 1);
-    auto wait_all = [&](uint32_t b, uint32_t parity) -> bool { return __all_sync(0xffffffffu, mbar_wait(b, parity, abort_flag)); };
+    auto wait_all = [&](uint32_t b, uint32_t parity) -> bool { return __all_sync(0xffffffffu, mbar_wait_limited(b, parity, abort_flag, p.wait_limit)); };
     auto issue_scores = [&](int j) -> bool {
       const int st = j & 1;
       if (j > 0 && !wait_all(s_free, (j - 1) & 1u)) return false;
@@ -344,7 +346,7 @@ __global__ void __launch_bounds__(kThreads, 2) tree_attention_wide_kernel(const 
     const int i_row = mine ? r / p.group : 0;
     constexpr float kRaise = 8.f, kRaiseSum = 256.f;
     float m = -INFINITY, l = 0.f;
-    auto wait_warp = [&](uint32_t b, uint32_t parity) -> bool { return __all_sync(0xffffffffu, mbar_wait(b, parity, abort_flag)); };
+    auto wait_warp = [&](uint32_t b, uint32_t parity) -> bool { return __all_sync(0xffffffffu, mbar_wait_limited(b, parity, abort_flag, p.wait_limit)); };
     for (int j = 0; j < n_steps; ++j) {
       const int st = j & 1, pos0 = begin + j * kStep;
       if (!wait_warp(s_full, j & 1u)) { ok = false; break; }
@@ -553,11 +555,30 @@ __global__ void __launch_bounds__(kThreads, 2) tree_attention_wide_kernel(const 
         else if (p.lse) p.lse[row * p.n_head + head] = l == 0.f ? -INFINITY : (m + log2f(l)) * kLn2;
       }
     }
+    if (!ok && mine) {  // a wait gave up: the row is NaN (with splits, the join makes NaN of a NaN sum)
+      const long row = s.first_row + i_row;
+      const int head = kvh * p.group + r % p.group;
+      const float nan = __int_as_float(0x7fc00000);
+      if (p.n_splits > 1) {
+        p.part_ml[(row * p.n_head + head) * p.n_splits + split] = make_float2(nan, nan);
+      } else {
+        uint4* to = reinterpret_cast<uint4*>(reinterpret_cast<__nv_bfloat16*>(p.out) + row * p.out_stride + (long)head * kDim);
+        for (int c = 0; c < kDim / 8; ++c) to[c] = make_uint4(0x7fc07fc0u, 0x7fc07fc0u, 0x7fc07fc0u, 0x7fc07fc0u);
+        if (p.lse) p.lse[row * p.n_head + head] = nan;
+      }
+    }
   }
   if (!ok && lane == 0) report(p.status, kGaveUp);
   tc_fence_before();
   __syncthreads();
   if (warp == 4) {
+    if (*abort_flag) {  // products may be in flight: they land before tensor memory and shared memory are given back
+      if (issuer) umma_commit(drain);
+      __syncwarp();
+      int never = 0;
+      mbar_wait_limited(drain, 0, &never, kWaitLimit);
+      __syncwarp();
+    }
     tc_fence_after();
     tmem_dealloc(tmem, 256);
   }

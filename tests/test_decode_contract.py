@@ -101,3 +101,44 @@ def test_workspace_sizes_are_kept_per_device(monkeypatch):
     assert d.tree_attention_workspace(*sizes, torch.device("cuda")) == 2000 and d.tree_attention_workspace(*sizes, "cuda:0") == 1000
     assert d.tree_attention_workspace(*sizes, torch.device("cuda", 1)) == 2000 and d.tree_attention_workspace(*sizes, 0) == 1000
     assert asked == [0, 1]
+
+
+# ---- waits that give up
+@pytest.mark.gpu
+@pytest.mark.parametrize("d,fmt", [(64, "e4m3"), (64, "path"), (128, "int8")])
+@pytest.mark.parametrize("hi", [100, 5000])
+def test_a_wait_that_gives_up_leaves_no_plausible_numbers(d, fmt, hi):
+    """Also where the caller passes no status word: rows are NaN, with one split and with many; rows behind the batch stay."""
+    from paper_2412_11272_b200.binding import STATUS_GAVE_UP
+    dec = _decoder(n_head=4, n_kv_head=2, d_head=d, cache_format=fmt, page_size=64)
+    rows, starts = [40, 0, 33], [hi, 3, 7]
+    n, longest = sum(rows), hi + 40
+    pages = -(-longest // 64)
+    cache = dec.cache(pages)
+    for t in (cache.k, cache.v):
+        if fmt == "path":
+            t.normal_()
+        else:
+            t.view(torch.uint8).random_(0, 100)
+    table = _dev(np.stack([np.arange(pages)] * 3))                                    # the sequences read the same pages
+    q = torch.randn(n + 3, 4, d, device="cuda").bfloat16()
+    args = (cache, table, _dev(np.concatenate([[0], np.cumsum(rows)])), _dev(starts), q, 40, longest)
+    assert (dec.tree_attention_workspace(3, n + 3, 40, longest) > 0) == (hi == 5000)
+
+    def run(**kw):
+        out, lse = torch.full((n + 3, 4, d), 5.0, device="cuda").bfloat16(), torch.full((n + 3, 4), 5.0, device="cuda")
+        dec.wf_tree_attention(*args, out=out, lse=lse, **kw)
+        assert (out[n:] == 5).all() and (lse[n:] == 5).all()
+        return out[:n], lse[:n]
+
+    want = run()
+    assert torch.isfinite(want[0]).all() and torch.isfinite(want[1]).all()
+    dec.wf_selftest_attention_timeout(True)
+    for status in (None, torch.zeros(1, dtype=torch.int32, device="cuda")):
+        out, lse = run(status=status)
+        assert torch.isnan(out).all() and torch.isnan(lse).all()
+    assert int(status) == STATUS_GAVE_UP
+    dec.wf_selftest_attention_timeout(False)
+    status.zero_()
+    got = run(status=status)
+    assert int(status) == 0 and torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
