@@ -423,8 +423,8 @@ typedef struct {
  *   k, v   dev  path dtype [n_rows][n_kv_head][d_head], heads contiguous, consecutive rows k_stride /
  *               v_stride elements apart: for instance one layer's columns of what wf_cross_kv wrote
  * wf_cache_read: the rows' values back, each rounded once to the path dtype, in the same layout.
- * Pointers are 16-byte aligned and row strides whole multiples of 16 bytes.  No two rows of a write stand for the
- * same place of the cache (sequences may share pages that the call does not write). */
+ * Pointers are 16-byte aligned and row strides whole multiples of 16 bytes.  n_rows <= 2^27, n_rows * n_kv_head < 2^32 - 1.  No
+ * two rows of a write stand for the same place of the cache (sequences may share pages that the call does not write). */
 wf_status wf_cache_write(wf_decoder *dec, const wf_cache *cache, const wf_rows *rows, const void *k,
                          long k_stride, const void *v, long v_stride, int *status, void *stream);
 wf_status wf_cache_read(wf_decoder *dec, const wf_cache *cache, const wf_rows *rows, void *k, long k_stride,

@@ -71,9 +71,11 @@ CacheView view_of(const wf_decoder* d, const wf_cache* c) {
 }
 RowsView view_of(const wf_rows* r) { return RowsView{r->n_seq, r->n_rows, r->cu_rows, r->start, r->page_table, r->table_stride}; }
 
-wf_status check_vectors(wf_decoder* d, const char* what, const void* k, long k_stride, const void* v, long v_stride) {
+wf_status check_vectors(wf_decoder* d, const char* what, const wf_rows* r, const void* k, long k_stride, const void* v, long v_stride) {
   const int esz = path_bytes(d->cfg);
   const long row = (long)d->cfg.n_kv_head * d->cfg.d_head;
+  if ((long)r->n_rows * d->cfg.n_kv_head >= (1L << 32) - 1)  // as in check_cache; a launch's blocks fit its grid then
+    return fail(d, WF_ERR_CAPACITY, "%s: more than 2^32 vectors in a call", what);
   if (!k || !v) return fail(d, WF_ERR_INVALID_ARG, "%s: NULL keys or values", what);
   if (!aligned16(k) || !aligned16(v) || k_stride * esz % 16 || v_stride * esz % 16)
     return fail(d, WF_ERR_INVALID_ARG, "%s: keys and values need 16-byte aligned pointers and row strides", what);
@@ -122,7 +124,7 @@ wf_status wf_cache_write(wf_decoder* d, const wf_cache* cache, const wf_rows* ro
   st = check_cache(d, "wf_cache_write", cache);
   if (st != WF_OK) return st;
   if (rows->n_seq == 0 || rows->n_rows == 0) return WF_OK;
-  st = check_vectors(d, "wf_cache_write", k, k_stride, v, v_stride);
+  st = check_vectors(d, "wf_cache_write", rows, k, k_stride, v, v_stride);
   if (st != WF_OK) return st;
   return cuda_result(d, "wf_cache_write",
                      launch_cache_write(view_of(d, cache), view_of(rows), d->cfg.d_head, d->cfg.dtype, d->cfg.cache_format, k, k_stride,
@@ -137,7 +139,7 @@ wf_status wf_cache_read(wf_decoder* d, const wf_cache* cache, const wf_rows* row
   st = check_cache(d, "wf_cache_read", cache);
   if (st != WF_OK) return st;
   if (rows->n_seq == 0 || rows->n_rows == 0) return WF_OK;
-  st = check_vectors(d, "wf_cache_read", k, k_stride, v, v_stride);
+  st = check_vectors(d, "wf_cache_read", rows, k, k_stride, v, v_stride);
   if (st != WF_OK) return st;
   return cuda_result(d, "wf_cache_read",
                      launch_cache_read(view_of(d, cache), view_of(rows), d->cfg.d_head, d->cfg.dtype, d->cfg.cache_format, k, k_stride, v,

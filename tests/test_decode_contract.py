@@ -142,3 +142,15 @@ def test_a_wait_that_gives_up_leaves_no_plausible_numbers(d, fmt, hi):
     status.zero_()
     got = run(status=status)
     assert int(status) == 0 and torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+
+
+def test_calls_that_no_launch_holds_are_refused():
+    """A call of 2^32 vectors a side or more (which no cache holds) would need more blocks than a grid counts."""
+    from paper_2412_11272_b200 import binding as Bn
+    P = 1 << 20
+    d = _decoder(n_head=1024, d_head=128, cache_format="path", page_size=16)
+    cache = Bn.wf_cache(P, P + 4096, None, None, 3)
+    for fn in (d.lib.wf_cache_write, d.lib.wf_cache_read):
+        for n in (1 << 27, (1 << 26) + 2, 1 << 22):                                   # (2^26 + 2 rows: 2^32 + 128 blocks)
+            assert fn(d.handle, cache, Bn.wf_rows(1, n, P, P, P, 4), P, 1024 * 128, P, 1024 * 128, None, None) == 4, n
+            assert "2^32 vectors" in _message(d)
