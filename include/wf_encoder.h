@@ -502,7 +502,8 @@ wf_status wf_beam_select(wf_decoder *dec, const void *logits, int logits_dtype, 
  *                  copied from the parent's.  (With n_beam pages set aside for every page index of a sequence no
  *                  allocation is needed: a page is written only while it is its beam's last one.)
  *   page_table, lengths  dev  int [B * n_beam][table_stride] (in place), int [B] positions held; NULL without caches
- * No row of one state, cache or the table may overlap another one's. */
+ * No row of one state, cache or the table may overlap another one's; a state, cache or table that is given twice, and states
+ * of one stride whose rows overlap, are refused.  With n_beam = 1 nothing can move, and nothing is looked at. */
 typedef struct {
   void *ptr;
   long row_bytes, stride_bytes;

@@ -778,7 +778,8 @@ class Decoder:
     def wf_beam_reorder(self, parents: torch.Tensor, states=(), caches=(), page_table=None, lengths=None, status=None, stream=None):
         """Moves every beam's states to the beams that grew from it, in place.  parents: [B, n_beam] (negative: stays).
         states: tensors [B * n_beam, ...] whose rows are contiguous (row stride free); caches: paged caches that share
-        ``page_table`` [B * n_beam, pages], the beams of a sequence holding ``lengths`` [B] positions."""
+        ``page_table`` [B * n_beam, pages], the beams of a sequence holding ``lengths`` [B] positions.  No two of them share
+        memory (one given twice is refused)."""
         device = parents.device
         if parents.dim() != 2 or device.type != "cuda":
             _refuse("parents must be a [B, n_beam] tensor in device memory")

@@ -84,6 +84,19 @@ wf_status check_vectors(wf_decoder* d, const char* what, const wf_rows* r, const
   return WF_OK;
 }
 
+// Whether two states of n rows certainly share bytes: the first row of one begins inside a row of the other, or (strides alike) a
+// row's end reaches into one.
+bool share_bytes(const wf_beam_state& a, const wf_beam_state& b, long n) {
+  if (a.row_bytes == 0 || b.row_bytes == 0) return false;
+  const uintptr_t a0 = (uintptr_t)a.ptr, b0 = (uintptr_t)b.ptr;
+  if (a0 >= b0 + (n - 1) * b.stride_bytes + b.row_bytes || b0 >= a0 + (n - 1) * a.stride_bytes + a.row_bytes) return false;
+  if (a0 >= b0 && (long)((a0 - b0) % b.stride_bytes) < b.row_bytes) return true;
+  if (b0 >= a0 && (long)((b0 - a0) % a.stride_bytes) < a.row_bytes) return true;
+  // the extents meet and neither begins inside a row: with one stride, one begins in a gap of the other that it overruns or fits
+  if (a.stride_bytes != b.stride_bytes) return false;
+  return a0 > b0 ? b.stride_bytes - (long)((a0 - b0) % b.stride_bytes) < a.row_bytes : a.stride_bytes - (long)((b0 - a0) % a.stride_bytes) < b.row_bytes;
+}
+
 }  // namespace
 
 extern "C" {
@@ -303,6 +316,23 @@ wf_status wf_beam_reorder(wf_decoder* d, const int* parents, int B, int n_beam, 
       return fail(d, WF_ERR_INVALID_ARG, "wf_beam_reorder: caches that share a page table have the same number of pages");
   }
   if (B == 0 || n_beam == 1) return WF_OK;  // one beam can only have grown from itself
+  // What a call is given twice would be moved twice, in any order.  (A table of pages is a state of its own here.)
+  const wf_beam_state table_state{page_table, n_caches > 0 ? (long)table_stride * 4 : 0, (long)table_stride * 4};
+  for (int i = 0; i < n_states; ++i) {
+    for (int j = 0; j < i; ++j)
+      if (share_bytes(states[i], states[j], (long)B * n_beam))
+        return fail(d, WF_ERR_INVALID_ARG, "wf_beam_reorder: states %d and %d share memory", j, i);
+    if (share_bytes(states[i], table_state, (long)B * n_beam))
+      return fail(d, WF_ERR_INVALID_ARG, "wf_beam_reorder: state %d and the page table share memory", i);
+  }
+  const bool scaled = d->cfg.cache_format != WF_CACHE_PATH;
+  for (int i = 0; i < n_caches; ++i)
+    for (int j = 0; j <= i; ++j) {
+      const wf_cache &x = caches[i], &y = caches[j];
+      const bool pages = x.k == y.v || (i != j && (x.k == y.k || x.v == y.k || x.v == y.v));
+      const bool scales = scaled && (x.k_scale == y.v_scale || (i != j && (x.k_scale == y.k_scale || x.v_scale == y.k_scale || x.v_scale == y.v_scale)));
+      if (pages || scales) return fail(d, WF_ERR_INVALID_ARG, "wf_beam_reorder: caches %d and %d (or the sides of one) share memory", j, i);
+    }
   const wf_decoder_config& c = d->cfg;
   ReorderPlan p{};
   p.parents = parents;

@@ -154,3 +154,38 @@ def test_calls_that_no_launch_holds_are_refused():
         for n in (1 << 27, (1 << 26) + 2, 1 << 22):                                   # (2^26 + 2 rows: 2^32 + 128 blocks)
             assert fn(d.handle, cache, Bn.wf_rows(1, n, P, P, P, 4), P, 1024 * 128, P, 1024 * 128, None, None) == 4, n
             assert "2^32 vectors" in _message(d)
+
+
+def test_reordering_refuses_memory_given_twice():
+    """A state, or a cache, that the call is given twice would be moved twice, in any order."""
+    from paper_2412_11272_b200 import binding as Bn
+    d = _decoder(n_head=1)
+    P = 1 << 20
+
+    def reorder(*states, caches=(), B=2, W=4):
+        s = (Bn.wf_beam_state * max(len(states), 1))(*[Bn.wf_beam_state(*x) for x in states])
+        c = (Bn.wf_cache * max(len(caches), 1))(*caches)
+        return d.lib.wf_beam_reorder(d.handle, P, B, W, s, len(states), c, len(caches), P, 4, P, None, None)
+
+    for bad in (((P, 64, 64), (P, 64, 64)),                                           # the same state
+                ((P, 64, 64), (P, 16, 128)),                                          # its first bytes under another stride
+                ((P, 64, 256), (P + 32, 64, 256)),                                    # columns that share bytes
+                ((P + 32, 64, 256), (P, 64, 256)),
+                ((P, 64, 256), (P + 3 * 256 + 63, 8, 256)),
+                ((P, 64, 256), (P - 256 + 200, 64, 256)),                             # its last bytes are the other's first
+                ((P, 64, 64), (P + 640, 4, 64), (P + 128, 4, 64))):
+        assert reorder(*bad) == 1, bad
+        assert "share memory" in _message(d)
+    one, two = Bn.wf_cache(P, 2 * P, 3 * P, 4 * P, 3), Bn.wf_cache(5 * P, 6 * P, 7 * P, 8 * P, 3)
+    for bad in ((one, one), (one, two, one), (Bn.wf_cache(P, P, 3 * P, 4 * P, 3),), (one, Bn.wf_cache(5 * P, 2 * P, 7 * P, 8 * P, 3)),
+                (Bn.wf_cache(P, 2 * P, 3 * P, 3 * P, 3),)):
+        assert reorder(caches=bad) == 1 and "share memory" in _message(d)
+    assert reorder((P, 16, 16), caches=(two,)) == 1 and "share memory" in _message(d)  # the page table, as a state too
+    # side by side, interleaved, behind one another or without bytes they are different states: no refusal (without a device they end there)
+    fine = (((P, 64, 64), (P + 512, 64, 64)), ((P, 64, 256), (P + 64, 64, 256), (P + 128, 128, 256)), ((P + 128, 128, 256), (P, 64, 256)),
+            ((P, 64, 64), (P, 0, 64)), ((P, 64, 256), (P - 256 + 192, 64, 256)))
+    if not torch.cuda.is_available():
+        for good in fine:
+            assert reorder(*good) == 5, good
+        assert reorder((2 * P, 16, 16), caches=(one, two)) == 5
+    assert reorder(*fine[0], B=0) == 0 and reorder((P, 64, 64), (P, 64, 64), W=1) == 0  # nothing moves
