@@ -544,7 +544,8 @@ def _vector(t, name: str, device, dtype=_INT, n: int | None = None):
 class KvCache:
     """One decoder layer's paged keys and values: tensors the caller owns (see ``Decoder.cache``).
     k, v: [n_pages, n_kv_head, page_size, d_head]; k_scale, v_scale: bfloat16 [n_pages, n_kv_head, page_size], None for a
-    cache of the path's own type."""
+    cache of the path's own type.  It stands for the tensors' memory as it is when it is made: their contents may change, but they are
+    not exchanged, and one that is resized or set to another storage needs another KvCache."""
 
     __slots__ = ("k", "v", "k_scale", "v_scale", "device", "shape", "c")
 
@@ -558,9 +559,16 @@ class KvCache:
         for s in (k_scale, v_scale):
             if s is not None and (s.shape != k.shape[:3] or s.dtype != _BF16 or s.device != k.device or not s.is_contiguous()):
                 _refuse("scales must be contiguous bfloat16 [n_pages, n_kv_head, page_size] beside their pages")
-        self.k, self.v, self.k_scale, self.v_scale, self.device, self.shape = k, v, k_scale, v_scale, k.device, tuple(k.shape)
-        self.c = wf_cache(k.data_ptr(), v.data_ptr(), None if k_scale is None else k_scale.data_ptr(),
-                          None if v_scale is None else v_scale.data_ptr(), k.shape[0])
+        c = wf_cache(k.data_ptr(), v.data_ptr(), None if k_scale is None else k_scale.data_ptr(),
+                     None if v_scale is None else v_scale.data_ptr(), k.shape[0])
+        for name, value in zip(self.__slots__, (k, v, k_scale, v_scale, k.device, tuple(k.shape), c)):
+            object.__setattr__(self, name, value)
+
+    def __setattr__(self, name, value):  # the descriptor holds the tensors' addresses
+        raise AttributeError(f"{name} of a KvCache is fixed: make another KvCache for other tensors")
+
+    def __delattr__(self, name):
+        self.__setattr__(name, None)
 
 
 class Decoder:

@@ -189,3 +189,17 @@ def test_reordering_refuses_memory_given_twice():
             assert reorder(*good) == 5, good
         assert reorder((2 * P, 16, 16), caches=(one, two)) == 5
     assert reorder(*fine[0], B=0) == 0 and reorder((P, 64, 64), (P, 64, 64), W=1) == 0  # nothing moves
+
+
+def test_the_tensors_of_a_cache_cannot_be_exchanged():
+    """A KvCache stands for the memory it was made with: another tensor needs another KvCache."""
+    from paper_2412_11272_b200.binding import KvCache
+    pages = torch.zeros(3, 4, 16, 64, dtype=torch.uint8).view(torch.float8_e4m3fn)
+    scale = torch.ones(3, 4, 16, dtype=torch.bfloat16)
+    cache = KvCache(pages, pages.clone(), scale, scale.clone())
+    for name in ("k", "v", "k_scale", "v_scale", "device", "shape", "c"):
+        with pytest.raises(AttributeError):
+            setattr(cache, name, getattr(cache, name))
+    with pytest.raises(AttributeError):
+        del cache.k
+    assert cache.k is pages and cache.c.k == pages.data_ptr() and cache.c.n_pages == 3
