@@ -233,3 +233,67 @@ def test_selections_with_more_blocks_than_sms(dtype, B, W, V, keep):
         assert np.array_equal(g.cpu().numpy()[sure], w[sure])
     again = dec.wf_beam_select(*args)
     assert all(torch.equal(a, b) for a, b in zip(got, again))
+
+
+# ---- 128-row tiles: magnitudes and scores far apart
+@pytest.mark.parametrize("fmt", ["path", "e4m3", "int8"])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("T", [200, 2500])
+def test_many_rows_with_vectors_of_very_different_sizes(fmt, d, T):
+    """Values from 1e-30 to 1e30 and keys down to 1e-30 beside ordinary ones, in one split and in several."""
+    rng = np.random.default_rng([d, T])
+    dec = _decoder(n_head=2, n_kv_head=1, d_head=d, cache_format=fmt, page_size=64)
+    k, v = (rng.normal(size=(T, 1, d)) for _ in range(2))
+    v *= 10.0 ** rng.integers(-30, 30, size=(T, 1, 1))
+    k[::3] *= 1e-30
+    k, v = (torch.as_tensor(x.astype(np.float32)).to(torch.bfloat16) for x in (k, v))
+    c = Case(rng, dec, rows=[50], starts=[T - 50], tail="causal", k=k, v=v)
+    out, lse = c.run()
+    wo, wl = c.want()
+    assert np.abs(lse.cpu().double().numpy() - wl).max() <= 1e-4
+    see = O.visible(T - 50, 50, "causal")
+    ks, vs = (O.stored(x.double().numpy(), fmt) for x in (k, v))
+    bound, _ = O.attend(c.q.double().numpy(), ks, np.abs(vs), see, d ** -0.5)
+    # of the sum of p |v| of each row and channel: half a step, 2^-8, for the weight's rounding and as much for the output's; the float32 part
+    # as in Case.check
+    assert (np.abs(out.double().cpu().numpy() - wo) <= (2.0 ** -7 + 1e-4) * bound).all()
+
+
+@pytest.mark.parametrize("fmt", ["path", "e4m3", "int8"])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("T", [400, 2500])
+def test_many_rows_with_scores_that_keep_growing(fmt, d, T):
+    """Rows whose largest score comes last, first or nowhere in particular, from -1e4 to 1e4: the reference is raised in every step, in none,
+    or in some rows of a tile only."""
+    rng = np.random.default_rng([d, T, 1])
+    dec = _decoder(n_head=2, n_kv_head=2, d_head=d, cache_format=fmt, page_size=32)
+    k = torch.zeros(T, 2, d)
+    # within a bfloat16 step of one another where unquantised, whole numbers where codes are to be exact
+    k[:, :, 0] = torch.linspace(-100, 100, T)[:, None] if fmt == "path" else (torch.arange(T)[:, None] * 97 // T - 48.0)
+    k[:, :, 1] = torch.as_tensor(rng.integers(-8, 9, size=(T, 2)).astype(np.float32))
+    k = k.to(torch.bfloat16)
+    v = torch.as_tensor(rng.normal(size=(T, 2, d)).astype(np.float32)).to(torch.bfloat16)
+    rows = 70
+    c = Case(rng, dec, rows=[rows], starts=[T - rows], tail="causal", k=k, v=v)
+    c.q = torch.zeros(rows, 2, d)
+    c.q[:, :, 0] = torch.as_tensor(rng.choice([800.0, -800.0, 8.0, -8.0, 0.5, 0.0, 100.0, -100.0], size=(rows, 2)).astype(np.float32))
+    c.q[:, :, 1] = torch.as_tensor(rng.choice([0.0, 1.0, -2.0], size=(rows, 2)).astype(np.float32))
+    c.q = c.q.to(torch.bfloat16)
+    (out, lse), (wo, wl) = c.run(), c.want()
+    # scores of up to 1e4: their float32 roundings (the products are exact, 2^-22 of the value covers the scale and log2(e)) move lse, and the
+    # weights by the same relative amount: 1e4 2^-22 = 2.4e-3
+    lse_tol = 1e-4 + 2.0 ** -22 * np.abs(wl)
+    assert (np.abs(lse.cpu().double().numpy() - wl) <= lse_tol).all()
+    assert (np.abs(out.double().cpu().numpy() - wo) <= (2.0 ** -7 + 1e-4 + 2 * lse_tol[..., None]) * float(v.abs().max())).all()
+
+
+@pytest.mark.parametrize("dtype,fmt,d,H,Hk", [("bf16", "e4m3", 64, 3, 1), ("bf16", "path", 128, 2, 2), ("f32", "int8", 64, 2, 1), ("f32", "path", 128, 1, 1)])
+def test_prompts_of_thousands_of_rows(dtype, fmt, d, H, Hk):
+    """A long causal prompt behind a committed prefix, beside a single token and a short prompt: many row tiles of one sequence, none of others."""
+    rng = np.random.default_rng([d, H])
+    dec = _decoder(n_head=H, n_kv_head=Hk, d_head=d, dtype=dtype, cache_format=fmt, page_size=256)
+    c = Batch(rng, dec, [2111, 1, 37], [45, 900, 0], "causal", 1)
+    got = c.run()
+    c.check(got, c.want())
+    again = c.run()
+    assert torch.equal(got[0], again[0]) and torch.equal(got[1], again[1])
