@@ -378,7 +378,9 @@ typedef struct wf_decoder wf_decoder;
  *   WF_CACHE_INT8   s = a / 127 (rounded to float32) rounded up to bfloat16;  code = the whole number
  *                   nearest to x / s, ties to even, the quotient not rounded before
  * s is at least 2^-126, and 1 if a = 0.  A vector that holds a NaN or an infinity gets s = NaN and
- * zero codes, and reads back as NaN.  A stored element stands for code * s. */
+ * zero codes, and reads back as NaN.  A stored element stands for code * s.  Codes are finite: the two
+ * e4m3 codes of NaN (0x7f, 0xff), which no write makes, are not part of the format, and what stands
+ * for them where a caller stores them is not defined (NaN or 480 s); a NaN scale is a vector of NaN. */
 typedef enum { WF_CACHE_PATH = 0, WF_CACHE_E4M3 = 1, WF_CACHE_INT8 = 2 } wf_cache_format;
 
 /* n_kv_head divides n_head (query head h reads key/value head h / (n_head / n_kv_head)); d_head is
@@ -445,7 +447,9 @@ typedef enum {
  * A row that sees nothing gets out = 0 and lse = -infinity.  What a row does not see has no influence
  * on it, whatever it holds (NaN included).  Scores, softmax and sums are float32, keys and values are the stored ones
  * (code * s).  WF_BF16: the products run on the tensor cores; a probability is rounded once to
- * bfloat16, in the quantised caches after multiplication with its value's scale.
+ * bfloat16, in the quantised caches after multiplication with its value's scale.  Magnitudes of queries
+ * and stored values are taken to lie below 2^80: products with codes and sums before the last division
+ * stay within float32 then.
  *   q          dev   path dtype [n_rows][n_head][d_head], rows q_stride elements apart
  *   tail       host  wf_tail;  mask  dev  uint32 [n_rows][mask_words], bit t % 32 of word t / 32 (WF_TAIL_MASK only)
  *   max_rows   host  no sequence has more rows in this call (mask_words * 32 >= max_rows)

@@ -6,7 +6,7 @@
 // heads of them, so that the codes of neighbouring positions, and their two-byte scales, leave side by side (heads lie whole runs
 // of positions apart), and the search for a row's sequence and page is paid once for its keys and values.
 // Bound by memory: d_head (esz + 1) + 2 bytes per vector, once.  35 M bfloat16 elements a side to e4m3 and back: 47 + 39 us, 4.9 TB/s, the
-// rest being addresses and conversions between the loads; 6,000 float32 rows of 8 heads of 128 to int8 and back: 43 us, 4.3 TB/s.
+// rest being addresses and conversions between the loads; 9,062 float32 rows of 8 heads of 128 to int8 and back: 43 us, 4.3 TB/s.
 #include <type_traits>
 
 #include "wf_decoder.h"

@@ -361,13 +361,21 @@ TreeAttnPlan plan_tree_attention(int dtype, int d_head, int n_head, int n_kv_hea
   const long units = tiles * n_kv_head * n_seq;
   if (wide) {
     // two blocks of an SM; sequences differ in length, so more blocks than fit at once even the load out, as long as a
-    // block's start (7 us of its 35 at 768 positions) stays small
+    // block's start (7 us of its 35 at 768 positions) stays small.  Splits of at least 256 / 768 positions, or none, measured in us: 448
+    // positions, 20 heads, 448 rows 28 / 19 / 19; 2 x 100 rows, 20 heads, 800 .. 1500 positions 22 / 25 / 31; 64 rows, 8 heads, 1500
+    // positions 16 / 28 / 44 (few tiles would gain from shorter ones); 16 x 48 rows, 32 / 8 heads, 100 .. 4096 positions 184 / 184 / 167.
     const long splits = std::max(1L, std::min((8L * num_sms + units - 1) / units, ((long)max_len + 767) / 768));
     plan.unit_warps = 0;
     plan.chunk = (int)(((long)max_len + splits * 64 - 1) / (splits * 64) * 64);
   } else if (dtype == WF_BF16) {
-    // Warps that the registers let reside: 16, 12 or 8 per SM.  A unit is shared by as few warps as fill them (each one has
-    // a start and an end to pay for), and cut into splits, all of one wave, where four are not enough.
+    // Warps taken to reside on an SM, by tile: 16, 12 or 8 (the launch bounds let 20, 12 and 8; shared memory 12 in 8-row tiles of
+    // unquantised caches of 128 channels).  A unit is shared by as few warps as fill them (each one has a start and an end to pay for).
+    // Four / two / one warp a unit, measured in us: single tokens of 320 sequences, 20 heads of 64 channels, e4m3, up to 219 positions
+    // (6400 units) 47 / 41 / 34, of 640 sequences 90 / 75 / 58, 160 sequences of up to 448 positions, 32 heads of 128 84 / 86 / 94;
+    // 900 x 5 rows, 32 / 8 heads of 64, 50 .. 300 positions 276 / 186 / 143.
+    // And cut into splits, all of one wave, where four are not enough, of at least 256 positions: 64 / 256 / 1024, measured in us: one
+    // token of one sequence, 1000 positions, 8 heads of 128, bfloat16 7.5 / 10.4 / 19; 5000 positions of one head 8.1 / 8.2 / 13; 448
+    // positions, 20 heads 8.5 / 7.7 / 6.9.
     const long resident = (long)num_sms * (tile == 8 ? 16 : tile == 16 && d_head == 64 ? 12 : 8);
     plan.unit_warps = units >= 4 * resident ? 1 : units >= 2 * resident ? 2 : 4;
     const long splits = std::max(1L, std::min(resident / (4 * units), ((long)max_len + 255) / 256));

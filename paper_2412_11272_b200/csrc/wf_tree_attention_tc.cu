@@ -14,9 +14,9 @@
 // multiplies the float32 score.  Values: codes as bfloat16, and the probability times the vector's scale rounded once
 // to bfloat16, whose range holds any scale.  Unquantised: bfloat16 throughout, the probability rounded to it.
 //
-// Bound by memory where few heads share long histories: 2 sequences of 99 and 131 thousand positions, 8 heads of 128
-// channels, bfloat16: 203 us, 5.0 TB/s.  Many short ones are bound by the starts and ends of their blocks and by issue: 64 sequences
-// of 75 .. 775 positions, 20 heads of 64 channels, e4m3: 26.7 us, 2.8 TB/s, half of the issue slots busy.  One token,
+// Bound by memory where few heads share long histories: 2 sequences of 119 and 131 thousand positions, 8 heads of 128
+// channels, bfloat16: 200 us, 5.1 TB/s.  Many short ones are bound by the starts and ends of their blocks and by issue: 64 sequences
+// of 75 .. 775 positions, 20 heads of 64 channels, e4m3: 27 us, 2.8 TB/s, half of the issue slots busy.  One token,
 // 20 heads, 151 positions: 4.6 us, the latency of three dependent loads (lengths, page, keys) and the join of the warps.
 #include "wf_ptx.cuh"
 #include "wf_tree_attention.cuh"
