@@ -410,7 +410,8 @@ typedef struct {
 /* New rows (tokens) of a batch of sequences, packed as everywhere in this library: sequence s has
  * rows cu_rows[s] .. cu_rows[s + 1] of the row arrays, and its row i sits at cache position
  * start[s] + i.  Position p is entry p % page_size of page page_table[s * table_stride + p / page_size].
- * Rows at or behind cu_rows[n_seq] (padding of a batch with a fixed size) are neither read nor written.
+ * Rows in front of cu_rows[0] (a call for some of a batch's sequences) and at or behind cu_rows[n_seq] (padding of a batch with
+ * a fixed size) are neither read nor written.
  *   n_seq, n_rows        host  sequences; rows that the row arrays have
  *   cu_rows, start       dev   int [n_seq + 1], int [n_seq]
  *   page_table           dev   int [n_seq][table_stride] */

@@ -130,15 +130,13 @@ __device__ __forceinline__ void dequantise(uint2 c, float s, float (&x)[8]) {
 }
 
 // Where a row lives in the cache: index of its first head's vector among all vectors of a side, or -1 (padding rows, bad tables).
+// Reports what is wrong with the row's start and page; the prefix sums are checked_sums' to report.
 __device__ __forceinline__ long locate(const CacheView& c, const RowsView& r, long row, int seq_hint, int* status) {
   if (row >= r.n_rows) return -1;
   int seq = seq_hint;
   while (seq + 1 < r.n_seq && __ldg(r.cu_rows + seq + 1) <= row) ++seq;
   const int first = __ldg(r.cu_rows + seq), next = __ldg(r.cu_rows + seq + 1);
-  if (row < first || row >= next || first < 0) {
-    if (row < first || next < first || first < 0) report(status, kBadRows);
-    return -1;
-  }
+  if (row < first || row >= next || first < 0) return -1;  // padding, or sums that do not fit
   const long pos = (long)__ldg(r.start + seq) + (row - first);
   const long index = pos >> c.page_shift;
   if (pos < 0 || index >= r.table_stride) {

@@ -203,3 +203,45 @@ def test_the_tensors_of_a_cache_cannot_be_exchanged():
     with pytest.raises(AttributeError):
         del cache.k
     assert cache.k is pages and cache.c.k == pages.data_ptr() and cache.c.n_pages == 3
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype,n", [("bf16", 4), ("bf16", 40), ("f32", 4)])
+def test_some_sequences_of_a_packed_batch(dtype, n):
+    """A slice of the prefix sums (with the starts and the table's rows that belong to it) stands for those sequences: rows in front of
+    the first one are padding like the rows behind the last, and nothing about that is wrong."""
+    rng = np.random.default_rng(n)
+    dec = _decoder(n_head=2, dtype=dtype)
+    rows, starts = [n, 3, 0, n - 1, 5], [20, 0, 7, 33, 2]
+    cu = np.concatenate([[0], np.cumsum(rows)])
+    total = int(cu[-1])
+    k, v, q = (torch.as_tensor(rng.normal(size=(total, 2, 64)).astype(np.float32)).to("cuda", dec.torch_dtype) for _ in range(3))
+    pages = 5
+    table = _dev(rng.permutation(5 * pages).reshape(5, pages))
+    status = torch.zeros(1, dtype=torch.int32, device="cuda")
+
+    def run(a, b, cache):
+        """Writes, reads back and attends the sequences a .. b - 1."""
+        args = (cache, table[a:b].contiguous(), _dev(cu[a:b + 1]), _dev(starts[a:b]))
+        dec.wf_cache_write(*args, k, v, status=status)
+        back = [torch.full_like(x, 9.0) for x in (k, v)]
+        dec.wf_cache_read(*args, total, k=back[0], v=back[1], status=status)
+        out, lse = torch.full_like(q, 9.0), torch.full((total, 2), 9.0, device="cuda")
+        dec.wf_tree_attention(*args, q, max(rows), 80, "causal", out=out, lse=lse, status=status)
+        return [*back, out, lse]
+
+    whole, part = dec.cache(5 * pages), dec.cache(5 * pages)
+    want, got = run(0, 5, whole), [None] * 4
+    for a, b in ((0, 1), (1, 4), (4, 5)):
+        here = run(a, b, part)
+        lo, hi = cu[a], cu[b]
+        for x in here:
+            assert (x[:lo] == 9).all() and (x[hi:] == 9).all()
+        got = [x[lo:hi] if g is None else torch.cat([g, x[lo:hi]]) for g, x in zip(got, here)]
+    assert int(status) == 0
+    for x, y in ((whole.k, part.k), (whole.v, part.v)):
+        assert torch.equal(x.view(torch.uint8), y.view(torch.uint8))
+    # the cache's values are the same; attention may split the positions otherwise: two answers within the tolerance of rounding
+    assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+    tol = 2.0 ** -6 + 2e-4 if dtype == "bf16" else 2e-4
+    assert (got[2].double() - want[2].double()).abs().max() <= tol * float(v.double().abs().max()) and (got[3] - want[3]).abs().max() <= 2e-4
