@@ -448,9 +448,9 @@ typedef enum {
  * A row that sees nothing gets out = 0 and lse = -infinity.  What a row does not see has no influence
  * on it, whatever it holds (NaN included).  Scores, softmax and sums are float32, keys and values are the stored ones
  * (code * s).  WF_BF16: the products run on the tensor cores; a probability is rounded once to
- * bfloat16, in the quantised caches after multiplication with its value's scale.  Magnitudes of queries
- * and stored values are taken to lie below 2^80: products with codes and sums before the last division
- * stay within float32 then.
+ * bfloat16, in the quantised caches after multiplication with its value's scale.  Products with codes and
+ * sums before the last division stay within float32 for queries below 2^100 and stored values times
+ * positions below 2^119 in magnitude.
  *   q          dev   path dtype [n_rows][n_head][d_head], rows q_stride elements apart
  *   tail       host  wf_tail;  mask  dev  uint32 [n_rows][mask_words], bit t % 32 of word t / 32 (WF_TAIL_MASK only)
  *   max_rows   host  no sequence has more rows in this call (mask_words * 32 >= max_rows)
