@@ -365,8 +365,10 @@ wf_status wf_attention_f32_static(const float *qkv, const int *cu_seqlens, int B
  *   1  a page index outside [0, n_pages): the position is treated as absent
  *   2  prefix sums, a start or a length that do not fit the rows or the page table.  Where prefix sums decrease, which
  *      of the sequences concerned has a row is not defined
- *   4  a parent beam outside [0, n_beam): the row stays as it is
+ *   4  a parent beam outside [0, n_beam): the row stays as it is; a parent or path of drafted rows that does not fit
  *   8  a bounded wait inside a kernel gave up: the outputs of the rows concerned are NaN
+ *   16 a sequence's rows were put off: no room for them, or no free pages (wf_page_plan)
+ *   32 a token outside the vocabulary or a temperature that is negative or not finite (wf_draft_verify)
  * A handle's calls come from one host thread at a time; distinct handles are independent. */
 typedef struct wf_decoder wf_decoder;
 
@@ -470,7 +472,8 @@ wf_status wf_tree_attention(wf_decoder *dec, const wf_cache *cache, const wf_row
                             int *status, void *stream);
 
 /* Exercises the failure path behind status bit 8 without any fault: while `on` is not 0, every bounded wait of the
- * handle's following wf_tree_attention calls gives up at once (where the call runs on 128-row tiles, the only ones that wait).
+ * handle's following wf_tree_attention calls gives up at once (where the call runs on 128-row tiles, the only ones that wait),
+ * and every one of its wf_gemm_e4m3 calls.
  * Such a call ends normally, its rows are NaN, and the handle stays usable; 0 restores the ordinary limit. */
 wf_status wf_selftest_attention_timeout(wf_decoder *dec, int on);
 
@@ -516,6 +519,93 @@ typedef struct {
 wf_status wf_beam_reorder(wf_decoder *dec, const int *parents, int B, int n_beam, const wf_beam_state *states,
                           int n_states, const wf_cache *caches, int n_caches, int *page_table, int table_stride,
                           const int *lengths, int *status, void *stream);
+
+/* wf_page_plan: rows and pages of one round for a batch whose sequences come and go, planned on the device.  Free pages are
+ * a ring: state = {head, count}, entries pages[(head + i) % n_pages] for i < count.  Sequence s holds lengths[s] positions in
+ * the first held[s] pages of its row of the page table, lengths[s] <= held[s] * page_size.  In this order, sequences by number:
+ *   - a sequence whose `ended` flag is set (its place goes to another one) gives its pages back behind the free ones and
+ *     begins at length 0; those pages are handed out by later calls, not by this one;
+ *   - a sequence asks for new_rows[s] rows, and for the pages that they lack beyond the held ones.  It gets them if the rows
+ *     asked for so far, its own included, are at most n_rows, and it needs no page or the pages asked for so far are at
+ *     most `count`.  Otherwise it gets no row and no page in this round (status bit 16); pages come from the ring's front.
+ * Written: the ring, its state, the page table, held and (of ended sequences) lengths, in place; and
+ *   cu_rows   dev  int [n_seq + 1]: prefix sums of the rows that were granted
+ *   row_seq, row_pos  dev  int [n_rows]: a row's sequence and its position lengths[s] + i, -1 behind the last row;  may be NULL
+ *   row_slot  dev  int64 [n_rows]: page * page_size + position % page_size, -1 behind the last row or without a page;  may be NULL
+ * The rows then go through wf_cache_write and wf_tree_attention with `lengths` as start, and wf_draft_commit adds them to the
+ * lengths.  A sequence whose numbers do not fit (a negative one, more positions than pages, rows beyond the page table) gets no
+ * rows, and of a pool whose state does not fit nothing is taken: bit 2.  n_seq <= 8192. */
+typedef struct {
+  int *pages, *state;
+  int n_pages;
+} wf_page_pool;
+wf_status wf_page_plan(wf_decoder *dec, const wf_page_pool *pool, int n_seq, const int *new_rows, const unsigned char *ended,
+                       int *lengths, int *held, int *page_table, int table_stride, int n_rows, int *cu_rows, int *row_seq,
+                       int *row_pos, long long *row_slot, int *status, void *stream);
+
+/* wf_draft_verify: which drafted tokens of every sequence the target keeps, and the token behind them (speculative
+ * sampling: what is kept is distributed as the target's own samples are).  Row 0 of a sequence is its last token, the
+ * others are drafts, each the child of an earlier row: a chain, or a tree as wf_tree_attention takes it.  At a row w, from
+ * row 0 on, p = softmax(logits_w / T) (T = 0: all of it on the largest logit, the lowest index of equals) and w's children are
+ * tried in row order.  With x a child's token and u its random number,
+ *   u q(x) < p(x):  the child is kept, and the same is done there;
+ *   otherwise       p <- max(p - q, 0) / sum of it (unless that sum is 0), and the next child is tried;
+ * where none is kept the token that follows is the first v with sum_{i<=v} p_i > u' sum_i p_i.  q is the distribution that w's
+ * children were drawn from, or, without `draft`, all of it on x (drafts that were looked up or chosen, not drawn).  T = 0: a
+ * child is kept if p(x) = 1.  Sums that decide a drawn token are float64, exponentials included.
+ *   logits       dev   float32 or bfloat16 (logits_dtype) [n_rows][vocab], rows `ld` elements apart
+ *   cu_rows      dev   int [n_seq + 1];  max_rows  host  no sequence has more rows in this call (longer ones are cut, bit 2)
+ *   tokens       dev   int [n_rows] (of a first row: not looked at);  parents  dev  int [n_rows], row of the sequence below the
+ *                      row's own, or NULL: chains.  A row with a parent or token that does not fit is never tried (bits 4, 32)
+ *   draft        dev   float32 [n_rows][vocab], rows draft_ld elements apart: row w is the q of w's children; or NULL
+ *   temperature  dev   float32 [n_seq], or NULL: 1.  One that does not fit: the sequence keeps nothing (bit 32)
+ *   accept_u, sample_u  dev  float32 [n_rows], [n_seq]: random numbers from [0, 1), u of every row and u' of every sequence
+ *   kept         dev   int [n_seq]: rows that stay, the first one included; as many as tokens that are new.  0 without rows
+ *   out_tokens   dev   int [n_seq][max_rows]: the kept drafts' tokens, then the one that follows; -1 behind
+ *   path         dev   int [n_seq][max_rows]: the rows that stay, 0 first; -1 behind
+ * A row whose logits hold a NaN or +infinity, or nothing but -infinity, has no distribution: none of its children is kept, and
+ * the token that follows is -1.  max_rows <= 1024, vocab <= 2^28. */
+wf_status wf_draft_verify(wf_decoder *dec, const void *logits, int logits_dtype, long ld, int vocab, int n_seq, int n_rows,
+                          int max_rows, const int *cu_rows, const int *tokens, const int *parents, const float *draft, long draft_ld,
+                          const float *temperature, const float *accept_u, const float *sample_u, int *kept, int *out_tokens,
+                          int *path, int *status, void *stream);
+
+/* wf_draft_commit: the rows that a verification keeps become the sequences' positions.  In every cache, the vectors at
+ * position start[s] + path[s][i] move to start[s] + i for i < kept[s], and lengths[s] = start[s] + kept[s].  With path = NULL
+ * (chains, prompts) nothing moves.
+ *   start, kept  dev   int [n_seq];  path  dev  int [n_seq][path_stride], increasing
+ *   lengths      dev   int [n_seq]; may be start itself
+ *   caches       host  every layer's cache; they share the page table (dev, int [n_seq][table_stride]).  The positions
+ *                      concerned are the sequence's own: no page that holds one is shared with another sequence
+ * A kept[s] that is negative or above path_stride counts as 0 (bit 2); a row that is not above the one before it stays where it
+ * is (bit 4), as one beyond the table or in a page that does not exist (bits 2, 1).  A cache that is given twice is refused.
+ * n_seq <= 65535, path_stride <= 1024. */
+wf_status wf_draft_commit(wf_decoder *dec, int n_seq, const int *start, const int *kept, const int *path, int path_stride, int *lengths,
+                          const wf_cache *caches, int n_caches, const int *page_table, int table_stride, int *status, void *stream);
+
+/* Matrices in 8 bits for a decoder's products: [rows, k] as e4m3 codes with one scale for each 128 channels of a row (the
+ * last block of a row may have fewer).  A scale is a power of two, kept as its exponent: byte b stands for 2^(b - 127), 255 for
+ * NaN.  An element is code * scale.
+ *   codes   dev  [rows][k], rows `ld` bytes apart, 16-byte aligned
+ *   scales  dev  [rows][ceil(k / 128)] bytes, rows scale_ld bytes apart, aligned to 4; a row has room for 4 ceil(k / 512) bytes */
+typedef struct {
+  void *codes;
+  unsigned char *scales;
+  long ld, scale_ld;
+} wf_e4m3;
+
+/* wf_quantise_e4m3: x [rows, k] (float32 or bfloat16, rows ldx elements apart) as codes and scales, activations as well as
+ * weights.  With a = max |x| over a block: scale = the least power of two s >= 2^-126 with a / s <= 448 (1 if a = 0), code =
+ * x / s (exact) rounded to the nearest e4m3 value, ties to even.  A block with a NaN or an infinity gets the scale NaN and
+ * zero codes.  The bytes behind a row's last scale, up to a multiple of 4, are written (127). */
+wf_status wf_quantise_e4m3(wf_decoder *dec, const void *x, int x_dtype, long ldx, long rows, int k, const wf_e4m3 *out, void *stream);
+
+/* wf_gemm_e4m3: C[m, n] = act(A W^T + bias), A [m, k], W [n, k]: the decoder's projections.  Products of codes and scales are
+ * exact, sums are the tensor cores' float32; act is the erf-form GELU if `gelu`, and C (out_dtype: float32 or bfloat16) is rounded
+ * once.  bias: dev float32 [n] or NULL.  C's rows are ldc elements apart, any alignment of its type; nothing behind a row's n
+ * elements is written.  A NaN scale or code makes the sums that it is part of NaN. */
+wf_status wf_gemm_e4m3(wf_decoder *dec, const wf_e4m3 *a, const wf_e4m3 *w, const float *bias, void *out, int out_dtype, long ldc, long m,
+                       int n, int k, int gelu, int *status, void *stream);
 
 #ifdef __cplusplus
 }

@@ -67,6 +67,14 @@ class wf_beam_state(C.Structure):
     _fields_ = [("ptr", C.c_void_p), ("row_bytes", C.c_long), ("stride_bytes", C.c_long)]
 
 
+class wf_page_pool(C.Structure):
+    _fields_ = [("pages", C.c_void_p), ("state", C.c_void_p), ("n_pages", C.c_int)]
+
+
+class wf_e4m3(C.Structure):
+    _fields_ = [("codes", C.c_void_p), ("scales", C.c_void_p), ("ld", C.c_long), ("scale_ld", C.c_long)]
+
+
 _PER_LAYER = ("ln1_g", "ln1_b", "wq", "bq", "wk", "wv", "bv", "wo", "bo", "ln2_g", "ln2_b",
               "w1", "b1", "w2", "b2")
 
@@ -76,7 +84,8 @@ EXPORTS = ("wf_encoder_create", "wf_logmel", "wf_encode", "wf_encode_raw_hush", 
            "wf_streams_create", "wf_streams_destroy", "wf_streams_length", "wf_streams_push", "wf_encode_streams", "wf_attention_f32_static",
            "wf_beam_pruner_create", "wf_beam_pruner_step", "wf_beam_pruner_state", "wf_beam_pruner_destroy",
            "wf_decoder_create", "wf_decoder_destroy", "wf_decoder_last_error", "wf_cache_write", "wf_cache_read",
-           "wf_tree_attention_workspace", "wf_tree_attention", "wf_selftest_attention_timeout", "wf_beam_select", "wf_beam_reorder")
+           "wf_tree_attention_workspace", "wf_tree_attention", "wf_selftest_attention_timeout", "wf_beam_select", "wf_beam_reorder",
+           "wf_page_plan", "wf_draft_verify", "wf_draft_commit", "wf_quantise_e4m3", "wf_gemm_e4m3")
 
 _lib = None
 
@@ -136,6 +145,12 @@ def load_library() -> C.CDLL:
     lib.wf_selftest_attention_timeout.argtypes = [vp, C.c_int]
     lib.wf_beam_select.argtypes = [vp, vp, C.c_int, C.c_long, C.c_int, C.c_int, C.c_int, vp, vp, vp, C.c_int, vp, C.c_int, vp, vp, vp, vp, vp, vp]
     lib.wf_beam_reorder.argtypes = [vp, vp, C.c_int, C.c_int, C.POINTER(wf_beam_state), C.c_int, cp, C.c_int, vp, C.c_int, vp, vp, vp]
+    ci, cl = C.c_int, C.c_long
+    lib.wf_page_plan.argtypes = [vp, C.POINTER(wf_page_pool), ci, vp, vp, vp, vp, vp, ci, ci, vp, vp, vp, vp, vp, vp]
+    lib.wf_draft_verify.argtypes = [vp, vp, ci, cl, ci, ci, ci, ci, vp, vp, vp, vp, cl, vp, vp, vp, vp, vp, vp, vp, vp]
+    lib.wf_draft_commit.argtypes = [vp, ci, vp, vp, vp, ci, vp, cp, ci, vp, ci, vp, vp]
+    lib.wf_quantise_e4m3.argtypes = [vp, vp, ci, cl, cl, ci, C.POINTER(wf_e4m3), vp]
+    lib.wf_gemm_e4m3.argtypes = [vp, C.POINTER(wf_e4m3), C.POINTER(wf_e4m3), vp, vp, ci, cl, cl, ci, ci, ci, vp, vp]
     for name in EXPORTS:
         if name not in ("wf_last_error", "wf_decoder_last_error"):
             getattr(lib, name).restype = C.c_int
@@ -524,8 +539,8 @@ class BeamPruner:
 
 TAILS = {"none": 0, "causal": 1, "mask": 2, "tree": 2}
 CACHE_FORMATS = {"path": 0, "e4m3": 1, "int8": 2}
-STATUS_BAD_PAGE, STATUS_BAD_ROWS, STATUS_BAD_PARENT, STATUS_GAVE_UP = 1, 2, 4, 8
-_INT, _U8, _F32, _BF16 = torch.int32, torch.uint8, torch.float32, torch.bfloat16
+STATUS_BAD_PAGE, STATUS_BAD_ROWS, STATUS_BAD_PARENT, STATUS_GAVE_UP, STATUS_PUT_OFF, STATUS_BAD_VALUE = 1, 2, 4, 8, 16, 32
+_INT, _U8, _F32, _BF16, _E4M3 = torch.int32, torch.uint8, torch.float32, torch.bfloat16, torch.float8_e4m3fn
 
 
 def _refuse(message: str):
@@ -569,6 +584,80 @@ class KvCache:
 
     def __delattr__(self, name):
         self.__setattr__(name, None)
+
+
+class PagePool:
+    """Free pages of a cache (see ``Decoder.page_pool``): a ring of page numbers, int32 [n_pages], and its state, int32 (head,
+    count).  Both are updated in place by ``wf_page_plan``; the tensors stay the caller's."""
+
+    __slots__ = ("pages", "state", "device")
+
+    def __init__(self, pages: torch.Tensor, state: torch.Tensor):
+        _vector(pages, "pages", pages.device)
+        _vector(state, "state", pages.device, n=2)
+        if pages.dim() != 1 or pages.numel() < 1:
+            _refuse("pages must be a vector of at least one page number")
+        self.pages, self.state, self.device = pages, state, pages.device
+
+
+class ScaledCodes:
+    """A matrix [rows, k] in 8 bits: e4m3 ``codes`` (rows 16-byte aligned) and ``scales``, uint8 [rows, 4 ceil(k / 512)]: byte b of
+    block j stands for 2^(b - 127), the scale of a row's channels 128 j .. 128 j + 127.  Made by ``Decoder.wf_quantise_e4m3``, or
+    from codes of other origin by ``pack``."""
+
+    __slots__ = ("codes", "scales")
+
+    def __init__(self, codes: torch.Tensor, scales: torch.Tensor):
+        if codes.dim() != 2 or codes.dtype is not _E4M3 or codes.shape[1] < 1 or (codes.stride(1) != 1 and codes.shape[1] > 1):
+            _refuse("codes must be float8_e4m3fn [rows, k], a row's elements contiguous")
+        if scales.dim() != 2 or scales.dtype is not _U8 or scales.device != codes.device or scales.shape[0] != codes.shape[0] \
+                or scales.shape[1] < (codes.shape[1] + 511) // 512 * 4 or scales.stride(1) != 1:
+            _refuse("scales must be uint8 [rows, 4 ceil(k / 512)] beside their codes, a row's bytes contiguous")
+        self.codes, self.scales = codes, scales
+
+    @property
+    def shape(self):
+        return self.codes.shape
+
+    @classmethod
+    def empty(cls, rows: int, k: int, device="cuda"):
+        """Room for a matrix, rows padded to 16 bytes."""
+        codes = torch.empty((rows, (k + 15) // 16 * 16), dtype=_U8, device=device).view(_E4M3)[:, :k]
+        return cls(codes, torch.empty((rows, (k + 511) // 512 * 4), dtype=_U8, device=device))
+
+    @classmethod
+    def pack(cls, codes: torch.Tensor, scales: torch.Tensor):
+        """Codes [rows, k] with scales as numbers: powers of two (or NaN), [rows, ceil(k / 128)], or one for each 128 x 128 block,
+        [ceil(rows / 128), ceil(k / 128)]."""
+        rows, k = codes.shape
+        blocks = (k + 127) // 128
+        if scales.dim() != 2 or scales.shape[1] != blocks or scales.shape[0] not in (rows, (rows + 127) // 128):
+            _refuse(f"scales must be [{rows} or {(rows + 127) // 128}, {blocks}] for these codes")
+        mantissa, exponent = torch.frexp(scales.float())
+        if not bool(((mantissa == 0.5) | scales.isnan()).all()) or not bool((((exponent >= -125) & (exponent <= 128)) | scales.isnan()).all()):
+            _refuse("scales must be powers of two from 2^-126 to 2^127")
+        byte = torch.where(scales.isnan(), 255, exponent + 126).to(_U8)
+        if scales.shape[0] != rows:
+            byte = byte.repeat_interleave(128, dim=0)[:rows]
+        out = cls.empty(rows, k, codes.device)
+        out.codes.view(_U8).copy_(codes.view(_U8))
+        out.scales.fill_(127)
+        out.scales[:, :blocks] = byte
+        return out
+
+    def values(self) -> torch.Tensor:
+        """What the matrix stands for, in float32."""
+        k = self.codes.shape[1]
+        s = torch.exp2(self.scales.double() - 127).float().masked_fill(self.scales == 255, float("nan"))
+        return self.codes.float() * s.repeat_interleave(128, dim=1)[:, :k]
+
+    def _c(self, name: str):
+        c, s = self.codes, self.scales
+        rows = c.shape[0]
+        if c.device.type != "cuda":
+            _refuse(f"{name} must be in device memory")
+        return wf_e4m3(c.data_ptr(), s.data_ptr(), c.stride(0) if rows > 1 else max(c.stride(0), (c.shape[1] + 15) // 16 * 16),
+                       s.stride(0) if rows > 1 else max(s.stride(0), s.shape[1]))
 
 
 class Decoder:
@@ -818,3 +907,125 @@ class Decoder:
             lens = _vector(lengths, "lengths", device, n=B)
         self._call(self.lib.wf_beam_reorder, device, stream, pp, B, W, state_array, len(states), cache_array, len(caches), table, stride or 0,
                    lens, self._status(status, device))
+
+    # -- rows and pages of a round
+    def page_pool(self, n_pages: int, device="cuda") -> PagePool:
+        """A pool in which all of ``n_pages`` pages are free, to be handed out in their order."""
+        return PagePool(torch.arange(n_pages, dtype=_INT, device=device), torch.tensor([0, n_pages], dtype=_INT, device=device))
+
+    def wf_page_plan(self, pool: PagePool, page_table, held, lengths, new_rows, n_rows: int, ended=None, status=None, stream=None):
+        """Plans a round: which sequences get the ``new_rows`` [n_seq] that they ask for, with at most ``n_rows`` rows in all, and the
+        pages that these lack.  ``pool``, ``page_table`` [n_seq, pages], ``held`` (pages) and ``lengths`` (positions) [n_seq] are updated in
+        place; sequences with an ``ended`` flag (uint8 or bool [n_seq]) first give their pages back and begin at 0.  Returns (cu_rows
+        [n_seq + 1], row_seq, row_pos int32 [n_rows], row_slot int64 [n_rows]); rows that nobody has hold -1."""
+        device = pool.device
+        if device.type != "cuda":
+            _refuse("the pool must be in device memory")
+        n_seq, shape = new_rows.numel(), page_table.shape
+        if len(shape) != 2 or shape[0] < n_seq:
+            _refuse("page_table must be [n_seq, pages]")
+        args = (_vector(new_rows, "new_rows", device),
+                None if ended is None else _vector(ended, "ended", device, torch.bool if ended.dtype == torch.bool else _U8, n_seq),
+                _vector(lengths, "lengths", device, n=n_seq), _vector(held, "held", device, n=n_seq), _vector(page_table, "page_table", device))
+        c = wf_page_pool(_vector(pool.pages, "pages", device), _vector(pool.state, "state", device, n=2), pool.pages.numel())
+        cu = self._empty(new_rows, n_seq + 1, _INT, stream)
+        seq, pos = self._empty(new_rows, max(n_rows, 0), _INT, stream), self._empty(new_rows, max(n_rows, 0), _INT, stream)
+        slot = self._empty(new_rows, max(n_rows, 0), torch.int64, stream)
+        self._call(self.lib.wf_page_plan, device, stream, c, n_seq, *args, shape[1], n_rows, cu.data_ptr(), seq.data_ptr(), pos.data_ptr(),
+                   slot.data_ptr(), self._status(status, device))
+        return cu, seq, pos, slot
+
+    # -- drafted tokens
+    def wf_draft_verify(self, logits: torch.Tensor, cu_rows, tokens, accept_u, sample_u, max_rows: int, parents=None, draft=None,
+                        temperature=None, status=None, stream=None):
+        """Which drafted tokens the target keeps, and the token behind them.  logits [n_rows, vocab] float32 or bfloat16 (row stride
+        free); tokens, parents int32 [n_rows] (parents None: chains); draft float32 [n_rows, vocab]: row w is the distribution that w's
+        children were drawn from (None: they were not drawn); temperature float32 [n_seq] (None: 1; 0: the largest logit); accept_u
+        float32 [n_rows] and sample_u [n_seq]: random numbers from [0, 1).  Returns int32 (kept [n_seq], tokens [n_seq, max_rows], path
+        [n_seq, max_rows]): how many rows stay, the new tokens (as many) and the rows that stay; -1 behind them."""
+        device = logits.device
+        if device.type != "cuda" or logits.dim() != 2 or logits.dtype not in (_F32, _BF16) or logits.stride(1) != 1:
+            _refuse("logits must be float32 or bfloat16 [n_rows, vocab] in device memory, a row's elements contiguous")
+        (n, V), n_seq = logits.shape, cu_rows.numel() - 1
+        if n_seq < 0 or max_rows < 1:
+            _refuse("cu_rows has n_seq + 1 entries, max_rows is at least 1")
+        dp, dld = None, 0
+        if draft is not None:
+            if draft.dim() != 2 or draft.shape[0] < n or draft.shape[1] != V or draft.dtype is not _F32 or draft.device != device or draft.stride(1) != 1:
+                _refuse(f"draft must be float32 [n_rows, {V}] beside the logits, a row's elements contiguous")
+            dp, dld = draft.data_ptr(), draft.stride(0) if draft.shape[0] > 1 else max(draft.stride(0), V)
+        kept = self._empty(logits, n_seq, _INT, stream)
+        out, path = self._empty(logits, (n_seq, max_rows), _INT, stream), self._empty(logits, (n_seq, max_rows), _INT, stream)
+        self._call(self.lib.wf_draft_verify, device, stream, logits.data_ptr(), WF_BF16 if logits.dtype is _BF16 else WF_F32,
+                   logits.stride(0) if n > 1 else max(logits.stride(0), V), V, n_seq, n, max_rows, _vector(cu_rows, "cu_rows", device),
+                   _vector(tokens, "tokens", device, n=n), None if parents is None else _vector(parents, "parents", device, n=n), dp, dld,
+                   None if temperature is None else _vector(temperature, "temperature", device, _F32, n_seq),
+                   _vector(accept_u, "accept_u", device, _F32, n), _vector(sample_u, "sample_u", device, _F32, n_seq), kept.data_ptr(),
+                   out.data_ptr(), path.data_ptr(), self._status(status, device))
+        return kept, out, path
+
+    def wf_draft_commit(self, start, kept, path=None, caches=(), page_table=None, lengths=None, status=None, stream=None):
+        """Moves the rows that stay (``path`` [n_seq, rows], the first ``kept`` [n_seq] of each; None: they lie as they should) behind
+        the ``start`` [n_seq] committed positions in every cache, and returns the new lengths start + kept.  ``lengths``: where these go
+        (``start`` itself: in place)."""
+        device, n_seq = start.device, start.numel()
+        if device.type != "cuda":
+            _refuse("start must be in device memory")
+        pp, stride = None, 0
+        if path is not None:
+            if path.dim() != 2 or path.shape[0] < n_seq:
+                _refuse("path must be [n_seq, rows]")
+            pp, stride = _vector(path, "path", device), path.shape[1]
+        cache_array = (wf_cache * len(caches))()
+        for i, c in enumerate(caches):
+            cache_array[i] = self._cache(c)
+            if c.device != device:
+                _refuse("caches and start are on different devices")
+        table = tstride = None
+        if caches:
+            if page_table is None or page_table.dim() != 2 or page_table.shape[0] < n_seq:
+                _refuse("caches need page_table [n_seq, pages]")
+            table, tstride = _vector(page_table, "page_table", device), page_table.shape[1]
+        if lengths is None:
+            lengths = self._empty(start, n_seq, _INT, stream)
+        self._call(self.lib.wf_draft_commit, device, stream, n_seq, _vector(start, "start", device), _vector(kept, "kept", device, n=n_seq), pp,
+                   stride, _vector(lengths, "lengths", device, n=n_seq), cache_array, len(caches), table, tstride or 0, self._status(status, device))
+        return lengths
+
+    # -- products with 8-bit codes
+    def wf_quantise_e4m3(self, x: torch.Tensor, out: ScaledCodes | None = None, stream=None) -> ScaledCodes:
+        """x [rows, k] (float32 or bfloat16, row stride free) as e4m3 codes with a power-of-two scale for each 128 channels of a row:
+        activations before a product, or weights, once."""
+        device = x.device
+        if device.type != "cuda" or x.dim() != 2 or x.dtype not in (_F32, _BF16) or x.shape[1] < 1 or (x.stride(1) != 1 and x.shape[1] > 1):
+            _refuse("x must be float32 or bfloat16 [rows, k] in device memory, a row's elements contiguous")
+        rows, k = x.shape
+        if out is None:
+            ld = (k + 15) // 16 * 16
+            codes = self._empty(x, (rows, ld), _E4M3, stream)
+            out = ScaledCodes(codes if ld == k else codes[:, :k], self._empty(x, (rows, (k + 511) // 512 * 4), _U8, stream))
+        elif out.shape != x.shape or out.codes.device != device:
+            _refuse("out must have the shape and the device of x")
+        self._call(self.lib.wf_quantise_e4m3, device, stream, x.data_ptr(), WF_BF16 if x.dtype is _BF16 else WF_F32,
+                   x.stride(0) if rows > 1 else max(x.stride(0), k), rows, k, out._c("out"))
+        return out
+
+    def wf_gemm_e4m3(self, a: ScaledCodes, w: ScaledCodes, bias=None, gelu: bool = False, out=None, out_dtype: str | None = None, status=None,
+                     stream=None) -> torch.Tensor:
+        """act(a w^T + bias): a [m, k], w [n, k], bias float32 [n]; ``gelu``: the activation.  Returns [m, n] in ``out_dtype`` ("bf16" or
+        "f32", default: the decoder's), or writes to ``out`` (row stride free)."""
+        (m, k), (n, kw), device = a.shape, w.shape, a.codes.device
+        if k != kw or w.codes.device != device:
+            _refuse(f"a has {k} channels and w {kw}, or they are on different devices")
+        if out is None:
+            if out_dtype not in (None, "bf16", "f32"):
+                _refuse("out_dtype is bf16 or f32")
+            out = self._empty(a.scales, (m, n), self.torch_dtype if out_dtype is None else _BF16 if out_dtype == "bf16" else _F32, stream)
+        elif out.shape != (m, n) or out.dtype not in (_F32, _BF16) or out.device != device or (out.stride(1) != 1 and n > 1):
+            _refuse(f"out must be float32 or bfloat16 [{m}, {n}] on {device}, a row's elements contiguous")
+        elif out_dtype is not None and out.dtype is not (_BF16 if out_dtype == "bf16" else _F32):
+            _refuse("out is not of out_dtype")
+        bp = None if bias is None else _vector(bias, "bias", device, _F32, n)
+        self._call(self.lib.wf_gemm_e4m3, device, stream, a._c("a"), w._c("w"), bp, out.data_ptr(), WF_BF16 if out.dtype is _BF16 else WF_F32,
+                   out.stride(0) if m > 1 else max(out.stride(0), n), m, n, k, int(gelu), self._status(status, device))
+        return out

@@ -390,4 +390,188 @@ wf_status wf_beam_reorder(wf_decoder* d, const int* parents, int B, int n_beam, 
   return cuda_result(d, "wf_beam_reorder", e);
 }
 
+wf_status wf_page_plan(wf_decoder* d, const wf_page_pool* pool, int n_seq, const int* new_rows, const unsigned char* ended, int* lengths,
+                       int* held, int* page_table, int table_stride, int n_rows, int* cu_rows, int* row_seq, int* row_pos, long long* row_slot,
+                       int* status, void* stream) {
+  if (!d) return WF_ERR_INVALID_ARG;
+  if (!pool || !pool->pages || !pool->state || pool->n_pages < 1) return fail(d, WF_ERR_INVALID_ARG, "wf_page_plan: NULL pool or no pages");
+  if (n_seq < 0 || n_rows < 0) return fail(d, WF_ERR_INVALID_ARG, "wf_page_plan: a negative size");
+  if (n_seq > kMaxPlanned || n_rows > (1 << 27) || table_stride > (1 << 27))
+    return fail(d, WF_ERR_CAPACITY, "wf_page_plan: more than %d sequences, 2^27 rows or 2^27 pages in a sequence", kMaxPlanned);
+  if (!cu_rows || (n_seq > 0 && (!new_rows || !lengths || !held || !page_table || table_stride < 1)))
+    return fail(d, WF_ERR_INVALID_ARG, "wf_page_plan: NULL argument");
+  PagePlanParams p{};
+  p.ring = pool->pages;
+  p.pool = pool->state;
+  p.n_pages = pool->n_pages;
+  p.page_shift = log2_of(d->cfg.page_size);
+  p.n_seq = n_seq;
+  p.n_rows = n_rows;
+  p.new_rows = new_rows;
+  p.ended = ended;
+  p.lengths = lengths;
+  p.held = held;
+  p.table = page_table;
+  p.table_stride = table_stride;
+  p.cu_rows = cu_rows;
+  p.row_seq = row_seq;
+  p.row_pos = row_pos;
+  p.row_slot = row_slot;
+  p.status = status;
+  return cuda_result(d, "wf_page_plan", launch_page_plan(p, (cudaStream_t)stream));
+}
+
+wf_status wf_draft_verify(wf_decoder* d, const void* logits, int logits_dtype, long ld, int vocab, int n_seq, int n_rows, int max_rows,
+                          const int* cu_rows, const int* tokens, const int* parents, const float* draft, long draft_ld,
+                          const float* temperature, const float* accept_u, const float* sample_u, int* kept, int* out_tokens, int* path,
+                          int* status, void* stream) {
+  if (!d) return WF_ERR_INVALID_ARG;
+  if (n_seq < 0 || n_rows < 0 || max_rows < 1 || vocab < 1) return fail(d, WF_ERR_INVALID_ARG, "wf_draft_verify: a size below its least");
+  if (n_seq > (1 << 24) || n_rows > (1 << 27) || max_rows > kMaxDrafts || vocab > (1 << 28))
+    return fail(d, WF_ERR_CAPACITY, "wf_draft_verify: more than 2^24 sequences, 2^27 rows, %d rows in a sequence or 2^28 tokens", kMaxDrafts);
+  const int esz = logits_dtype == WF_BF16 ? 2 : 4;
+  if ((logits_dtype != WF_F32 && logits_dtype != WF_BF16) || ld < vocab || (draft && draft_ld < vocab))
+    return fail(d, WF_ERR_INVALID_ARG, "wf_draft_verify: unknown logits type, or rows shorter than the vocabulary");
+  if (n_seq == 0) return WF_OK;
+  if (!cu_rows || !sample_u || !kept || !out_tokens || !path || (n_rows > 0 && (!logits || !tokens || !accept_u)))
+    return fail(d, WF_ERR_INVALID_ARG, "wf_draft_verify: NULL argument");
+  if ((uintptr_t)logits % esz || (uintptr_t)draft % 4) return fail(d, WF_ERR_INVALID_ARG, "wf_draft_verify: logits or draft are not aligned to their type");
+  int sms = 0;
+  const wf_status st = sm_count(d, &sms);
+  if (st != WF_OK) return st;
+  DraftVerifyParams p{};
+  p.logits = logits;
+  p.ld = ld;
+  p.vocab = vocab;
+  p.n_seq = n_seq;
+  p.n_rows = n_rows;
+  p.max_rows = max_rows;
+  p.cu_rows = cu_rows;
+  p.tokens = tokens;
+  p.parents = parents;
+  p.draft = draft;
+  p.draft_ld = draft_ld;
+  p.temperature = temperature;
+  p.accept_u = accept_u;
+  p.sample_u = sample_u;
+  p.kept = kept;
+  p.out_tokens = out_tokens;
+  p.path = path;
+  p.status = status;
+  return cuda_result(d, "wf_draft_verify", launch_draft_verify(p, logits_dtype, sms, (cudaStream_t)stream));
+}
+
+wf_status wf_draft_commit(wf_decoder* d, int n_seq, const int* start, const int* kept, const int* path, int path_stride, int* lengths,
+                          const wf_cache* caches, int n_caches, const int* page_table, int table_stride, int* status, void* stream) {
+  if (!d) return WF_ERR_INVALID_ARG;
+  if (n_seq < 0 || n_caches < 0 || (path && path_stride < 1)) return fail(d, WF_ERR_INVALID_ARG, "wf_draft_commit: a size below its least");
+  if (n_seq > 65535 || (path && path_stride > kMaxDrafts))
+    return fail(d, WF_ERR_CAPACITY, "wf_draft_commit: more than 65535 sequences, or %d rows in a sequence", kMaxDrafts);
+  if (n_caches > 0 && (!caches || !page_table || table_stride < 1)) return fail(d, WF_ERR_INVALID_ARG, "wf_draft_commit: NULL argument");
+  for (int i = 0; i < n_caches; ++i) {
+    const wf_status st = check_cache(d, "wf_draft_commit", caches + i);
+    if (st != WF_OK) return st;
+    if (caches[i].n_pages != caches[0].n_pages)
+      return fail(d, WF_ERR_INVALID_ARG, "wf_draft_commit: caches that share a page table have the same number of pages");
+  }
+  const bool scaled = d->cfg.cache_format != WF_CACHE_PATH;
+  for (int i = 0; i < n_caches; ++i)  // what is given twice would be moved twice, in any order
+    for (int j = 0; j <= i; ++j) {
+      const wf_cache &x = caches[i], &y = caches[j];
+      const bool pages = x.k == y.v || (i != j && (x.k == y.k || x.v == y.k || x.v == y.v));
+      const bool scales = scaled && (x.k_scale == y.v_scale || (i != j && (x.k_scale == y.k_scale || x.v_scale == y.k_scale || x.v_scale == y.v_scale)));
+      if (pages || scales) return fail(d, WF_ERR_INVALID_ARG, "wf_draft_commit: caches %d and %d (or the sides of one) share memory", j, i);
+    }
+  if (n_seq == 0) return WF_OK;
+  if (!start || !kept || !lengths) return fail(d, WF_ERR_INVALID_ARG, "wf_draft_commit: NULL argument");
+  const bool in_place = lengths == start;
+  if (!in_place && lengths < start + n_seq && start < lengths + n_seq)
+    return fail(d, WF_ERR_INVALID_ARG, "wf_draft_commit: lengths may be start itself, but not overlap it otherwise");
+  const wf_decoder_config& c = d->cfg;
+  CommitPlan p{};
+  p.n_seq = n_seq;
+  p.start = start;
+  p.kept = kept;
+  p.path = path;
+  p.path_stride = path_stride;
+  p.page_table = page_table;
+  p.table_stride = table_stride;
+  p.page_shift = log2_of(c.page_size);
+  p.n_pages = n_caches > 0 ? caches[0].n_pages : 0;
+  p.n_kv_head = c.n_kv_head;
+  p.vec_units = c.d_head * code_bytes(c) / 16;
+  p.status = status;
+  cudaError_t e = cudaSuccess;
+  bool written = false;
+  for (int i = 0; path && i < n_caches && e == cudaSuccess; i += kCommitItems / 2) {
+    p.n_items = 0;
+    for (int j = i; j < n_caches && j < i + kCommitItems / 2; ++j)
+      for (int side = 0; side < 2; ++side)
+        p.item[p.n_items++] = CommitItem{(char*)(side == 0 ? caches[j].k : caches[j].v),
+                                         scaled ? (__nv_bfloat16*)(side == 0 ? caches[j].k_scale : caches[j].v_scale) : nullptr};
+    p.lengths = i == 0 && !in_place ? lengths : nullptr;
+    e = launch_draft_commit(p, (cudaStream_t)stream);
+    written |= p.lengths != nullptr;
+  }
+  if (!written && e == cudaSuccess) {  // the moves read start: in place, the lengths come behind them
+    p.lengths = lengths;
+    e = launch_draft_lengths(p, (cudaStream_t)stream);
+  }
+  return cuda_result(d, "wf_draft_commit", e);
+}
+
+namespace {
+wf_status check_codes(wf_decoder* d, const char* what, const wf_e4m3* x, int k) {
+  if (!x || !x->codes || !x->scales) return fail(d, WF_ERR_INVALID_ARG, "%s: NULL codes or scales", what);
+  if (!aligned16(x->codes) || x->ld % 16 || ((uintptr_t)x->scales & 3) || x->scale_ld % 4)
+    return fail(d, WF_ERR_INVALID_ARG, "%s: codes need 16-byte aligned rows, scales rows aligned to 4 bytes", what);
+  if (x->ld < k || x->scale_ld < (long)(k + 511) / 512 * 4)
+    return fail(d, WF_ERR_INVALID_ARG, "%s: a row of codes or scales is shorter than %d channels need", what, k);
+  return WF_OK;
+}
+}  // namespace
+
+wf_status wf_quantise_e4m3(wf_decoder* d, const void* x, int x_dtype, long ldx, long rows, int k, const wf_e4m3* out, void* stream) {
+  if (!d) return WF_ERR_INVALID_ARG;
+  if (rows < 0 || k < 1) return fail(d, WF_ERR_INVALID_ARG, "wf_quantise_e4m3: negative rows or no channels");
+  if (rows > (1 << 27) || k > (1 << 24)) return fail(d, WF_ERR_CAPACITY, "wf_quantise_e4m3: more than 2^27 rows or 2^24 channels");
+  if ((x_dtype != WF_F32 && x_dtype != WF_BF16) || ldx < k) return fail(d, WF_ERR_INVALID_ARG, "wf_quantise_e4m3: unknown type, or rows shorter than k");
+  if (rows == 0) return WF_OK;
+  const wf_status st = check_codes(d, "wf_quantise_e4m3", out, k);
+  if (st != WF_OK) return st;
+  if (!x || (uintptr_t)x % (x_dtype == WF_BF16 ? 2 : 4)) return fail(d, WF_ERR_INVALID_ARG, "wf_quantise_e4m3: x is NULL or not aligned to its type");
+  return cuda_result(d, "wf_quantise_e4m3", launch_quantise_e4m3(x, x_dtype, ldx, rows, k, out->codes, out->ld, out->scales, out->scale_ld, (cudaStream_t)stream));
+}
+
+wf_status wf_gemm_e4m3(wf_decoder* d, const wf_e4m3* a, const wf_e4m3* w, const float* bias, void* out, int out_dtype, long ldc, long m, int n, int k,
+                       int gelu, int* status, void* stream) {
+  if (!d) return WF_ERR_INVALID_ARG;
+  if (m < 0 || n < 0 || k < 1) return fail(d, WF_ERR_INVALID_ARG, "wf_gemm_e4m3: a negative size or no channels");
+  if (m > (1 << 27) || n > (1 << 27) || k > (1 << 24)) return fail(d, WF_ERR_CAPACITY, "wf_gemm_e4m3: more than 2^27 rows or columns, or 2^24 channels");
+  if ((out_dtype != WF_F32 && out_dtype != WF_BF16) || ldc < n) return fail(d, WF_ERR_INVALID_ARG, "wf_gemm_e4m3: unknown output type, or rows shorter than n");
+  if (m == 0 || n == 0) return WF_OK;
+  wf_status st = check_codes(d, "wf_gemm_e4m3 (a)", a, k);
+  if (st == WF_OK) st = check_codes(d, "wf_gemm_e4m3 (w)", w, k);
+  if (st != WF_OK) return st;
+  if (!out || (uintptr_t)out % (out_dtype == WF_BF16 ? 2 : 4) || (uintptr_t)bias % 4)
+    return fail(d, WF_ERR_INVALID_ARG, "wf_gemm_e4m3: out is NULL, or out or bias not aligned to their type");
+  int sms = 0;
+  st = sm_count(d, &sms);
+  if (st != WF_OK) return st;
+  E4m3GemmParams p{};
+  p.a = E4m3Operand{a->codes, a->scales, a->ld, a->scale_ld};
+  p.w = E4m3Operand{w->codes, w->scales, w->ld, w->scale_ld};
+  p.m = (int)m;
+  p.n = n;
+  p.k = k;
+  p.bias = bias;
+  p.gelu = gelu != 0;
+  p.out = out;
+  p.out_dtype = out_dtype;
+  p.ldc = ldc;
+  p.status = status;
+  p.wait_limit = d->no_waits ? 0 : ptx::kWaitLimit;
+  return cuda_result(d, "wf_gemm_e4m3", launch_gemm_e4m3(p, sms, (cudaStream_t)stream));
+}
+
 }  // extern "C"

@@ -12,7 +12,7 @@
 namespace wf {
 
 // Bits of the caller's status word.
-enum DeviceStatus : int { kBadPage = 1, kBadRows = 2, kBadParent = 4, kGaveUp = 8 };
+enum DeviceStatus : int { kBadPage = 1, kBadRows = 2, kBadParent = 4, kGaveUp = 8, kPutOff = 16, kBadValue = 32 };
 
 constexpr int kMaxBeams = 16;
 
@@ -138,5 +138,79 @@ struct ReorderPlan {
 };
 constexpr int kReorderThreads = 256;
 cudaError_t launch_beam_reorder(const ReorderPlan& p, int B, int n_blocks, cudaStream_t s);
+
+// ---- rows and pages of a round (wf_page_plan.cu)
+constexpr int kMaxPlanned = 8192;  // sequences: five integers each in shared memory
+struct PagePlanParams {
+  int *ring, *pool;
+  int n_pages, page_shift;
+  int n_seq, n_rows;
+  const int* new_rows;
+  const unsigned char* ended;
+  int *lengths, *held, *table;
+  int table_stride;
+  int *cu_rows, *row_seq, *row_pos;
+  long long* row_slot;
+  int* status;
+};
+cudaError_t launch_page_plan(const PagePlanParams& p, cudaStream_t s);
+
+// ---- verification and commit of drafted tokens (wf_draft.cu)
+constexpr int kMaxDrafts = 1024;  // rows of a sequence
+struct DraftVerifyParams {
+  const void* logits;
+  long ld;
+  int vocab, n_seq, n_rows, max_rows;
+  const int *cu_rows, *tokens, *parents;
+  const float* draft;
+  long draft_ld;
+  const float *temperature, *accept_u, *sample_u;
+  int *kept, *out_tokens, *path;
+  int* status;
+};
+cudaError_t launch_draft_verify(const DraftVerifyParams& p, int dtype, int num_sms, cudaStream_t s);
+
+// One side (keys or values) of a layer's cache.
+struct CommitItem {
+  char* ptr;
+  __nv_bfloat16* scale;  // NULL: not quantised
+};
+constexpr int kCommitItems = 128;
+struct CommitPlan {
+  CommitItem item[kCommitItems];
+  int n_items;
+  int n_seq;
+  const int *start, *kept, *path;
+  int path_stride;
+  int* lengths;  // NULL: not this launch
+  const int* page_table;
+  int table_stride, page_shift, n_pages, n_kv_head;
+  int vec_units;  // 16-byte units of a vector
+  int* status;
+};
+cudaError_t launch_draft_commit(const CommitPlan& p, cudaStream_t s);
+cudaError_t launch_draft_lengths(const CommitPlan& p, cudaStream_t s);
+
+// ---- products with 8-bit codes (wf_gemm_e4m3.cu)
+constexpr int kScaleBlock = 128;  // channels of a row that share a scale
+struct E4m3Operand {
+  const void* codes;
+  const unsigned char* scales;
+  long ld, scale_ld;  // bytes between rows
+};
+cudaError_t launch_quantise_e4m3(const void* x, int dtype, long ldx, long rows, int k, void* codes, long ld_codes, unsigned char* scales,
+                                 long ld_scales, cudaStream_t s);
+struct E4m3GemmParams {
+  E4m3Operand a, w;  // [m, k], [n, k]
+  int m, n, k;
+  const float* bias;
+  int gelu;
+  void* out;
+  int out_dtype;
+  long ldc;
+  int* status;
+  unsigned wait_limit;
+};
+cudaError_t launch_gemm_e4m3(const E4m3GemmParams& p, int num_sms, cudaStream_t s);
 
 }  // namespace wf
