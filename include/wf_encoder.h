@@ -587,7 +587,8 @@ wf_status wf_draft_commit(wf_decoder *dec, int n_seq, const int *start, const in
  * last block of a row may have fewer).  A scale is a power of two, kept as its exponent: byte b stands for 2^(b - 127), 255 for
  * NaN.  An element is code * scale.
  *   codes   dev  [rows][k], rows `ld` bytes apart, 16-byte aligned
- *   scales  dev  [rows][ceil(k / 128)] bytes, rows scale_ld bytes apart, aligned to 4; a row has room for 4 ceil(k / 512) bytes */
+ *   scales  dev  bytes [ceil(k / 512)][scale_ld][4], aligned to 4: block b of row r is byte b % 4 at [b / 4][r], so that a
+ *                word holds four blocks of a row and consecutive rows lie side by side.  scale_ld >= rows */
 typedef struct {
   void *codes;
   unsigned char *scales;
@@ -597,7 +598,7 @@ typedef struct {
 /* wf_quantise_e4m3: x [rows, k] (float32 or bfloat16, rows ldx elements apart) as codes and scales, activations as well as
  * weights.  With a = max |x| over a block: scale = the least power of two s >= 2^-126 with a / s <= 448 (1 if a = 0), code =
  * x / s (exact) rounded to the nearest e4m3 value, ties to even.  A block with a NaN or an infinity gets the scale NaN and
- * zero codes.  The bytes behind a row's last scale, up to a multiple of 4, are written (127). */
+ * zero codes.  The bytes behind a row's last block, up to a whole word, are written (127).  k <= 2^22. */
 wf_status wf_quantise_e4m3(wf_decoder *dec, const void *x, int x_dtype, long ldx, long rows, int k, const wf_e4m3 *out, void *stream);
 
 /* wf_gemm_e4m3: C[m, n] = act(A W^T + bias), A [m, k], W [n, k]: the decoder's projections.  Products of codes and scales are

@@ -601,29 +601,32 @@ class PagePool:
 
 
 class ScaledCodes:
-    """A matrix [rows, k] in 8 bits: e4m3 ``codes`` (rows 16-byte aligned) and ``scales``, uint8 [rows, 4 ceil(k / 512)]: byte b of
-    block j stands for 2^(b - 127), the scale of a row's channels 128 j .. 128 j + 127.  Made by ``Decoder.wf_quantise_e4m3``, or
-    from codes of other origin by ``pack``."""
+    """A matrix [rows, k] in 8 bits: e4m3 ``codes`` (rows 16-byte aligned) and ``scales``, uint8 [ceil(k / 512), rows, 4]: byte b at
+    [j, r, i] stands for 2^(b - 127), the scale of row r's channels 128 (4 j + i) and the 127 behind them.  Made by
+    ``Decoder.wf_quantise_e4m3``, or from codes of other origin by ``pack``."""
 
-    __slots__ = ("codes", "scales")
+    __slots__ = ("codes", "scales", "shape", "device")
 
     def __init__(self, codes: torch.Tensor, scales: torch.Tensor):
         if codes.dim() != 2 or codes.dtype is not _E4M3 or codes.shape[1] < 1 or (codes.stride(1) != 1 and codes.shape[1] > 1):
             _refuse("codes must be float8_e4m3fn [rows, k], a row's elements contiguous")
-        if scales.dim() != 2 or scales.dtype is not _U8 or scales.device != codes.device or scales.shape[0] != codes.shape[0] \
-                or scales.shape[1] < (codes.shape[1] + 511) // 512 * 4 or scales.stride(1) != 1:
-            _refuse("scales must be uint8 [rows, 4 ceil(k / 512)] beside their codes, a row's bytes contiguous")
-        self.codes, self.scales = codes, scales
+        rows, k = codes.shape
+        if scales.dtype is not _U8 or scales.device != codes.device or scales.shape != ((k + 511) // 512, rows, 4) or \
+                (rows > 0 and (scales.stride(2) != 1 or (rows > 1 and scales.stride(1) != 4) or (k > 512 and scales.stride(0) % 4))):
+            _refuse("scales must be uint8 [ceil(k / 512), rows, 4] beside their codes, the words of consecutive rows side by side")
+        self.codes, self.scales, self.shape, self.device = codes, scales, (rows, k), codes.device
 
-    @property
-    def shape(self):
-        return self.codes.shape
+    def __getitem__(self, rows: slice):
+        """Some of the rows."""
+        if not isinstance(rows, slice) or rows.step not in (None, 1):
+            _refuse("rows are taken by a slice without a step")
+        return ScaledCodes(self.codes[rows], self.scales[:, rows])
 
     @classmethod
     def empty(cls, rows: int, k: int, device="cuda"):
         """Room for a matrix, rows padded to 16 bytes."""
         codes = torch.empty((rows, (k + 15) // 16 * 16), dtype=_U8, device=device).view(_E4M3)[:, :k]
-        return cls(codes, torch.empty((rows, (k + 511) // 512 * 4), dtype=_U8, device=device))
+        return cls(codes, torch.empty(((k + 511) // 512, rows, 4), dtype=_U8, device=device))
 
     @classmethod
     def pack(cls, codes: torch.Tensor, scales: torch.Tensor):
@@ -641,23 +644,24 @@ class ScaledCodes:
             byte = byte.repeat_interleave(128, dim=0)[:rows]
         out = cls.empty(rows, k, codes.device)
         out.codes.view(_U8).copy_(codes.view(_U8))
-        out.scales.fill_(127)
-        out.scales[:, :blocks] = byte
+        words = torch.full((rows, out.scales.shape[0] * 4), 127, dtype=_U8, device=codes.device)
+        words[:, :blocks] = byte
+        out.scales.copy_(words.view(rows, -1, 4).transpose(0, 1))
         return out
 
     def values(self) -> torch.Tensor:
         """What the matrix stands for, in float32."""
-        k = self.codes.shape[1]
-        s = torch.exp2(self.scales.double() - 127).float().masked_fill(self.scales == 255, float("nan"))
+        rows, k = self.shape
+        b = self.scales.transpose(0, 1).reshape(rows, -1)
+        s = torch.exp2(b.double() - 127).float().masked_fill(b == 255, float("nan"))
         return self.codes.float() * s.repeat_interleave(128, dim=1)[:, :k]
 
     def _c(self, name: str):
-        c, s = self.codes, self.scales
-        rows = c.shape[0]
-        if c.device.type != "cuda":
+        rows, k = self.shape
+        if self.device.type != "cuda":
             _refuse(f"{name} must be in device memory")
-        return wf_e4m3(c.data_ptr(), s.data_ptr(), c.stride(0) if rows > 1 else max(c.stride(0), (c.shape[1] + 15) // 16 * 16),
-                       s.stride(0) if rows > 1 else max(s.stride(0), s.shape[1]))
+        return wf_e4m3(self.codes.data_ptr(), self.scales.data_ptr(), self.codes.stride(0) if rows > 1 else (k + 15) // 16 * 16,
+                       self.scales.stride(0) // 4 if k > 512 else max(rows, 1))
 
 
 class Decoder:
@@ -1003,8 +1007,8 @@ class Decoder:
         if out is None:
             ld = (k + 15) // 16 * 16
             codes = self._empty(x, (rows, ld), _E4M3, stream)
-            out = ScaledCodes(codes if ld == k else codes[:, :k], self._empty(x, (rows, (k + 511) // 512 * 4), _U8, stream))
-        elif out.shape != x.shape or out.codes.device != device:
+            out = ScaledCodes(codes if ld == k else codes[:, :k], self._empty(x, ((k + 511) // 512, rows, 4), _U8, stream))
+        elif out.shape != tuple(x.shape) or out.device != device:
             _refuse("out must have the shape and the device of x")
         self._call(self.lib.wf_quantise_e4m3, device, stream, x.data_ptr(), WF_BF16 if x.dtype is _BF16 else WF_F32,
                    x.stride(0) if rows > 1 else max(x.stride(0), k), rows, k, out._c("out"))
@@ -1014,8 +1018,8 @@ class Decoder:
                      stream=None) -> torch.Tensor:
         """act(a w^T + bias): a [m, k], w [n, k], bias float32 [n]; ``gelu``: the activation.  Returns [m, n] in ``out_dtype`` ("bf16" or
         "f32", default: the decoder's), or writes to ``out`` (row stride free)."""
-        (m, k), (n, kw), device = a.shape, w.shape, a.codes.device
-        if k != kw or w.codes.device != device:
+        (m, k), (n, kw), device = a.shape, w.shape, a.device
+        if k != kw or w.device != device:
             _refuse(f"a has {k} channels and w {kw}, or they are on different devices")
         if out is None:
             if out_dtype not in (None, "bf16", "f32"):

@@ -521,12 +521,12 @@ wf_status wf_draft_commit(wf_decoder* d, int n_seq, const int* start, const int*
 }
 
 namespace {
-wf_status check_codes(wf_decoder* d, const char* what, const wf_e4m3* x, int k) {
+wf_status check_codes(wf_decoder* d, const char* what, const wf_e4m3* x, long rows, int k) {
   if (!x || !x->codes || !x->scales) return fail(d, WF_ERR_INVALID_ARG, "%s: NULL codes or scales", what);
-  if (!aligned16(x->codes) || x->ld % 16 || ((uintptr_t)x->scales & 3) || x->scale_ld % 4)
-    return fail(d, WF_ERR_INVALID_ARG, "%s: codes need 16-byte aligned rows, scales rows aligned to 4 bytes", what);
-  if (x->ld < k || x->scale_ld < (long)(k + 511) / 512 * 4)
-    return fail(d, WF_ERR_INVALID_ARG, "%s: a row of codes or scales is shorter than %d channels need", what, k);
+  if (!aligned16(x->codes) || x->ld % 16 || ((uintptr_t)x->scales & 3))
+    return fail(d, WF_ERR_INVALID_ARG, "%s: codes need 16-byte aligned rows, scales an alignment of 4 bytes", what);
+  if (x->ld < k || x->scale_ld < rows)
+    return fail(d, WF_ERR_INVALID_ARG, "%s: rows of codes are shorter than %d channels, or scales have no room for %ld rows", what, k, rows);
   return WF_OK;
 }
 }  // namespace
@@ -534,10 +534,10 @@ wf_status check_codes(wf_decoder* d, const char* what, const wf_e4m3* x, int k) 
 wf_status wf_quantise_e4m3(wf_decoder* d, const void* x, int x_dtype, long ldx, long rows, int k, const wf_e4m3* out, void* stream) {
   if (!d) return WF_ERR_INVALID_ARG;
   if (rows < 0 || k < 1) return fail(d, WF_ERR_INVALID_ARG, "wf_quantise_e4m3: negative rows or no channels");
-  if (rows > (1 << 27) || k > (1 << 24)) return fail(d, WF_ERR_CAPACITY, "wf_quantise_e4m3: more than 2^27 rows or 2^24 channels");
+  if (rows > (1 << 27) || k > (1 << 22)) return fail(d, WF_ERR_CAPACITY, "wf_quantise_e4m3: more than 2^27 rows or 2^22 channels");
   if ((x_dtype != WF_F32 && x_dtype != WF_BF16) || ldx < k) return fail(d, WF_ERR_INVALID_ARG, "wf_quantise_e4m3: unknown type, or rows shorter than k");
   if (rows == 0) return WF_OK;
-  const wf_status st = check_codes(d, "wf_quantise_e4m3", out, k);
+  const wf_status st = check_codes(d, "wf_quantise_e4m3", out, rows, k);
   if (st != WF_OK) return st;
   if (!x || (uintptr_t)x % (x_dtype == WF_BF16 ? 2 : 4)) return fail(d, WF_ERR_INVALID_ARG, "wf_quantise_e4m3: x is NULL or not aligned to its type");
   return cuda_result(d, "wf_quantise_e4m3", launch_quantise_e4m3(x, x_dtype, ldx, rows, k, out->codes, out->ld, out->scales, out->scale_ld, (cudaStream_t)stream));
@@ -547,11 +547,11 @@ wf_status wf_gemm_e4m3(wf_decoder* d, const wf_e4m3* a, const wf_e4m3* w, const 
                        int gelu, int* status, void* stream) {
   if (!d) return WF_ERR_INVALID_ARG;
   if (m < 0 || n < 0 || k < 1) return fail(d, WF_ERR_INVALID_ARG, "wf_gemm_e4m3: a negative size or no channels");
-  if (m > (1 << 27) || n > (1 << 27) || k > (1 << 24)) return fail(d, WF_ERR_CAPACITY, "wf_gemm_e4m3: more than 2^27 rows or columns, or 2^24 channels");
+  if (m > (1 << 27) || n > (1 << 27) || k > (1 << 22)) return fail(d, WF_ERR_CAPACITY, "wf_gemm_e4m3: more than 2^27 rows or columns, or 2^22 channels");
   if ((out_dtype != WF_F32 && out_dtype != WF_BF16) || ldc < n) return fail(d, WF_ERR_INVALID_ARG, "wf_gemm_e4m3: unknown output type, or rows shorter than n");
   if (m == 0 || n == 0) return WF_OK;
-  wf_status st = check_codes(d, "wf_gemm_e4m3 (a)", a, k);
-  if (st == WF_OK) st = check_codes(d, "wf_gemm_e4m3 (w)", w, k);
+  wf_status st = check_codes(d, "wf_gemm_e4m3 (a)", a, m, k);
+  if (st == WF_OK) st = check_codes(d, "wf_gemm_e4m3 (w)", w, n, k);
   if (st != WF_OK) return st;
   if (!out || (uintptr_t)out % (out_dtype == WF_BF16 ? 2 : 4) || (uintptr_t)bias % 4)
     return fail(d, WF_ERR_INVALID_ARG, "wf_gemm_e4m3: out is NULL, or out or bias not aligned to their type");
@@ -559,8 +559,8 @@ wf_status wf_gemm_e4m3(wf_decoder* d, const wf_e4m3* a, const wf_e4m3* w, const 
   st = sm_count(d, &sms);
   if (st != WF_OK) return st;
   E4m3GemmParams p{};
-  p.a = E4m3Operand{a->codes, a->scales, a->ld, a->scale_ld};
-  p.w = E4m3Operand{w->codes, w->scales, w->ld, w->scale_ld};
+  p.a = E4m3Operand{a->codes, (const uint32_t*)a->scales, a->ld, a->scale_ld};
+  p.w = E4m3Operand{w->codes, (const uint32_t*)w->scales, w->ld, w->scale_ld};
   p.m = (int)m;
   p.n = n;
   p.k = k;

@@ -195,8 +195,8 @@ cudaError_t launch_draft_lengths(const CommitPlan& p, cudaStream_t s);
 constexpr int kScaleBlock = 128;  // channels of a row that share a scale
 struct E4m3Operand {
   const void* codes;
-  const unsigned char* scales;
-  long ld, scale_ld;  // bytes between rows
+  const uint32_t* scales;  // words of four blocks' bytes: [ceil(k / 512)][scale_ld], a word for each row
+  long ld, scale_ld;       // bytes between rows of codes; words between groups of blocks
 };
 cudaError_t launch_quantise_e4m3(const void* x, int dtype, long ldx, long rows, int k, void* codes, long ld_codes, unsigned char* scales,
                                  long ld_scales, cudaStream_t s);

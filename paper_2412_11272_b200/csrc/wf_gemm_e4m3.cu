@@ -22,48 +22,73 @@ using namespace ptx;
 constexpr int kQuantThreads = 256;
 constexpr int kQuantItems = 4;  // blocks that a group of lanes has in flight
 
-__device__ __forceinline__ void load8(const float* x, float (&v)[8]) {
-  const float4 a = __ldg(reinterpret_cast<const float4*>(x)), b = __ldg(reinterpret_cast<const float4*>(x) + 1);
-  v[0] = a.x, v[1] = a.y, v[2] = a.z, v[3] = a.w, v[4] = b.x, v[5] = b.y, v[6] = b.z, v[7] = b.w;
+// What eight elements are before they are needed as numbers.
+__device__ __forceinline__ void load_raw(const float* x, uint4 (&u)[2]) {
+  u[0] = __ldg(reinterpret_cast<const uint4*>(x));
+  u[1] = __ldg(reinterpret_cast<const uint4*>(x) + 1);
 }
-__device__ __forceinline__ void load8(const __nv_bfloat16* x, float (&v)[8]) {
-  const uint4 u = __ldg(reinterpret_cast<const uint4*>(x));
-  const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+__device__ __forceinline__ void load_raw(const __nv_bfloat16* x, uint4 (&u)[1]) { u[0] = __ldg(reinterpret_cast<const uint4*>(x)); }
+__device__ __forceinline__ void eight(const uint4 (&u)[2], float (&v)[8]) {
+  const uint32_t w[8] = {u[0].x, u[0].y, u[0].z, u[0].w, u[1].x, u[1].y, u[1].z, u[1].w};
+#pragma unroll
+  for (int i = 0; i < 8; ++i) v[i] = __uint_as_float(w[i]);
+}
+__device__ __forceinline__ void eight(const uint4 (&u)[1], float (&v)[8]) {
+  const uint32_t w[4] = {u[0].x, u[0].y, u[0].z, u[0].w};
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     v[2 * i] = __uint_as_float(w[i] << 16);
     v[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
   }
 }
-__device__ __forceinline__ float load1(const float* x) { return __ldg(x); }
-__device__ __forceinline__ float load1(const __nv_bfloat16* x) { return __bfloat162float(*x); }
+__device__ __forceinline__ uint32_t bits_of(const float* x) { return __ldg(reinterpret_cast<const uint32_t*>(x)); }
+__device__ __forceinline__ uint32_t bits_of(const __nv_bfloat16* x) { return __ldg(reinterpret_cast<const unsigned short*>(x)); }
 
+// The blocks of `rows_each` rows are counted through: block i of them is block i % blocks of row i / blocks (`magic`: 2^32 / blocks rounded up; exact as i * blocks < 2^32).
 template <typename T, bool kAligned>
-__global__ void __launch_bounds__(kQuantThreads) quantise_e4m3_kernel(const T* __restrict__ x, long ldx, long items, int k, int blocks,
-                                                                     unsigned char* __restrict__ codes, long ld_codes,
-                                                                     unsigned char* __restrict__ scales, long ld_scales) {
+__global__ void __launch_bounds__(kQuantThreads) quantise_e4m3_kernel(const T* __restrict__ x, long ldx, long rows, int k, int blocks,
+                                                                     uint32_t magic, int rows_each, unsigned char* __restrict__ codes,
+                                                                     long ld_codes, unsigned char* __restrict__ scales, long ld_scales) {
+  constexpr int kWords = sizeof(T) == 2 ? 1 : 2;
   griddep_launch_dependents();
   const int lane16 = threadIdx.x & 15;
-  const long group = ((long)blockIdx.x * kQuantThreads + threadIdx.x) >> 4, groups = ((long)gridDim.x * kQuantThreads) >> 4;
-  float v[kQuantItems][8];
+  const long row0 = (long)blockIdx.y * rows_each;
+  const uint32_t items = (uint32_t)min((long)rows_each, rows - row0) * (uint32_t)blocks;
+  const uint32_t first = (uint32_t)blockIdx.x * (kQuantThreads / 16 * kQuantItems) + (threadIdx.x >> 4);
+  x += row0 * ldx;
+  codes += row0 * ld_codes;
+  scales += row0 * 4;
+  uint4 raw[kQuantItems][kWords];
 #pragma unroll
   for (int u = 0; u < kQuantItems; ++u) {
-    const long item = group + u * groups, row = item / blocks;
+    const uint32_t item = first + u * (kQuantThreads / 16), row = __umulhi(item, magic) + (blocks == 1 ? item : 0u);
     const int c = (int)(item - row * blocks) * kScaleBlock + lane16 * 8;
+    const T* from = x + (long)row * ldx + c;
     if (item < items && kAligned && c + 8 <= k) {
-      load8(x + row * ldx + c, v[u]);
+      load_raw(from, raw[u]);
     } else {
+      uint32_t w[4 * kWords];
 #pragma unroll
-      for (int e = 0; e < 8; ++e) v[u][e] = item < items && c + e < k ? load1(x + row * ldx + c + e) : 0.f;
+      for (int i = 0; i < 4 * kWords; ++i) {
+        constexpr int per = 4 / (int)sizeof(T);
+        w[i] = 0;
+#pragma unroll
+        for (int e = 0; e < per; ++e)
+          if (item < items && c + i * per + e < k) w[i] |= bits_of(from + i * per + e) << (16 * e);
+      }
+#pragma unroll
+      for (int i = 0; i < kWords; ++i) raw[u][i] = make_uint4(w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3]);
     }
   }
 #pragma unroll
   for (int u = 0; u < kQuantItems; ++u) {
-    const long item = group + u * groups, row = item / blocks;
+    const uint32_t item = first + u * (kQuantThreads / 16), row = __umulhi(item, magic) + (blocks == 1 ? item : 0u);
     const int b = (int)(item - row * blocks), c = b * kScaleBlock + lane16 * 8;
+    float v[8];
+    eight(raw[u], v);
     uint32_t top = 0;  // as bits: a NaN or an infinity is the largest
 #pragma unroll
-    for (int e = 0; e < 8; ++e) top = max(top, __float_as_uint(v[u][e]) & 0x7fffffffu);
+    for (int e = 0; e < 8; ++e) top = max(top, __float_as_uint(v[e]) & 0x7fffffffu);
 #pragma unroll
     for (int o = 8; o > 0; o /= 2) top = max(top, __shfl_xor_sync(0xffffffffu, top, o));
     if (item >= items) continue;
@@ -77,35 +102,61 @@ __global__ void __launch_bounds__(kQuantThreads) quantise_e4m3_kernel(const T* _
       uint32_t two[2];
 #pragma unroll
       for (int j = 0; j < 2; ++j)
-        two[j] = __nv_cvt_float2_to_fp8x2(make_float2(v[u][4 * h + 2 * j] * inv, v[u][4 * h + 2 * j + 1] * inv), __NV_SATFINITE, __NV_E4M3);
+        two[j] = __nv_cvt_float2_to_fp8x2(make_float2(v[4 * h + 2 * j] * inv, v[4 * h + 2 * j + 1] * inv), __NV_SATFINITE, __NV_E4M3);
       word[h] = scale == 255 ? 0u : two[0] | (two[1] << 16);
     }
-    unsigned char* to = codes + row * ld_codes + c;
+    unsigned char* to = codes + (long)row * ld_codes + c;
     if (c + 8 <= k) {
       *reinterpret_cast<uint2*>(to) = make_uint2(word[0], word[1]);
     } else {
       for (int i = 0; c + i < k && i < 8; ++i) to[i] = (unsigned char)(word[i >> 2] >> (8 * (i & 3)));
     }
-    if (lane16 == 0) scales[row * ld_scales + b] = (unsigned char)scale;
-    // the row's scales end with the four of a word
-    if (b == blocks - 1 && lane16 > 0 && lane16 <= 3 - ((blocks - 1) & 3)) scales[row * ld_scales + b + lane16] = 127;
+    unsigned char* mark = scales + ((b >> 2) * ld_scales + (long)row) * 4 + (b & 3);
+    if (lane16 == 0) *mark = (unsigned char)scale;
+    // a row's last word has all its bytes
+    if (b == blocks - 1 && lane16 > 0 && lane16 <= 3 - (b & 3)) mark[lane16] = 127;
   }
 }
 
 // ---------------------------------------------------------------------------------------------
-constexpr int kTileN = 128;  // rows of W in a tile: the accumulator's lanes
+constexpr int kTileN = 128;  // rows of W that a block has in a tile: the accumulator's lanes
 constexpr int kBlockBytes = 128;
-constexpr int kGemmThreads = 320;
+constexpr int kEpiWarps = 16, kScaleWarp = kEpiWarps, kCopyWarp = kScaleWarp + 4, kMathWarp = kCopyWarp + 1;
+constexpr int kEpiTurns = kEpiWarps / 4;
+constexpr int kGemmThreads = (kMathWarp + 1) * 32;
+constexpr int kStoreRows = 16;                         // rows of C, all 128 columns, that four warps turn round in shared memory at a time
+constexpr int kStoreBytes = kStoreRows * kTileN * 2;   // two such pieces for each four warps
 constexpr int kScaleCols = 512 - 24;  // tensor memory: two buffers of 4 columns of W's scales and 8 of A's
 
-__device__ __forceinline__ void umma_e4m3(uint32_t d_tmem, uint64_t adesc, uint64_t bdesc, uint32_t idesc, uint32_t sa, uint32_t sb,
-                                          uint32_t accumulate) {
+// Whether a barrier's phase is over, without waiting for it.
+__device__ __forceinline__ bool mbar_test(uint32_t bar, uint32_t parity) {
+  uint32_t ok;
   asm volatile(
       "{\n\t.reg .pred p;\n\t"
-      "setp.ne.b32 p, %6, 0;\n\t"
-      "tcgen05.mma.cta_group::1.kind::mxf8f6f4.block_scale.scale_vec::1X [%0], %1, %2, %3, [%4], [%5], p;\n\t}"
-      ::"r"(d_tmem), "l"(adesc), "l"(bdesc), "r"(idesc), "r"(sa), "r"(sb), "r"(accumulate)
+      "mbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
+      "selp.u32 %0, 1, 0, p;\n\t}"
+      : "=r"(ok)
+      : "r"(bar), "r"(parity)
       : "memory");
+  return ok != 0;
+}
+template <int CG>
+__device__ __forceinline__ void umma_e4m3(uint32_t d_tmem, uint64_t adesc, uint64_t bdesc, uint32_t idesc, uint32_t sa, uint32_t sb,
+                                          uint32_t accumulate) {
+  if constexpr (CG == 1)
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "setp.ne.b32 p, %6, 0;\n\t"
+        "tcgen05.mma.cta_group::1.kind::mxf8f6f4.block_scale.scale_vec::1X [%0], %1, %2, %3, [%4], [%5], p;\n\t}"
+        ::"r"(d_tmem), "l"(adesc), "l"(bdesc), "r"(idesc), "r"(sa), "r"(sb), "r"(accumulate)
+        : "memory");
+  else
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "setp.ne.b32 p, %6, 0;\n\t"
+        "tcgen05.mma.cta_group::2.kind::mxf8f6f4.block_scale.scale_vec::1X [%0], %1, %2, %3, [%4], [%5], p;\n\t}"
+        ::"r"(d_tmem), "l"(adesc), "l"(bdesc), "r"(idesc), "r"(sa), "r"(sb), "r"(accumulate)
+        : "memory");
 }
 // Instruction descriptor: e4m3 operands, both K-major, scales 2^(b - 127); `number` picks the byte of a scale column.
 __device__ __forceinline__ constexpr uint32_t e4m3_idesc(int M, int N, int number) {
@@ -114,71 +165,143 @@ __device__ __forceinline__ constexpr uint32_t e4m3_idesc(int M, int N, int numbe
 __device__ __forceinline__ void tmem_st_x4(uint32_t taddr, const uint32_t* r) {
   asm volatile("tcgen05.st.sync.aligned.32x32b.x4.b32 [%0], {%1, %2, %3, %4};" ::"r"(taddr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]) : "memory");
 }
+__device__ __forceinline__ void tmem_ld_x8(uint32_t taddr, uint32_t (&r)[8]) {
+  asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7])
+               : "r"(taddr)
+               : "memory");
+}
+// 16 lanes x 16 columns as matrix fragments: thread t has columns 2 (t % 4), + 1 of lane t / 4 (r[0], r[1]) and of lane
+// t / 4 + 8 (r[2], r[3]), and the same eight columns further on (r[4] .. r[7]).
+__device__ __forceinline__ void tmem_ld_fragments(uint32_t taddr, uint32_t* r) {
+  asm volatile("tcgen05.ld.sync.aligned.16x256b.x2.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7])
+               : "r"(taddr)
+               : "memory");
+}
+// Four 8 x 8 matrices of 16-bit elements, transposed on their way: thread t names the 16 bytes of row t % 8 of matrix t / 8.
+__device__ __forceinline__ void stmatrix_trans(uint32_t addr, uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
+  asm volatile("stmatrix.sync.aligned.m8n8.x4.trans.shared.b16 [%0], {%1, %2, %3, %4};" ::"r"(addr), "r"(a), "r"(b), "r"(c), "r"(d) : "memory");
+}
 __device__ __forceinline__ void tmem_st_x8(uint32_t taddr, const uint32_t* r) {
   asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"r"(taddr), "r"(r[0]), "r"(r[1]), "r"(r[2]),
                "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7])
                : "memory");
 }
 
-template <int BN>
+// Shared memory of a block.  BN: rows of A in a tile; CG: blocks that share the tile (each has 128 rows of W and BN / CG of A);
+// kSplit: room for the partial sums of a split, 128 x BN float32, in place of the pieces of C that are turned round.
+template <int BN, int CG, bool kSplit>
 struct E4m3Plan {
-  static constexpr int kWBytes = kTileN * kBlockBytes, kABytes = BN * kBlockBytes;
+  static constexpr int kWBytes = kTileN * kBlockBytes, kABytes = BN / CG * kBlockBytes;
   static constexpr int kStageBytes = kWBytes + kABytes;
-  static constexpr int kFit = 216 * 1024 / kStageBytes;
+  static constexpr int kSideBytes = kSplit ? kTileN * BN * 4 : kEpiTurns * 2 * kStoreBytes;
+  static constexpr int kFit = (225 * 1024 - kSideBytes) / kStageBytes;
   static constexpr int kStages = kFit > 12 ? 12 : kFit;
   static constexpr int kBars = 2 * kStages + 9;  // full, empty, scales full / empty, accumulator full / empty, drain
-  static constexpr int kBarOffset = kStages * kStageBytes;
+  static constexpr int kSideOffset = kStages * kStageBytes;
+  static constexpr int kBarOffset = kSideOffset + kSideBytes;
   static constexpr int kBytes = kBarOffset + 8 * kBars + 16 + 1024;
-  static_assert(2 * BN <= kScaleCols && kStageBytes % 1024 == 0 && kBytes <= 227 * 1024, "tile plan");
+  static_assert(2 * BN <= kScaleCols && kABytes % 1024 == 0 && kStages >= 4 && kBytes <= 227 * 1024, "tile plan");
 };
 
 // The four bytes of scales of `row` that belong to blocks 4 g .. 4 g + 3; rows that do not exist count as 1.
 __device__ __forceinline__ uint32_t scale_word(const E4m3Operand& x, long row, long rows, int g) {
-  return row < rows ? __ldg(reinterpret_cast<const uint32_t*>(x.scales + row * x.scale_ld) + g) : 0x7f7f7f7fu;
+  return row < rows ? __ldg(x.scales + g * x.scale_ld + row) : 0x7f7f7f7fu;
 }
 
-// One accumulator column block: `v` are 16 rows of C (from row `r0`) at column `col` (one per lane).
-__device__ __forceinline__ void store16(const E4m3GemmParams& p, int r0, int col, const float (&v)[16]) {
-  const int lane = threadIdx.x & 31;
-  if (p.out_dtype == WF_F32) {
-    float* out = reinterpret_cast<float*>(p.out) + (long)r0 * p.ldc + col;
+// GELU for bfloat16 outputs, two values: x Phi(x) = max(x, 0) - |x| h, h = erfc(|x| / sqrt 2) / 2 = 2^q with q(|x|) a polynomial
+// of degree 5 fitted to log2 h over [0, 5.5] (minimax of the relative error: 1.6e-4 up to |x| = 4.2, 2.1e-3 at 5.5, behind which
+// h is held: |x| h < 3e-7).  A twelfth of half a step of bfloat16, in the tail as well, for six instructions a value;
+// erff takes some 30, which would bound the kernel (at 1280 channels a tile's products take 20 issue slots per value of C).
+__device__ __forceinline__ void gelu_pair(float& x0, float& x1) {
+  auto both = [](float c) { return pack_f32x2(c, c); };
+  const float n0 = fmaxf(-fabsf(x0), -5.5f), n1 = fmaxf(-fabsf(x1), -5.5f);
+  const uint64_t n = pack_f32x2(n0, n1);
+  uint64_t q = fma_f32x2(n, both(2.69073704e-04f), both(5.29495657e-03f));
+  q = fma_f32x2(n, q, both(4.63313932e-02f));
+  q = fma_f32x2(n, q, both(-4.66863768e-01f));
+  q = fma_f32x2(n, q, both(1.14782169f));
+  q = fma_f32x2(n, q, both(-1.00022509f));
+  float q0, q1, p0, p1;
+  unpack_f32x2(q, q0, q1);
+  asm("max.NaN.f32 %0, %1, %2;" : "=f"(p0) : "f"(x0), "f"(0.f));  // (a NaN stays one)
+  asm("max.NaN.f32 %0, %1, %2;" : "=f"(p1) : "f"(x1), "f"(0.f));
+  unpack_f32x2(fma_f32x2(n, pack_f32x2(ex2_approx(q0), ex2_approx(q1)), pack_f32x2(p0, p1)), x0, x1);
+}
+
+// Bias and activation of NC accumulator columns, and their store: v[i] belongs to row r0 + i of C and to this lane's column.
+template <int NC>
+__device__ __forceinline__ void finish(const E4m3GemmParams& p, int r0, int col, float bias, float (&v)[NC]) {
+  const bool wide = p.out_dtype == WF_F32;
+  const uint64_t b2 = pack_f32x2(bias, bias);
 #pragma unroll
-    for (int i = 0; i < 16; ++i)
-      if (r0 + i < p.m && col < p.n) out[(long)i * p.ldc] = v[i];
+  for (int i = 0; i < NC; i += 2) unpack_f32x2(add_f32x2(pack_f32x2(v[i], v[i + 1]), b2), v[i], v[i + 1]);
+  if (p.gelu) {
+#pragma unroll
+    for (int i = 0; i < NC; i += 2) {
+      if (wide) v[i] = gelu_erf(v[i]), v[i + 1] = gelu_erf(v[i + 1]);
+      else gelu_pair(v[i], v[i + 1]);
+    }
+  }
+  const bool whole = r0 + NC <= p.m;
+  if (wide) {
+    float* out = reinterpret_cast<float*>(p.out) + (long)r0 * p.ldc + col;
+    if (col < p.n) {
+#pragma unroll
+      for (int i = 0; i < NC; ++i)
+        if (whole || r0 + i < p.m) out[(long)i * p.ldc] = v[i];
+    }
     return;
   }
   __nv_bfloat16* out = reinterpret_cast<__nv_bfloat16*>(p.out);
   if (((p.ldc & 1) == 0) && ((uintptr_t)p.out & 3) == 0) {
     // two lanes swap halves of two rows, so that each writes four bytes of one of them
-    const int odd = lane & 1, even_col = col - odd;
+    const int odd = threadIdx.x & 1, even_col = col - odd;
+    const uint32_t pick = odd ? 0x3276u : 0x5410u;
+    __nv_bfloat16* to = out + (long)(r0 + odd) * p.ldc + even_col;
+    const bool both = even_col + 1 < p.n, one = even_col < p.n;
 #pragma unroll
-    for (int i = 0; i < 16; i += 2) {
-      const float other = __shfl_xor_sync(0xffffffffu, odd ? v[i] : v[i + 1], 1);
-      const __nv_bfloat162 two = __floats2bfloat162_rn(odd ? other : v[i], odd ? v[i + 1] : other);
-      const int r = r0 + i + odd;
-      if (r < p.m) {
-        __nv_bfloat16* to = out + (long)r * p.ldc + even_col;
-        if (even_col + 1 < p.n) *reinterpret_cast<__nv_bfloat162*>(to) = two;
-        else if (even_col < p.n) *to = two.x;
+    for (int i = 0; i < NC; i += 2) {
+      const __nv_bfloat162 mine = __floats2bfloat162_rn(v[i], v[i + 1]);
+      const uint32_t word = *reinterpret_cast<const uint32_t*>(&mine);
+      const uint32_t two = __byte_perm(word, __shfl_xor_sync(0xffffffffu, word, 1), pick);
+      if (whole || r0 + i + odd < p.m) {
+        if (both) *reinterpret_cast<uint32_t*>(to) = two;
+        else if (one) *to = __ushort_as_bfloat16((unsigned short)two);
       }
+      to += 2 * p.ldc;
     }
-  } else {
+  } else if (col < p.n) {
 #pragma unroll
-    for (int i = 0; i < 16; ++i)
-      if (r0 + i < p.m && col < p.n) out[(long)(r0 + i) * p.ldc + col] = __float2bfloat16_rn(v[i]);
+    for (int i = 0; i < NC; ++i)
+      if (whole || r0 + i < p.m) out[(long)(r0 + i) * p.ldc + col] = __float2bfloat16_rn(v[i]);
   }
 }
 
-// A tile is 128 rows of W by BN rows of A: W's rows are the lanes of the accumulator, so that a handful of rows of A costs a
-// handful of columns, and C's rows are written in runs of 32 columns per warp.
-//   warps 0..3  read the accumulator, apply bias and activation, store
-//   warps 4..7  bring the scales of 512 channels to tensor memory (each its quarter of the lanes, which hold copies)
-//   warp 8      one lane issues the TMA copies of the codes;   warp 9  one lane issues the products
-template <int BN>
+template <int NC>
+__device__ __forceinline__ void finish_nan(const E4m3GemmParams& p, int r0, int col) {
+  float v[NC];
+#pragma unroll
+  for (int i = 0; i < NC; ++i) v[i] = __uint_as_float(0x7fc00000u);
+  finish(p, r0, col, 0.f, v);
+}
+
+// A tile is 128 rows of W for each block by BN rows of A: W's rows are the lanes of the accumulator, so that a handful of rows
+// of A costs a handful of columns, and C's rows are written in runs of 32 columns per warp.
+//   warps 0..7   read the accumulator (a quarter of its lanes each, two warps in turn), apply bias and activation, store
+//   warps 8..11  bring the scales of 512 channels to tensor memory (each its quarter of the lanes, which hold copies)
+//   warp 12      one lane issues the TMA copies of the codes;   warp 13  one lane issues the products
+// CG = 2: a pair of blocks shares a tile of 256 rows of W by BN of A, each block stages its own 128 rows of W and half of A's.
+// The copies of both signal the first block's barriers, which alone issues the products; its commits reach both.
+// kSplit: a cluster of blocks shares a tile, each has a part of the channels; every block sums a part of the columns, in the
+// order of the blocks, from what the others leave in its shared memory.
+template <int BN, int CG, bool kSplit>
 __global__ void __launch_bounds__(kGemmThreads, 1) gemm_e4m3_kernel(const __grid_constant__ CUtensorMap tmap_w,
                                                                    const __grid_constant__ CUtensorMap tmap_a,
-                                                                   const __grid_constant__ E4m3GemmParams p) {
-  using Plan = E4m3Plan<BN>;
+                                                                   const __grid_constant__ E4m3GemmParams p, int split, int wide_rows) {
+  static_assert(CG == 1 || !kSplit, "pairs do not split");
+  using Plan = E4m3Plan<BN, CG, kSplit>;
   constexpr int kStages = Plan::kStages;
   extern __shared__ uint8_t smem_raw[];
   const uint32_t smem_base = (smem_u32(smem_raw) + 1023u) & ~1023u;
@@ -194,6 +317,7 @@ __global__ void __launch_bounds__(kGemmThreads, 1) gemm_e4m3_kernel(const __grid
   volatile uint32_t* tmem_slot = reinterpret_cast<volatile uint32_t*>(smem_gen + Plan::kBarOffset + 8 * Plan::kBars);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(smem_gen + Plan::kBarOffset + 8 * Plan::kBars + 8);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int rank = CG == 2 || kSplit ? (int)cluster_ctarank() : 0;
 
   if (threadIdx.x == 0) {
     for (int s = 0; s < kStages; ++s) {
@@ -201,168 +325,363 @@ __global__ void __launch_bounds__(kGemmThreads, 1) gemm_e4m3_kernel(const __grid
       mbar_init(empty_bar(s), 1);
     }
     for (int b = 0; b < 2; ++b) {
-      mbar_init(sfull_bar(b), 4);
+      mbar_init(sfull_bar(b), 4 * CG);
       mbar_init(sempty_bar(b), 1);
       mbar_init(tfull_bar(b), 1);
-      mbar_init(tempty_bar(b), 4);
+      mbar_init(tempty_bar(b), kEpiWarps * CG);
     }
     mbar_init(drain_bar, 1);
     *abort_flag = 0;
     fence_mbar_init();
   }
-  if (warp == 9) {
-    tmem_alloc(smem_u32(const_cast<uint32_t*>(tmem_slot)), 512);
-    tmem_relinquish();
+  if (warp == kMathWarp) {
+    if constexpr (CG == 2) {
+      tmem_alloc_pair(smem_u32(const_cast<uint32_t*>(tmem_slot)), 512);
+      tmem_relinquish_pair();
+    } else {
+      tmem_alloc(smem_u32(const_cast<uint32_t*>(tmem_slot)), 512);
+      tmem_relinquish();
+    }
   }
   tc_fence_before();
-  __syncthreads();
+  if constexpr (CG == 2 || kSplit) cluster_sync_all();  // every block's barriers and memory are there before another one uses them
+  else __syncthreads();
   tc_fence_after();
   const uint32_t tmem = *tmem_slot;
   griddep_wait();
   griddep_launch_dependents();
 
-  const int num_w = (p.n + kTileN - 1) / kTileN, num_a = (p.m + BN - 1) / BN, num_k = (p.k + kScaleBlock - 1) / kScaleBlock;
-  const long num_tiles = (long)num_w * num_a;
+  const int num_w = (p.n + CG * kTileN - 1) / (CG * kTileN), num_a = (p.m + BN - 1) / BN;
+  const int num_k = (p.k + kScaleBlock - 1) / kScaleBlock;
+  const int num_tiles = num_w * num_a;
+  const int share = CG == 2 ? 2 : kSplit ? split : 1;  // blocks of a tile
+  const int tile0 = (int)blockIdx.x / share, tile_step = (int)gridDim.x / share;
+  const int kb0 = kSplit ? (int)((long)rank * num_k / split) : 0, kb1 = kSplit ? (int)((long)(rank + 1) * num_k / split) : num_k;
   auto wait = [&](uint32_t bar, uint32_t parity) { return mbar_wait_limited(bar, parity, abort_flag, p.wait_limit); };
+  bool done = true;  // epilogue warps of a split: the accumulator is complete
 
-  if (warp == 8) {
+  if (warp == kCopyWarp) {
     if (lane == 0) {
       prefetch_tmap(&tmap_w);
       prefetch_tmap(&tmap_a);
       int stage = 0;
       uint32_t phase = 0, armed = 0, armed_parity = 0;
       bool ok = true;
-      for (long tile = blockIdx.x; ok && tile < num_tiles; tile += gridDim.x) {
-        const int n0 = (int)(tile % num_w) * kTileN, m0 = (int)(tile / num_w) * BN;
-        for (int kb = 0; kb < num_k; ++kb) {
+      for (int tile = tile0; ok && tile < num_tiles; tile += tile_step) {
+        const int n0 = (tile % num_w * CG + (CG == 2 ? rank : 0)) * kTileN;
+        const int m0 = tile / num_w * BN + (CG == 2 ? rank * (BN / 2) : 0);
+        for (int kb = kb0; kb < kb1; ++kb) {
           if (!wait(empty_bar(stage), phase ^ 1u)) { ok = false; break; }
           const uint32_t at = smem_base + stage * Plan::kStageBytes;
-          mbar_arrive_expect_tx(full_bar(stage), Plan::kStageBytes);
-          tma_load_2d(at, &tmap_w, kb * kBlockBytes, n0, full_bar(stage));
-          tma_load_2d(at + Plan::kWBytes, &tmap_a, kb * kBlockBytes, m0, full_bar(stage));
+          if constexpr (CG == 2) {
+            const uint32_t bar = map_to_cta(full_bar(stage), 0);
+            if (rank == 0) mbar_arrive_expect_tx(full_bar(stage), 2 * Plan::kStageBytes);
+            tma_load_2d_pair(at, &tmap_w, kb * kBlockBytes, n0, bar);
+            tma_load_2d_pair(at + Plan::kWBytes, &tmap_a, kb * kBlockBytes, m0, bar);
+          } else {
+            mbar_arrive_expect_tx(full_bar(stage), Plan::kStageBytes);
+            tma_load_2d(at, &tmap_w, kb * kBlockBytes, n0, full_bar(stage));
+            tma_load_2d(at + Plan::kWBytes, &tmap_a, kb * kBlockBytes, m0, full_bar(stage));
+          }
           armed |= 1u << stage;
           armed_parity = (armed_parity & ~(1u << stage)) | (phase << stage);
           if (++stage == kStages) { stage = 0; phase ^= 1u; }
         }
       }
-      if (!ok)  // no copy may land after the block has gone
+      // After giving up: no copy may land once the block has gone.  (The second block of a pair sees its copies only by their
+      // stages being released; what is still in flight has the time of that bounded wait.)
+      if (!ok)
         for (int s = 0; s < kStages; ++s)
-          if (armed >> s & 1u)
-            for (uint32_t it = 0; it < kWaitLimit && !mbar_try_wait(full_bar(s), armed_parity >> s & 1u); ++it) {}
+          if (armed >> s & 1u) {
+            const uint32_t bar = CG == 2 && rank == 1 ? empty_bar(s) : full_bar(s);
+            for (uint32_t it = 0; it < (CG == 2 ? 1u << 16 : kWaitLimit) && !mbar_try_wait(bar, armed_parity >> s & 1u); ++it) {}
+          }
     }
-  } else if (warp == 9) {
-    if (lane == 0) {
+  } else if (warp == kMathWarp) {
+    // The whole warp walks along (so that descriptors stay in uniform registers), one lane issues.
+    if (CG == 1 || rank == 0) {
+      const bool one = elect_one();
+      auto commit = [&](uint32_t bar) {
+        if (one) {
+          if constexpr (CG == 2) umma_commit_pair(bar, 3);
+          else umma_commit(bar);
+        }
+        __syncwarp();
+      };
+      auto ready = [&](uint32_t bar, uint32_t parity) { return __all_sync(0xffffffffu, wait(bar, parity)); };
+      const uint64_t desc = umma_desc_k_sw128(0);
+      const uint32_t first = (smem_base & 0x3ffff) >> 4;
       int stage = 0, acc = 0, buf = 0;
       uint32_t phase = 0, acc_phase = 0, buf_phase = 0;
-      bool ok = true;
-      for (long tile = blockIdx.x; ok && tile < num_tiles; tile += gridDim.x) {
-        if (!wait(tempty_bar(acc), acc_phase ^ 1u)) { ok = false; break; }
+      bool ok = true, peeked = false;
+      for (int tile = tile0; ok && tile < num_tiles; tile += tile_step) {
+        if (!ready(tempty_bar(acc), acc_phase ^ 1u)) { ok = false; break; }
         tc_fence_after();
-        for (int kb = 0; kb < num_k; ++kb) {
-          if ((kb & 3) == 0 && !wait(sfull_bar(buf), buf_phase)) { ok = false; break; }
-          if (!wait(full_bar(stage), phase)) { ok = false; break; }
+        for (int kb = kb0; kb < kb1; ++kb) {
+          if (((kb & 3) == 0 || kb == kb0) && !ready(sfull_bar(buf), buf_phase)) { ok = false; break; }
+          if (!peeked && !ready(full_bar(stage), phase)) { ok = false; break; }
           tc_fence_after();
-          const uint32_t at = smem_base + stage * Plan::kStageBytes;
-          const uint64_t wdesc = umma_desc_k_sw128(at), adesc = umma_desc_k_sw128(at + Plan::kWBytes);
-          const uint32_t idesc = e4m3_idesc(kTileN, BN, kb & 3), scales = tmem + kScaleCols + 12 * buf;
-#pragma unroll
-          for (int j = 0; j < 4; ++j)  // 32 channels: 32 bytes further inside the swizzled row
-            umma_e4m3(tmem + acc * BN, wdesc + 2 * j, adesc + 2 * j, idesc, scales, scales + 4, (kb | j) != 0 ? 1u : 0u);
-          umma_commit(empty_bar(stage));
+          const uint64_t wdesc = desc + (first + stage * (Plan::kStageBytes >> 4));
+          const uint64_t adesc = wdesc + (Plan::kWBytes >> 4);
+          const uint32_t idesc = e4m3_idesc(CG * kTileN, BN, kb & 3), scales = tmem + kScaleCols + 12 * buf, to = tmem + acc * BN;
+          const uint32_t empty = empty_bar(stage);
           if (++stage == kStages) { stage = 0; phase ^= 1u; }
-          if ((kb & 3) == 3 || kb == num_k - 1) {
-            umma_commit(sempty_bar(buf));
+          if (one) {
+#pragma unroll
+            for (int j = 0; j < 4; ++j)  // 32 channels: 32 bytes further inside the swizzled row
+              umma_e4m3<CG>(to, wdesc + 2 * j, adesc + 2 * j, idesc, scales, scales + 4, kb != kb0 || j != 0 ? 1u : 0u);
+          }
+          __syncwarp();
+          // The next stage is looked for while these products run: the queue of products is short, and waiting behind them
+          // would leave the tensor cores idle for the time of a look.
+          peeked = __all_sync(0xffffffffu, mbar_test(full_bar(stage), phase));
+          commit(empty);
+          if ((kb & 3) == 3 || kb == kb1 - 1) {
+            commit(sempty_bar(buf));
             if (++buf == 2) { buf = 0; buf_phase ^= 1u; }
           }
         }
         if (!ok) break;
-        umma_commit(tfull_bar(acc));
+        commit(tfull_bar(acc));
         if (++acc == 2) { acc = 0; acc_phase ^= 1u; }
       }
       if (!ok) {  // products in flight end before tensor memory is given back
-        umma_commit(drain_bar);
+        commit(drain_bar);
         for (uint32_t it = 0; it < kWaitLimit && !mbar_try_wait(drain_bar, 0); ++it) {}
       }
     }
-  } else if (warp >= 4) {
+  } else if (warp >= kScaleWarp) {
     const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
     int buf = 0;
     uint32_t buf_phase = 0;
     bool ok = true;
-    for (long tile = blockIdx.x; ok && tile < num_tiles; tile += gridDim.x) {
-      const long n0 = (tile % num_w) * kTileN, m0 = (tile / num_w) * BN;
-      for (int g = 0; 4 * g < num_k; ++g) {
-        uint32_t sw[4], sa[8];
+    // words are loaded two groups ahead: a load takes longer than the products of a group
+    struct Words {
+      uint32_t w[4], a[8];
+    };
+    int tile_next = tile0;
+    int g_next = kb0 >> 2;
+    auto load = [&](Words& x) {
+      if (tile_next >= num_tiles) return;
+      const int n0 = (tile_next % num_w * CG + (CG == 2 ? rank : 0)) * kTileN, m0 = tile_next / num_w * BN;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) sw[i] = scale_word(p.w, n0 + 32 * i + lane, p.n, g);
+      for (int i = 0; i < 4; ++i) x.w[i] = scale_word(p.w, n0 + 32 * i + lane, p.n, g_next);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) sa[i] = 32 * i < BN ? scale_word(p.a, m0 + 32 * i + lane, p.m, g) : 0x7f7f7f7fu;
-        ok = __all_sync(0xffffffffu, wait(sempty_bar(buf), buf_phase ^ 1u));
-        if (!ok) break;
-        tc_fence_after();
-        const uint32_t to = tmem + lanes + kScaleCols + 12 * buf;
-        tmem_st_x4(to, sw);
-        if (BN <= 128) tmem_st_x4(to + 4, sa);
-        else tmem_st_x8(to + 4, sa);
-        tmem_st_wait();
-        tc_fence_before();
-        __syncwarp();
-        if (lane == 0) mbar_arrive(sfull_bar(buf));
-        if (++buf == 2) { buf = 0; buf_phase ^= 1u; }
+      for (int i = 0; i < 8; ++i) x.a[i] = 32 * i < BN ? scale_word(p.a, m0 + 32 * i + lane, p.m, g_next) : 0x7f7f7f7fu;
+      if (4 * ++g_next >= kb1) {
+        g_next = kb0 >> 2;
+        tile_next += tile_step;
       }
+    };
+    auto pass = [&](const Words& x) {  // to tensor memory, behind the last product that used the buffer
+      ok = __all_sync(0xffffffffu, wait(sempty_bar(buf), buf_phase ^ 1u));
+      if (!ok) return;
+      tc_fence_after();
+      const uint32_t to = tmem + lanes + kScaleCols + 12 * buf;
+      tmem_st_x4(to, x.w);
+      if (BN <= 128) tmem_st_x4(to + 4, x.a);
+      else tmem_st_x8(to + 4, x.a);
+      tmem_st_wait();
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) {
+        if constexpr (CG == 2) mbar_arrive_cluster(map_to_cta(sfull_bar(buf), 0));
+        else mbar_arrive(sfull_bar(buf));
+      }
+      if (++buf == 2) { buf = 0; buf_phase ^= 1u; }
+    };
+    const int groups = tile0 < num_tiles ? ((num_tiles - tile0 + tile_step - 1) / tile_step) * (((kb1 + 3) >> 2) - (kb0 >> 2)) : 0;
+    Words even, odd;
+    load(even);
+    load(odd);
+    for (int i = 0; ok && i < groups; i += 2) {
+      pass(even);
+      load(even);
+      if (!ok || i + 1 >= groups) break;
+      pass(odd);
+      load(odd);
     }
-  } else {
-    int acc = 0;
+  } else if constexpr (!kSplit) {
+    const int quarter = warp & 3, turn = warp >> 2;
+    int acc = 0, pieces = 0;
     uint32_t acc_phase = 0;
     bool ok = true;
-    for (long tile = blockIdx.x; tile < num_tiles; tile += gridDim.x) {
-      const int n0 = (int)(tile % num_w) * kTileN, m0 = (int)(tile / num_w) * BN;
-      const int col = n0 + warp * 32 + lane;
+    for (int tile = tile0; tile < num_tiles; tile += tile_step) {
+      const int n0 = (tile % num_w * CG + (CG == 2 ? rank : 0)) * kTileN, m0 = tile / num_w * BN;
+      const int col = n0 + quarter * 32 + lane, stop = min(BN, p.m - m0);
       const float bias = p.bias && col < p.n ? __ldg(p.bias + col) : 0.f;
       ok = ok && __all_sync(0xffffffffu, wait(tfull_bar(acc), acc_phase));
-      if (ok) tc_fence_after();
-      else if (lane == 0) report(p.status, kGaveUp);  // what was not computed is NaN
-      const uint32_t from = tmem + ((uint32_t)(warp * 32) << 16) + acc * BN;
+      if (!ok) {  // what was not computed is NaN
+        if (lane == 0) report(p.status, kGaveUp);
+        for (int c = turn * 8; c < stop; c += 8 * kEpiTurns) finish_nan<8>(p, m0 + c, col);
+        continue;
+      }
+      tc_fence_after();
+      const uint32_t from = tmem + ((uint32_t)(quarter * 32) << 16) + acc * BN;
+      if (wide_rows) {
+        float b4[4];  // of this thread's lanes of the fragments
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const int at = n0 + quarter * 32 + 8 * i + (lane >> 2);
+          b4[i] = p.bias && at < p.n ? __ldg(p.bias + at) : 0.f;
+        }
+        // Pieces of 16 rows by 128 columns: in shared memory a row is two halves of 128 bytes, 16-byte chunks exclusive-or'd with
+        // the row against bank conflicts.  A thread names a row of a matrix to be stored, and copies a chunk of two rows out.
+        const int chunk_in = (quarter & 1) * 4 + (lane >> 3), row_out = quarter * 4 + (lane >> 4), chunk_out = lane & 15;
+        const uint32_t area = smem_base + Plan::kSideOffset + (uint32_t)(turn * 2 * kStoreBytes);
+        const uint32_t in = area + (quarter >> 1) * (kStoreBytes / 2) + (lane & 7) * 128 + ((chunk_in ^ (lane & 7)) << 4);
+        const uint32_t half_out = area + (chunk_out >> 3) * (kStoreBytes / 2);
+        const uint32_t out_a = half_out + row_out * 128 + (((chunk_out & 7) ^ (row_out & 7)) << 4);
+        const uint32_t out_b = half_out + (row_out + 2) * 128 + (((chunk_out & 7) ^ ((row_out + 2) & 7)) << 4);
+        const int at = n0 + chunk_out * 8, columns = min(8, p.n - at);  // of this thread's chunk
+        __nv_bfloat16* to = reinterpret_cast<__nv_bfloat16*>(p.out) + (long)(m0 + turn * 16 + row_out) * p.ldc + at;
+        const long two_rows = 2 * p.ldc, next_piece = 16L * kEpiTurns * p.ldc - two_rows;
+        auto copy_out = [&](uint32_t from_smem, bool exists) {
+          uint4 u;
+          ld_shared_v4(from_smem, u.x, u.y, u.z, u.w);
+          if (exists && columns == 8) *reinterpret_cast<uint4*>(to) = u;
+        };
+        auto copy_ragged = [&](uint32_t from_smem, bool exists) {  // the last columns of C, one by one
+          if (!exists || columns >= 8) return;
+          for (int e = 0; e < columns; ++e) {
+            unsigned short h;
+            asm volatile("ld.shared.u16 %0, [%1];" : "=h"(h) : "r"(from_smem + 2 * e) : "memory");
+            to[e] = __ushort_as_bfloat16(h);
+          }
+        };
+        const bool ragged = n0 + kTileN > p.n;
+        auto fetch = [&](int c, uint32_t (&r)[16]) {
+          tmem_ld_fragments(from + c, r);
+          tmem_ld_fragments(from + (16u << 16) + c, r + 8);
+        };
+        auto piece = [&](int c, const uint32_t (&r)[16]) {
+          float v[16];
+          uint32_t word[8];  // [lanes 0 .. 7, 8 .. 15, 16 .. 23, 24 .. 31] of eight columns, then of the next eight
+#pragma unroll
+          for (int i = 0; i < 8; ++i) {
+            const float b = b4[(i & 1) | (i >> 2) << 1];
+            unpack_f32x2(add_f32x2(pack_f32x2(__uint_as_float(r[2 * i]), __uint_as_float(r[2 * i + 1])), pack_f32x2(b, b)), v[2 * i], v[2 * i + 1]);
+          }
+          if (p.gelu) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) gelu_pair(v[2 * i], v[2 * i + 1]);
+          }
+#pragma unroll
+          for (int i = 0; i < 8; ++i) {
+            const __nv_bfloat162 two = __floats2bfloat162_rn(v[2 * i], v[2 * i + 1]);
+            word[((i >> 1) & 1) * 4 + ((i & 1) | (i >> 2) << 1)] = *reinterpret_cast<const uint32_t*>(&two);
+          }
+          const uint32_t side = (uint32_t)(pieces++ & 1) * kStoreBytes;
+          stmatrix_trans(in + side, word[0], word[1], word[2], word[3]);
+          stmatrix_trans(in + side + 8 * 128, word[4], word[5], word[6], word[7]);
+          asm volatile("bar.sync %0, 128;" ::"r"(1 + turn) : "memory");  // (the other piece has been read by then)
+          const bool exists_a = c + row_out < stop, exists_b = c + row_out + 2 < stop;
+          copy_out(out_a + side, exists_a);
+          if (ragged) copy_ragged(out_a + side, exists_a);
+          to += two_rows;
+          copy_out(out_b + side, exists_b);
+          if (ragged) copy_ragged(out_b + side, exists_b);
+          to += next_piece;
+        };
+        uint32_t even[16], odd[16];
+        int c = turn * 16;
+        constexpr int kStep = 16 * kEpiTurns;
+        if (c < stop) fetch(c, even);
 #pragma unroll 1
-      for (int c = 0; c < BN && m0 + c < p.m; c += 16) {
-        float v[16];
-        if (ok) {
-          uint32_t r[16];
-          tmem_ld_32x16(from + c, r);
+        while (c < stop) {
+          tmem_ld_wait();
+          if (c + kStep < stop) fetch(c + kStep, odd);
+          piece(c, even);
+          c += kStep;
+          if (c >= stop) break;
+          tmem_ld_wait();
+          if (c + kStep < stop) fetch(c + kStep, even);
+          piece(c, odd);
+          c += kStep;
+        }
+      } else {
+        uint32_t next[8];
+        if (turn * 8 < stop) tmem_ld_x8(from + turn * 8, next);
+#pragma unroll 1
+        for (int c = turn * 8; c < stop; c += 8 * kEpiTurns) {
+          float v[8];
           tmem_ld_wait();
 #pragma unroll
-          for (int i = 0; i < 16; ++i) {
-            v[i] = __uint_as_float(r[i]) + bias;
-            if (p.gelu) v[i] = gelu_erf(v[i]);
-          }
-        } else {
-#pragma unroll
-          for (int i = 0; i < 16; ++i) v[i] = __uint_as_float(0x7fc00000u);
+          for (int i = 0; i < 8; ++i) v[i] = __uint_as_float(next[i]);
+          if (c + 8 * kEpiTurns < stop) tmem_ld_x8(from + c + 8 * kEpiTurns, next);
+          finish(p, m0 + c, col, bias, v);
         }
-        store16(p, m0 + c, col, v);
       }
-      if (ok) {
-        tc_fence_before();
-        __syncwarp();
-        if (lane == 0) mbar_arrive(tempty_bar(acc));
-        if (++acc == 2) { acc = 0; acc_phase ^= 1u; }
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) {
+        if constexpr (CG == 2) mbar_arrive_cluster(map_to_cta(tempty_bar(acc), 0));
+        else mbar_arrive(tempty_bar(acc));
+      }
+      if (++acc == 2) { acc = 0; acc_phase ^= 1u; }
+    }
+  } else {
+    // ---- a split: this block's sums of every other block's columns go there (one tile per cluster).  Partial sums of block r
+    // lie at [r][column / 4][row][4] of the receiving block.
+    const int quarter = warp & 3, turn = warp >> 2, row = quarter * 32 + lane, mine = BN / split;
+    done = __all_sync(0xffffffffu, wait(tfull_bar(0), 0));
+    tc_fence_after();
+    const uint32_t from = tmem + ((uint32_t)(quarter * 32) << 16);
+#pragma unroll 1
+    for (int c = turn * 8; c < BN; c += 8 * kEpiTurns) {
+      uint32_t r[8];
+      if (done) {
+        tmem_ld_x8(from + c, r);
+        tmem_ld_wait();
+      } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) r[i] = 0x7fc00000u;
+      }
+#pragma unroll
+      for (int q = 0; q < 2; ++q) {
+        const int column = c + 4 * q, owner = column / mine, within = (rank * mine + column - owner * mine) / 4;
+        st_cluster_v4(map_to_cta(smem_base + Plan::kSideOffset + (uint32_t)(within * kTileN + row) * 16u, owner), r[4 * q], r[4 * q + 1],
+                      r[4 * q + 2], r[4 * q + 3]);
       }
     }
+    if (!done && lane == 0) report(p.status, kGaveUp);
   }
 
   tc_fence_before();
-  __syncthreads();
-  if (warp == 9) {
+  __syncwarp();
+  if constexpr (CG == 2 || kSplit) cluster_sync_all();  // partial sums are there; nobody leaves while another one may still use its memory
+  else __syncthreads();
+  if (warp == kMathWarp) {
     tc_fence_after();
-    tmem_dealloc(tmem, 512);
+    if constexpr (CG == 2) tmem_dealloc_pair(tmem, 512);
+    else tmem_dealloc(tmem, 512);
+  }
+  if constexpr (kSplit) {
+    if (warp < kEpiWarps) {
+      const int quarter = warp & 3, turn = warp >> 2, row = quarter * 32 + lane, mine = BN / split;
+      const int n0 = tile0 % num_w * kTileN, m0 = tile0 / num_w * BN + rank * mine;
+      const int col = n0 + row;
+      const float bias = p.bias && col < p.n ? __ldg(p.bias + col) : 0.f;
+      for (int c = turn * 4; c < mine && m0 + c < p.m; c += 4 * kEpiTurns) {
+        float v[4] = {0.f, 0.f, 0.f, 0.f};
+        for (int r = 0; r < split; ++r) {
+          uint32_t q[4];
+          ld_shared_v4(smem_base + Plan::kSideOffset + (uint32_t)((r * mine + c) / 4 * kTileN + row) * 16u, q[0], q[1], q[2], q[3]);
+#pragma unroll
+          for (int i = 0; i < 4; ++i) v[i] += __uint_as_float(q[i]);
+        }
+        finish(p, m0 + c, col, bias, v);
+      }
+    }
   }
 }
 
 typedef CUresult (*EncodeTiled)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*, const cuuint32_t*,
                                 const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
 
-// Codes [rows, k] as tiles of 128 channels by `box_rows` rows; channels and rows that do not exist read as zeros.
-bool codes_map(CUtensorMap* m, const E4m3Operand& x, long rows, int k, int box_rows) {
+// A matrix [rows, cols] in device memory, rows `ld` bytes apart, as boxes; what lies outside reads as zeros and is not written.
+bool matrix_map(CUtensorMap* m, CUtensorMapDataType type, const void* base, long cols, long rows, long ld, int box_cols, int box_rows,
+                CUtensorMapSwizzle swizzle) {
   static std::atomic<void*> encode{nullptr};  // the driver's entry point, the same for every caller
   void* fn = encode.load(std::memory_order_relaxed);
   if (fn == nullptr) {
@@ -370,35 +689,53 @@ bool codes_map(CUtensorMap* m, const E4m3Operand& x, long rows, int k, int box_r
     if (!tma_api_init(&api)) return false;
     encode.store(fn = api.encode_tiled, std::memory_order_relaxed);
   }
-  const cuuint64_t dims[2] = {(cuuint64_t)k, (cuuint64_t)rows}, strides[1] = {(cuuint64_t)x.ld};
-  const cuuint32_t box[2] = {(cuuint32_t)kBlockBytes, (cuuint32_t)box_rows}, steps[2] = {1, 1};
-  return reinterpret_cast<EncodeTiled>(fn)(m, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<void*>(x.codes), dims, strides, box, steps,
-                                           CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
-                                           CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+  const cuuint64_t dims[2] = {(cuuint64_t)cols, (cuuint64_t)rows}, strides[1] = {(cuuint64_t)ld};
+  const cuuint32_t box[2] = {(cuuint32_t)box_cols, (cuuint32_t)box_rows}, steps[2] = {1, 1};
+  return reinterpret_cast<EncodeTiled>(fn)(m, type, 2, const_cast<void*>(base), dims, strides, box, steps, CU_TENSOR_MAP_INTERLEAVE_NONE, swizzle,
+                                           CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+bool codes_map(CUtensorMap* m, const E4m3Operand& x, long rows, int k, int box_rows) {
+  return matrix_map(m, CU_TENSOR_MAP_DATA_TYPE_UINT8, x.codes, k, rows, x.ld, kBlockBytes, box_rows, CU_TENSOR_MAP_SWIZZLE_128B);
+}
+
+template <int BN, int CG, bool kSplit>
+cudaError_t launch_tiles(const E4m3GemmParams& p, int split, int num_sms, cudaStream_t s) {
+  using Plan = E4m3Plan<BN, CG, kSplit>;
+  CUtensorMap tw, ta;
+  if (!codes_map(&tw, p.w, p.n, p.k, kTileN) || !codes_map(&ta, p.a, p.m, p.k, BN / CG)) return cudaErrorInvalidValue;
+  // bfloat16 rows of whole 16-byte chunks go through shared memory, others straight from registers
+  const bool wide = p.out_dtype == WF_BF16 && ((uintptr_t)p.out & 15) == 0 && p.ldc % 8 == 0;
+  const long tiles = (long)((p.n + CG * kTileN - 1) / (CG * kTileN)) * ((p.m + BN - 1) / BN);
+  if (tiles * 8 > 0x7fffffffL) return cudaErrorInvalidValue;  // (C would have 2^39 elements)
+  const int share = CG == 2 ? 2 : kSplit ? split : 1;
+  const long groups = kSplit ? tiles : tiles < num_sms / share ? tiles : num_sms / share;
+  auto kernel = gemm_e4m3_kernel<BN, CG, kSplit>;
+  const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, Plan::kBytes);
+  if (e != cudaSuccess) return e;
+  return launch_dependent(kernel, dim3((unsigned)(groups * share)), dim3(kGemmThreads), Plan::kBytes, s, share, true, tw, ta, p, split, (int)wide);
 }
 
 template <int BN>
-cudaError_t launch_tiles(const E4m3GemmParams& p, int num_sms, cudaStream_t s) {
-  CUtensorMap tw, ta;
-  if (!codes_map(&tw, p.w, p.n, p.k, kTileN) || !codes_map(&ta, p.a, p.m, p.k, BN)) return cudaErrorInvalidValue;
-  const long tiles = (long)((p.n + kTileN - 1) / kTileN) * ((p.m + BN - 1) / BN);
-  const cudaError_t e = cudaFuncSetAttribute(gemm_e4m3_kernel<BN>, cudaFuncAttributeMaxDynamicSharedMemorySize, E4m3Plan<BN>::kBytes);
-  if (e != cudaSuccess) return e;
-  return launch_dependent(gemm_e4m3_kernel<BN>, dim3((unsigned)(tiles < num_sms ? tiles : num_sms)), dim3(kGemmThreads), E4m3Plan<BN>::kBytes, s, 1,
-                          true, tw, ta, p);
+cudaError_t launch_single(const E4m3GemmParams& p, int split, int num_sms, cudaStream_t s) {
+  return split > 1 ? launch_tiles<BN, 1, true>(p, split, num_sms, s) : launch_tiles<BN, 1, false>(p, 1, num_sms, s);
 }
 
 }  // namespace
 
 cudaError_t launch_quantise_e4m3(const void* x, int dtype, long ldx, long rows, int k, void* codes, long ld_codes, unsigned char* scales,
                                  long ld_scales, cudaStream_t s) {
-  const int blocks = (k + kScaleBlock - 1) / kScaleBlock;
-  const long items = rows * blocks, per_block = (long)kQuantThreads / 16 * kQuantItems;
+  const int blocks = (k + kScaleBlock - 1) / kScaleBlock, per_block = kQuantThreads / 16 * kQuantItems;
+  // rows that are counted through together: as many as fill 16 thread blocks, so that it counts in 32 bits (a grid has 65535 of them in y)
+  long rows_each = 16 * per_block / blocks > 0 ? 16 * per_block / blocks : 1;
+  if ((rows + rows_each - 1) / rows_each > 65535) rows_each = (rows + 65534) / 65535;
+  if (rows_each > rows) rows_each = rows;
   const bool aligned = ((uintptr_t)x & 15) == 0 && ldx * (dtype == WF_BF16 ? 2 : 4) % 16 == 0;
-  const dim3 grid((unsigned)((items + per_block - 1) / per_block));
+  const dim3 grid((unsigned)((rows_each * blocks + per_block - 1) / per_block), (unsigned)((rows + rows_each - 1) / rows_each));
+  const uint32_t magic = (uint32_t)(((1ull << 32) + blocks - 1) / blocks);
   unsigned char* c = (unsigned char*)codes;
   auto go = [&](auto kernel, auto* from) {
-    return launch_dependent(kernel, grid, dim3(kQuantThreads), 0, s, 1, false, from, ldx, items, k, blocks, c, ld_codes, scales, ld_scales);
+    return launch_dependent(kernel, grid, dim3(kQuantThreads), 0, s, 1, false, from, ldx, rows, k, blocks, magic, (int)rows_each, c, ld_codes, scales,
+                            ld_scales);
   };
   if (dtype == WF_BF16) {
     auto* from = (const __nv_bfloat16*)x;
@@ -408,12 +745,41 @@ cudaError_t launch_quantise_e4m3(const void* x, int dtype, long ldx, long rows, 
   return aligned ? go(quantise_e4m3_kernel<float, true>, from) : go(quantise_e4m3_kernel<float, false>, from);
 }
 
+// Which tile: rows of A (224 of them: on pairs of blocks), and over how many blocks its channels are split.  Estimated time of
+// a call in us, from the times measured for 55 shapes of m = 1 .. 4000, n = 640 .. 50021, k = 512 .. 5120 (the choice is within
+// 8 % of the best tile for 50 of them, 20 % for all): a launch 3.6 (0.8 more on pairs), then as many rounds of tiles as the SMs need,
+// a block of 128 channels taking the time of its bytes.  One SM draws 95 GB/s, all of them together 8.6 TB/s.  A split costs
+// an exchange.  Examples, one tile of the kind against another: m = 1, n = k = 1280: 16 rows split 4: 4.4, whole 4.9;
+// m = 320, n = 1280, k = 5120: 128 rows split 4: 9.6, whole 13.7, pairs 14.8; m = 775, n = 5120, k = 1280: 128 rows 10.5, 64: 14.3,
+// pairs 10.7; m = 4000: pairs 23, 128 rows 32.
+double estimate_us(long m, long n, long k, int bn, int split, int num_sms) {
+  const int cg = bn == 224 ? 2 : 1, share = cg * split;
+  const long tiles = (n + kTileN * cg - 1) / (kTileN * cg) * ((m + bn - 1) / bn), blocks_k = (k + kScaleBlock - 1) / kScaleBlock;
+  if (split > 1 && (tiles * split * 20 > num_sms * 19 || split > blocks_k)) return 1e30;  // (a cluster needs its blocks at one time)
+  const long at_once = num_sms / share, rounds = (tiles + at_once - 1) / at_once;
+  const double active = (double)(tiles < at_once ? tiles : at_once) * share;
+  const double rate = active * 95e3 < 8.6e6 ? 95e3 : 8.6e6 / active;  // bytes per us and SM
+  const double block = (kTileN + bn / cg) * (double)kBlockBytes / rate;
+  return 3.6 + (cg == 2 ? 0.8 : 0.0) + (split > 1 ? 0.8 + 0.008 * bn : 0.0) +
+         (double)rounds * ((double)((blocks_k + split - 1) / split) * (block > 0.1 ? block : 0.1) + 0.004 * bn);
+}
+
 cudaError_t launch_gemm_e4m3(const E4m3GemmParams& p, int num_sms, cudaStream_t s) {
-  if (p.m <= 16) return launch_tiles<16>(p, num_sms, s);
-  if (p.m <= 32) return launch_tiles<32>(p, num_sms, s);
-  if (p.m <= 64) return launch_tiles<64>(p, num_sms, s);
-  if (p.m <= 128) return launch_tiles<128>(p, num_sms, s);
-  return launch_tiles<224>(p, num_sms, s);
+  static const int tiles[][2] = {{16, 1}, {16, 2}, {16, 4}, {32, 1}, {32, 2}, {32, 4}, {32, 8}, {64, 1}, {64, 2}, {64, 4},
+                                 {64, 8}, {128, 1}, {128, 2}, {128, 4}, {128, 8}, {224, 1}};
+  int bn = 0, split = 1;
+  double least = 1e30;
+  for (const auto& t : tiles) {
+    const double us = estimate_us(p.m, p.n, p.k, t[0], t[1], num_sms);
+    if (us < least) least = us, bn = t[0], split = t[1];
+  }
+  switch (bn) {
+    case 16: return launch_single<16>(p, split, num_sms, s);
+    case 32: return launch_single<32>(p, split, num_sms, s);
+    case 64: return launch_single<64>(p, split, num_sms, s);
+    case 128: return launch_single<128>(p, split, num_sms, s);
+    default: return launch_tiles<224, 2, false>(p, 1, num_sms, s);
+  }
 }
 
 }  // namespace wf
