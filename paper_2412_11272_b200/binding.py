@@ -603,9 +603,10 @@ class PagePool:
 class ScaledCodes:
     """A matrix [rows, k] in 8 bits: e4m3 ``codes`` (rows 16-byte aligned) and ``scales``, uint8 [ceil(k / 512), rows, 4]: byte b at
     [j, r, i] stands for 2^(b - 127), the scale of row r's channels 128 (4 j + i) and the 127 behind them.  Made by
-    ``Decoder.wf_quantise_e4m3``, or from codes of other origin by ``pack``."""
+    ``Decoder.wf_quantise_e4m3``, or from codes of other origin by ``pack``.
+    It stands for the tensors' memory as it is when it is made, as a KvCache does."""
 
-    __slots__ = ("codes", "scales", "shape", "device")
+    __slots__ = ("codes", "scales", "shape", "device", "c")
 
     def __init__(self, codes: torch.Tensor, scales: torch.Tensor):
         if codes.dim() != 2 or codes.dtype is not _E4M3 or codes.shape[1] < 1 or (codes.stride(1) != 1 and codes.shape[1] > 1):
@@ -614,7 +615,22 @@ class ScaledCodes:
         if scales.dtype is not _U8 or scales.device != codes.device or scales.shape != ((k + 511) // 512, rows, 4) or \
                 (rows > 0 and (scales.stride(2) != 1 or (rows > 1 and scales.stride(1) != 4) or (k > 512 and scales.stride(0) % 4))):
             _refuse("scales must be uint8 [ceil(k / 512), rows, 4] beside their codes, the words of consecutive rows side by side")
-        self.codes, self.scales, self.shape, self.device = codes, scales, (rows, k), codes.device
+        self._set(codes, scales, rows, k, codes.device, codes.stride(0) if rows > 1 else (k + 15) // 16 * 16,
+                  scales.stride(0) // 4 if k > 512 else max(rows, 1))
+
+    def _set(self, codes, scales, rows, k, device, ld, scale_ld):
+        put = object.__setattr__
+        put(self, "codes", codes)
+        put(self, "scales", scales)
+        put(self, "shape", (rows, k))
+        put(self, "device", device)
+        put(self, "c", wf_e4m3(codes.data_ptr(), scales.data_ptr(), ld, scale_ld) if device.type == "cuda" else None)
+        return self
+
+    def __setattr__(self, name, value):  # the descriptor holds the tensors' addresses
+        raise AttributeError(f"{name} of ScaledCodes is fixed: make others for other tensors")
+
+    __delattr__ = KvCache.__delattr__
 
     def __getitem__(self, rows: slice):
         """Some of the rows."""
@@ -655,13 +671,6 @@ class ScaledCodes:
         b = self.scales.transpose(0, 1).reshape(rows, -1)
         s = torch.exp2(b.double() - 127).float().masked_fill(b == 255, float("nan"))
         return self.codes.float() * s.repeat_interleave(128, dim=1)[:, :k]
-
-    def _c(self, name: str):
-        rows, k = self.shape
-        if self.device.type != "cuda":
-            _refuse(f"{name} must be in device memory")
-        return wf_e4m3(self.codes.data_ptr(), self.scales.data_ptr(), self.codes.stride(0) if rows > 1 else (k + 15) // 16 * 16,
-                       self.scales.stride(0) // 4 if k > 512 else max(rows, 1))
 
 
 class Decoder:
@@ -1000,18 +1009,19 @@ class Decoder:
     def wf_quantise_e4m3(self, x: torch.Tensor, out: ScaledCodes | None = None, stream=None) -> ScaledCodes:
         """x [rows, k] (float32 or bfloat16, row stride free) as e4m3 codes with a power-of-two scale for each 128 channels of a row:
         activations before a product, or weights, once."""
-        device = x.device
-        if device.type != "cuda" or x.dim() != 2 or x.dtype not in (_F32, _BF16) or x.shape[1] < 1 or (x.stride(1) != 1 and x.shape[1] > 1):
+        device, shape, dtype, strides = x.device, x.shape, x.dtype, x.stride()
+        if device.type != "cuda" or len(shape) != 2 or (dtype is not _F32 and dtype is not _BF16) or shape[1] < 1 or (strides[1] != 1 and shape[1] > 1):
             _refuse("x must be float32 or bfloat16 [rows, k] in device memory, a row's elements contiguous")
-        rows, k = x.shape
+        rows, k = shape
         if out is None:
-            ld = (k + 15) // 16 * 16
+            ld, groups = (k + 15) // 16 * 16, (k + 511) // 512
             codes = self._empty(x, (rows, ld), _E4M3, stream)
-            out = ScaledCodes(codes if ld == k else codes[:, :k], self._empty(x, ((k + 511) // 512, rows, 4), _U8, stream))
-        elif out.shape != tuple(x.shape) or out.device != device:
+            out = ScaledCodes.__new__(ScaledCodes)._set(codes if ld == k else codes[:, :k], self._empty(x, (groups, rows, 4), _U8, stream), rows, k,
+                                                        device, ld, max(rows, 1))
+        elif out.shape != (rows, k) or out.device != device:
             _refuse("out must have the shape and the device of x")
-        self._call(self.lib.wf_quantise_e4m3, device, stream, x.data_ptr(), WF_BF16 if x.dtype is _BF16 else WF_F32,
-                   x.stride(0) if rows > 1 else max(x.stride(0), k), rows, k, out._c("out"))
+        self._call(self.lib.wf_quantise_e4m3, device, stream, x.data_ptr(), WF_BF16 if dtype is _BF16 else WF_F32,
+                   strides[0] if rows > 1 else max(strides[0], k), rows, k, out.c)
         return out
 
     def wf_gemm_e4m3(self, a: ScaledCodes, w: ScaledCodes, bias=None, gelu: bool = False, out=None, out_dtype: str | None = None, status=None,
@@ -1019,17 +1029,20 @@ class Decoder:
         """act(a w^T + bias): a [m, k], w [n, k], bias float32 [n]; ``gelu``: the activation.  Returns [m, n] in ``out_dtype`` ("bf16" or
         "f32", default: the decoder's), or writes to ``out`` (row stride free)."""
         (m, k), (n, kw), device = a.shape, w.shape, a.device
-        if k != kw or w.device != device:
-            _refuse(f"a has {k} channels and w {kw}, or they are on different devices")
+        if k != kw or w.device != device or device.type != "cuda":
+            _refuse(f"a has {k} channels and w {kw}, or they are not in one device's memory")
         if out is None:
             if out_dtype not in (None, "bf16", "f32"):
                 _refuse("out_dtype is bf16 or f32")
-            out = self._empty(a.scales, (m, n), self.torch_dtype if out_dtype is None else _BF16 if out_dtype == "bf16" else _F32, stream)
+            dtype, ld = self.torch_dtype if out_dtype is None else _BF16 if out_dtype == "bf16" else _F32, n
+            out = self._empty(a.scales, (m, n), dtype, stream)
         elif out.shape != (m, n) or out.dtype not in (_F32, _BF16) or out.device != device or (out.stride(1) != 1 and n > 1):
             _refuse(f"out must be float32 or bfloat16 [{m}, {n}] on {device}, a row's elements contiguous")
         elif out_dtype is not None and out.dtype is not (_BF16 if out_dtype == "bf16" else _F32):
             _refuse("out is not of out_dtype")
+        else:
+            dtype, ld = out.dtype, out.stride(0) if m > 1 else max(out.stride(0), n)
         bp = None if bias is None else _vector(bias, "bias", device, _F32, n)
-        self._call(self.lib.wf_gemm_e4m3, device, stream, a._c("a"), w._c("w"), bp, out.data_ptr(), WF_BF16 if out.dtype is _BF16 else WF_F32,
-                   out.stride(0) if m > 1 else max(out.stride(0), n), m, n, k, int(gelu), self._status(status, device))
+        self._call(self.lib.wf_gemm_e4m3, device, stream, a.c, w.c, bp, out.data_ptr(), WF_BF16 if dtype is _BF16 else WF_F32, ld, m, n, k,
+                   int(gelu), self._status(status, device))
         return out

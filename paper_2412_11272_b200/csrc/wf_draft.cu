@@ -22,8 +22,10 @@ namespace {
 
 constexpr int kVerThreads = 512;
 constexpr int kVerWarps = kVerThreads / 32;
-constexpr int kVerTiles = 1024;  // runs of the vocabulary whose sums a block keeps
+constexpr int kAhead = 4;  // 16-byte pieces of a row that a thread has in flight
 constexpr int kMaxCluster = 8;
+constexpr int kRowBytes = 24;  // shared memory for a row of the sequence
+constexpr int kHoldBytes = 216 * 1024;  // shared memory that a block may ask for
 
 template <typename T>
 struct VecOf;
@@ -34,6 +36,8 @@ struct VecOf<float> {
     y[0] = __uint_as_float(u.x), y[1] = __uint_as_float(u.y), y[2] = __uint_as_float(u.z), y[3] = __uint_as_float(u.w);
   }
   static __device__ __forceinline__ float one(const float* x) { return __ldg(x); }
+  static constexpr uint32_t nothing = 0xff800000u;  // -infinity
+  static __device__ __forceinline__ void put(uint32_t (&w)[4], int e, const float* x) { w[e] = __float_as_uint(*x); }
 };
 template <>
 struct VecOf<__nv_bfloat16> {
@@ -47,7 +51,25 @@ struct VecOf<__nv_bfloat16> {
     }
   }
   static __device__ __forceinline__ float one(const __nv_bfloat16* x) { return __bfloat162float(*x); }
+  static constexpr uint32_t nothing = 0xff80ff80u;
+  static __device__ __forceinline__ void put(uint32_t (&w)[4], int e, const __nv_bfloat16* x) {
+    const uint32_t h = __bfloat16_as_ushort(*x);
+    w[e >> 1] = e & 1 ? (w[e >> 1] & 0xffffu) | h << 16 : (w[e >> 1] & 0xffff0000u) | h;
+  }
 };
+
+// Elements v .. of a row, those outside it -infinity (its first and last piece: kept out of line, the kernel's code is fetched anew
+// by every launch, and its size shows in the time of a small one).
+template <typename T>
+__device__ __noinline__ uint4 partial_piece(const T* x, int vocab, int v) {
+  uint32_t w[4];
+#pragma unroll
+  for (int e = 0; e < 4; ++e) w[e] = VecOf<T>::nothing;
+#pragma unroll
+  for (int e = 0; e < VecOf<T>::n; ++e)
+    if (v + e >= 0 && v + e < vocab) VecOf<T>::put(w, e, x + v + e);
+  return make_uint4(w[0], w[1], w[2], w[3]);
+}
 
 // A row of logits cut into 16-byte pieces from the boundary at or below its first element: piece i holds the elements
 // i n - shift .. ; what lies outside the row counts as -infinity.
@@ -60,14 +82,10 @@ struct LogitRow {
     pieces = (int)(((long)v + shift + VecOf<T>::n - 1) / VecOf<T>::n);
   }
   __device__ __forceinline__ int first(int i) const { return i * VecOf<T>::n - shift; }
-  __device__ __forceinline__ void load(int i, float (&y)[VecOf<T>::n]) const {
+  __device__ __forceinline__ uint4 load(int i) const {
     const int v = first(i);
-    if (i < pieces && v >= 0 && v <= vocab - VecOf<T>::n) {
-      VecOf<T>::unpack(__ldg(reinterpret_cast<const uint4*>(x + v)), y);
-    } else {
-#pragma unroll
-      for (int e = 0; e < VecOf<T>::n; ++e) y[e] = i < pieces && v + e >= 0 && v + e < vocab ? VecOf<T>::one(x + v + e) : -INFINITY;
-    }
+    if (i < pieces && v >= 0 && v <= vocab - VecOf<T>::n) return __ldg(reinterpret_cast<const uint4*>(x + v));
+    return i < pieces ? partial_piece(x, vocab, v) : make_uint4(VecOf<T>::nothing, VecOf<T>::nothing, VecOf<T>::nothing, VecOf<T>::nothing);
   }
 };
 
@@ -78,21 +96,49 @@ struct __align__(16) Part {
   double sum;
 };
 
-template <typename T>
-__global__ void __launch_bounds__(kVerThreads) draft_verify_kernel(const __grid_constant__ DraftVerifyParams p, int cluster) {
+// 2^(z / 64) for z <= 0 to some 1e-15: 2^(j / 64) from a table (z's nearest whole number is 64 i + j), the rest, at most half a
+// 64th, by the exponential series to the fifth power.  Eleven float64 operations where exp() takes about three times as many; the
+// draws are bound by them.
+// z below -64000 gives no number: the caller takes 0 there.
+constexpr double kLn2By64 = 0.010830424696249145;
+__constant__ double kSeries[6] = {kLn2By64,
+                                  kLn2By64 * kLn2By64 / 2.0,
+                                  kLn2By64 * kLn2By64 * kLn2By64 / 6.0,
+                                  kLn2By64 * kLn2By64 * kLn2By64 * kLn2By64 / 24.0,
+                                  kLn2By64 * kLn2By64 * kLn2By64 * kLn2By64 * kLn2By64 / 120.0,
+                                  6755399441055744.0};  // 1.5 * 2^52: a sum with it is rounded to a whole number
+__device__ __forceinline__ double exp2_64th(double z, const double* table) {
+  const double sum = z + kSeries[5], f = z - (sum - kSeries[5]);
+  const int k = __double2loint(sum);
+  double q = fma(f, kSeries[4], kSeries[3]);
+  q = fma(f, q, kSeries[2]);
+  q = fma(f, q, kSeries[1]);
+  q = fma(f, q, kSeries[0]) * f;
+  const double t = table[k & 63], r = fma(t, q, t);
+  return __hiloint2double(__double2hiint(r) + ((k >> 6) << 20), __double2loint(r));
+}
+
+// kHold: the block keeps its part of p in shared memory (`hold`), so that a refusal costs a subtraction for each element and
+// not an exponential; vocabularies whose part does not fit are computed anew.
+template <typename T, bool kHold>
+__global__ void __launch_bounds__(kVerThreads, 2) draft_verify_kernel(const __grid_constant__ DraftVerifyParams p, int cluster, int hold_length) {
   constexpr int kVec = VecOf<T>::n;
+  extern __shared__ __align__(16) double dynamic[];
   __shared__ Part gather[2][kMaxCluster * kVerWarps];
-  __shared__ double tile_sum[kVerTiles];
-  __shared__ double inverse[kMaxDrafts];  // of the sums left after each refusal at the present row
-  __shared__ int token[kMaxDrafts], parent[kMaxDrafts];
-  __shared__ float chance[kMaxDrafts];
-  __shared__ int refused[kMaxDrafts];     // tokens that were not drawn and not taken at the present row
+  __shared__ double table[64];
+  double* inverse = dynamic;                                   // of the sums left after each refusal at the present row
+  int* token = reinterpret_cast<int*>(dynamic + p.max_rows);
+  int* parent = token + p.max_rows;
+  float* chance = reinterpret_cast<float*>(parent + p.max_rows);
+  int* refused = reinterpret_cast<int*>(chance + p.max_rows);  // tokens that were not drawn and not taken at the present row
+  double* hold = dynamic + kRowBytes / 8 * p.max_rows;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int rank = cluster > 1 ? (int)ptx::cluster_ctarank() : 0;
   const int s = (int)blockIdx.x / cluster;
   int turn = 0;  // which of the two gather buffers the next exchange uses
 
   const int row0 = __ldg(p.cu_rows + s), end = __ldg(p.cu_rows + s + 1);
+  const float t = p.temperature ? __ldg(p.temperature + s) : 1.f, draw = __ldg(p.sample_u + s);
   int n = end - row0, problems = 0;
   if (row0 < 0 || end < row0 || end > p.n_rows) {
     problems |= kBadRows;
@@ -117,16 +163,16 @@ __global__ void __launch_bounds__(kVerThreads) draft_verify_kernel(const __grid_
     parent[i] = i > 0 ? up : -1;
     chance[i] = __ldg(p.accept_u + row0 + i);
   }
-  const float t = p.temperature ? __ldg(p.temperature + s) : 1.f;
+  if (tid < 64) table[tid] = exp2((double)tid / 64.0);
   if (n > 0 && !(t >= 0.f && t < INFINITY)) {
     problems |= kBadValue;
     n = 0;
   }
   if (problems != 0) report(p.status, problems);
   const bool greedy = t == 0.f;
-  const double per_t = greedy ? 0.0 : 1.0 / (double)t;
+  const double per_t = greedy ? 0.0 : 64.0 * 1.4426950408889634 / (double)t;  // exp(x / T) = 2^(x per_t / 64)
   // (a temperature near the smallest float must not make 0 x infinity of the largest logit)
-  const float per_t_log2 = greedy ? 0.f : fminf((float)(1.4426950408889634 * per_t), 3.0e38f);
+  const float per_t_log2 = greedy ? 0.f : fminf((float)(per_t / 64.0), 3.0e38f);
   if (cluster > 1) ptx::cluster_sync_all();  // every block of the cluster runs: its memory may be written
   else __syncthreads();
 
@@ -144,10 +190,12 @@ __global__ void __launch_bounds__(kVerThreads) draft_verify_kernel(const __grid_
     __syncwarp();
     if (cluster > 1) ptx::cluster_sync_all();
     else __syncthreads();
-    Part all{-INFINITY, 0x7fffffff, 0.0};
-    for (int i = lane; i < cluster * kVerWarps; i += 32) {
-      const Part x = gather[turn][i];
-      if (x.top > all.top || (x.top == all.top && x.at < all.at)) all.top = x.top, all.at = x.at;
+    Part all{-INFINITY, 0x7fffffff, 0.0}, part[kMaxCluster * kVerWarps / 32];
+#pragma unroll
+    for (int i = 0; i < kMaxCluster * kVerWarps / 32; ++i) {
+      part[i] = Part{-INFINITY, 0x7fffffff, 0.0};
+      if (i * 32 + lane < cluster * kVerWarps) part[i] = gather[turn][i * 32 + lane];
+      if (part[i].top > all.top || (part[i].top == all.top && part[i].at < all.at)) all.top = part[i].top, all.at = part[i].at;
     }
 #pragma unroll
     for (int o = 16; o > 0; o /= 2) {
@@ -156,14 +204,11 @@ __global__ void __launch_bounds__(kVerThreads) draft_verify_kernel(const __grid_
       if (top > all.top || (top == all.top && at < all.at)) all.top = top, all.at = at;
     }
     // sums of exponentials relative to each part's own largest logit
-    double sum = 0.0;
-    for (int i = lane; i < cluster * kVerWarps; i += 32) {
-      const Part x = gather[turn][i];
-      sum += greedy || x.top == all.top ? x.sum : x.sum * (double)exp2f((x.top - all.top) * per_t_log2);
-    }
 #pragma unroll
-    for (int o = 16; o > 0; o /= 2) sum += __shfl_xor_sync(0xffffffffu, sum, o);
-    all.sum = sum;
+    for (int i = 0; i < kMaxCluster * kVerWarps / 32; ++i)
+      all.sum += greedy || part[i].top == all.top ? part[i].sum : part[i].sum * (double)exp2f((part[i].top - all.top) * per_t_log2);
+#pragma unroll
+    for (int o = 16; o > 0; o /= 2) all.sum += __shfl_xor_sync(0xffffffffu, all.sum, o);
     turn ^= 1;
     return all;
   };
@@ -176,100 +221,145 @@ __global__ void __launch_bounds__(kVerThreads) draft_verify_kernel(const __grid_
   double whole = 0.0;     // its sum in float64, once something needs it (0: not yet)
   int n_cut = 0;          // refusals that changed p: sums in `inverse` (drawn drafts) or tokens in `refused`
   double gone = 0.0;      // probability of the refused tokens (drafts that were not drawn)
-  int have = -1;          // tile_sum holds the sums of p after this many refusals
+  int have = -1;          // the last pass (and hold) has p after this many refusals, not divided by the last one's sum
   double have_total = 0.0;
 
-  // p's weight at an element, after `cuts` refusals; unnormalised by the last of them
-  auto weight = [&](float y, int v, float q, int cuts) -> double {
-    double r = exp(((double)y - (double)row.top) * per_t);
-    if (y == row.top) r = 1.0;
-    if (q_row == nullptr) {
-      for (int i = 0; i < cuts; ++i)
-        if (refused[i] == v) r = 0.0;
-    } else if (cuts > 0) {
-      r *= 1.0 / whole;
-      for (int i = 0; i < cuts; ++i) {
-        const double d = r - (double)q;
-        r = d > 0.0 ? d : 0.0;
-        if (i + 1 < cuts) r *= inverse[i];
-      }
-    }
-    return r;
-  };
-
-  // One float64 pass over the row: sums of runs of 32 `sub` pieces in tile_sum, the whole returned.
-  auto slice = [&](const LogitRow<T>& x, int& sub, int& first, int& tiles) {
-    const int share = (x.pieces + cluster - 1) / cluster;
-    sub = (share + 32 * kVerTiles - 1) / (32 * kVerTiles);
-    tiles = (share + 32 * sub - 1) / (32 * sub);
-    first = rank * tiles * 32 * sub;
-  };
-  auto weights_of = [&](const LogitRow<T>& x, int i, int cuts, double (&w)[kVec]) {
-    float y[kVec];
-    x.load(i, y);
-    const int v = x.first(i);
-#pragma unroll
-    for (int e = 0; e < kVec; ++e) {
-      const bool in = i < x.pieces && v + e >= 0 && v + e < p.vocab;
-      const float q = in && cuts > 0 && q_row != nullptr ? __ldg(q_row + v + e) : 0.f;
-      w[e] = in ? weight(y[e], v + e, q, cuts) : 0.0;
-    }
-  };
-  auto sum_pass = [&](const LogitRow<T>& x, int cuts) -> double {
-    int sub, first, tiles;
-    slice(x, sub, first, tiles);
-    double mine = 0.0;
-    for (int k = warp; k < tiles; k += kVerWarps) {
-      double sum = 0.0;
-      for (int u = 0; u < sub; ++u) {
-        double w[kVec];
-        weights_of(x, first + (k * sub + u) * 32 + lane, cuts, w);
-#pragma unroll
-        for (int e = 0; e < kVec; ++e) sum += w[e];
-      }
-#pragma unroll
-      for (int o = 16; o > 0; o /= 2) sum += __shfl_xor_sync(0xffffffffu, sum, o);
-      if (lane == 0) tile_sum[k] = sum;
-      mine += sum;
-    }
-    have = cuts;
-    have_total = exchange(Part{0.f, 0, mine}).sum;
-    return have_total;
-  };
   auto row_at = [&](int i) { return LogitRow<T>(reinterpret_cast<const T*>(p.logits) + (long)(row0 + i) * p.ld, p.vocab); };
-
-  while (kept > 0) {
-    // ---- the row's largest logit and sum of exponentials
-    const LogitRow<T> x = row_at(cur);
-    q_row = p.draft ? p.draft + (long)(row0 + cur) * p.draft_ld : nullptr;
-    float top = -INFINITY, sum = 0.f;
-    int at = 0x7fffffff;
-    bool odd = false;  // a NaN
-    const int share = (x.pieces + cluster - 1) / cluster, stop = min(x.pieces, (rank + 1) * share);
-    constexpr int kAhead = 4;
-    for (int i0 = rank * share + tid; i0 < stop; i0 += kAhead * kVerThreads) {
-      float y[kAhead][kVec];
+  double top64 = 0.0;     // row.top, and the logit below which a weight is zero
+  float least = 0.f;
+  auto power = [&](float y) {
+    const double r = exp2_64th(((double)y - top64) * per_t, table);
+    return y > least ? r : 0.0;
+  };
+  // A row is cut into runs of 32 `length` pieces, one for every warp of the cluster, in order.
+  const int runs = cluster * kVerWarps;
+  auto run_length = [&](const LogitRow<T>& x) { return (x.pieces + runs * 32 - 1) / (runs * 32); };
+  // p's weights at the elements of piece i, after `cuts` refusals
+  auto weights_of = [&](const LogitRow<T>& x, int i, uint4 raw, int cuts, double (&w)[kVec]) {
+    float y[kVec];
+    VecOf<T>::unpack(raw, y);
+    const int v = x.first(i);
+    float q[kVec];
 #pragma unroll
-      for (int a = 0; a < kAhead; ++a) x.load(i0 + a * kVerThreads < stop ? i0 + a * kVerThreads : x.pieces, y[a]);
-      float high = top;
+    for (int e = 0; e < kVec; ++e) q[e] = cuts > 0 && q_row != nullptr && i < x.pieces && v + e >= 0 && v + e < p.vocab ? __ldg(q_row + v + e) : 0.f;
 #pragma unroll
-      for (int a = 0; a < kAhead; ++a)
+    for (int e = 0; e < kVec; ++e) w[e] = power(y[e]);  // (what lies outside the row is -infinity)
+    if (cuts == 0) return;
+    if (q_row == nullptr) {
+#pragma unroll 1
+      for (int c = 0; c < cuts; ++c)
+#pragma unroll
+        for (int e = 0; e < kVec; ++e)
+          if (refused[c] == v + e) w[e] = 0.0;
+      return;
+    }
+#pragma unroll
+    for (int e = 0; e < kVec; ++e) w[e] *= 1.0 / whole;
+#pragma unroll 1
+    for (int c = 0; c < cuts; ++c)
+#pragma unroll
+      for (int e = 0; e < kVec; ++e) {
+        w[e] = fmax(w[e] - (double)q[e], 0.0);
+        if (c + 1 < cuts) w[e] *= inverse[c];
+      }
+  };
+  auto held = [&](int u, int e) -> double& { return hold[((warp * hold_length + u) * 32 + lane) * kVec + (e ^ (lane & (kVec - 1)))]; };
+  // One pass over the row; returns the whole.  `on`: from what is held, one refusal further.
+  auto sum_pass = [&](const LogitRow<T>& x, int cuts, bool on) -> double {
+    const int length = run_length(x), first = (rank * kVerWarps + warp) * length * 32 + lane;
+    double sum = 0.0;
+    if (kHold && on) {
+      const double factor = cuts == 1 ? 1.0 / whole : inverse[cuts - 2];
+#pragma unroll 1
+      for (int u = 0; u < length; ++u) {
+        const int i = first + u * 32, v = x.first(i);
+        float q[kVec];
+#pragma unroll
+        for (int e = 0; e < kVec; ++e) q[e] = i < x.pieces && v + e >= 0 && v + e < p.vocab ? __ldg(q_row + v + e) : 0.f;
 #pragma unroll
         for (int e = 0; e < kVec; ++e) {
-          if (y[a][e] > high) {
-            high = y[a][e];
-            at = x.first(i0 + a * kVerThreads) + e;
-          }
-          odd |= y[a][e] != y[a][e];
+          double& w = held(u, e);
+          w = fmax(w * factor - (double)q[e], 0.0);
+          sum += w;
         }
-      if (!greedy && high > -INFINITY) {
-        sum *= top == high ? 1.f : exp2f((top - high) * per_t_log2);
-#pragma unroll
-        for (int a = 0; a < kAhead; ++a)
-#pragma unroll
-          for (int e = 0; e < kVec; ++e) sum += ptx::ex2_approx((y[a][e] - high) * per_t_log2);
       }
-      top = high;
+    } else {
+      uint4 raw = x.load(first);
+#pragma unroll 1
+      for (int u = 0; u < length; ++u) {
+        const uint4 now = raw;
+        if (u + 1 < length) raw = x.load(first + (u + 1) * 32);
+        double w[kVec];
+        weights_of(x, first + u * 32, now, cuts, w);
+#pragma unroll
+        for (int e = 0; e < kVec; ++e) {
+          if (kHold) held(u, e) = w[e];
+          sum += w[e];
+        }
+      }
+    }
+#pragma unroll
+    for (int o = 16; o > 0; o /= 2) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+    have = cuts;
+    have_total = exchange(Part{0.f, 0, sum}).sum;
+    return have_total;
+  };
+  // The first child of the present row behind row `after`, n if there is none.
+  auto child_behind = [&](int after) {
+    for (int base = (after + 1) & ~31; base < n; base += 32) {
+      const unsigned who = __ballot_sync(0xffffffffu, base + lane < n && base + lane > after && parent[base + lane] == cur);
+      if (who != 0) return base + __ffs(who) - 1;
+    }
+    return n;
+  };
+
+  while (kept > 0) {
+    // ---- the row's largest logit and sum of exponentials; what its first child needs is on its way meanwhile
+    const LogitRow<T> x = row_at(cur);
+    q_row = p.draft ? p.draft + (long)(row0 + cur) * p.draft_ld : nullptr;
+    int child = child_behind(cur);
+    float child_y = 0.f, child_q = 0.f;
+    auto look = [&]() {
+      if (child >= n) return;
+      child_y = VecOf<T>::one(x.x + token[child]);
+      if (q_row != nullptr) child_q = __ldg(q_row + token[child]);
+    };
+    look();
+    float top = -INFINITY, sum = 0.f;
+    int at = 0x7fffffff;
+    const int length = run_length(x), mine = (rank * kVerWarps + warp) * length * 32 + lane;
+#pragma unroll 1
+    for (int u0 = 0; u0 < length; u0 += kAhead) {
+      uint4 raw[kAhead];
+#pragma unroll
+      for (int a = 0; a < kAhead; ++a) raw[a] = x.load(u0 + a < length ? mine + (u0 + a) * 32 : x.pieces);
+#pragma unroll
+      for (int a = 0; a < kAhead; ++a) {
+        float y[kVec];
+        VecOf<T>::unpack(raw[a], y);
+        if (greedy) {
+#pragma unroll
+          for (int e = 0; e < kVec; ++e) {
+            if (y[e] > top) top = y[e], at = x.first(mine + (u0 + a) * 32) + e;
+            sum += y[e] != y[e] ? y[e] : 0.f;  // a NaN shows
+          }
+        } else {
+          float high = top;
+#pragma unroll
+          for (int e = 0; e < kVec; ++e) high = fmaxf(high, y[e]);
+          if (high > -INFINITY) {
+            if (high > top) sum *= exp2f((top - high) * per_t_log2);
+            float part = 0.f;
+#pragma unroll
+            for (int e = 0; e < kVec; ++e) part += ptx::ex2_approx((y[e] - high) * per_t_log2);
+            sum += part;
+            top = high;
+          } else {
+#pragma unroll
+            for (int e = 0; e < kVec; ++e) sum += y[e] != y[e] ? y[e] : 0.f;
+          }
+        }
+      }
     }
     float high = top;
     int place = at;
@@ -282,9 +372,10 @@ __global__ void __launch_bounds__(kVerThreads) draft_verify_kernel(const __grid_
     double wide = greedy || top == high ? (double)sum : (double)(sum * exp2f((top - high) * per_t_log2));
 #pragma unroll
     for (int o = 16; o > 0; o /= 2) wide += __shfl_xor_sync(0xffffffffu, wide, o);
-    if (__any_sync(0xffffffffu, odd)) wide = __longlong_as_double(0x7ff8000000000000ll);
     row = exchange(Part{high, place, wide});
     if (row.at >= p.vocab) row.at = 0;  // (nothing but -infinity)
+    top64 = (double)row.top;
+    least = (float)fmax(top64 - 64000.0 / per_t, -3.4028234663852886e38);
     whole = gone = 0.0;
     n_cut = 0;
     have = -1;
@@ -292,44 +383,47 @@ __global__ void __launch_bounds__(kVerThreads) draft_verify_kernel(const __grid_
 
     // ---- its children, in row order
     int taken = -1;
-    for (int base = (cur + 1) & ~31; base < n && taken < 0; base += 32) {
-      unsigned who = __ballot_sync(0xffffffffu, base + lane < n && base + lane > cur && parent[base + lane] == cur);
-      while (who != 0 && taken < 0) {
-        const int i = base + __ffs(who) - 1, v = token[i];
-        who &= who - 1;
-        if (greedy) {
-          if (v == row.at) taken = i;
-          continue;
+    for (; child < n && taken < 0; child = child_behind(child), look()) {
+      const int v = token[child];
+      if (greedy) {
+        if (v == row.at) taken = child;
+        continue;
+      }
+      const double u = (double)chance[child];
+      double e = power(child_y);
+      if (q_row == nullptr) {
+        for (int j = 0; j < n_cut; ++j)
+          if (refused[j] == v) e = 0.0;
+        if (u * (1.0 - gone) * row.sum < e) {
+          taken = child;
+        } else if (e > 0.0 && (1.0 - gone) * row.sum - e > 0.0) {
+          __syncthreads();  // all warps have read the list
+          if (tid == 0) refused[n_cut] = v;
+          __syncthreads();
+          ++n_cut;
+          gone += e / row.sum;
         }
-        const float y = VecOf<T>::one(x.x + v);
-        double e = y == row.top ? 1.0 : exp(((double)y - (double)row.top) * per_t);
-        if (q_row == nullptr) {
-          for (int j = 0; j < n_cut; ++j)
-            if (refused[j] == v) e = 0.0;
-          const double share_v = e / row.sum;
-          if ((double)chance[i] * (1.0 - gone) < share_v) {
-            taken = i;
-          } else if (share_v > 0.0 && 1.0 - gone - share_v > 0.0) {
-            __syncthreads();  // all warps have read the list
-            if (tid == 0) refused[n_cut] = v;
+      } else if (n_cut == 0 && u * (double)child_q * row.sum < e) {
+        taken = child;
+      } else {
+        double r = 0.0;
+        if (n_cut > 0) {
+          r = e * (1.0 / whole);
+          for (int j = 0; j < n_cut; ++j) r = fmax(r - (double)child_q, 0.0) * inverse[j];
+        }
+        if (n_cut > 0 && u * (double)child_q < r) {
+          taken = child;
+        } else {
+          double left = 0.0;
+#pragma unroll 1
+          for (int step = whole == 0.0 ? 0 : 1; step < 2; ++step) {  // p itself first, where nothing has needed it so far
+            left = sum_pass(x, step == 0 ? 0 : n_cut + 1, step != 0 && have == n_cut);
+            if (step == 0) whole = left;
+          }
+          if (left > 0.0) {
+            if (tid == 0) inverse[n_cut] = 1.0 / left;
             __syncthreads();
             ++n_cut;
-            gone += share_v;
-          }
-        } else {
-          const float qv = __ldg(q_row + v);
-          double r = n_cut == 0 ? e / row.sum : e * (1.0 / whole);
-          for (int j = 0; j < n_cut; ++j) r = (r - (double)qv > 0.0 ? r - (double)qv : 0.0) * inverse[j];
-          if ((double)chance[i] * (double)qv < r) {
-            taken = i;
-          } else {
-            if (whole == 0.0) whole = sum_pass(x, 0);
-            const double left = sum_pass(x, n_cut + 1);
-            if (left > 0.0) {
-              if (tid == 0) inverse[n_cut] = 1.0 / left;
-              __syncthreads();
-              ++n_cut;
-            }
           }
         }
       }
@@ -350,55 +444,57 @@ __global__ void __launch_bounds__(kVerThreads) draft_verify_kernel(const __grid_
   // ---- the token behind the path
   if (draws) {
     const LogitRow<T> x = row_at(cur);
-    if (have != n_cut) sum_pass(x, n_cut);
-    if (!(have_total > 0.0) && n_cut > 0) sum_pass(x, n_cut = 0);
-    const double target = (double)__ldg(p.sample_u + s) * have_total;
-    // the block whose run of the vocabulary holds the target (behind all: the last with any weight)
-    const Part* parts = gather[turn ^ 1];
-    double before = 0.0, at_owner = 0.0;
-    int owner = 0;
-    bool found = false;
-    for (int r = 0; r < cluster && !found; ++r) {
-      double sum = 0.0;
-      for (int w = 0; w < kVerWarps; ++w) sum += parts[r * kVerWarps + w].sum;
-      if (sum > 0.0) owner = r, at_owner = before;
-      before += sum;
-      found = sum > 0.0 && before > target;
+#pragma unroll 1
+    while (have != n_cut || (n_cut > 0 && !(have_total > 0.0))) {  // (where the refusals leave nothing they do not count)
+      if (have == n_cut) n_cut = 0;
+      sum_pass(x, n_cut, false);
     }
-    if (owner == rank && warp == 0) {
-      int sub, first, tiles;
-      slice(x, sub, first, tiles);
-      const double want = target - at_owner;
-      const int each = (tiles + 31) / 32, k0 = min(tiles, lane * each), k1 = min(tiles, k0 + each);
-      double sum = 0.0;
-      for (int k = k0; k < k1; ++k) sum += tile_sum[k];
-      double run = sum;
+    const double target = (double)draw * have_total;
+    // the run that holds the target (behind all: the last with any weight); a lane looks at four of the at most 128
+    static_assert(kMaxCluster * kVerWarps == 128, "four runs for each lane");
+    const Part* parts = gather[turn ^ 1];
+    double part[4], run = 0.0;
 #pragma unroll
-      for (int o = 1; o < 32; o *= 2) {
-        const double up = __shfl_up_sync(0xffffffffu, run, o);
-        if (lane >= o) run += up;
+    for (int i = 0; i < 4; ++i) {
+      part[i] = 4 * lane + i < runs ? parts[4 * lane + i].sum : 0.0;
+      run += part[i];
+    }
+    double before = run;
+#pragma unroll
+    for (int o = 1; o < 32; o *= 2) {
+      const double up = __shfl_up_sync(0xffffffffu, before, o);
+      if (lane >= o) before += up;
+    }
+    before -= run;
+    int hit = -1, last = -1;
+    double hit_before = 0.0, last_before = 0.0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      if (part[i] > 0.0) {
+        last = 4 * lane + i, last_before = before;
+        if (hit < 0 && before + part[i] > target) hit = 4 * lane + i, hit_before = before;
       }
-      run -= sum;
-      // the first run of pieces whose end lies behind the target, else the last that has any weight
-      int k_hit = -1, k_last = -1;
-      double hit_before = 0.0, last_before = 0.0;
-      for (int k = k0; k < k1; ++k) {
-        const double y = tile_sum[k];
-        if (y > 0.0) {
-          k_last = k, last_before = run;
-          if (k_hit < 0 && run + y > want) k_hit = k, hit_before = run;
-        }
-        run += y;
-      }
-      const unsigned hit = __ballot_sync(0xffffffffu, k_hit >= 0), any = __ballot_sync(0xffffffffu, k_last >= 0);
-      const int from = hit ? __ffs(hit) - 1 : 31 - __clz(any | 1);
-      const int k = __shfl_sync(0xffffffffu, hit ? k_hit : k_last, from);
-      double done = __shfl_sync(0xffffffffu, hit ? hit_before : last_before, from);
-      int best = -1, last = -1;
-      for (int u = 0; k >= 0 && u < sub && best < 0; ++u) {
-        const int i = first + (k * sub + u) * 32 + lane;
+      before += part[i];
+    }
+    const unsigned hits = __ballot_sync(0xffffffffu, hit >= 0), some = __ballot_sync(0xffffffffu, last >= 0);
+    const int from = hits ? __ffs(hits) - 1 : 31 - __clz(some | 1);
+    const int owner = __shfl_sync(0xffffffffu, hits ? hit : last, from);
+    const double want = target - __shfl_sync(0xffffffffu, hits ? hit_before : last_before, from);
+    if (owner == rank * kVerWarps + warp) {
+      // ---- its warp goes through it once more, up to the element
+      const int length = run_length(x), first = owner * length * 32 + lane;
+      double done = 0.0;
+      int best = -1, best_last = -1;  // (where rounding has moved the target out of reach: the last element with any weight)
+#pragma unroll 1
+      for (int u = 0; u < length && best < 0; ++u) {
+        const int i = first + u * 32;
         double w[kVec], mine = 0.0;
-        weights_of(x, i, n_cut, w);
+        if (kHold) {
+#pragma unroll
+          for (int e = 0; e < kVec; ++e) w[e] = held(u, e);
+        } else {
+          weights_of(x, i, x.load(i), n_cut, w);
+        }
 #pragma unroll
         for (int e = 0; e < kVec; ++e) mine += w[e];
         double up_to = mine;
@@ -408,21 +504,21 @@ __global__ void __launch_bounds__(kVerThreads) draft_verify_kernel(const __grid_
           if (lane >= o) up_to += up;
         }
         double here = done + (up_to - mine);
-        int mine_hit = -1, mine_last = -1;
+        int e_hit = -1, e_last = -1;
 #pragma unroll
         for (int e = 0; e < kVec; ++e) {
           here += w[e];
           if (w[e] > 0.0) {
-            mine_last = x.first(i) + e;
-            if (mine_hit < 0 && here > want) mine_hit = x.first(i) + e;
+            e_last = x.first(i) + e;
+            if (e_hit < 0 && here > want) e_hit = e_last;
           }
         }
-        const unsigned h = __ballot_sync(0xffffffffu, mine_hit >= 0), l = __ballot_sync(0xffffffffu, mine_last >= 0);
-        if (h) best = __shfl_sync(0xffffffffu, mine_hit, __ffs(h) - 1);
-        if (l) last = __shfl_sync(0xffffffffu, mine_last, 31 - __clz(l));
+        const unsigned h = __ballot_sync(0xffffffffu, e_hit >= 0), l = __ballot_sync(0xffffffffu, e_last >= 0);
+        if (h) best = __shfl_sync(0xffffffffu, e_hit, __ffs(h) - 1);
+        if (l) best_last = __shfl_sync(0xffffffffu, e_last, 31 - __clz(l));
         done += __shfl_sync(0xffffffffu, up_to, 31);
       }
-      if (lane == 0) p.out_tokens[(long)s * p.max_rows + kept - 1] = best >= 0 ? best : last;
+      if (lane == 0) p.out_tokens[(long)s * p.max_rows + kept - 1] = best >= 0 ? best : best_last;
     }
   }
   if (rank == 0) {
@@ -546,8 +642,15 @@ cudaError_t launch_draft_verify(const DraftVerifyParams& p, int dtype, int num_s
   const int piece = dtype == WF_BF16 ? VecOf<__nv_bfloat16>::n : VecOf<float>::n;
   int cluster = 1;
   while (cluster < kMaxCluster && (long)p.n_seq * cluster <= num_sms && p.vocab > cluster * kVerThreads * piece) cluster *= 2;
-  auto kernel = dtype == WF_BF16 ? draft_verify_kernel<__nv_bfloat16> : draft_verify_kernel<float>;
-  return launch_dependent(kernel, dim3((unsigned)(p.n_seq * cluster)), dim3(kVerThreads), 0, s, cluster, false, p, cluster);
+  // pieces of a run at any alignment of a row, and what a block holds of them
+  const long pieces = ((long)p.vocab + 2 * piece - 2) / piece, per = (long)cluster * kVerWarps * 32, length = (pieces + per - 1) / per;
+  const size_t rows = (size_t)p.max_rows * kRowBytes, part = (size_t)(length * kVerThreads * piece) * sizeof(double);
+  const bool hold = p.draft != nullptr && rows + part <= kHoldBytes;  // (drafts that were not drawn leave p as it is but for their tokens)
+  auto kernel = dtype == WF_BF16 ? (hold ? draft_verify_kernel<__nv_bfloat16, true> : draft_verify_kernel<__nv_bfloat16, false>)
+                                 : (hold ? draft_verify_kernel<float, true> : draft_verify_kernel<float, false>);
+  const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kHoldBytes);
+  if (e != cudaSuccess) return e;
+  return launch_dependent(kernel, dim3((unsigned)(p.n_seq * cluster)), dim3(kVerThreads), rows + (hold ? part : 0), s, cluster, false, p, cluster, (int)length);
 }
 
 cudaError_t launch_draft_commit(const CommitPlan& p, cudaStream_t s) {
