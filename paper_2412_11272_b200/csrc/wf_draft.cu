@@ -225,11 +225,10 @@ __global__ void __launch_bounds__(kVerThreads, 2) draft_verify_kernel(const __gr
   double have_total = 0.0;
 
   auto row_at = [&](int i) { return LogitRow<T>(reinterpret_cast<const T*>(p.logits) + (long)(row0 + i) * p.ld, p.vocab); };
-  double top64 = 0.0;     // row.top, and the logit below which a weight is zero
-  float least = 0.f;
+  double top64 = 0.0;     // row.top
   auto power = [&](float y) {
-    const double r = exp2_64th(((double)y - top64) * per_t, table);
-    return y > least ? r : 0.0;
+    const double z = ((double)y - top64) * per_t, r = exp2_64th(z, table);
+    return z > -64000.0 ? r : 0.0;
   };
   // A row is cut into runs of 32 `length` pieces, one for every warp of the cluster, in order.
   const int runs = cluster * kVerWarps;
@@ -375,7 +374,6 @@ __global__ void __launch_bounds__(kVerThreads, 2) draft_verify_kernel(const __gr
     row = exchange(Part{high, place, wide});
     if (row.at >= p.vocab) row.at = 0;  // (nothing but -infinity)
     top64 = (double)row.top;
-    least = (float)fmax(top64 - 64000.0 / per_t, -3.4028234663852886e38);
     whole = gone = 0.0;
     n_cut = 0;
     have = -1;
@@ -449,6 +447,7 @@ __global__ void __launch_bounds__(kVerThreads, 2) draft_verify_kernel(const __gr
       if (have == n_cut) n_cut = 0;
       sum_pass(x, n_cut, false);
     }
+    draws = have_total > 0.0;  // (always so: the largest logit's weight is 1)
     const double target = (double)draw * have_total;
     // the run that holds the target (behind all: the last with any weight); a lane looks at four of the at most 128
     static_assert(kMaxCluster * kVerWarps == 128, "four runs for each lane");
@@ -480,7 +479,7 @@ __global__ void __launch_bounds__(kVerThreads, 2) draft_verify_kernel(const __gr
     const int from = hits ? __ffs(hits) - 1 : 31 - __clz(some | 1);
     const int owner = __shfl_sync(0xffffffffu, hits ? hit : last, from);
     const double want = target - __shfl_sync(0xffffffffu, hits ? hit_before : last_before, from);
-    if (owner == rank * kVerWarps + warp) {
+    if (draws && owner == rank * kVerWarps + warp) {
       // ---- its warp goes through it once more, up to the element
       const int length = run_length(x), first = owner * length * 32 + lane;
       double done = 0.0;
