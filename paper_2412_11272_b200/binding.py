@@ -562,7 +562,7 @@ class KvCache:
     cache of the path's own type.  It stands for the tensors' memory as it is when it is made: their contents may change, but they are
     not exchanged, and one that is resized or set to another storage needs another KvCache."""
 
-    __slots__ = ("k", "v", "k_scale", "v_scale", "device", "shape", "c")
+    __slots__ = ("k", "v", "k_scale", "v_scale", "device", "shape", "c", "raw", "kind")
 
     def __init__(self, k: torch.Tensor, v: torch.Tensor, k_scale: torch.Tensor | None = None, v_scale: torch.Tensor | None = None):
         if k.shape != v.shape or k.dim() != 4 or k.dtype != v.dtype or k.device != v.device:
@@ -576,7 +576,8 @@ class KvCache:
                 _refuse("scales must be contiguous bfloat16 [n_pages, n_kv_head, page_size] beside their pages")
         c = wf_cache(k.data_ptr(), v.data_ptr(), None if k_scale is None else k_scale.data_ptr(),
                      None if v_scale is None else v_scale.data_ptr(), k.shape[0])
-        for name, value in zip(self.__slots__, (k, v, k_scale, v_scale, k.device, tuple(k.shape), c)):
+        kind = (*k.shape[1:], k.dtype, k_scale is not None, k.device.type)  # what a decoder compares with its own
+        for name, value in zip(self.__slots__, (k, v, k_scale, v_scale, k.device, tuple(k.shape), c, bytes(c), kind)):
             object.__setattr__(self, name, value)
 
     def __setattr__(self, name, value):  # the descriptor holds the tensors' addresses
@@ -690,6 +691,7 @@ class Decoder:
         self.dtype, self.cache_format = dtype, cache_format
         self.torch_dtype = _BF16 if dtype == "bf16" else _F32
         self.code_dtype = {"path": self.torch_dtype, "e4m3": torch.float8_e4m3fn, "int8": torch.int8}[cache_format]
+        self._kind = (self.n_kv_head, self.page_size, self.d_head, self.code_dtype, cache_format != "path", "cuda")
         cfg = wf_decoder_config(self.n_head, self.n_kv_head, self.d_head, WF_BF16 if dtype == "bf16" else WF_F32,
                                 CACHE_FORMATS[cache_format], self.page_size)
         handle = C.c_void_p()
@@ -726,6 +728,8 @@ class Decoder:
         return KvCache(k, v, *(torch.ones(shape[:3], dtype=_BF16, device=device) for _ in range(2)))
 
     def _cache(self, cache: KvCache):
+        if cache.kind == self._kind:
+            return cache.c
         if cache.shape[1:] != (self.n_kv_head, self.page_size, self.d_head) or cache.k.dtype != self.code_dtype:
             _refuse(f"the cache is {cache.k.dtype} {cache.shape}, this decoder's pages are {self.code_dtype} "
                     f"[n, {self.n_kv_head}, {self.page_size}, {self.d_head}]")
@@ -734,6 +738,15 @@ class Decoder:
         if cache.device.type != "cuda":
             _refuse("the cache must be in device memory")
         return cache.c
+
+    def _caches(self, caches, device):
+        """The descriptors of several layers' caches, one behind the other."""
+        for c in caches:
+            if c.kind != self._kind:
+                self._cache(c)
+            if c.device != device:
+                _refuse("a cache is on another device than the call's arrays")
+        return (wf_cache * len(caches)).from_buffer_copy(b"".join([c.raw for c in caches])) if caches else (wf_cache * 0)()
 
     def _rows(self, page_table, cu_rows, start, n_rows, device):
         n_seq, shape = cu_rows.numel() - 1, page_table.shape
@@ -758,10 +771,10 @@ class Decoder:
     def _empty(like, shape, dtype, stream):
         """Memory beside ``like`` for a call on ``stream``: the allocator then gives it to nobody else before that stream is
         done with it."""
-        if stream is None:
-            return like.new_empty(shape, dtype=dtype)
+        if stream is None:  # (the shorter way where the type is the same)
+            return like.new_empty(shape) if like.dtype is dtype else torch.empty(shape, dtype=dtype, device=like.device)
         with torch.cuda.stream(stream):
-            return like.new_empty(shape, dtype=dtype)
+            return torch.empty(shape, dtype=dtype, device=like.device)
 
     @staticmethod
     def _status(status, device):
@@ -907,12 +920,8 @@ class Decoder:
             if step < size:
                 _refuse(f"state {i}: rows overlap")
             state_array[i] = wf_beam_state(t.data_ptr(), size, step)
-        cache_array = (wf_cache * len(caches))()
+        cache_array = self._caches(caches, device)
         table = stride = lens = None
-        for i, c in enumerate(caches):
-            cache_array[i] = self._cache(c)
-            if c.device != device:
-                _refuse("caches and parents are on different devices")
         if caches:
             if page_table is None or lengths is None or page_table.dim() != 2 or page_table.shape[0] != B * W:
                 _refuse("paged caches need page_table [B * n_beam, pages] and lengths [B]")
@@ -989,11 +998,7 @@ class Decoder:
             if path.dim() != 2 or path.shape[0] < n_seq:
                 _refuse("path must be [n_seq, rows]")
             pp, stride = _vector(path, "path", device), path.shape[1]
-        cache_array = (wf_cache * len(caches))()
-        for i, c in enumerate(caches):
-            cache_array[i] = self._cache(c)
-            if c.device != device:
-                _refuse("caches and start are on different devices")
+        cache_array = self._caches(caches, device)
         table = tstride = None
         if caches:
             if page_table is None or page_table.dim() != 2 or page_table.shape[0] < n_seq:
