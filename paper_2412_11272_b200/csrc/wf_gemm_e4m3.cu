@@ -17,104 +17,115 @@ namespace {
 using namespace ptx;
 
 // ---------------------------------------------------------------------------------------------
-// Codes of the rows of x: sixteen lanes take the 128 channels of a block, eight each.
+// Codes of the rows of x: eight lanes take the 128 channels of a block, sixteen each.
 //   s = the least power of two with max |x| / s <= 448, code = x / s (exact) rounded to the nearest e4m3 value, ties to even.
+// Bound by memory for large matrices, once the instructions a value are few: sixteen values a lane share the look-up of
+// their place and the exchange of the maximum, and the maximum of bfloat16 values is taken two at a time.
 constexpr int kQuantThreads = 256;
-constexpr int kQuantItems = 4;  // blocks that a group of lanes has in flight
+constexpr int kQuantItems = 2;  // blocks that a group of lanes has in flight
+constexpr int kQuantEach = 16, kQuantLanes = kScaleBlock / kQuantEach;
 
-// What eight elements are before they are needed as numbers.
-__device__ __forceinline__ void load_raw(const float* x, uint4 (&u)[2]) {
-  u[0] = __ldg(reinterpret_cast<const uint4*>(x));
-  u[1] = __ldg(reinterpret_cast<const uint4*>(x) + 1);
-}
-__device__ __forceinline__ void load_raw(const __nv_bfloat16* x, uint4 (&u)[1]) { u[0] = __ldg(reinterpret_cast<const uint4*>(x)); }
-__device__ __forceinline__ void eight(const uint4 (&u)[2], float (&v)[8]) {
-  const uint32_t w[8] = {u[0].x, u[0].y, u[0].z, u[0].w, u[1].x, u[1].y, u[1].z, u[1].w};
+// What sixteen elements are before they are needed as numbers: bits, two bfloat16 or one float32 a word.
+template <typename T>
+struct Sixteen {
+  static constexpr int words = kQuantEach * (int)sizeof(T) / 4;
+  uint32_t w[words];
+};
+template <typename T>
+__device__ __forceinline__ void load_whole(const T* x, Sixteen<T>& r) {
 #pragma unroll
-  for (int i = 0; i < 8; ++i) v[i] = __uint_as_float(w[i]);
-}
-__device__ __forceinline__ void eight(const uint4 (&u)[1], float (&v)[8]) {
-  const uint32_t w[4] = {u[0].x, u[0].y, u[0].z, u[0].w};
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    v[2 * i] = __uint_as_float(w[i] << 16);
-    v[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+  for (int i = 0; i < Sixteen<T>::words / 4; ++i) {
+    const uint4 u = __ldg(reinterpret_cast<const uint4*>(x) + i);
+    r.w[4 * i] = u.x, r.w[4 * i + 1] = u.y, r.w[4 * i + 2] = u.z, r.w[4 * i + 3] = u.w;
   }
 }
-__device__ __forceinline__ uint32_t bits_of(const float* x) { return __ldg(reinterpret_cast<const uint32_t*>(x)); }
-__device__ __forceinline__ uint32_t bits_of(const __nv_bfloat16* x) { return __ldg(reinterpret_cast<const unsigned short*>(x)); }
+// The first n of them (n <= 0: none), the rest zero.
+__device__ __forceinline__ void load_some(const float* x, int n, Sixteen<float>& r) {
+#pragma unroll
+  for (int i = 0; i < 16; ++i) r.w[i] = i < n ? __float_as_uint(__ldg(x + i)) : 0u;
+}
+__device__ __forceinline__ void load_some(const __nv_bfloat16* x, int n, Sixteen<__nv_bfloat16>& r) {
+  const unsigned short* h = reinterpret_cast<const unsigned short*>(x);
+#pragma unroll
+  for (int i = 0; i < 8; ++i) r.w[i] = (2 * i < n ? (uint32_t)__ldg(h + 2 * i) : 0u) | (2 * i + 1 < n ? (uint32_t)__ldg(h + 2 * i + 1) << 16 : 0u);
+}
+// The bits of the largest magnitude as float32 (a NaN or an infinity is the largest).
+__device__ __forceinline__ uint32_t top_of(const Sixteen<float>& r) {
+  uint32_t top = 0;
+#pragma unroll
+  for (int i = 0; i < 16; ++i) top = max(top, r.w[i] & 0x7fffffffu);
+  return top;
+}
+__device__ __forceinline__ uint32_t top_of(const Sixteen<__nv_bfloat16>& r) {
+  uint32_t two = 0;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) two = __vmaxu2(two, r.w[i] & 0x7fff7fffu);
+  return max(two << 16, two & 0xffff0000u);
+}
+__device__ __forceinline__ float2 pair_of(const Sixteen<float>& r, int i) { return make_float2(__uint_as_float(r.w[2 * i]), __uint_as_float(r.w[2 * i + 1])); }
+__device__ __forceinline__ float2 pair_of(const Sixteen<__nv_bfloat16>& r, int i) {
+  return make_float2(__uint_as_float(r.w[i] << 16), __uint_as_float(r.w[i] & 0xffff0000u));
+}
 
-// The blocks of `rows_each` rows are counted through: block i of them is block i % blocks of row i / blocks (`magic`: 2^32 / blocks rounded up; exact as i * blocks < 2^32).
+// The blocks of `rows_each` rows are counted through: block i of them is block i % blocks of row i / blocks (`magic`: 2^32 / blocks
+// rounded up; exact as i * blocks < 2^32).
 template <typename T, bool kAligned>
 __global__ void __launch_bounds__(kQuantThreads) quantise_e4m3_kernel(const T* __restrict__ x, long ldx, long rows, int k, int blocks,
                                                                      uint32_t magic, int rows_each, unsigned char* __restrict__ codes,
                                                                      long ld_codes, unsigned char* __restrict__ scales, long ld_scales) {
-  constexpr int kWords = sizeof(T) == 2 ? 1 : 2;
   griddep_launch_dependents();
-  const int lane16 = threadIdx.x & 15;
+  constexpr int kGroups = kQuantThreads / kQuantLanes;
+  const int lane = threadIdx.x % kQuantLanes;
   const long row0 = (long)blockIdx.y * rows_each;
   const uint32_t items = (uint32_t)min((long)rows_each, rows - row0) * (uint32_t)blocks;
-  const uint32_t first = (uint32_t)blockIdx.x * (kQuantThreads / 16 * kQuantItems) + (threadIdx.x >> 4);
+  const uint32_t first = (uint32_t)blockIdx.x * (kGroups * kQuantItems) + threadIdx.x / kQuantLanes;
   x += row0 * ldx;
   codes += row0 * ld_codes;
   scales += row0 * 4;
-  uint4 raw[kQuantItems][kWords];
+  Sixteen<T> raw[kQuantItems];
+  uint32_t row[kQuantItems];
+  int b[kQuantItems], n[kQuantItems];  // block of the row; this lane's elements of it
 #pragma unroll
   for (int u = 0; u < kQuantItems; ++u) {
-    const uint32_t item = first + u * (kQuantThreads / 16), row = __umulhi(item, magic) + (blocks == 1 ? item : 0u);
-    const int c = (int)(item - row * blocks) * kScaleBlock + lane16 * 8;
-    const T* from = x + (long)row * ldx + c;
-    if (item < items && kAligned && c + 8 <= k) {
-      load_raw(from, raw[u]);
-    } else {
-      uint32_t w[4 * kWords];
-#pragma unroll
-      for (int i = 0; i < 4 * kWords; ++i) {
-        constexpr int per = 4 / (int)sizeof(T);
-        w[i] = 0;
-#pragma unroll
-        for (int e = 0; e < per; ++e)
-          if (item < items && c + i * per + e < k) w[i] |= bits_of(from + i * per + e) << (16 * e);
-      }
-#pragma unroll
-      for (int i = 0; i < kWords; ++i) raw[u][i] = make_uint4(w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3]);
-    }
+    const uint32_t item = first + u * kGroups;
+    row[u] = __umulhi(item, magic) + (blocks == 1 ? item : 0u);
+    b[u] = (int)(item - row[u] * blocks);
+    const int c = b[u] * kScaleBlock + lane * kQuantEach;
+    n[u] = item < items ? min(kQuantEach, k - c) : 0;
+    const T* from = x + (long)row[u] * ldx + c;
+    if (kAligned && n[u] == kQuantEach) load_whole(from, raw[u]);
+    else load_some(from, n[u], raw[u]);
   }
 #pragma unroll
   for (int u = 0; u < kQuantItems; ++u) {
-    const uint32_t item = first + u * (kQuantThreads / 16), row = __umulhi(item, magic) + (blocks == 1 ? item : 0u);
-    const int b = (int)(item - row * blocks), c = b * kScaleBlock + lane16 * 8;
-    float v[8];
-    eight(raw[u], v);
-    uint32_t top = 0;  // as bits: a NaN or an infinity is the largest
+    uint32_t top = top_of(raw[u]);
 #pragma unroll
-    for (int e = 0; e < 8; ++e) top = max(top, __float_as_uint(v[e]) & 0x7fffffffu);
-#pragma unroll
-    for (int o = 8; o > 0; o /= 2) top = max(top, __shfl_xor_sync(0xffffffffu, top, o));
-    if (item >= items) continue;
+    for (int o = kQuantLanes / 2; o > 0; o /= 2) top = max(top, __shfl_xor_sync(0xffffffffu, top, o));
+    if (first + u * kGroups >= items) continue;
     const int e = (int)(top >> 23);
     const int scale = top == 0 ? 127 : e == 255 ? 255 : max(e - 8 + ((top & 0x7fffffu) > 0x600000u ? 1 : 0), 1);
     // 1 / s is a power of two as well: the products are exact, or so small that their code is zero either way
     const float inv = scale == 255 ? 0.f : __uint_as_float((uint32_t)(254 - scale) << 23);
-    uint32_t word[2];
+    uint32_t word[4];
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      uint32_t two[2];
-#pragma unroll
-      for (int j = 0; j < 2; ++j)
-        two[j] = __nv_cvt_float2_to_fp8x2(make_float2(v[4 * h + 2 * j] * inv, v[4 * h + 2 * j + 1] * inv), __NV_SATFINITE, __NV_E4M3);
-      word[h] = scale == 255 ? 0u : two[0] | (two[1] << 16);
+    for (int h = 0; h < 4; ++h) {
+      const float2 p = pair_of(raw[u], 2 * h), q = pair_of(raw[u], 2 * h + 1);
+      const uint32_t lo = __nv_cvt_float2_to_fp8x2(make_float2(p.x * inv, p.y * inv), __NV_SATFINITE, __NV_E4M3);
+      const uint32_t hi = __nv_cvt_float2_to_fp8x2(make_float2(q.x * inv, q.y * inv), __NV_SATFINITE, __NV_E4M3);
+      word[h] = scale == 255 ? 0u : lo | (hi << 16);
     }
-    unsigned char* to = codes + (long)row * ld_codes + c;
-    if (c + 8 <= k) {
-      *reinterpret_cast<uint2*>(to) = make_uint2(word[0], word[1]);
+    unsigned char* to = codes + (long)row[u] * ld_codes + b[u] * kScaleBlock + lane * kQuantEach;
+    if (n[u] == kQuantEach) {
+      *reinterpret_cast<uint4*>(to) = make_uint4(word[0], word[1], word[2], word[3]);
     } else {
-      for (int i = 0; c + i < k && i < 8; ++i) to[i] = (unsigned char)(word[i >> 2] >> (8 * (i & 3)));
+#pragma unroll
+      for (int i = 0; i < kQuantEach; ++i)
+        if (i < n[u]) to[i] = (unsigned char)(word[i >> 2] >> (8 * (i & 3)));
     }
-    unsigned char* mark = scales + ((b >> 2) * ld_scales + (long)row) * 4 + (b & 3);
-    if (lane16 == 0) *mark = (unsigned char)scale;
+    unsigned char* mark = scales + ((b[u] >> 2) * ld_scales + (long)row[u]) * 4 + (b[u] & 3);
+    if (lane == 0) *mark = (unsigned char)scale;
     // a row's last word has all its bytes
-    if (b == blocks - 1 && lane16 > 0 && lane16 <= 3 - (b & 3)) mark[lane16] = 127;
+    if (b[u] == blocks - 1 && lane > 0 && lane <= 3 - (b[u] & 3)) mark[lane] = 127;
   }
 }
 
@@ -506,10 +517,24 @@ __global__ void __launch_bounds__(kGemmThreads, 1) gemm_e4m3_kernel(const __grid
     int acc = 0, pieces = 0;
     uint32_t acc_phase = 0;
     bool ok = true;
+    // What does not depend on the tile.  Pieces of 16 rows by 128 columns: in shared memory a row is two halves of 128 bytes,
+    // 16-byte chunks exclusive-or'd with the row against bank conflicts.  A thread names a row of a matrix to be stored, and
+    // copies a chunk of two rows out.
+    const int chunk_in = (quarter & 1) * 4 + (lane >> 3), row_out = quarter * 4 + (lane >> 4), chunk_out = lane & 15;
+    const uint32_t area = smem_base + Plan::kSideOffset + (uint32_t)(turn * 2 * kStoreBytes);
+    const uint32_t in = area + (quarter >> 1) * (kStoreBytes / 2) + (lane & 7) * 128 + ((chunk_in ^ (lane & 7)) << 4);
+    const uint32_t out_a = area + (chunk_out >> 3) * (kStoreBytes / 2) + row_out * 128 + (((chunk_out & 7) ^ (row_out & 7)) << 4);
+    const uint32_t out_b = out_a ^ ((2u << 4) | (2u * 128u));  // two rows on (row_out is even in its second bit: 0, 1, 4, 5, ..)
+    const long two_rows = 2 * p.ldc, next_piece = 16L * kEpiTurns * p.ldc - two_rows;
+    const uint32_t lanes_at = (uint32_t)(quarter * 32) << 16;
+    int wn = tile0 % num_w, wm = tile0 / num_w;
+    const int step_n = tile_step % num_w, step_m = tile_step / num_w;
     for (int tile = tile0; tile < num_tiles; tile += tile_step) {
-      const int n0 = (tile % num_w * CG + (CG == 2 ? rank : 0)) * kTileN, m0 = tile / num_w * BN;
+      const int n0 = (wn * CG + (CG == 2 ? rank : 0)) * kTileN, m0 = wm * BN;
+      wn += step_n;
+      wm += step_m;
+      if (wn >= num_w) wn -= num_w, ++wm;
       const int col = n0 + quarter * 32 + lane, stop = min(BN, p.m - m0);
-      const float bias = p.bias && col < p.n ? __ldg(p.bias + col) : 0.f;
       ok = ok && __all_sync(0xffffffffu, wait(tfull_bar(acc), acc_phase));
       if (!ok) {  // what was not computed is NaN
         if (lane == 0) report(p.status, kGaveUp);
@@ -517,39 +542,21 @@ __global__ void __launch_bounds__(kGemmThreads, 1) gemm_e4m3_kernel(const __grid
         continue;
       }
       tc_fence_after();
-      const uint32_t from = tmem + ((uint32_t)(quarter * 32) << 16) + acc * BN;
-      if (wide_rows) {
-        float b4[4];  // of this thread's lanes of the fragments
+      const uint32_t from = tmem + lanes_at + acc * BN;
+      if (wide_rows && n0 + kTileN <= p.n) {
+        float b4[4] = {0.f, 0.f, 0.f, 0.f};  // of this thread's lanes of the fragments
+        if (p.bias) {
+          const int first = n0 + quarter * 32 + (lane >> 2);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const int at = n0 + quarter * 32 + 8 * i + (lane >> 2);
-          b4[i] = p.bias && at < p.n ? __ldg(p.bias + at) : 0.f;
+          for (int i = 0; i < 4; ++i)
+            b4[i] = __ldg(p.bias + first + 8 * i);
         }
-        // Pieces of 16 rows by 128 columns: in shared memory a row is two halves of 128 bytes, 16-byte chunks exclusive-or'd with
-        // the row against bank conflicts.  A thread names a row of a matrix to be stored, and copies a chunk of two rows out.
-        const int chunk_in = (quarter & 1) * 4 + (lane >> 3), row_out = quarter * 4 + (lane >> 4), chunk_out = lane & 15;
-        const uint32_t area = smem_base + Plan::kSideOffset + (uint32_t)(turn * 2 * kStoreBytes);
-        const uint32_t in = area + (quarter >> 1) * (kStoreBytes / 2) + (lane & 7) * 128 + ((chunk_in ^ (lane & 7)) << 4);
-        const uint32_t half_out = area + (chunk_out >> 3) * (kStoreBytes / 2);
-        const uint32_t out_a = half_out + row_out * 128 + (((chunk_out & 7) ^ (row_out & 7)) << 4);
-        const uint32_t out_b = half_out + (row_out + 2) * 128 + (((chunk_out & 7) ^ ((row_out + 2) & 7)) << 4);
-        const int at = n0 + chunk_out * 8, columns = min(8, p.n - at);  // of this thread's chunk
-        __nv_bfloat16* to = reinterpret_cast<__nv_bfloat16*>(p.out) + (long)(m0 + turn * 16 + row_out) * p.ldc + at;
-        const long two_rows = 2 * p.ldc, next_piece = 16L * kEpiTurns * p.ldc - two_rows;
+        __nv_bfloat16* to = reinterpret_cast<__nv_bfloat16*>(p.out) + (long)(m0 + turn * 16 + row_out) * p.ldc + n0 + chunk_out * 8;
         auto copy_out = [&](uint32_t from_smem, bool exists) {
           uint4 u;
           ld_shared_v4(from_smem, u.x, u.y, u.z, u.w);
-          if (exists && columns == 8) *reinterpret_cast<uint4*>(to) = u;
+          if (exists) *reinterpret_cast<uint4*>(to) = u;
         };
-        auto copy_ragged = [&](uint32_t from_smem, bool exists) {  // the last columns of C, one by one
-          if (!exists || columns >= 8) return;
-          for (int e = 0; e < columns; ++e) {
-            unsigned short h;
-            asm volatile("ld.shared.u16 %0, [%1];" : "=h"(h) : "r"(from_smem + 2 * e) : "memory");
-            to[e] = __ushort_as_bfloat16(h);
-          }
-        };
-        const bool ragged = n0 + kTileN > p.n;
         auto fetch = [&](int c, uint32_t (&r)[16]) {
           tmem_ld_fragments(from + c, r);
           tmem_ld_fragments(from + (16u << 16) + c, r + 8);
@@ -575,12 +582,9 @@ __global__ void __launch_bounds__(kGemmThreads, 1) gemm_e4m3_kernel(const __grid
           stmatrix_trans(in + side, word[0], word[1], word[2], word[3]);
           stmatrix_trans(in + side + 8 * 128, word[4], word[5], word[6], word[7]);
           asm volatile("bar.sync %0, 128;" ::"r"(1 + turn) : "memory");  // (the other piece has been read by then)
-          const bool exists_a = c + row_out < stop, exists_b = c + row_out + 2 < stop;
-          copy_out(out_a + side, exists_a);
-          if (ragged) copy_ragged(out_a + side, exists_a);
+          copy_out(out_a + side, c + row_out < stop);
           to += two_rows;
-          copy_out(out_b + side, exists_b);
-          if (ragged) copy_ragged(out_b + side, exists_b);
+          copy_out(out_b + side, c + row_out + 2 < stop);
           to += next_piece;
         };
         uint32_t even[16], odd[16];
@@ -600,6 +604,7 @@ __global__ void __launch_bounds__(kGemmThreads, 1) gemm_e4m3_kernel(const __grid
           c += kStep;
         }
       } else {
+        const float bias = p.bias && col < p.n ? __ldg(p.bias + col) : 0.f;
         uint32_t next[8];
         if (turn * 8 < stop) tmem_ld_x8(from + turn * 8, next);
 #pragma unroll 1
@@ -703,7 +708,7 @@ cudaError_t launch_tiles(const E4m3GemmParams& p, int split, int num_sms, cudaSt
   using Plan = E4m3Plan<BN, CG, kSplit>;
   CUtensorMap tw, ta;
   if (!codes_map(&tw, p.w, p.n, p.k, kTileN) || !codes_map(&ta, p.a, p.m, p.k, BN / CG)) return cudaErrorInvalidValue;
-  // bfloat16 rows of whole 16-byte chunks go through shared memory, others straight from registers
+  // bfloat16 rows of whole 16-byte chunks go through shared memory, others (and the last columns) straight from registers
   const bool wide = p.out_dtype == WF_BF16 && ((uintptr_t)p.out & 15) == 0 && p.ldc % 8 == 0;
   const long tiles = (long)((p.n + CG * kTileN - 1) / (CG * kTileN)) * ((p.m + BN - 1) / BN);
   if (tiles * 8 > 0x7fffffffL) return cudaErrorInvalidValue;  // (C would have 2^39 elements)
@@ -724,7 +729,7 @@ cudaError_t launch_single(const E4m3GemmParams& p, int split, int num_sms, cudaS
 
 cudaError_t launch_quantise_e4m3(const void* x, int dtype, long ldx, long rows, int k, void* codes, long ld_codes, unsigned char* scales,
                                  long ld_scales, cudaStream_t s) {
-  const int blocks = (k + kScaleBlock - 1) / kScaleBlock, per_block = kQuantThreads / 16 * kQuantItems;
+  const int blocks = (k + kScaleBlock - 1) / kScaleBlock, per_block = kQuantThreads / kQuantLanes * kQuantItems;
   // rows that are counted through together: as many as fill 16 thread blocks, so that it counts in 32 bits (a grid has 65535 of them in y)
   long rows_each = 16 * per_block / blocks > 0 ? 16 * per_block / blocks : 1;
   if ((rows + rows_each - 1) / rows_each > 65535) rows_each = (rows + 65534) / 65535;
