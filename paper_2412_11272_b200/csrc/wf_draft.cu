@@ -213,6 +213,30 @@ __global__ void __launch_bounds__(kVerThreads, 2) draft_verify_kernel(const __gr
     return all;
   };
 
+  // The same for a sum alone: each warp's goes to gather's memory as doubles, in the order of the warps.
+  auto exchange_sum = [&](double mine) -> double {
+    double* sums = reinterpret_cast<double*>(gather[turn]);
+    if (lane < cluster) {
+      if (cluster > 1) {
+        const long long bits = __double_as_longlong(mine);
+        ptx::st_cluster_v2(ptx::map_to_cta(ptx::smem_u32(sums + rank * kVerWarps + warp), lane), (uint32_t)bits, (uint32_t)(bits >> 32));
+      } else {
+        sums[warp] = mine;
+      }
+    }
+    __syncwarp();
+    if (cluster > 1) ptx::cluster_sync_all();
+    else __syncthreads();
+    double all = 0.0;
+#pragma unroll
+    for (int i = 0; i < kMaxCluster * kVerWarps / 32; ++i)
+      if (i * 32 + lane < cluster * kVerWarps) all += sums[i * 32 + lane];
+#pragma unroll
+    for (int o = 16; o > 0; o /= 2) all += __shfl_xor_sync(0xffffffffu, all, o);
+    turn ^= 1;
+    return all;
+  };
+
   const float* q_row = nullptr;
   int kept = n > 0 ? 1 : 0, cur = 0;
   int next = -1;          // the token that follows the path
@@ -300,7 +324,7 @@ __global__ void __launch_bounds__(kVerThreads, 2) draft_verify_kernel(const __gr
 #pragma unroll
     for (int o = 16; o > 0; o /= 2) sum += __shfl_xor_sync(0xffffffffu, sum, o);
     have = cuts;
-    have_total = exchange(Part{0.f, 0, sum}).sum;
+    have_total = exchange_sum(sum);
     return have_total;
   };
   // The first child of the present row behind row `after`, n if there is none.
@@ -360,17 +384,14 @@ __global__ void __launch_bounds__(kVerThreads, 2) draft_verify_kernel(const __gr
         }
       }
     }
-    float high = top;
-    int place = at;
+    // (as ordered integers: one instruction takes the largest of a warp)
+    const int bits = __float_as_int(top), order = bits ^ ((bits >> 31) & 0x7fffffff), most = __reduce_max_sync(0xffffffffu, order);
+    const float high = __int_as_float(most ^ ((most >> 31) & 0x7fffffff));
+    const int place = greedy ? (int)__reduce_min_sync(0xffffffffu, (unsigned)(order == most ? at : 0x7fffffff)) : 0x7fffffff;
+    float part = greedy || top == high ? sum : sum * exp2f((top - high) * per_t_log2);
 #pragma unroll
-    for (int o = 16; o > 0; o /= 2) {
-      const float h = __shfl_xor_sync(0xffffffffu, high, o);
-      const int a = __shfl_xor_sync(0xffffffffu, place, o);
-      if (h > high || (h == high && a < place)) high = h, place = a;
-    }
-    double wide = greedy || top == high ? (double)sum : (double)(sum * exp2f((top - high) * per_t_log2));
-#pragma unroll
-    for (int o = 16; o > 0; o /= 2) wide += __shfl_xor_sync(0xffffffffu, wide, o);
+    for (int o = 16; o > 0; o /= 2) part += __shfl_xor_sync(0xffffffffu, part, o);
+    const double wide = (double)part;
     row = exchange(Part{high, place, wide});
     if (row.at >= p.vocab) row.at = 0;  // (nothing but -infinity)
     top64 = (double)row.top;
@@ -451,11 +472,11 @@ __global__ void __launch_bounds__(kVerThreads, 2) draft_verify_kernel(const __gr
     const double target = (double)draw * have_total;
     // the run that holds the target (behind all: the last with any weight); a lane looks at four of the at most 128
     static_assert(kMaxCluster * kVerWarps == 128, "four runs for each lane");
-    const Part* parts = gather[turn ^ 1];
+    const double* sums = reinterpret_cast<const double*>(gather[turn ^ 1]);
     double part[4], run = 0.0;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      part[i] = 4 * lane + i < runs ? parts[4 * lane + i].sum : 0.0;
+      part[i] = 4 * lane + i < runs ? sums[4 * lane + i] : 0.0;
       run += part[i];
     }
     double before = run;
@@ -646,7 +667,9 @@ cudaError_t launch_draft_verify(const DraftVerifyParams& p, int dtype, int num_s
   // pieces of a run at any alignment of a row, and what a block holds of them
   const long pieces = ((long)p.vocab + 2 * piece - 2) / piece, per = (long)cluster * kVerWarps * 32, length = (pieces + per - 1) / per;
   const size_t rows = (size_t)p.max_rows * kRowBytes, part = (size_t)(length * kVerThreads * piece) * sizeof(double);
-  const bool hold = p.draft != nullptr && rows + part <= kHoldBytes;  // (drafts that were not drawn leave p as it is but for their tokens)
+  // Held where it fits and pays: for drawn drafts, whose refusals go on from it, and where a block has its SM to itself, so that the
+  // draw is read back and not computed again (one stream 20 -> 19 us; 64 streams of drafts that were not drawn 30 -> 36: not there).
+  const bool hold = rows + part <= kHoldBytes && (p.draft != nullptr || (long)p.n_seq * cluster <= num_sms);
   auto kernel = dtype == WF_BF16 ? (hold ? draft_verify_kernel<__nv_bfloat16, true> : draft_verify_kernel<__nv_bfloat16, false>)
                                  : (hold ? draft_verify_kernel<float, true> : draft_verify_kernel<float, false>);
   const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kHoldBytes);
