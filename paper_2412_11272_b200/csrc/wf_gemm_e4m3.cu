@@ -412,52 +412,56 @@ __global__ void __launch_bounds__(kGemmThreads, 1) gemm_e4m3_kernel(const __grid
     // The whole warp walks along (so that descriptors stay in uniform registers), one lane issues.
     if (CG == 1 || rank == 0) {
       const bool one = elect_one();
-      auto commit = [&](uint32_t bar) {
-        if (one) {
-          if constexpr (CG == 2) umma_commit_pair(bar, 3);
-          else umma_commit(bar);
-        }
-        __syncwarp();
+      auto commit = [&](uint32_t bar) {  // (by the electing lane)
+        if constexpr (CG == 2) umma_commit_pair(bar, 3);
+        else umma_commit(bar);
       };
       auto ready = [&](uint32_t bar, uint32_t parity) { return __all_sync(0xffffffffu, wait(bar, parity)); };
-      const uint64_t desc = umma_desc_k_sw128(0);
-      const uint32_t first = (smem_base & 0x3ffff) >> 4;
+      auto seen = [&](uint32_t bar, uint32_t parity) { return __all_sync(0xffffffffu, mbar_test(bar, parity)); };
+      const uint64_t desc = umma_desc_k_sw128(0) + ((smem_base & 0x3ffff) >> 4);
       int stage = 0, acc = 0, buf = 0;
       uint32_t phase = 0, acc_phase = 0, buf_phase = 0;
-      bool ok = true, peeked = false;
+      bool ok = true, full_seen = false, scales_seen = false;
       for (int tile = tile0; ok && tile < num_tiles; tile += tile_step) {
         if (!ready(tempty_bar(acc), acc_phase ^ 1u)) { ok = false; break; }
-        tc_fence_after();
-        for (int kb = kb0; kb < kb1; ++kb) {
-          if (((kb & 3) == 0 || kb == kb0) && !ready(sfull_bar(buf), buf_phase)) { ok = false; break; }
-          if (!peeked && !ready(full_bar(stage), phase)) { ok = false; break; }
-          tc_fence_after();
-          const uint64_t wdesc = desc + (first + stage * (Plan::kStageBytes >> 4));
-          const uint64_t adesc = wdesc + (Plan::kWBytes >> 4);
-          const uint32_t idesc = e4m3_idesc(CG * kTileN, BN, kb & 3), scales = tmem + kScaleCols + 12 * buf, to = tmem + acc * BN;
-          const uint32_t empty = empty_bar(stage);
-          if (++stage == kStages) { stage = 0; phase ^= 1u; }
-          if (one) {
+        const uint32_t to = tmem + acc * BN;
+        uint32_t more = 0;  // the tile's first product overwrites the accumulator
+        for (int g = kb0 >> 2; ok && 4 * g < kb1; ++g) {
+          if (!scales_seen && !ready(sfull_bar(buf), buf_phase)) { ok = false; break; }
+          const uint32_t scales = tmem + kScaleCols + 12 * buf, free_scales = sempty_bar(buf);
+          if (++buf == 2) { buf = 0; buf_phase ^= 1u; }
 #pragma unroll
-            for (int j = 0; j < 4; ++j)  // 32 channels: 32 bytes further inside the swizzled row
-              umma_e4m3<CG>(to, wdesc + 2 * j, adesc + 2 * j, idesc, scales, scales + 4, kb != kb0 || j != 0 ? 1u : 0u);
-          }
-          __syncwarp();
-          // The next stage is looked for while these products run: the queue of products is short, and waiting behind them
-          // would leave the tensor cores idle for the time of a look.
-          peeked = __all_sync(0xffffffffu, mbar_test(full_bar(stage), phase));
-          commit(empty);
-          if ((kb & 3) == 3 || kb == kb1 - 1) {
-            commit(sempty_bar(buf));
-            if (++buf == 2) { buf = 0; buf_phase ^= 1u; }
+          for (int number = 0; number < 4; ++number) {
+            const int kb = 4 * g + number;
+            if ((kSplit && kb < kb0) || kb >= kb1) continue;
+            if (!full_seen && !ready(full_bar(stage), phase)) { ok = false; break; }
+            tc_fence_after();
+            const uint64_t wdesc = desc + (uint32_t)stage * (uint32_t)(Plan::kStageBytes >> 4), adesc = wdesc + (Plan::kWBytes >> 4);
+            const uint32_t empty = empty_bar(stage);
+            const bool last = number == 3 || kb == kb1 - 1;
+            if (++stage == kStages) { stage = 0; phase ^= 1u; }
+            if (one) {
+#pragma unroll
+              for (int j = 0; j < 4; ++j)  // 32 channels: 32 bytes further inside the swizzled row
+                umma_e4m3<CG>(to, wdesc + 2 * j, adesc + 2 * j, e4m3_idesc(CG * kTileN, BN, number), scales, scales + 4, j != 0 ? 1u : more);
+              commit(empty);
+              if (last) commit(free_scales);
+              if (kb == kb1 - 1) commit(tfull_bar(acc));
+            }
+            __syncwarp();
+            more = 1;
+            // The next stage (and scales) are looked for while these products run: the queue of products is short, and
+            // waiting behind them would leave the tensor cores idle for the time of a look.
+            full_seen = seen(full_bar(stage), phase);
+            if (last) scales_seen = seen(sfull_bar(buf), buf_phase);
           }
         }
         if (!ok) break;
-        commit(tfull_bar(acc));
         if (++acc == 2) { acc = 0; acc_phase ^= 1u; }
       }
       if (!ok) {  // products in flight end before tensor memory is given back
-        commit(drain_bar);
+        if (one) commit(drain_bar);
+        __syncwarp();
         for (uint32_t it = 0; it < kWaitLimit && !mbar_try_wait(drain_bar, 0); ++it) {}
       }
     }
@@ -543,6 +547,7 @@ __global__ void __launch_bounds__(kGemmThreads, 1) gemm_e4m3_kernel(const __grid
       }
       tc_fence_after();
       const uint32_t from = tmem + lanes_at + acc * BN;
+      const int begin = turn ^ (acc << 1);  // (14 pieces for four turns: those that take one more change with the tile)
       if (wide_rows && n0 + kTileN <= p.n) {
         float b4[4] = {0.f, 0.f, 0.f, 0.f};  // of this thread's lanes of the fragments
         if (p.bias) {
@@ -551,17 +556,18 @@ __global__ void __launch_bounds__(kGemmThreads, 1) gemm_e4m3_kernel(const __grid
           for (int i = 0; i < 4; ++i)
             b4[i] = __ldg(p.bias + first + 8 * i);
         }
-        __nv_bfloat16* to = reinterpret_cast<__nv_bfloat16*>(p.out) + (long)(m0 + turn * 16 + row_out) * p.ldc + n0 + chunk_out * 8;
+        __nv_bfloat16* to = reinterpret_cast<__nv_bfloat16*>(p.out) + (long)(m0 + begin * 16 + row_out) * p.ldc + n0 + chunk_out * 8;
         auto copy_out = [&](uint32_t from_smem, bool exists) {
           uint4 u;
           ld_shared_v4(from_smem, u.x, u.y, u.z, u.w);
           if (exists) *reinterpret_cast<uint4*>(to) = u;
         };
-        auto fetch = [&](int c, uint32_t (&r)[16]) {
+#pragma unroll 1
+        for (int c = begin * 16; c < stop; c += 16 * kEpiTurns) {
+          uint32_t r[16];
           tmem_ld_fragments(from + c, r);
           tmem_ld_fragments(from + (16u << 16) + c, r + 8);
-        };
-        auto piece = [&](int c, const uint32_t (&r)[16]) {
+          tmem_ld_wait();
           float v[16];
           uint32_t word[8];  // [lanes 0 .. 7, 8 .. 15, 16 .. 23, 24 .. 31] of eight columns, then of the next eight
 #pragma unroll
@@ -586,22 +592,6 @@ __global__ void __launch_bounds__(kGemmThreads, 1) gemm_e4m3_kernel(const __grid
           to += two_rows;
           copy_out(out_b + side, c + row_out + 2 < stop);
           to += next_piece;
-        };
-        uint32_t even[16], odd[16];
-        int c = turn * 16;
-        constexpr int kStep = 16 * kEpiTurns;
-        if (c < stop) fetch(c, even);
-#pragma unroll 1
-        while (c < stop) {
-          tmem_ld_wait();
-          if (c + kStep < stop) fetch(c + kStep, odd);
-          piece(c, even);
-          c += kStep;
-          if (c >= stop) break;
-          tmem_ld_wait();
-          if (c + kStep < stop) fetch(c + kStep, even);
-          piece(c, odd);
-          c += kStep;
         }
       } else {
         const float bias = p.bias && col < p.n ? __ldg(p.bias + col) : 0.f;
