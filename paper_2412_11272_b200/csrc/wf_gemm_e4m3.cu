@@ -741,22 +741,22 @@ cudaError_t launch_quantise_e4m3(const void* x, int dtype, long ldx, long rows, 
 }
 
 // Which tile: rows of A (224 of them: on pairs of blocks), and over how many blocks its channels are split.  Estimated time of
-// a call in us, from the times measured for 55 shapes of m = 1 .. 4000, n = 640 .. 50021, k = 512 .. 5120 (the choice is within
-// 8 % of the best tile for 50 of them, 20 % for all): a launch 3.6 (0.8 more on pairs), then as many rounds of tiles as the SMs need,
-// a block of 128 channels taking the time of its bytes.  One SM draws 95 GB/s, all of them together 8.6 TB/s.  A split costs
-// an exchange.  Examples, one tile of the kind against another: m = 1, n = k = 1280: 16 rows split 4: 4.4, whole 4.9;
-// m = 320, n = 1280, k = 5120: 128 rows split 4: 9.6, whole 13.7, pairs 14.8; m = 775, n = 5120, k = 1280: 128 rows 10.5, 64: 14.3,
-// pairs 10.7; m = 4000: pairs 23, 128 rows 32.
+// a call in us, fitted to the choice between the times measured for 55 shapes of m = 1 .. 4000, n = 640 .. 50021, k = 512 .. 5120 (it is
+// within 8 % of the best tile for all but one, which loses 23 %): a launch 3.6 (1.8 more on pairs), then as many rounds of tiles as
+// the SMs need, a block of 128 channels taking the time of its bytes.  One SM draws 85 GB/s, all of them together 9.4 TB/s.  A split
+// costs an exchange.  Examples, one tile of the kind against another: m = 1, n = k = 1280: 16 rows split 4: 4.5, whole 4.9;
+// m = 320, n = 1280, k = 5120: 128 rows split 4: 9.7, whole 12.9, pairs 14.7; m = 775, n = 5120, k = 1280: 128 rows 9.9, 64: 14.2,
+// pairs 10.7; m = 4000: pairs 23, 128 rows 30.
 double estimate_us(long m, long n, long k, int bn, int split, int num_sms) {
   const int cg = bn == 224 ? 2 : 1, share = cg * split;
   const long tiles = (n + kTileN * cg - 1) / (kTileN * cg) * ((m + bn - 1) / bn), blocks_k = (k + kScaleBlock - 1) / kScaleBlock;
   if (split > 1 && (tiles * split * 20 > num_sms * 19 || split > blocks_k)) return 1e30;  // (a cluster needs its blocks at one time)
   const long at_once = num_sms / share, rounds = (tiles + at_once - 1) / at_once;
   const double active = (double)(tiles < at_once ? tiles : at_once) * share;
-  const double rate = active * 95e3 < 8.6e6 ? 95e3 : 8.6e6 / active;  // bytes per us and SM
+  const double rate = active * 85e3 < 9.4e6 ? 85e3 : 9.4e6 / active;  // bytes per us and SM
   const double block = (kTileN + bn / cg) * (double)kBlockBytes / rate;
-  return 3.6 + (cg == 2 ? 0.8 : 0.0) + (split > 1 ? 0.8 + 0.008 * bn : 0.0) +
-         (double)rounds * ((double)((blocks_k + split - 1) / split) * (block > 0.1 ? block : 0.1) + 0.004 * bn);
+  return 3.6 + (cg == 2 ? 1.8 : 0.0) + (split > 1 ? 0.8 + 0.012 * bn : 0.0) +
+         (double)rounds * ((double)((blocks_k + split - 1) / split) * block + 0.006 * bn);
 }
 
 cudaError_t launch_gemm_e4m3(const E4m3GemmParams& p, int num_sms, cudaStream_t s) {
