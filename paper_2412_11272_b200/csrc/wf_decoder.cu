@@ -487,6 +487,7 @@ wf_status wf_draft_commit(wf_decoder* d, int n_seq, const int* start, const int*
   const bool in_place = lengths == start;
   if (!in_place && lengths < start + n_seq && start < lengths + n_seq)
     return fail(d, WF_ERR_INVALID_ARG, "wf_draft_commit: lengths may be start itself, but not overlap it otherwise");
+  if (lengths < kept + n_seq && kept < lengths + n_seq) return fail(d, WF_ERR_INVALID_ARG, "wf_draft_commit: lengths and kept share memory");
   const wf_decoder_config& c = d->cfg;
   CommitPlan p{};
   p.n_seq = n_seq;

@@ -751,7 +751,7 @@ double estimate_us(long m, long n, long k, int bn, int split, int num_sms) {
   const int cg = bn == 224 ? 2 : 1, share = cg * split;
   const long tiles = (n + kTileN * cg - 1) / (kTileN * cg) * ((m + bn - 1) / bn), blocks_k = (k + kScaleBlock - 1) / kScaleBlock;
   if (split > 1 && (tiles * split * 20 > num_sms * 19 || split > blocks_k)) return 1e30;  // (a cluster needs its blocks at one time)
-  const long at_once = num_sms / share, rounds = (tiles + at_once - 1) / at_once;
+  const long at_once = num_sms > share ? num_sms / share : 1, rounds = (tiles + at_once - 1) / at_once;
   const double active = (double)(tiles < at_once ? tiles : at_once) * share;
   const double rate = active * 85e3 < 9.4e6 ? 85e3 : 9.4e6 / active;  // bytes per us and SM
   const double block = (kTileN + bn / cg) * (double)kBlockBytes / rate;

@@ -88,7 +88,7 @@ __global__ void __launch_bounds__(kPlanThreads) page_plan_kernel(const __grid_co
     int need = 0;
     if (want > 0) {
       const long long end = (long long)l + want;
-      if (end > (long long)p.table_stride * page) {
+      if (end > (long long)p.table_stride * page || end > INT_MAX) {
         problems |= kBadRows;
         want = 0;
       } else {

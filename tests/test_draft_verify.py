@@ -79,7 +79,7 @@ def test_commit_refusals():
         a = {**base, **kw}
         return d.lib.wf_draft_commit(*(a[k] for k in base))
 
-    for bad in (dict(h=None), dict(n=-1), dict(nc=-1), dict(start=None), dict(kept=None), dict(stride=0), dict(lengths=None), dict(lengths=P + 4), dict(caches=None),
+    for bad in (dict(h=None), dict(n=-1), dict(nc=-1), dict(start=None), dict(kept=None), dict(stride=0), dict(lengths=None), dict(lengths=P + 4), dict(kept=P + 68), dict(caches=None),
                 dict(table=None), dict(ts=0), dict(caches=twice, nc=2), dict(caches=other, nc=2), dict(caches=(Bn.wf_cache * 1)(Bn.wf_cache(P, P, P, P + 16, 3)))):
         assert call(**bad) == 1, bad
     assert call(n=65536) == 4 and call(stride=1025) == 4 and call(n=0) == 0 and call(n=0, caches=two, nc=2) == 0

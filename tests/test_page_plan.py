@@ -206,3 +206,20 @@ def test_captured_and_replayed_on_another_stream(rows):
         graph.replay()
         torch.cuda.synchronize()
         st.check(dev, out, st.plan(w, rows, gone), status)
+
+
+@pytest.mark.gpu
+def test_positions_that_pass_31_bits():
+    """A sequence of nearly 2^31 positions: rows up to the last of them, none beyond."""
+    from paper_2412_11272_b200.binding import PagePool
+    dec, stride, first = _decoder(256), (1 << 23) + 4, 2 ** 31 - 300
+    table = torch.arange(stride, dtype=torch.int32, device="cuda")[None].contiguous()
+    for new, rows in ((299, 400), (300, 400), (299, 3000), (2000, 3000)):
+        pool, held, lengths = PagePool(_dev([0] * (stride + 5)), _dev([0, 0])), _dev([stride]), _dev([first])
+        status = torch.zeros(1, dtype=torch.int32, device="cuda")
+        cu, _, pos, slot = dec.wf_page_plan(pool, table, held, lengths, _dev([new]), rows, status=status)
+        if new == 299:
+            assert int(status) == 0 and cu.tolist() == [0, 299] and pos[:299].tolist() == list(range(first, first + 299))
+            assert slot[:299].tolist() == list(range(first, first + 299)) and (slot[299:] == -1).all()
+        else:
+            assert int(status) == 2 and cu.tolist() == [0, 0] and (pos == -1).all()
