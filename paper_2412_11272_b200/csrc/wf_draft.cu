@@ -356,33 +356,44 @@ __global__ void __launch_bounds__(kVerThreads, 2) draft_verify_kernel(const __gr
       uint4 raw[kAhead];
 #pragma unroll
       for (int a = 0; a < kAhead; ++a) raw[a] = x.load(u0 + a < length ? mine + (u0 + a) * 32 : x.pieces);
+      if (greedy) {
 #pragma unroll
-      for (int a = 0; a < kAhead; ++a) {
-        float y[kVec];
-        VecOf<T>::unpack(raw[a], y);
-        if (greedy) {
+        for (int a = 0; a < kAhead; ++a) {
+          if (u0 + a >= length) break;
+          float y[kVec];
+          VecOf<T>::unpack(raw[a], y);
 #pragma unroll
           for (int e = 0; e < kVec; ++e) {
             if (y[e] > top) top = y[e], at = x.first(mine + (u0 + a) * 32) + e;
             sum += y[e] != y[e] ? y[e] : 0.f;  // a NaN shows
           }
-        } else {
-          float high = top;
-#pragma unroll
-          for (int e = 0; e < kVec; ++e) high = fmaxf(high, y[e]);
-          if (high > -INFINITY) {
-            if (high > top) sum *= exp2f((top - high) * per_t_log2);
-            float part = 0.f;
-#pragma unroll
-            for (int e = 0; e < kVec; ++e) part += ptx::ex2_approx((y[e] - high) * per_t_log2);
-            sum += part;
-            top = high;
-          } else {
-#pragma unroll
-            for (int e = 0; e < kVec; ++e) sum += y[e] != y[e] ? y[e] : 0.f;
-          }
         }
+        continue;
       }
+      float high = top;  // of all the pieces first: one rescaling, and no chain from piece to piece
+#pragma unroll
+      for (int a = 0; a < kAhead; ++a) {
+        if (u0 + a >= length) break;
+        float y[kVec];
+        VecOf<T>::unpack(raw[a], y);
+#pragma unroll
+        for (int e = 0; e < kVec; ++e) high = fmaxf(high, y[e]);
+      }
+      if (high > top) sum *= exp2f((top - high) * per_t_log2);
+      const float from = high > -INFINITY ? high : 0.f;  // (nothing but -infinity: no weight; a NaN shows)
+      float part[kAhead];
+#pragma unroll
+      for (int a = 0; a < kAhead; ++a) {
+        part[a] = 0.f;
+        if (u0 + a >= length) continue;
+        float y[kVec];
+        VecOf<T>::unpack(raw[a], y);
+#pragma unroll
+        for (int e = 0; e < kVec; ++e) part[a] += ptx::ex2_approx((y[e] - from) * per_t_log2);
+      }
+#pragma unroll
+      for (int a = 0; a < kAhead; ++a) sum += part[a];
+      top = high;
     }
     // (as ordered integers: one instruction takes the largest of a warp)
     const int bits = __float_as_int(top), order = bits ^ ((bits >> 31) & 0x7fffffff), most = __reduce_max_sync(0xffffffffu, order);
