@@ -607,7 +607,7 @@ class ScaledCodes:
     ``Decoder.wf_quantise_e4m3``, or from codes of other origin by ``pack``.
     It stands for the tensors' memory as it is when it is made, as a KvCache does."""
 
-    __slots__ = ("codes", "scales", "shape", "device", "c")
+    __slots__ = ("_codes", "_scales", "_memory", "shape", "device", "c")
 
     def __init__(self, codes: torch.Tensor, scales: torch.Tensor):
         if codes.dim() != 2 or codes.dtype is not _E4M3 or codes.shape[1] < 1 or (codes.stride(1) != 1 and codes.shape[1] > 1):
@@ -616,22 +616,37 @@ class ScaledCodes:
         if scales.dtype is not _U8 or scales.device != codes.device or scales.shape != ((k + 511) // 512, rows, 4) or \
                 (rows > 0 and (scales.stride(2) != 1 or (rows > 1 and scales.stride(1) != 4) or (k > 512 and scales.stride(0) % 4))):
             _refuse("scales must be uint8 [ceil(k / 512), rows, 4] beside their codes, the words of consecutive rows side by side")
-        self._set(codes, scales, rows, k, codes.device, codes.stride(0) if rows > 1 else (k + 15) // 16 * 16,
-                  scales.stride(0) // 4 if k > 512 else max(rows, 1))
+        self._codes, self._scales, self._memory, self.shape, self.device = codes, scales, None, (rows, k), codes.device
+        self.c = wf_e4m3(codes.data_ptr(), scales.data_ptr(), codes.stride(0) if rows > 1 else (k + 15) // 16 * 16,
+                         scales.stride(0) // 4 if k > 512 else max(rows, 1)) if self.device.type == "cuda" else None
 
-    def _set(self, codes, scales, rows, k, device, ld, scale_ld):
-        put = object.__setattr__
-        put(self, "codes", codes)
-        put(self, "scales", scales)
-        put(self, "shape", (rows, k))
-        put(self, "device", device)
-        put(self, "c", wf_e4m3(codes.data_ptr(), scales.data_ptr(), ld, scale_ld) if device.type == "cuda" else None)
+    @classmethod
+    def _within(cls, memory: torch.Tensor, rows: int, k: int, device):
+        """Codes (rows padded to 16 bytes) and, behind them, scales in bytes of one tensor; the views of it are made when they are asked for."""
+        self, ld = cls.__new__(cls), (k + 15) // 16 * 16
+        self._codes = self._scales = None
+        self._memory, self.shape, self.device = memory, (rows, k), device
+        at = memory.data_ptr()
+        self.c = wf_e4m3(at, at + rows * ld, ld, rows) if device.type == "cuda" else None
         return self
 
-    def __setattr__(self, name, value):  # the descriptor holds the tensors' addresses
-        raise AttributeError(f"{name} of ScaledCodes is fixed: make others for other tensors")
+    @staticmethod
+    def _bytes(rows: int, k: int) -> int:
+        return rows * ((k + 15) // 16 * 16 + (k + 511) // 512 * 4)
 
-    __delattr__ = KvCache.__delattr__
+    @property
+    def codes(self) -> torch.Tensor:
+        if self._codes is None:
+            (rows, k), ld = self.shape, self.c.ld if self.c else (self.shape[1] + 15) // 16 * 16
+            self._codes = self._memory[:rows * ld].view(_E4M3).view(rows, ld)[:, :k]
+        return self._codes
+
+    @property
+    def scales(self) -> torch.Tensor:
+        if self._scales is None:
+            rows, k = self.shape
+            self._scales = self._memory[rows * ((k + 15) // 16 * 16):].view((k + 511) // 512, rows, 4)
+        return self._scales
 
     def __getitem__(self, rows: slice):
         """Some of the rows."""
@@ -642,8 +657,8 @@ class ScaledCodes:
     @classmethod
     def empty(cls, rows: int, k: int, device="cuda"):
         """Room for a matrix, rows padded to 16 bytes."""
-        codes = torch.empty((rows, (k + 15) // 16 * 16), dtype=_U8, device=device).view(_E4M3)[:, :k]
-        return cls(codes, torch.empty(((k + 511) // 512, rows, 4), dtype=_U8, device=device))
+        memory = torch.empty(cls._bytes(rows, k), dtype=_U8, device=device)
+        return cls._within(memory, rows, k, memory.device)
 
     @classmethod
     def pack(cls, codes: torch.Tensor, scales: torch.Tensor):
@@ -1019,10 +1034,7 @@ class Decoder:
             _refuse("x must be float32 or bfloat16 [rows, k] in device memory, a row's elements contiguous")
         rows, k = shape
         if out is None:
-            ld, groups = (k + 15) // 16 * 16, (k + 511) // 512
-            codes = self._empty(x, (rows, ld), _E4M3, stream)
-            out = ScaledCodes.__new__(ScaledCodes)._set(codes if ld == k else codes[:, :k], self._empty(x, (groups, rows, 4), _U8, stream), rows, k,
-                                                        device, ld, max(rows, 1))
+            out = ScaledCodes._within(self._empty(x, ScaledCodes._bytes(rows, k), _U8, stream), rows, k, device)
         elif out.shape != (rows, k) or out.device != device:
             _refuse("out must have the shape and the device of x")
         self._call(self.lib.wf_quantise_e4m3, device, stream, x.data_ptr(), WF_BF16 if dtype is _BF16 else WF_F32,
@@ -1040,7 +1052,7 @@ class Decoder:
             if out_dtype not in (None, "bf16", "f32"):
                 _refuse("out_dtype is bf16 or f32")
             dtype, ld = self.torch_dtype if out_dtype is None else _BF16 if out_dtype == "bf16" else _F32, n
-            out = self._empty(a.scales, (m, n), dtype, stream)
+            out = self._empty(a._codes if a._memory is None else a._memory, (m, n), dtype, stream)
         elif out.shape != (m, n) or out.dtype not in (_F32, _BF16) or out.device != device or (out.stride(1) != 1 and n > 1):
             _refuse(f"out must be float32 or bfloat16 [{m}, {n}] on {device}, a row's elements contiguous")
         elif out_dtype is not None and out.dtype is not (_BF16 if out_dtype == "bf16" else _F32):
