@@ -306,9 +306,9 @@ __device__ __forceinline__ void finish_nan(const E4m3GemmParams& p, int r0, int 
 // CG = 2: a pair of blocks shares a tile of 256 rows of W by BN of A, each block stages its own 128 rows of W and half of A's.
 // The copies of both signal the first block's barriers, which alone issues the products; its commits reach both.
 // The queue of products is short: what the issuing warp does between two stages shows (it walks whole, so that descriptors stay in
-// uniform registers: 344 us with a single lane, 287 so, 49,600 x 5120 x 1280), and the epilogue shares its schedulers.  That product
-// takes 251 to 268 us (2.4 to 2.6 PFLOP/s at 1.3 GHz under the power cap) and 291 to 300 with GELU; with 5120 channels for 1280, n
-// and k exchanged, 225 us, 95 % of the tensor cores' cycles.  64 rows by 50,021 x 1280: 15 us, 79 % of the copy rate.
+// uniform registers: without GELU 344 us with a single lane, 287 so, 49,600 x 5120 x 1280), and the epilogue shares its schedulers.
+// That product takes 251 to 265 us (2.45 to 2.6 PFLOP/s, near 1.3 GHz under the power cap) and 291 to 300 with GELU; n and k
+// exchanged 225 to 238 us, products for 92 % of the cycles.  64 rows by 50,021 x 1280: 15 us, with the output 78 % of the copy rate.
 // kSplit: a cluster of blocks shares a tile, each has a part of the channels; every block sums a part of the columns, in the
 // order of the blocks, from what the others leave in its shared memory.
 template <int BN, int CG, bool kSplit>
