@@ -602,8 +602,9 @@ typedef struct {
 wf_status wf_quantise_e4m3(wf_decoder *dec, const void *x, int x_dtype, long ldx, long rows, int k, const wf_e4m3 *out, void *stream);
 
 /* wf_gemm_e4m3: C[m, n] = act(A W^T + bias), A [m, k], W [n, k]: the decoder's projections.  Products of codes and scales are
- * exact, sums are the tensor cores' float32; act is the erf-form GELU if `gelu`, and C (out_dtype: float32 or bfloat16) is rounded
- * once.  bias: dev float32 [n] or NULL.  C's rows are ldc elements apart, any alignment of its type; nothing behind a row's n
+ * exact, sums are the tensor cores' float32; act is the erf-form GELU if `gelu` (for bfloat16 outputs within 8e-6 of it, relative, down to
+ * sums of -5, within half a step of bfloat16 down to -8, and 0 below -16; NaN of -infinity), and C (out_dtype: float32 or bfloat16) is
+ * rounded once.  bias: dev float32 [n] or NULL.  C's rows are ldc elements apart, any alignment of its type; nothing behind a row's n
  * elements is written.  A NaN scale or code makes the sums that it is part of NaN. */
 wf_status wf_gemm_e4m3(wf_decoder *dec, const wf_e4m3 *a, const wf_e4m3 *w, const float *bias, void *out, int out_dtype, long ldc, long m,
                        int n, int k, int gelu, int *status, void *stream);

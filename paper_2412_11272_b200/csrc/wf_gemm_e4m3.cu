@@ -222,23 +222,24 @@ __device__ __forceinline__ uint32_t scale_word(const E4m3Operand& x, long row, l
 }
 
 // GELU for bfloat16 outputs, two values: x Phi(x) = max(x, 0) - |x| h, h = erfc(|x| / sqrt 2) / 2 = 2^q with q(|x|) a polynomial
-// of degree 5 fitted to log2 h over [0, 5.5] (minimax of the relative error: 1.6e-4 up to |x| = 4.2, 2.1e-3 at 5.5, behind which
-// h is held: |x| h < 3e-7).  A twelfth of half a step of bfloat16, in the tail as well, for six instructions a value;
-// erff takes some 30, which would bound the kernel (at 1280 channels a tile's products take 20 issue slots per value of C).
+// of degree 7 fitted to log2 h over [0, 7], evaluated in float32: relative error 4e-6 up to |x| = 3, 8e-6 to 5, 6e-5 to 7, 4e-3 at
+// 8; from there it falls faster than h does, to 0 at 16.  Half a step of bfloat16 is 4e-3.  (Degree 5 over [0, 5.5] was one
+// instruction a value shorter, but 1.6e-4 off, and a constant below -5.5.)  Some eight instructions a value; erff takes some 30, which would
+// bound the kernel (at 1280 channels a tile's products take 20 issue slots per value of C).  NaN for NaN and -infinity, as gelu_erf.
 __device__ __forceinline__ void gelu_pair(float& x0, float& x1) {
   auto both = [](float c) { return pack_f32x2(c, c); };
-  const float n0 = fmaxf(-fabsf(x0), -5.5f), n1 = fmaxf(-fabsf(x1), -5.5f);
-  const uint64_t n = pack_f32x2(n0, n1);
-  uint64_t q = fma_f32x2(n, both(2.69073704e-04f), both(5.29495657e-03f));
-  q = fma_f32x2(n, q, both(4.63313932e-02f));
-  q = fma_f32x2(n, q, both(-4.66863768e-01f));
-  q = fma_f32x2(n, q, both(1.14782169f));
-  q = fma_f32x2(n, q, both(-1.00022509f));
-  float q0, q1, p0, p1;
+  const uint64_t n = pack_f32x2(fmaxf(-fabsf(x0), -16.f), fmaxf(-fabsf(x1), -16.f));
+  uint64_t q = fma_f32x2(n, both(1.76883373e-06f), both(6.03389999e-05f));
+  q = fma_f32x2(n, q, both(9.21197818e-04f));
+  q = fma_f32x2(n, q, both(8.47389456e-03f));
+  q = fma_f32x2(n, q, both(5.38961962e-02f));
+  q = fma_f32x2(n, q, both(-4.58523482e-01f));
+  q = fma_f32x2(n, q, both(1.15122795f));
+  q = fma_f32x2(n, q, both(-0.999997795f));
+  float q0, q1;
   unpack_f32x2(q, q0, q1);
-  asm("max.NaN.f32 %0, %1, %2;" : "=f"(p0) : "f"(x0), "f"(0.f));  // (a NaN stays one)
-  asm("max.NaN.f32 %0, %1, %2;" : "=f"(p1) : "f"(x1), "f"(0.f));
-  unpack_f32x2(fma_f32x2(n, pack_f32x2(ex2_approx(q0), ex2_approx(q1)), pack_f32x2(p0, p1)), x0, x1);
+  const uint64_t p = fma_f32x2(pack_f32x2(x0, x1), both(0.5f), pack_f32x2(0.5f * fabsf(x0), 0.5f * fabsf(x1)));  // max(x, 0), exactly
+  unpack_f32x2(fma_f32x2(n, pack_f32x2(ex2_approx(q0), ex2_approx(q1)), p), x0, x1);
 }
 
 // Bias and activation of NC accumulator columns, and their store: v[i] belongs to row r0 + i of C and to this lane's column.
