@@ -473,7 +473,8 @@ wf_status wf_tree_attention(wf_decoder *dec, const wf_cache *cache, const wf_row
 
 /* Exercises the failure path behind status bit 8 without any fault: while `on` is not 0, every bounded wait of the
  * handle's following wf_tree_attention calls gives up at once (where the call runs on 128-row tiles, the only ones that wait),
- * and every one of its wf_gemm_e4m3 calls.
+ * and every one of its wf_gemm_e4m3 calls.  on = -1 - w: in wf_gemm_e4m3 only the waits of every block's warp w (0 .. 21) give up at
+ * once, the others after 4096 looks, so that some warps go on while others have given up.
  * Such a call ends normally, its rows are NaN, and the handle stays usable; 0 restores the ordinary limit. */
 wf_status wf_selftest_attention_timeout(wf_decoder *dec, int on);
 

@@ -883,8 +883,9 @@ class Decoder:
             self._workspace_bytes[key] = n.value
         return self._workspace_bytes[key]
 
-    def wf_selftest_attention_timeout(self, on: bool = True):
-        """While on, the bounded waits of ``wf_tree_attention`` on 128-row tiles give up at once: rows are NaN, status bit 8."""
+    def wf_selftest_attention_timeout(self, on: bool | int = True):
+        """While on, the bounded waits of ``wf_tree_attention`` on 128-row tiles and of ``wf_gemm_e4m3`` give up at once: rows are NaN, status
+        bit 8.  -1 - w: in ``wf_gemm_e4m3`` at first those of warp w alone."""
         self._check(self.lib.wf_selftest_attention_timeout(self.handle, int(on)))
 
     def wf_beam_select(self, logits: torch.Tensor, scores: torch.Tensor, keep: int, beams=None, finished=None, end_token: int = -1,

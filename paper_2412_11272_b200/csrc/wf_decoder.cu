@@ -12,7 +12,7 @@ using namespace wf;
 
 struct wf_decoder {
   wf_decoder_config cfg;
-  bool no_waits;  // wf_selftest_attention_timeout
+  int no_waits;  // wf_selftest_attention_timeout
   char err[512];
 };
 
@@ -107,7 +107,7 @@ wf_status wf_decoder_create(const wf_decoder_config* cfg, wf_decoder** out) {
   wf_decoder* d = new (std::nothrow) wf_decoder();
   if (!d) return WF_ERR_INVALID_ARG;
   d->cfg = *cfg;
-  d->no_waits = false;
+  d->no_waits = 0;
   d->err[0] = 0;
   *out = d;  // returned even on failure so that the caller can read the message, then destroy
   const wf_decoder_config& c = d->cfg;
@@ -253,7 +253,7 @@ wf_status wf_tree_attention(wf_decoder* d, const wf_cache* cache, const wf_rows*
 
 wf_status wf_selftest_attention_timeout(wf_decoder* d, int on) {
   if (!d) return WF_ERR_INVALID_ARG;
-  d->no_waits = on != 0;
+  d->no_waits = on;
   return WF_OK;
 }
 
@@ -571,7 +571,8 @@ wf_status wf_gemm_e4m3(wf_decoder* d, const wf_e4m3* a, const wf_e4m3* w, const 
   p.out_dtype = out_dtype;
   p.ldc = ldc;
   p.status = status;
-  p.wait_limit = d->no_waits ? 0 : ptx::kWaitLimit;
+  p.wait_limit = d->no_waits > 0 ? 0 : d->no_waits < 0 ? 1u << 12 : ptx::kWaitLimit;
+  p.hasty_warp = d->no_waits < 0 ? -1 - d->no_waits : -1;
   return cuda_result(d, "wf_gemm_e4m3", launch_gemm_e4m3(p, sms, (cudaStream_t)stream));
 }
 

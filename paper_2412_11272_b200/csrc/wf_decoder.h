@@ -210,6 +210,7 @@ struct E4m3GemmParams {
   long ldc;
   int* status;
   unsigned wait_limit;
+  int hasty_warp;  // a warp that gives up at its first wait (-1: none)
 };
 cudaError_t launch_gemm_e4m3(const E4m3GemmParams& p, int num_sms, cudaStream_t s);
 

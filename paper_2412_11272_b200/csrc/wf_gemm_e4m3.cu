@@ -374,15 +374,23 @@ __global__ void __launch_bounds__(kGemmThreads, 1) gemm_e4m3_kernel(const __grid
   const int tile0 = (int)blockIdx.x / share, tile_step = (int)gridDim.x / share;
   const int kb0 = kSplit ? (int)((long)rank * num_k / split) : 0, kb1 = kSplit ? (int)((long)(rank + 1) * num_k / split) : num_k;
   auto wait = [&](uint32_t bar, uint32_t parity) { return mbar_wait_limited(bar, parity, abort_flag, p.wait_limit); };
+  // Whether a warp begins at all.  (A limit of its own for each warp would say the same, and cost 0.4 us a call.)
+  auto begins = [&]() {
+    if (warp != p.hasty_warp) return true;
+    *abort_flag = 1;
+    return false;
+  };
   bool done = true;  // epilogue warps of a split: the accumulator is complete
+  uint32_t armed = 0, armed_parity = 0;  // copying lane: stages that copies went to, and the parity of the last ones
+  bool one = false;                      // the lane that issues the products
 
   if (warp == kCopyWarp) {
     if (lane == 0) {
       prefetch_tmap(&tmap_w);
       prefetch_tmap(&tmap_a);
       int stage = 0;
-      uint32_t phase = 0, armed = 0, armed_parity = 0;
-      bool ok = true;
+      uint32_t phase = 0;
+      bool ok = begins();
       for (int tile = tile0; ok && tile < num_tiles; tile += tile_step) {
         const int n0 = (tile % num_w * CG + (CG == 2 ? rank : 0)) * kTileN;
         const int m0 = tile / num_w * BN + (CG == 2 ? rank * (BN / 2) : 0);
@@ -404,19 +412,11 @@ __global__ void __launch_bounds__(kGemmThreads, 1) gemm_e4m3_kernel(const __grid
           if (++stage == kStages) { stage = 0; phase ^= 1u; }
         }
       }
-      // After giving up: no copy may land once the block has gone.  (The second block of a pair sees its copies only by their
-      // stages being released; what is still in flight has the time of that bounded wait.)
-      if (!ok)
-        for (int s = 0; s < kStages; ++s)
-          if (armed >> s & 1u) {
-            const uint32_t bar = CG == 2 && rank == 1 ? empty_bar(s) : full_bar(s);
-            for (uint32_t it = 0; it < (CG == 2 ? 1u << 16 : kWaitLimit) && !mbar_try_wait(bar, armed_parity >> s & 1u); ++it) {}
-          }
     }
   } else if (warp == kMathWarp) {
     // The whole warp walks along (so that descriptors stay in uniform registers), one lane issues.
     if (CG == 1 || rank == 0) {
-      const bool one = elect_one();
+      one = elect_one();
       auto commit = [&](uint32_t bar) {  // (by the electing lane)
         if constexpr (CG == 2) umma_commit_pair(bar, 3);
         else umma_commit(bar);
@@ -426,7 +426,7 @@ __global__ void __launch_bounds__(kGemmThreads, 1) gemm_e4m3_kernel(const __grid
       const uint64_t desc = umma_desc_k_sw128(0) + ((smem_base & 0x3ffff) >> 4);
       int stage = 0, acc = 0, buf = 0;
       uint32_t phase = 0, acc_phase = 0, buf_phase = 0;
-      bool ok = true, full_seen = false, scales_seen = false;
+      bool ok = begins(), full_seen = false, scales_seen = false;
       for (int tile = tile0; ok && tile < num_tiles; tile += tile_step) {
         if (!ready(tempty_bar(acc), acc_phase ^ 1u)) { ok = false; break; }
         const uint32_t to = tmem + acc * BN;
@@ -464,17 +464,12 @@ __global__ void __launch_bounds__(kGemmThreads, 1) gemm_e4m3_kernel(const __grid
         if (!ok) break;
         if (++acc == 2) { acc = 0; acc_phase ^= 1u; }
       }
-      if (!ok) {  // products in flight end before tensor memory is given back
-        if (one) commit(drain_bar);
-        __syncwarp();
-        for (uint32_t it = 0; it < kWaitLimit && !mbar_try_wait(drain_bar, 0); ++it) {}
-      }
     }
   } else if (warp >= kScaleWarp) {
     const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
     int buf = 0;
     uint32_t buf_phase = 0;
-    bool ok = true;
+    bool ok = begins();
     // words are loaded two groups ahead: a load takes longer than the products of a group
     struct Words {
       uint32_t w[4], a[8];
@@ -525,7 +520,7 @@ __global__ void __launch_bounds__(kGemmThreads, 1) gemm_e4m3_kernel(const __grid
     const int quarter = warp & 3, turn = warp >> 2;
     int acc = 0, pieces = 0;
     uint32_t acc_phase = 0;
-    bool ok = true;
+    bool ok = begins();
     // What does not depend on the tile.  Pieces of 16 rows by 128 columns: in shared memory a row is two halves of 128 bytes,
     // 16-byte chunks exclusive-or'd with the row against bank conflicts.  A thread names a row of a matrix to be stored, and
     // copies a chunk of two rows out.
@@ -624,7 +619,7 @@ __global__ void __launch_bounds__(kGemmThreads, 1) gemm_e4m3_kernel(const __grid
     // ---- a split: this block's sums of every other block's columns go there (one tile per cluster).  Partial sums of block r
     // lie at [r][column / 4][row][4] of the receiving block.
     const int quarter = warp & 3, turn = warp >> 2, row = quarter * 32 + lane, mine = BN / split;
-    done = __all_sync(0xffffffffu, wait(tfull_bar(0), 0));
+    done = begins() && __all_sync(0xffffffffu, wait(tfull_bar(0), 0));
     tc_fence_after();
     const uint32_t from = tmem + ((uint32_t)(quarter * 32) << 16);
 #pragma unroll 1
@@ -649,8 +644,39 @@ __global__ void __launch_bounds__(kGemmThreads, 1) gemm_e4m3_kernel(const __grid
 
   tc_fence_before();
   __syncwarp();
+  if constexpr (CG == 2) {  // what one block of a pair has given up, the other one hears of
+    __syncthreads();
+    if (threadIdx.x == 0 && *abort_flag) st_cluster_v2(map_to_cta(bars + 8u * Plan::kBars + 8u, rank ^ 1), 1u, 0u);
+    __syncwarp();
+  }
   if constexpr (CG == 2 || kSplit) cluster_sync_all();  // partial sums are there; nobody leaves while another one may still use its memory
   else __syncthreads();
+  if (*abort_flag) {
+    // Somebody has given up.  Copies and products in flight, which those who issued them need not have waited for, end before the
+    // block's memory and tensor memory are given back (where nobody has, the accumulators were complete, and so all copies).
+    // The second block of a pair sees its copies only by their stages being released, and the first one waits for both blocks'
+    // bytes: where these do not come, what is still in flight has the time of the looks, hundreds of microseconds or more.
+    if (warp == kCopyWarp && lane == 0) {
+      uint32_t looks = CG == 2 ? 1u << 14 : kWaitLimit;
+#pragma unroll 1
+      for (int s = 0; s < kStages; ++s)
+        if (armed >> s & 1u) {
+          const uint32_t bar = CG == 2 && rank == 1 ? empty_bar(s) : full_bar(s);
+          while (looks > 0 && !mbar_try_wait(bar, armed_parity >> s & 1u)) --looks;
+        }
+    } else if (warp == kMathWarp && (CG == 1 || rank == 0)) {
+      if (one) {
+        if constexpr (CG == 2) umma_commit_pair(drain_bar, 1);
+        else umma_commit(drain_bar);
+      }
+      __syncwarp();
+      for (uint32_t it = 0; it < kWaitLimit && !mbar_try_wait(drain_bar, 0); ++it) {}
+    }
+    if constexpr (CG == 2) {
+      __syncwarp();
+      cluster_sync_all();
+    }
+  }
   if (warp == kMathWarp) {
     tc_fence_after();
     if constexpr (CG == 2) tmem_dealloc_pair(tmem, 512);

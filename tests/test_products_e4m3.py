@@ -339,3 +339,33 @@ def test_gelu_is_rounded_once(m, pad):
     y = first[8:].double().numpy()
     off = np.flatnonzero((y < low) | (y > high))
     assert not len(off), (len(off), bias[8 + off[0]], y[off[0]], low[off[0]], high[off[0]])
+
+
+def _one_warp_gives_up(m, n, k, warp, gelu=False):
+    """A call in which at first one warp of every block gives up: it ends, says so, and the handle and the next call are as ever."""
+    from paper_2412_11272_b200.binding import STATUS_GAVE_UP
+    dec = _decoder()
+    a, w = _matrix(m, k, 1), _matrix(n, k, 2)
+    plain = dec.wf_gemm_e4m3(a, w, gelu=gelu)
+    status = torch.zeros(1, dtype=torch.int32, device="cuda")
+    got = torch.full_like(plain, 77.0)
+    dec.wf_selftest_attention_timeout(-1 - warp)
+    for _ in range(3):
+        got.fill_(77.0)
+        dec.wf_gemm_e4m3(a, w, gelu=gelu, out=got, status=status)
+    dec.wf_selftest_attention_timeout(False)
+    torch.cuda.synchronize()
+    assert int(status) == STATUS_GAVE_UP
+    status.zero_()
+    assert torch.equal(dec.wf_gemm_e4m3(a, w, gelu=gelu, status=status), plain) and int(status) == 0
+    return got, plain
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("warp", [16, 19, 20, 21])
+@pytest.mark.parametrize("m,n,k", [(1, 128, 512), (1, 1280, 5120), (64, 5000, 512), (775, 5120, 1280), (5000, 3000, 640)])
+def test_scales_copies_or_products_that_give_up(m, n, k, warp):
+    """Scales, copies or products: nothing is computed.  What is in flight when the products give up, every copy of a tile of few
+    channels among it, lands before the block has gone."""
+    got, _ = _one_warp_gives_up(m, n, k, warp)
+    assert got.isnan().all()
