@@ -242,6 +242,20 @@ __device__ __forceinline__ void gelu_pair(float& x0, float& x1) {
   unpack_f32x2(fma_f32x2(n, pack_f32x2(ex2_approx(q0), ex2_approx(q1)), p), x0, x1);
 }
 
+// Whether all 128 threads that share barrier `id` say so.
+__device__ __forceinline__ bool all_of_128(int id, bool mine) {
+  uint32_t all;
+  asm volatile(
+      "{\n\t.reg .pred p, q;\n\t"
+      "setp.ne.u32 p, %2, 0;\n\t"
+      "bar.red.and.pred q, %1, 128, p;\n\t"
+      "selp.u32 %0, 1, 0, q;\n\t}"
+      : "=r"(all)
+      : "r"(id), "r"((uint32_t)mine)
+      : "memory");
+  return all != 0;
+}
+
 // Bias and activation of NC accumulator columns, and their store: v[i] belongs to row r0 + i of C and to this lane's column.
 template <int NC>
 __device__ __forceinline__ void finish(const E4m3GemmParams& p, int r0, int col, float bias, float (&v)[NC]) {
@@ -539,7 +553,8 @@ __global__ void __launch_bounds__(kGemmThreads, 1) gemm_e4m3_kernel(const __grid
       wm += step_m;
       if (wn >= num_w) wn -= num_w, ++wm;
       const int col = n0 + quarter * 32 + lane, stop = min(BN, p.m - m0);
-      ok = ok && __all_sync(0xffffffffu, wait(tfull_bar(acc), acc_phase));
+      // (the four warps of a turn share barriers further down: they go on together or not at all)
+      ok = all_of_128(1 + turn, ok && __all_sync(0xffffffffu, wait(tfull_bar(acc), acc_phase)));
       if (!ok) {  // what was not computed is NaN
         if (lane == 0) report(p.status, kGaveUp);
         for (int c = turn * 8; c < stop; c += 8 * kEpiTurns) finish_nan<8>(p, m0 + c, col);

@@ -369,3 +369,12 @@ def test_scales_copies_or_products_that_give_up(m, n, k, warp):
     channels among it, lands before the block has gone."""
     got, _ = _one_warp_gives_up(m, n, k, warp)
     assert got.isnan().all()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("warp", range(16))
+@pytest.mark.parametrize("m,n,k", [(1, 1280, 5120), (64, 5000, 512), (775, 5120, 1280), (5000, 3000, 640)])
+def test_a_warp_of_the_epilogue_that_gives_up(m, n, k, warp):
+    """One of the warps that read the accumulator gives up, the others find it complete: those that share barriers with it do not wait for it."""
+    got, _ = _one_warp_gives_up(m, n, k, warp, gelu=True)
+    assert got.isnan().any() or 8 * (warp // 4) >= m  # (warp w reads columns 8 (w / 4) .. of a tile: rows of A, which may not exist)
