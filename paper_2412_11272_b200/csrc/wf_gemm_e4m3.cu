@@ -555,15 +555,19 @@ __global__ void __launch_bounds__(kGemmThreads, 1) gemm_e4m3_kernel(const __grid
       const int col = n0 + quarter * 32 + lane, stop = min(BN, p.m - m0);
       // (the four warps of a turn share barriers further down: they go on together or not at all)
       ok = all_of_128(1 + turn, ok && __all_sync(0xffffffffu, wait(tfull_bar(acc), acc_phase)));
-      if (!ok) {  // what was not computed is NaN
+      const bool pieces_of_16 = wide_rows && n0 + kTileN <= p.n;
+      const int begin = turn ^ (acc << 1);  // (14 pieces for four turns: those that take one more change with the tile)
+      if (!ok) {  // what was not computed is NaN: the rows that these warps would have stored, the other turns may have theirs
         if (lane == 0) report(p.status, kGaveUp);
-        for (int c = turn * 8; c < stop; c += 8 * kEpiTurns) finish_nan<8>(p, m0 + c, col);
+        const int each = pieces_of_16 ? 16 : 8;
+        for (int c = (pieces_of_16 ? begin : turn) * each; c < stop; c += each * kEpiTurns)
+          for (int i = 0; i < each; i += 8) finish_nan<8>(p, m0 + c + i, col);
+        acc ^= 1;
         continue;
       }
       tc_fence_after();
       const uint32_t from = tmem + lanes_at + acc * BN;
-      const int begin = turn ^ (acc << 1);  // (14 pieces for four turns: those that take one more change with the tile)
-      if (wide_rows && n0 + kTileN <= p.n) {
+      if (pieces_of_16) {
         float b4[4] = {0.f, 0.f, 0.f, 0.f};  // of this thread's lanes of the fragments
         if (p.bias) {
           const int first = n0 + quarter * 32 + (lane >> 2);

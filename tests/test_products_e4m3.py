@@ -378,3 +378,13 @@ def test_a_warp_of_the_epilogue_that_gives_up(m, n, k, warp):
     """One of the warps that read the accumulator gives up, the others find it complete: those that share barriers with it do not wait for it."""
     got, _ = _one_warp_gives_up(m, n, k, warp, gelu=True)
     assert got.isnan().any() or 8 * (warp // 4) >= m  # (warp w reads columns 8 (w / 4) .. of a tile: rows of A, which may not exist)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("warp", [0, 5, 10, 15])
+@pytest.mark.parametrize("m,n,k", [(64, 5000, 512), (64, 5120, 512), (100, 1024, 3000), (775, 5120, 1280), (5000, 3000, 640), (4500, 5120, 256)])
+def test_every_value_is_written_where_some_warps_give_up(m, n, k, warp):
+    """What was not computed is NaN, whatever the other warps of the tile have stored; nothing is left as it was."""
+    got, plain = _one_warp_gives_up(m, n, k, warp)
+    assert (got.isnan() | (got == plain)).all(), int((got == 77.0).sum())
+    assert got.isnan().any() or m < 100                                # (of small tiles not every warp has rows)
