@@ -395,8 +395,8 @@ __global__ void __launch_bounds__(kVerThreads, 2) draft_verify_kernel(const __gr
       for (int a = 0; a < kAhead; ++a) sum += part[a];
       top = high;
     }
-    // (as ordered integers: one instruction takes the largest of a warp)
-    const int bits = __float_as_int(top), order = bits ^ ((bits >> 31) & 0x7fffffff), most = __reduce_max_sync(0xffffffffu, order);
+    // (as ordered integers: one instruction takes the largest of a warp; a sum with +0 makes -0 and +0 one number)
+    const int bits = __float_as_int(top + 0.f), order = bits ^ ((bits >> 31) & 0x7fffffff), most = __reduce_max_sync(0xffffffffu, order);
     const float high = __int_as_float(most ^ ((most >> 31) & 0x7fffffff));
     const int place = greedy ? (int)__reduce_min_sync(0xffffffffu, (unsigned)(order == most ? at : 0x7fffffff)) : 0x7fffffff;
     float part = greedy || top == high ? sum : sum * exp2f((top - high) * per_t_log2);

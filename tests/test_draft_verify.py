@@ -395,3 +395,22 @@ def test_commit_of_what_does_not_fit():
                 continue                                         # (the second row of those did move)
             assert torch.equal(cache.k, k) and torch.equal(cache.v, v)
             assert got.tolist() == ([start[0]] if bits == 2 and (kept[0] in (-1, 3) or abs(start[0]) > 30 or start[0] < 0) and path != [[0, 2]] else [start[0] + kept[0]])
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("V", [2, 70, 5000, 50_021])
+def test_zeros_of_both_signs_are_equal(dtype, V):
+    """The largest logit is zero and occurs with either sign, in one lane, in several, in other warps: the lowest index, greedy or not."""
+    rng = np.random.default_rng(V)
+    dec, n = _decoder(), 24
+    x = -1.0 - torch.rand(n, V, generator=torch.Generator().manual_seed(V))
+    tok = np.zeros(n, np.int64)
+    for r in range(n):
+        at = np.sort(rng.choice(V, min(V, 2 + r % 5), replace=False))
+        x[r, at] = torch.tensor([-0.0 if (i + r // 2) % 2 == 0 else 0.0 for i in range(len(at))])
+        if r % 2 == 0:
+            tok[r + 1] = at[0 if r % 4 == 0 else -1]                 # the draft behind it: the first of the equals, or another one
+    x = x.to(torch.bfloat16 if dtype == "bf16" else torch.float32).cuda()
+    for t in (0.0, 1.0):
+        assert _run(dec, x, [2] * (n // 2), tok, None, rng.random(n), rng.random(n // 2), t=[t] * (n // 2)) == 0
