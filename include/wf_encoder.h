@@ -553,7 +553,7 @@ wf_status wf_page_plan(wf_decoder *dec, const wf_page_pool *pool, int n_seq, con
  *   otherwise       p <- max(p - q, 0) / sum of it (unless that sum is 0), and the next child is tried;
  * where none is kept the token that follows is the first v with sum_{i<=v} p_i > u' sum_i p_i.  q is the distribution that w's
  * children were drawn from, or, without `draft`, all of it on x (drafts that were looked up or chosen, not drawn).  T = 0: a
- * child is kept if p(x) = 1.  Sums that decide a drawn token are float64, exponentials included.
+ * child is kept if p(x) = 1.  What is decided, a draft or the token that follows, is decided by sums in float64, exponentials included.
  *   logits       dev   float32 or bfloat16 (logits_dtype) [n_rows][vocab], rows `ld` elements apart
  *   cu_rows      dev   int [n_seq + 1];  max_rows  host  no sequence has more rows in this call (longer ones are cut, bit 2)
  *   tokens       dev   int [n_rows] (of a first row: not looked at);  parents  dev  int [n_rows], row of the sequence below the

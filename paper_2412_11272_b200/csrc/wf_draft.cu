@@ -9,9 +9,10 @@
 // Bytes: the logits of the rows on the path, once, and one row of q; what bounds a call is the chain of row after row, each
 // a pass over the vocabulary and an exchange.  So one cluster of blocks per sequence walks its path in one launch: a pass is
 // shared by the blocks, partial results go to every block's shared memory, and all blocks then take the same decision from
-// the same numbers.  Rows off the path are not read.  The sums that decide a drawn token are float64, exponentials
-// included: a vocabulary's running sum has steps of 1e-6 or less, so in float32 the token would depend on the order of
-// summation.  Acceptance needs the row's sum alone, where float32 exponentials (1e-7) are enough.
+// the same numbers.  Rows off the path are not read.  The sums that decide are float64, exponentials included: a
+// vocabulary's running sum has steps of 1e-6 or less, so in float32 the token would depend on the order of summation, and after refusals
+// what is left of p may be small beside what it is taken from.  A first child is weighed against the row's sum in float32,
+// which the first pass makes beside the largest logit; where that sum's error could decide (1e-5 of all cases), against one in float64.
 #include <math.h>
 
 #include "wf_decoder.h"
@@ -118,6 +119,42 @@ __device__ __forceinline__ double exp2_64th(double z, const double* table) {
   return __hiloint2double(__double2hiint(r) + ((k >> 6) << 20), __double2loint(r));
 }
 
+// exp(x / T)'s parts of a power of two: 2^((y - top) per_t / 64), in float64.
+__device__ __forceinline__ double power_of(float y, double top, double per_t, const double* table) {
+  const double z = ((double)y - top) * per_t, r = exp2_64th(z, table);
+  return z > -64000.0 ? r : 0.0;
+}
+
+// A row's sum in float64 without some tokens, handed to all blocks by way of `sums`: for the few cases in which the float32 sum's
+// error could decide.  Out of line and plain: once in 1e5 rows, and the kernel's registers are short.
+template <typename T>
+__device__ __noinline__ double exact_sum(const T* row, int vocab, double top, double per_t, const double* table, const int* refused, int n_refused, double* sums,
+                                         int cluster) {
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, rank = cluster > 1 ? (int)ptx::cluster_ctarank() : 0;
+  double sum = 0.0;
+  for (int v = rank * kVerThreads + (int)threadIdx.x; v < vocab; v += cluster * kVerThreads) {
+    double w = power_of(VecOf<T>::one(row + v), top, per_t, table);
+    for (int j = 0; j < n_refused; ++j)
+      if (refused[j] == v) w = 0.0;
+    sum += w;
+  }
+  for (int o = 16; o > 0; o /= 2) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+  double* to = sums + rank * kVerWarps + warp;
+  if (cluster == 1) {
+    if (lane == 0) *to = sum;
+    __syncthreads();
+  } else {
+    const long long bits = __double_as_longlong(sum);
+    if (lane < cluster) ptx::st_cluster_v2(ptx::map_to_cta(ptx::smem_u32(to), lane), (uint32_t)bits, (uint32_t)(bits >> 32));
+    __syncwarp();
+    ptx::cluster_sync_all();
+  }
+  sum = 0.0;
+  for (int i = lane; i < cluster * kVerWarps; i += 32) sum += sums[i];
+  for (int o = 16; o > 0; o /= 2) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+  return sum;
+}
+
 // kHold: the block keeps its part of p in shared memory (`hold`), so that a refusal costs a subtraction for each element and
 // not an exponential; vocabularies whose part does not fit are computed anew.
 template <typename T, bool kHold>
@@ -126,6 +163,7 @@ __global__ void __launch_bounds__(kVerThreads, 2) draft_verify_kernel(const __gr
   extern __shared__ __align__(16) double dynamic[];
   __shared__ Part gather[2][kMaxCluster * kVerWarps];
   __shared__ double table[64];
+  __shared__ float bound[kVerWarps];  // of the error of a row's float32 sum, each warp's own copy (a register fewer)
   double* inverse = dynamic;                                   // of the sums left after each refusal at the present row
   int* token = reinterpret_cast<int*>(dynamic + p.max_rows);
   int* parent = token + p.max_rows;
@@ -242,18 +280,15 @@ __global__ void __launch_bounds__(kVerThreads, 2) draft_verify_kernel(const __gr
   int next = -1;          // the token that follows the path
   bool draws = false;     // it is drawn from what is left of p
   Part row{};             // largest logit and sum of the row `cur`
-  double whole = 0.0;     // its sum in float64, once something needs it (0: not yet)
+  double whole = 0.0;     // its sum (of drafts that were not drawn: without those refused), in float64 once something needs that
   int n_cut = 0;          // refusals that changed p: sums in `inverse` (drawn drafts) or tokens in `refused`
-  double gone = 0.0;      // probability of the refused tokens (drafts that were not drawn)
-  int have = -1;          // the last pass (and hold) has p after this many refusals, not divided by the last one's sum
+  int have = -1;          // the last pass (and hold) has p after this many refusals, not divided by the last one's sum; -1: no sum in float64 at this row
+                          // so far, -2: none that can be gone on from
   double have_total = 0.0;
 
   auto row_at = [&](int i) { return LogitRow<T>(reinterpret_cast<const T*>(p.logits) + (long)(row0 + i) * p.ld, p.vocab); };
   double top64 = 0.0;     // row.top
-  auto power = [&](float y) {
-    const double z = ((double)y - top64) * per_t, r = exp2_64th(z, table);
-    return z > -64000.0 ? r : 0.0;
-  };
+  auto power = [&](float y) { return power_of(y, top64, per_t, table); };
   // A row is cut into runs of 32 `length` pieces, one for every warp of the cluster, in order.
   const int runs = cluster * kVerWarps;
   auto run_length = [&](const LogitRow<T>& x) { return (x.pieces + runs * 32 - 1) / (runs * 32); };
@@ -406,12 +441,16 @@ __global__ void __launch_bounds__(kVerThreads, 2) draft_verify_kernel(const __gr
     row = exchange(Part{high, place, wide});
     if (row.at >= p.vocab) row.at = 0;  // (nothing but -infinity)
     top64 = (double)row.top;
-    whole = gone = 0.0;
+    whole = row.sum;
     n_cut = 0;
     have = -1;
     if (!(row.top > -INFINITY && row.top < INFINITY) || row.sum != row.sum) break;  // no distribution: nothing follows
 
-    // ---- its children, in row order
+    // ---- its children, in row order.  A draft is weighed against float32 sums where that is beyond doubt, and else against
+    // sums in float64 (then a pass has been made).  The bound: an exponential's own error and its argument's (rounded thrice, and 28
+    // binary digits are as much as a row's weights differ where they count), the additions of a lane and a warp.
+    if (lane == 0) bound[warp] = (float)whole * ((float)(96 + 4 * length) * (1.f / (1 << 23)));
+    __syncwarp();
     int taken = -1;
     for (; child < n && taken < 0; child = child_behind(child), look()) {
       const int v = token[child];
@@ -419,43 +458,54 @@ __global__ void __launch_bounds__(kVerThreads, 2) draft_verify_kernel(const __gr
         if (v == row.at) taken = child;
         continue;
       }
-      const double u = (double)chance[child];
-      double e = power(child_y);
-      if (q_row == nullptr) {
+      double e = power(child_y), against = (double)chance[child];
+      if (q_row != nullptr) {
+        against *= (double)child_q;
+        if (n_cut > 0) {
+          e *= 1.0 / whole;
+          for (int j = 0; j < n_cut; ++j) e = fmax(e - (double)child_q, 0.0) * inverse[j];
+        }
+      } else {
         for (int j = 0; j < n_cut; ++j)
           if (refused[j] == v) e = 0.0;
-        if (u * (1.0 - gone) * row.sum < e) {
-          taken = child;
-        } else if (e > 0.0 && (1.0 - gone) * row.sum - e > 0.0) {
-          __syncthreads();  // all warps have read the list
-          if (tid == 0) refused[n_cut] = v;
-          __syncthreads();
-          ++n_cut;
-          gone += e / row.sum;
+      }
+      if (q_row == nullptr || n_cut == 0) {
+        if (have == -1 && fabs(against * whole - e) <= against * (double)bound[warp]) {
+          whole = exact_sum<T>(x.x, p.vocab, top64, per_t, table, refused, q_row == nullptr ? n_cut : 0, reinterpret_cast<double*>(gather[turn]), cluster);
+          turn ^= 1;
+          have = -2;
         }
-      } else if (n_cut == 0 && u * (double)child_q * row.sum < e) {
+        against *= whole;
+      }
+      if (against < e) {
         taken = child;
-      } else {
-        double r = 0.0;
-        if (n_cut > 0) {
-          r = e * (1.0 / whole);
-          for (int j = 0; j < n_cut; ++j) r = fmax(r - (double)child_q, 0.0) * inverse[j];
+        continue;
+      }
+      if (q_row == nullptr) {
+        if (!(e > 0.0)) continue;  // (nothing is taken from p)
+        __syncthreads();           // all warps have read the list
+        if (tid == 0) refused[n_cut] = v;
+        __syncthreads();
+        // what is left by subtraction, while that says enough (in float64: halved sixteen times at most)
+        if (have == -1 ? whole - e > 2.0 * (double)bound[warp] : e <= 0.5 * whole && n_cut - have < 16) {
+          whole -= e;
+          ++n_cut;
+          continue;
         }
-        if (n_cut > 0 && u * (double)child_q < r) {
-          taken = child;
-        } else {
-          double left = 0.0;
+      }
+      double left = 0.0;
 #pragma unroll 1
-          for (int step = whole == 0.0 ? 0 : 1; step < 2; ++step) {  // p itself first, where nothing has needed it so far
-            left = sum_pass(x, step == 0 ? 0 : n_cut + 1, step != 0 && have == n_cut);
-            if (step == 0) whole = left;
-          }
-          if (left > 0.0) {
-            if (tid == 0) inverse[n_cut] = 1.0 / left;
-            __syncthreads();
-            ++n_cut;
-          }
-        }
+      for (int step = q_row != nullptr && have < 0 ? 0 : 1; step < 2; ++step) {  // p itself first, where nothing has needed it so far
+        left = sum_pass(x, step == 0 ? 0 : n_cut + 1, q_row != nullptr && step != 0 && have == n_cut);
+        if (step == 0) whole = left;
+      }
+      if (left > 0.0) {
+        if (q_row == nullptr) whole = left;
+        if (tid == 0) inverse[n_cut] = 1.0 / left;
+        __syncthreads();
+        ++n_cut;
+      } else if (q_row == nullptr) {  // the refusal does not count
+        have = -2;
       }
     }
     if (taken < 0) {

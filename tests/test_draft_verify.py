@@ -414,3 +414,60 @@ def test_zeros_of_both_signs_are_equal(dtype, V):
     x = x.to(torch.bfloat16 if dtype == "bf16" else torch.float32).cuda()
     for t in (0.0, 1.0):
         assert _run(dec, x, [2] * (n // 2), tok, None, rng.random(n), rng.random(n // 2), t=[t] * (n // 2)) == 0
+
+
+def _near(rng, value):
+    """A float32 random number within a few steps of `value`, on either side."""
+    u = np.float32(min(max(value, 0.0), 1.0 - 2.0 ** -24))
+    for _ in range(int(rng.integers(1, 6))):
+        u = np.nextafter(u, np.float32(rng.integers(0, 2)))
+    return float(min(max(u, np.float32(0)), np.float32(1.0 - 2.0 ** -24)))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("drawn", [False, True])
+@pytest.mark.parametrize("V,n_seq", [(40, 12), (3000, 12), (50_021, 8), (300_007, 2)])
+def test_decisions_next_to_a_border(dtype, drawn, V, n_seq):
+    """Random numbers a few float32 steps beside the probability that they are compared with, for a first child and behind up to seven refusals that
+    leave a thousandth of p or less each: decided as in float64."""
+    rng = np.random.default_rng(V + n_seq)
+    dec, kids, t = _decoder(), 9, 0.75
+    rows = [kids] * n_seq
+    n, tokens, u = sum(rows), np.zeros(sum(rows), np.int64), np.full(sum(rows), 1.0 - 2.0 ** -24)
+    g = torch.Generator().manual_seed(V)
+    x = 0.5 * torch.randn(n, V, generator=g) - 40.0
+    at = [rng.choice(V, kids, replace=False) for _ in range(n_seq)]
+    for b in range(n_seq):
+        x[kids * b, at[b]] = torch.tensor([8.0 - i * rng.uniform(1.0, 5.5) for i in range(kids)], dtype=torch.float32)
+    x = x.to(torch.bfloat16 if dtype == "bf16" else torch.float32)
+    q = torch.softmax(x.float() / t + 0.3 * torch.randn(n, V, generator=g), 1) if drawn else None
+    for b in range(n_seq):
+        i0, depth = kids * b, b % 8 if not drawn else b % 4              # the child whose number lies at the border
+        p, qd = O.distribution(x[i0].double().numpy(), np.float32(t)), None if q is None else q[i0].double().numpy()
+        order = at[b] if not drawn else rng.choice(at[b], kids)
+        tokens[i0 + 1:i0 + kids] = order[:kids - 1]
+        for c in range(kids - 1):
+            v = int(order[c])
+            border = p[v] / (1.0 if qd is None else qd[v])
+            if c == depth:
+                u[i0 + 1 + c] = _near(rng, border)
+                break
+            u[i0 + 1 + c] = min(1.0 - 2.0 ** -24, border * 1.5 + 1e-3)
+            rest = np.where(np.arange(V) == v, 0.0, p) if qd is None else np.maximum(p - qd, 0.0)
+            if np.float32(u[i0 + 1 + c]) * (1.0 if qd is None else qd[v]) >= p[v] and rest.sum() > 0:
+                p = rest / rest.sum()
+    u, last = u.astype(np.float32), rng.random(n_seq).astype(np.float32)
+    star = np.tile([-1] + [0] * (kids - 1), n_seq)
+    kept, out, path = (y.cpu().numpy() for y in dec.wf_draft_verify(
+        x.cuda(), _dev(np.arange(0, n + 1, kids)), _dev(tokens), _dev(u, torch.float32), _dev(last, torch.float32), kids, parents=_dev(star),
+        draft=None if q is None else q.cuda(), temperature=_dev([t] * n_seq, torch.float32)))
+    decided = 0
+    for b in range(n_seq):
+        r = slice(kids * b, kids * (b + 1))
+        want, stay, margin = O.draft_verify(x[r].double().numpy(), tokens[r], star[r], u[r], last[b], float(np.float32(t)), None if q is None else q[r].double().numpy())
+        if margin < 1e-3:                                              # 1e-9 of a probability: beyond the 64 bits of a small rest
+            continue
+        decided += 1
+        assert kept[b] == len(stay) and out[b, :len(want)].tolist() == want and path[b, :len(stay)].tolist() == stay, (b, want, stay, out[b], path[b], margin)
+    assert decided >= n_seq / 2
