@@ -471,3 +471,26 @@ def test_decisions_next_to_a_border(dtype, drawn, V, n_seq):
         decided += 1
         assert kept[b] == len(stay) and out[b, :len(want)].tolist() == want and path[b, :len(stay)].tolist() == stay, (b, want, stay, out[b], path[b], margin)
     assert decided >= n_seq / 2
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype,V", [("bf16", 300_007), ("f32", 300_007), ("f32", 1_000_003), ("bf16", 50_021)])
+@pytest.mark.parametrize("drawn", [False, True])
+def test_few_sequences_and_none_left_out(dtype, V, drawn):
+    """Two or three sequences of large vocabularies, each of them compared: no decision lies within 1e-9 of its border."""
+    rng = np.random.default_rng(V)
+    rows = [5, 3] if V > 100_000 else [6, 1, 4]
+    x, tok, up, u, last, q = _batch(rng, rows, V, True, drawn, dtype, siblings=4)
+    t, cu = [1.0, 0.8, 0.6][:len(rows)], np.concatenate([[0], np.cumsum(rows)])
+    status = torch.zeros(1, dtype=torch.int32, device="cuda")
+    kept, out, path = (y.cpu().numpy() for y in _decoder().wf_draft_verify(
+        x, _dev(cu), _dev(tok), _dev(u, torch.float32), _dev(last, torch.float32), max(rows), parents=_dev(up), draft=q,
+        temperature=_dev(t, torch.float32), status=status))
+    assert int(status) == 0
+    for b, m in enumerate(rows):
+        r = slice(cu[b], cu[b + 1])
+        want, stay, margin = O.draft_verify(x[r].double().cpu().numpy(), tok[r], up[r], u[r], last[b], float(np.float32(t[b])),
+                                            None if q is None else q[r].double().cpu().numpy())
+        k = len(stay)
+        assert margin >= 1e-3 and kept[b] == k, (b, margin, kept[b], k)
+        assert out[b].tolist() == want + [-1] * (max(rows) - k) and path[b].tolist() == stay + [-1] * (max(rows) - k), (b, want, out[b])
