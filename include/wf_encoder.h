@@ -579,7 +579,8 @@ wf_status wf_draft_verify(wf_decoder *dec, const void *logits, int logits_dtype,
  *   caches       host  every layer's cache; they share the page table (dev, int [n_seq][table_stride]).  The positions
  *                      concerned are the sequence's own: no page that holds one is shared with another sequence
  * A kept[s] that is negative or above path_stride counts as 0 (bit 2); a row that is not above the one before it stays where it
- * is (bit 4), as one beyond the table or in a page that does not exist (bits 2, 1).  A cache that is given twice is refused.
+ * is (bit 4), as one beyond the table or in a page that does not exist (bits 2, 1; reported of rows that need not move as well).  Without
+ * path or caches a length beyond the table, if there is one, is reported (bit 2).  A cache that is given twice is refused.
  * n_seq <= 65535, path_stride <= 1024. */
 wf_status wf_draft_commit(wf_decoder *dec, int n_seq, const int *start, const int *kept, const int *path, int path_stride, int *lengths,
                           const wf_cache *caches, int n_caches, const int *page_table, int table_stride, int *status, void *stream);

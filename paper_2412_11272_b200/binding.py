@@ -1016,7 +1016,7 @@ class Decoder:
             pp, stride = _vector(path, "path", device), path.shape[1]
         cache_array = self._caches(caches, device)
         table = tstride = None
-        if caches:
+        if caches or page_table is not None:
             if page_table is None or page_table.dim() != 2 or page_table.shape[0] < n_seq:
                 _refuse("caches need page_table [n_seq, pages]")
             table, tstride = _vector(page_table, "page_table", device), page_table.shape[1]

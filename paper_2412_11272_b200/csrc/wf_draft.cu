@@ -664,7 +664,7 @@ __global__ void __launch_bounds__(kCommitThreads) draft_commit_kernel(const __gr
         const int row = __ldg(path + i), last = i > 0 ? __ldg(path + i - 1) : -1;
         if (row < i || row <= last) {
           problems |= kBadParent;
-        } else if (row != i) {
+        } else {  // (a row that stays is looked up like one that moves, so that it is reported where it has no place)
           const long a = (long)start + row, b = (long)start + i;
           const int mask = (1 << p.page_shift) - 1;
           if ((a >> p.page_shift) >= p.table_stride) {
@@ -675,7 +675,7 @@ __global__ void __launch_bounds__(kCommitThreads) draft_commit_kernel(const __gr
             if (pa < 0 || pa >= p.n_pages || pb < 0 || pb >= p.n_pages) {
               problems |= kBadPage;
             } else {
-              moves = true;
+              moves = row != i;
               src = (((uint32_t)pa * (uint32_t)p.n_kv_head) << p.page_shift) + (uint32_t)(a & mask);
               dst = (((uint32_t)pb * (uint32_t)p.n_kv_head) << p.page_shift) + (uint32_t)(b & mask);
             }
@@ -713,8 +713,9 @@ __global__ void draft_lengths_kernel(const __grid_constant__ CommitPlan p) {
   const int s = (int)(blockIdx.x * blockDim.x + threadIdx.x);
   if (s >= p.n_seq) return;
   int problems = 0;
-  const int start = p.start[s];
-  p.lengths[s] = start + committed(p, s, start, &problems);
+  const int start = p.start[s], kept = committed(p, s, start, &problems);
+  if (kept > 0 && p.page_table != nullptr && (long)start + kept > (long)p.table_stride << p.page_shift) problems |= kBadRows;
+  p.lengths[s] = start + kept;
   if (problems != 0) report(p.status, problems);
 }
 

@@ -494,3 +494,28 @@ def test_few_sequences_and_none_left_out(dtype, V, drawn):
         k = len(stay)
         assert margin >= 1e-3 and kept[b] == k, (b, margin, kept[b], k)
         assert out[b].tolist() == want + [-1] * (max(rows) - k) and path[b].tolist() == stay + [-1] * (max(rows) - k), (b, want, out[b])
+
+
+@pytest.mark.gpu
+def test_commit_reports_rows_that_stay_without_a_place():
+    """A row that need not move has a place too: behind the table, or in a page that does not exist, it is reported, and nothing else changes."""
+    dec = _decoder(n_head=2, cache_format="path", page_size=16)
+    cache = dec.cache(4)
+    cache.k.normal_()
+    cache.v.normal_()
+    k, v = cache.k.clone(), cache.v.clone()
+    for table, start, kept, path, bits in (
+            ([[0, 1]], [30], [2], [[0, 1]], 0), ([[0, 1]], [31], [2], [[0, 1]], 2), ([[0, 1]], [32], [1], [[0, 7]], 2), ([[0, 1]], [40], [0], [[0, 1]], 0),
+            ([[0, -1]], [15], [1], [[0, 1]], 0), ([[0, -1]], [15], [2], [[0, 1]], 1), ([[0, 4]], [16], [1], [[0, 1]], 1),
+            ([[0, 1]], [30], [2], None, 0), ([[0, 1]], [30], [3], None, 2), ([[0, 1]], [33], [0], None, 0), ([[0, 1]], [2 ** 31 - 9], [9], None, 2)):
+        for in_place in (False, True):
+            for caches in ([cache], []):
+                status, first = torch.zeros(1, dtype=torch.int32, device="cuda"), _dev(start)
+                got = dec.wf_draft_commit(first, _dev(kept), None if path is None else _dev(path), caches=caches, page_table=_dev(table),
+                                          lengths=first if in_place else None, status=status)
+                want = bits if caches else bits & 2                    # (without caches no page is looked at)
+                assert int(status) == want and got.tolist() == [min(start[0] + kept[0], 2 ** 31 - 1) if start[0] + kept[0] < 2 ** 31 else start[0]], \
+                    (table, start, kept, path, bool(caches), int(status), got.tolist())
+                assert torch.equal(cache.k, k) and torch.equal(cache.v, v)
+    status = torch.zeros(1, dtype=torch.int32, device="cuda")
+    assert dec.wf_draft_commit(_dev([500]), _dev([9]), status=status).tolist() == [509] and int(status) == 0   # no table: nothing to compare with
