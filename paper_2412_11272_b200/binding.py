@@ -1011,8 +1011,8 @@ class Decoder:
             _refuse("start must be in device memory")
         pp, stride = None, 0
         if path is not None:
-            if path.dim() != 2 or path.shape[0] < n_seq:
-                _refuse("path must be [n_seq, rows]")
+            if path.dim() != 2 or path.shape[0] < n_seq or path.shape[1] < 1:  # (an empty one has no address, as if there were none)
+                _refuse("path must be [n_seq, rows], of one row at least")
             pp, stride = _vector(path, "path", device), path.shape[1]
         cache_array = self._caches(caches, device)
         table = tstride = None

@@ -519,3 +519,14 @@ def test_commit_reports_rows_that_stay_without_a_place():
                 assert torch.equal(cache.k, k) and torch.equal(cache.v, v)
     status = torch.zeros(1, dtype=torch.int32, device="cuda")
     assert dec.wf_draft_commit(_dev([500]), _dev([9]), status=status).tolist() == [509] and int(status) == 0   # no table: nothing to compare with
+
+
+@pytest.mark.gpu
+def test_commit_refuses_a_path_without_rows():
+    """A path of no columns is not the same as none (with which all kept rows count)."""
+    from paper_2412_11272_b200.binding import WfError
+    first, kept = _dev([3, 5]), _dev([2, 1])
+    with pytest.raises(WfError) as e:
+        _decoder().wf_draft_commit(first, kept, torch.empty(2, 0, dtype=torch.int32, device="cuda"))
+    assert e.value.status == "WF_ERR_INVALID_ARG"
+    assert _decoder().wf_draft_commit(first, kept, torch.zeros(2, 1, dtype=torch.int32, device="cuda")).tolist() == [3, 6]  # two of one row: none
