@@ -663,7 +663,7 @@ class ScaledCodes:
     @classmethod
     def pack(cls, codes: torch.Tensor, scales: torch.Tensor):
         """Codes [rows, k] with scales as numbers: powers of two (or NaN), [rows, ceil(k / 128)], or one for each 128 x 128 block,
-        [ceil(rows / 128), ceil(k / 128)]."""
+        [ceil(rows / 128), ceil(k / 128)].  For weights, once: it waits for the device (the scales' values are checked) and cannot be captured."""
         rows, k = codes.shape
         blocks = (k + 127) // 128
         if scales.dim() != 2 or scales.shape[1] != blocks or scales.shape[0] not in (rows, (rows + 127) // 128):

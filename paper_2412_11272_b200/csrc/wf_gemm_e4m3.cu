@@ -314,16 +314,21 @@ __device__ __forceinline__ void finish_nan(const E4m3GemmParams& p, int r0, int 
 }
 
 // A tile is 128 rows of W for each block by BN rows of A: W's rows are the lanes of the accumulator, so that a handful of rows
-// of A costs a handful of columns, and C's rows are written in runs of 32 columns per warp.
-//   warps 0..7   read the accumulator (a quarter of its lanes each, two warps in turn), apply bias and activation, store
-//   warps 8..11  bring the scales of 512 channels to tensor memory (each its quarter of the lanes, which hold copies)
-//   warp 12      one lane issues the TMA copies of the codes;   warp 13  one lane issues the products
+// of A costs a handful of columns, and C's rows are written in runs of 128 columns (by way of shared memory, bfloat16 rows of whole
+// 16-byte chunks) or of 32 per warp (float32, other rows, the last columns, splits).
+//   warps 0..15   read the accumulator (warp w the quarter w % 4 of its lanes; four turns, w / 4, take pieces of its columns alternately), apply
+//                 bias and activation, store
+//   warps 16..19  bring the scales of 512 channels to tensor memory (each its quarter of the lanes, which hold copies)
+//   warp 20       one lane issues the TMA copies of the codes
+//   warp 21       issues the products: all of it walks along, one lane issues
 // CG = 2: a pair of blocks shares a tile of 256 rows of W by BN of A, each block stages its own 128 rows of W and half of A's.
 // The copies of both signal the first block's barriers, which alone issues the products; its commits reach both.
 // The queue of products is short: what the issuing warp does between two stages shows (it walks whole, so that descriptors stay in
 // uniform registers: without GELU 344 us with a single lane, 287 so, 49,600 x 5120 x 1280), and the epilogue shares its schedulers.
-// That product takes 251 to 265 us (2.45 to 2.6 PFLOP/s, near 1.3 GHz under the power cap) and 291 to 300 with GELU; n and k
-// exchanged 225 to 238 us, products for 92 % of the cycles.  64 rows by 50,021 x 1280: 15 us, with the output 78 % of the copy rate.
+// That product takes 259 us in a short burst (2.51 PFLOP/s; by the box 254 to 277) and 298 for seconds on end (SMs at 1.3 GHz under the power
+// cap), with GELU 285 (to 308) and 327; n and k exchanged 221 to 239 and 265.  Float32 outputs: 318 us, 464 with GELU (erff).  64 rows by
+// 50,021 x 1280, float32 out: 15.3 us, with the output 77 % of the copy rate; bfloat16 rows of odd length, stored by two bytes a lane, 15.0
+// (50,048: 14.2), 4000 of them 291 us (231).
 // kSplit: a cluster of blocks shares a tile, each has a part of the channels; every block sums a part of the columns, in the
 // order of the blocks, from what the others leave in its shared memory.
 template <int BN, int CG, bool kSplit>
