@@ -449,7 +449,9 @@ __global__ void __launch_bounds__(kVerThreads, 2) draft_verify_kernel(const __gr
     // ---- its children, in row order.  A draft is weighed against float32 sums where that is beyond doubt, and else against
     // sums in float64 (then a pass has been made).  The bound: an exponential's own error and its argument's (rounded thrice, and 28
     // binary digits are as much as a row's weights differ where they count), the additions of a lane and a warp.
-    if (lane == 0) bound[warp] = (float)whole * ((float)(96 + 4 * length) * (1.f / (1 << 23)));
+    // (Temperatures above 2^100 give weight to logits that differ by more than float32 holds, and where 1 / T is more than float32
+    // holds it has been cut: the sum says nothing then.)
+    if (lane == 0) bound[warp] = per_t_log2 < 0x1p-100f || per_t_log2 >= 3.0e38f ? INFINITY : (float)whole * ((float)(96 + 4 * length) * (1.f / (1 << 23)));
     __syncwarp();
     int taken = -1;
     for (; child < n && taken < 0; child = child_behind(child), look()) {

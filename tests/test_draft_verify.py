@@ -530,3 +530,36 @@ def test_commit_refuses_a_path_without_rows():
         _decoder().wf_draft_commit(first, kept, torch.empty(2, 0, dtype=torch.int32, device="cuda"))
     assert e.value.status == "WF_ERR_INVALID_ARG"
     assert _decoder().wf_draft_commit(first, kept, torch.zeros(2, 1, dtype=torch.int32, device="cuda")).tolist() == [3, 6]  # two of one row: none
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("drawn", [False, True])
+@pytest.mark.parametrize("V", [70, 9000])
+def test_logits_further_apart_than_float32_holds(drawn, V):
+    """Temperatures at which logits of -3e38 beside one of 3e38 have weight: every one of them counts."""
+    rng = np.random.default_rng(V)
+    n = 16
+    x = torch.full((4 * n, V), -3e38)
+    x[:, 3], x[::2, 5] = 3e38, 1e38
+    tok = np.tile([0, 3, 5, 9], n)
+    t = (10.0 ** rng.uniform(37.3, 38.5, n)).astype(np.float32)
+    q = torch.rand(4 * n, V, generator=torch.Generator().manual_seed(1)) if drawn else None
+    q = None if q is None else (q / q.sum(1, keepdim=True)).cuda()
+    u = rng.random(4 * n)
+    if not drawn:
+        for b in range(n):                                             # beside the border of the first child, where the rest's weight decides
+            u[4 * b + 1] = min(O.distribution(x[4 * b].double().numpy(), t[b])[3] * rng.choice([0.98, 1.02]), 0.999)
+    assert _run(_decoder(), x.cuda(), [4] * n, tok, np.tile([-1, 0, 0, 0], n), u, rng.random(n), t=t, draft=q) == 0
+
+
+@pytest.mark.gpu
+def test_logits_that_differ_by_subnormal_numbers():
+    """Temperatures whose reciprocal float32 does not hold: logits of 0 and -1e-40 differ."""
+    n, V = 12, 300
+    x = torch.full((2 * n, V), -1e-40)
+    x[:, 3] = 0.0
+    t = np.tile([1e-39, 1e-40, 1e-42, 1e-45], 3).astype(np.float32)
+    u = np.full(2 * n, 0.5)
+    for b in range(n):
+        u[2 * b + 1] = min(O.distribution(x[2 * b].double().numpy(), float(t[b]))[3] * (0.98, 1.02)[b % 2], 0.999)
+    assert _run(_decoder(), x.cuda(), [2] * n, np.tile([0, 3], n), None, u, np.linspace(0.1, 0.9, n), t=t) == 0
